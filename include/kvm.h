@@ -50,7 +50,7 @@ enum {
     KVM_OK = 0,
     KVM_E_INVAL = 1,        /* NULL or inconsistent argument, bad layer index */
     KVM_E_SPAN = 2,         /* deletion span unsorted, overlapping, empty or outside the live cache */
-    KVM_E_CAPACITY = 3,     /* L' + M exceeds a character's capacity, or sum M exceeds max_tail_tokens */
+    KVM_E_CAPACITY = 3,     /* L' + M exceeds a character's capacity, or sum M exceeds max_tail_tokens; host memory */
     KVM_E_CUDA = 4,         /* CUDA runtime / launch failure (text in kvm_last_error) */
     KVM_E_DEVICE = 5,       /* a kernel reported a bounds violation or an expired wait */
     KVM_E_UNSUPPORTED = 6   /* shape outside what the kernels implement */
@@ -231,6 +231,18 @@ kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* live, const
 kvm_status kvm_plan_partition(int32_t n_chars, const int64_t* cost, int32_t n_ranks, int32_t* rank_of,
                               int64_t* rank_cost);
 
+/* The trees of a draft (kvm_draft_begin, whose checks of them these are):
+ * node_cu host [n_chars+1], parent host [sum n]; per node its depth and the word
+ * of its ancestors (bit j: node j is the node itself or an ancestor), host
+ * [sum n], either may be NULL.  Errors: KVM_E_INVAL, KVM_E_UNSUPPORTED. */
+kvm_status kvm_plan_draft(int32_t n_chars, const int32_t* node_cu, const int32_t* parent, int32_t* depth,
+                          uint64_t* ancestors);
+
+/* Whether these paths could be committed to these trees (the checks of
+ * kvm_draft_commit).  Errors: KVM_E_INVAL, KVM_E_UNSUPPORTED. */
+kvm_status kvm_plan_draft_path(int32_t n_chars, const int32_t* node_cu, const int32_t* parent,
+                               const int32_t* path_cu, const int32_t* path);
+
 /* ------------------------------------------------------------ hot path */
 
 /* Eq. 2: remove the live entries named by the spans from every attention
@@ -368,6 +380,93 @@ typedef struct kvm_round {
 
 kvm_status kvm_update_round(kvm_ctx* ctx, const kvm_round* round, void* stream);
 
+/* ------------------------------------------------------------ drafts
+ * Several guessed continuations of each character, scored in one pass, judged,
+ * and one of them kept.  The guesses form a tree of nodes per character, at
+ * most 64: node i has a parent with a smaller index, or -1 for a root, which
+ * follows the last live token (several roots are allowed, except in
+ * kvm_draft_verify).  A node's depth is its number of ancestors.  One step is
+ * kvm_draft_begin, then one kvm_draft_attn or kvm_draft_gdn per layer, then
+ * kvm_draft_commit of one path from a root in each tree; kvm_draft_verify
+ * finds such paths from the model's and the draft's probabilities.
+ *
+ * A draft changes nothing before its commit: nodes' keys and values wait in
+ * slots behind the live entries, the recurrent and convolution states are only
+ * read.  Beginning another draft, or any call that changes caches, states or
+ * lengths, ends an open one; the draft calls then fail with KVM_E_INVAL.
+ * Tensors of nodes are packed like tails, [sum n][heads][dim] with character
+ * b's nodes at rows node_cu[b] .. node_cu[b+1]-1, and must be finite.  Every
+ * device pointer is checked for its 16-byte alignment, and out may not overlap
+ * an input.  The context's device must be current.  All calls enqueue on
+ * `stream` and may be captured into a graph; the host's lengths and cursors move
+ * when kvm_draft_commit is called, not when such a graph is launched. */
+
+/* Room for trees of max_nodes nodes (all characters together) in this context:
+ * per delta-rule layer, node and head d_v fp32 and d_k bf16 values (with the
+ * convolution the node's raw inputs too).  Allocates, and synchronizes the
+ * device if it has to grow; the calls below allocate nothing.  Ends an open
+ * draft if it grows.  Errors: KVM_E_INVAL (max_nodes outside [1,
+ * max_tail_tokens]), KVM_E_UNSUPPORTED (more than 1024 delta-rule layers),
+ * KVM_E_CUDA. */
+kvm_status kvm_draft_reserve(kvm_ctx* ctx, int32_t max_nodes);
+
+/* Announce a step's trees: node_cu host [n_chars+1], parent host [sum n]
+ * (indices within the character's nodes, -1: a root).  A character without
+ * nodes takes no part.  Errors: KVM_E_INVAL (offsets, a parent that is no
+ * smaller index), KVM_E_UNSUPPORTED (a tree of more than 64 nodes),
+ * KVM_E_CAPACITY (more nodes than reserved, live + n beyond a character's
+ * capacity, position ids past int32). */
+kvm_status kvm_draft_begin(kvm_ctx* ctx, const int32_t* node_cu, const int32_t* parent, void* stream);
+
+/* One attention layer over the draft: rotate node i's query and key at
+ * position p_b + depth(i), put keys and values behind the live entries, then
+ * o_i = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j over every live entry, node
+ * i's ancestors and itself.  Tensors as kvm_tail_attn_prefill's, of which a
+ * draft that is one chain is the equal.  Errors: KVM_E_INVAL. */
+kvm_status kvm_draft_attn(kvm_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                          void* out, void* stream);
+
+/* One gated-delta-rule layer over the draft: o_i = S_i q_i with S_i the carried
+ * state advanced along node i's ancestors and itself (kvm_gdn_chunk_scan_from_state
+ * on that path; with conv_kernel = 4 the convolution runs along the path too,
+ * from the carried inputs, and its outputs are rounded to bf16 as there).
+ * Tensors as kvm_gdn_chunk_scan_from_state's.  Errors: KVM_E_INVAL. */
+kvm_status kvm_draft_gdn(kvm_ctx* ctx, int32_t layer, const void* q, const void* k, const void* v,
+                         const float* alpha, const float* beta, void* out, void* stream);
+
+/* The verdict over the draft's tokens.  Node 0 of each tree is its one root, a
+ * token already decided (the last step's next token).  target, draft: device
+ * [sum n][vocab] probabilities after each node, the model's and those that the
+ * node's children were drawn from, independently and in index order; both fp32
+ * or both bf16 (prob_type).  Rows are probabilities: what is not a finite
+ * positive number counts as 0.  tokens device int32 [sum n]; u device fp32
+ * [sum n] and u_next device fp32 [n_chars] uniform in [0, 1).
+ * From node 0 on, the children c of the current node are tried in order: with t
+ * = tokens[c], c is accepted where u[c] q(t) Z < w(t), w = p and Z = 1 at first;
+ * after each child that is not, w becomes max(w - Z q, 0) and Z its sum.  The
+ * first accepted child is the next current node; where none is, the next token
+ * is the smallest x with sum_{y <= x} w(y) > u_next sum w (w = p again where
+ * nothing is left of it).  So path and next token are distributed as the
+ * target's samples.  Sums are good to ~2^-45.
+ * Outputs, device int32: path [sum n], character b's accepted nodes (node 0
+ * first) from node_cu[b] on, then -1; count [n_chars] of them; next [n_chars],
+ * -1 where the row holds nothing or the character has no nodes.  A token
+ * outside [0, vocab) is not accepted and is reported by kvm_check (KVM_E_DEVICE).
+ * Errors: KVM_E_INVAL (several roots), KVM_E_UNSUPPORTED (vocab > 2^24). */
+enum { KVM_PROB_F32 = 0, KVM_PROB_BF16 = 1 };
+kvm_status kvm_draft_verify(kvm_ctx* ctx, int32_t vocab, int32_t prob_type, const int32_t* tokens,
+                            const void* target, const void* draft, const float* u, const float* u_next,
+                            int32_t* path, int32_t* count, int32_t* next, void* stream);
+
+/* Keep one path of each tree: path_cu host [n_chars+1], path host (node
+ * indices; the first a root, each next a child of the one before; empty: the
+ * character keeps nothing).  Every layer must have run on the draft.  The
+ * path's keys and values become live entries at positions p_b, p_b + 1, ..,
+ * the recurrent states S <- prod(alpha) S + sum of the path's updates, the
+ * convolution states its last three inputs; live lengths and cursors grow by
+ * the path's length and the draft ends.  Errors: KVM_E_INVAL. */
+kvm_status kvm_draft_commit(kvm_ctx* ctx, const int32_t* path_cu, const int32_t* path, void* stream);
+
 /* Allocation-free compaction for callers that cannot call cudaMalloc --
  * for example an engine that owns all device memory through its own fixed
  * arena and forbids other allocations during a session, or a frame loop in
@@ -459,7 +558,8 @@ kvm_status kvm_fork(kvm_ctx* dst, const kvm_ctx* src, void* stream);
  * reads); launches beyond it are neither timed nor counted here
  * (kvm_launch_count counts every launch). */
 enum { KVM_K_COMPACT = 0, KVM_K_ROPE_APPEND = 1, KVM_K_ATTENTION = 2, KVM_K_ATTN_COMBINE = 3,
-       KVM_K_GDN = 4, KVM_K_GATHER = 5, KVM_K_GDN_PREP = 6, KVM_K_GDN_CONV = 7, KVM_K_COUNT = 8 };
+       KVM_K_GDN = 4, KVM_K_GATHER = 5, KVM_K_GDN_PREP = 6, KVM_K_GDN_CONV = 7, KVM_K_DRAFT_TREE = 8,
+       KVM_K_DRAFT_GDN = 9, KVM_K_DRAFT_VERIFY = 10, KVM_K_DRAFT_COMMIT = 11, KVM_K_COUNT = 12 };
 kvm_status kvm_profile_enable(kvm_ctx* ctx, int32_t enable);
 kvm_status kvm_profile_read(kvm_ctx* ctx, int32_t kernel, int64_t* launches, double* total_ms,
                             int32_t reset);

@@ -498,3 +498,70 @@ def refill(layer_kind, inputs: dict, Hkv, D, H, dk, dv, R, theta, conv_weights=N
     positions 0 .. n-1 (the reference construction of §5.2)."""
     empty = CharacterState.empty(layer_kind, Hkv, D, H, dk, dv)
     return maintenance_round(empty, layer_kind, [], [], inputs, R, theta, conv_weights=conv_weights)
+
+
+# ----------------------------------------------------------------------------
+# Drafts: trees of guessed tokens.  A node's result is that of the chain of its
+# ancestors and itself, so each node is run as a tail of its own.
+# ----------------------------------------------------------------------------
+def draft_path(parent, i: int) -> list:
+    """The nodes from node i's root down to i (parent[i] < i, -1: a root)."""
+    path = []
+    while i >= 0:
+        path.append(i)
+        i = int(parent[i])
+    return path[::-1]
+
+
+def draft_attention(cache: AttnCache, q, k_new, v_new, parent, p: int, R: int, theta: float) -> np.ndarray:
+    """out [n][Hq][D] of a tree's nodes: the last token of each node's path as a tail."""
+    out = np.zeros(np.asarray(q).shape)
+    for i in range(len(parent)):
+        t = draft_path(parent, i)
+        out[i] = tail_attn_prefill(cache, q[t], k_new[t], v_new[t], p, R, theta)[0][-1]
+    return out
+
+
+def draft_gdn(q, k, v, alpha, beta, S0, parent, conv_state=None, w=None):
+    """(out [n][H][d_v], per node its state) of a tree's nodes, with the short convolution when w is given."""
+    out = np.zeros(np.asarray(v).shape)
+    states = []
+    for i in range(len(parent)):
+        t = draft_path(parent, i)
+        x = (q[t], k[t], v[t])
+        if w is not None:
+            x = gdn_conv_inputs(*x, conv_state, w)[:3]
+        o, S = gdn_recurrent(*x, alpha[t], beta[t], S0)
+        out[i] = o[-1]
+        states.append(S)
+    return out, states
+
+
+def draft_verdict(parent, tokens, target, draft, u, u_next):
+    """(accepted nodes, next token): node 0 is decided; from the current node the children are tried in index order,
+    each against what the ones before it left of the target's row (normalised residuals, one after another); the next
+    token is the smallest x whose running sum passes u_next times the whole.  Entries that are not finite and positive
+    are 0; -1 where the last row holds nothing."""
+    clean = lambda x: np.where(np.isfinite(x) & (np.asarray(x) > 0), x, 0.0).astype(np.float64)
+    path = [0]
+    while True:
+        p, q = clean(target[path[-1]]), clean(draft[path[-1]])
+        w, taken, fresh = p, None, True
+        for c in (i for i in range(len(parent)) if parent[i] == path[-1]):
+            t = int(tokens[c])
+            total = 1.0 if fresh else math.fsum(w)
+            if float(u[c]) * q[t] * total < w[t]:
+                taken = c
+                break
+            if total == 0.0:
+                break
+            w, fresh = np.maximum(w - total * q, 0.0), False
+        if taken is None:
+            break
+        path.append(taken)
+    if math.fsum(w) == 0.0:
+        w = p
+    if math.fsum(w) == 0.0:
+        return path, -1
+    cum = np.cumsum(w.astype(np.longdouble))
+    return path, int(np.searchsorted(cum, np.longdouble(u_next) * cum[-1], side="right"))

@@ -1,0 +1,191 @@
+// Drafts: a tree of guessed tokens behind each character's live entries, and
+// the commit of one of its paths (kvm_draft_begin, kvm_draft_commit).
+//
+//  draft_tree   : each node's ancestors as the bits of one word, and its
+//                 position, cursor + depth.  Once a step, for every layer.
+//  draft_commit : one launch for every layer.  The nodes of a path are the
+//                 character's next tokens:
+//                 * attention caches: the path's key and value rows move from
+//                   live + node to live + rank.  A path's indices increase, so
+//                   rank <= node, and a block that reads all rows of its slab
+//                   before it writes the first moves them in place;
+//                 * states: S <- G S + sum_r w_r u_r k_r^T, with G the product
+//                   of alpha along the path and w_r that of the nodes after r.
+//                   u_r, the delta rule's update at node r, depends on the
+//                   node's ancestors only and was kept by the draft's layer
+//                   (draft_gdn.cu), so nothing is solved again and the sum has
+//                   no chain over the tokens;
+//                 * convolution states: the last three of the carried inputs
+//                   and the path's raw ones.
+//                 Bound by reading and writing S once (128 KB a head of 128 x
+//                 128); a block holds 32 rows of it in registers.
+#include "kvm_internal.cuh"
+
+namespace kvm {
+namespace {
+
+__global__ void __launch_bounds__(kDraftNodes) draft_tree_kernel(const __grid_constant__ DraftTreeParams p) {
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int b = blockIdx.x, i = threadIdx.x;
+    const int n0 = p.cu[b];
+    if (i >= p.cu[b + 1] - n0) return;
+    uint64_t anc = 0;
+    for (int j = i; j >= 0; j = p.parent[n0 + j]) anc |= 1ull << j;   // parents have smaller indices (checked on the host)
+    p.anc[n0 + i] = anc;
+    if (p.pos) p.pos[n0 + i] = (int32_t)(p.cursor[b] + __popcll(anc) - 1);
+}
+
+constexpr int kThreads = 128;
+constexpr int kStateRows = 32;               // rows of S a block
+constexpr int kTile = 16;                    // path nodes staged at a time
+constexpr int kMoveVec = kDraftNodes * 256 / 8 / kThreads;   // 16-byte pieces a thread moves, longest path of the widest rows
+
+// Blocks of one character (blockIdx.y), in blockIdx.x order: states [layer][head][32-row slice], cache slabs
+// [K, V][layer][KV head], convolution states [layer][1024-channel piece], position ids.
+struct Parts {
+    int state, kv, conv;
+};
+__host__ __device__ inline Parts parts_of(const DraftCommitParams& p) {
+    Parts x;
+    x.state = p.n_gdn * p.H * (p.dv / kStateRows);
+    x.kv = 2 * p.n_attn * p.Hkv;
+    x.conv = p.n_gdn * ((p.channels + 8 * kThreads - 1) / (8 * kThreads));
+    return x;
+}
+
+template <int DK>
+__device__ void commit_state(const DraftCommitParams& p, int b, int item, const int8_t* path, int d) {
+    constexpr int NP = DK / 32;
+    __shared__ __align__(16) float ks[kTile][DK];
+    __shared__ float us[kTile][kStateRows];
+    __shared__ float al[kDraftNodes], wt[kDraftNodes + 1];
+    const int slices = p.dv / kStateRows;
+    const int sl = item % slices, h = item / slices % p.H, g = item / slices / p.H;
+    const int tid = threadIdx.x, j = tid & 7, row = tid >> 3;   // this thread: rows 2 row, 2 row + 1; float4 groups j, j + 8, ..
+    const int64_t node0 = (int64_t)g * p.rec_nodes + p.node0[b];
+    float* S = p.S + ((((int64_t)g * p.n_chars + b) * p.H + h) * p.dv + sl * kStateRows + 2 * row) * DK + 4 * j;
+    float4 s[2][NP];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) s[r][i] = *reinterpret_cast<const float4*>(S + r * DK + 32 * i);
+    if (tid < d) al[tid] = p.rec_a[(node0 + path[tid]) * p.H + h];
+    __syncthreads();
+    if (tid <= d) {                                  // wt[r]: product of alpha after the r-th node of the path; wt[d] == G at r = -1
+        float w = 1.f;
+        for (int t = tid == d ? 0 : tid + 1; t < d; ++t) w *= al[t];
+        wt[tid] = w;
+    }
+    __syncthreads();
+    const float G = wt[d];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) { s[r][i].x *= G; s[r][i].y *= G; s[r][i].z *= G; s[r][i].w *= G; }
+    for (int t0 = 0; t0 < d; t0 += kTile) {
+        const int nt = min(kTile, d - t0);
+        if (t0 > 0) __syncthreads();
+        for (int e = tid; e < nt * (DK / 2); e += kThreads) {
+            const int t = e / (DK / 2), c = e % (DK / 2);
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(
+                p.rec_k + ((node0 + path[t0 + t]) * p.H + h) * DK + 2 * c);
+            *reinterpret_cast<float2*>(&ks[t][2 * c]) = __bfloat1622float2(x);
+        }
+        for (int e = tid; e < nt * kStateRows; e += kThreads) {
+            const int t = e / kStateRows, r = e % kStateRows;
+            us[t][r] = wt[t0 + t] * p.rec_u[((node0 + path[t0 + t]) * p.H + h) * p.dv + sl * kStateRows + r];
+        }
+        __syncthreads();
+        for (int t = 0; t < nt; ++t) {
+            const float u0 = us[t][2 * row], u1 = us[t][2 * row + 1];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const float4 k = *reinterpret_cast<const float4*>(&ks[t][4 * j + 32 * i]);
+                s[0][i].x = fmaf(u0, k.x, s[0][i].x); s[0][i].y = fmaf(u0, k.y, s[0][i].y);
+                s[0][i].z = fmaf(u0, k.z, s[0][i].z); s[0][i].w = fmaf(u0, k.w, s[0][i].w);
+                s[1][i].x = fmaf(u1, k.x, s[1][i].x); s[1][i].y = fmaf(u1, k.y, s[1][i].y);
+                s[1][i].z = fmaf(u1, k.z, s[1][i].z); s[1][i].w = fmaf(u1, k.w, s[1][i].w);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) *reinterpret_cast<float4*>(S + r * DK + 32 * i) = s[r][i];
+}
+
+__device__ void commit_kv(const DraftCommitParams& p, int b, int item, const int8_t* path, int d) {
+    bool moves = false;
+    for (int r = 0; r < d; ++r) moves |= path[r] != r;
+    if (!moves) return;                              // uniform
+    const int slabs = p.n_attn * p.Hkv;
+    const int slab = item % slabs;
+    uint4* rows = reinterpret_cast<uint4*>((item < slabs ? p.K : p.V) + ((int64_t)slab * p.slab_rows + p.slot[b]) * p.D);
+    const int vec = p.D / 8, n = d * vec;
+    uint4 v[kMoveVec];
+#pragma unroll
+    for (int e = 0; e < kMoveVec; ++e) {
+        const int x = threadIdx.x + e * kThreads;
+        if (x < n) v[e] = rows[path[x / vec] * vec + x % vec];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kMoveVec; ++e) {
+        const int x = threadIdx.x + e * kThreads;
+        if (x < n) rows[x] = v[e];
+    }
+}
+
+__device__ void commit_conv(const DraftCommitParams& p, int b, int item, const int8_t* path, int d) {
+    const int pieces = (p.channels + 8 * kThreads - 1) / (8 * kThreads);
+    const int g = item / pieces, c = 8 * (item % pieces * kThreads + (int)threadIdx.x);
+    if (c >= p.channels) return;
+    const int cur = p.conv_par[g >> 5] >> (g & 31) & 1;
+    __nv_bfloat16* st = p.conv_state + (((int64_t)cur * p.n_gdn + g) * p.n_chars + b) * 3 * p.channels + c;
+    const __nv_bfloat16* x = p.rec_x + ((int64_t)g * p.rec_nodes + p.node0[b]) * p.channels + c;
+    uint4 v[3];
+#pragma unroll
+    for (int r = 0; r < 3; ++r) {
+        const int t = d - 3 + r;                     // place in the path; negative: the carried row t + 3
+        v[r] = *reinterpret_cast<const uint4*>(t >= 0 ? x + (int64_t)path[t] * p.channels : st + (int64_t)(t + 3) * p.channels);
+    }
+#pragma unroll
+    for (int r = 0; r < 3; ++r) *reinterpret_cast<uint4*>(st + (int64_t)r * p.channels) = v[r];
+}
+
+__global__ void __launch_bounds__(kThreads) draft_commit_kernel(const __grid_constant__ DraftCommitParams p) {
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int b = blockIdx.y;
+    const int d = p.path_cu[b + 1] - p.path_cu[b];
+    if (d <= 0) return;
+    __shared__ int8_t path[kDraftNodes];
+    if ((int)threadIdx.x < d) path[threadIdx.x] = p.path[p.path_cu[b] + threadIdx.x];
+    __syncthreads();
+    const Parts n = parts_of(p);
+    int x = blockIdx.x;
+    if (x < n.state) {
+        if (p.dk == 64) commit_state<64>(p, b, x, path, d);
+        else commit_state<128>(p, b, x, path, d);
+        return;
+    }
+    x -= n.state;
+    if (x < n.kv) return commit_kv(p, b, x, path, d);
+    x -= n.kv;
+    if (x < n.conv) return commit_conv(p, b, x, path, d);
+    if (p.pos && (int)threadIdx.x < d) p.pos[p.slot[b] + threadIdx.x] = p.first_pos[b] + threadIdx.x;
+}
+
+}  // namespace
+
+void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s) {
+    launch_pdl(draft_tree_kernel, dim3(p.n_chars), dim3(kDraftNodes), 0, s, p);
+}
+
+void launch_draft_commit(const DraftCommitParams& p, cudaStream_t s) {
+    const Parts n = parts_of(p);
+    launch_pdl(draft_commit_kernel, dim3(n.state + n.kv + n.conv + 1, p.n_chars), dim3(kThreads), 0, s, p);
+}
+
+}  // namespace kvm

@@ -10,9 +10,12 @@
 // the kernels as kernel parameters: nothing is allocated or uploaded per call.
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
+#include <initializer_list>
 #include <numeric>
 #include <string>
 #include <vector>
@@ -73,6 +76,13 @@ constexpr int kFlagStride = 32;     // compaction read flags: one per 128-byte l
 // tokens 14 : 12.7 and 21 : 18 for 1 and 8.
 constexpr int recur_tail(int dk) { return dk == 64 ? 48 : 32; }
 constexpr int kRecurTile = 16;      // tokens it stages at a time when blocks share an SM
+
+// An attention layer's partition (see plan_attention).
+struct AttnPlan {
+    int n_tiles = 0, n_ctas = 0, waves = 0;
+    std::vector<int> n_qtiles, tile_off;             // per character
+    std::vector<int32_t> cta_tile, cta_k, split_cb;  // [n_ctas + 1], [n_ctas + 1], [number of split tiles]
+};
 
 }  // namespace
 
@@ -167,6 +177,21 @@ struct kvm_ctx {
     // (with KVM_DEBUG the user bytes sit between two canary bands)
     struct DevAlloc { void* base; size_t bytes; const char* name; };
     std::vector<DevAlloc> allocs;
+    // drafts (kvm_draft_*): room for draft_cap nodes; the open draft's tree on the
+    // host (packed parents) and as ancestor words and positions on the device; the
+    // attention's partition for it, one for all layers; which layers have run; and per
+    // delta-rule layer what a commit needs of each node
+    int draft_cap = 0;
+    bool draft_open = false;
+    std::vector<int32_t> draft_cu, draft_parent;
+    std::vector<char> draft_done;
+    AttnPlan draft_plan;
+    uint64_t* draft_anc = nullptr;
+    int32_t* draft_pos = nullptr;
+    float* draft_u = nullptr;             // [n_gdn][draft_cap][H][d_v]
+    __nv_bfloat16* draft_k = nullptr;     // [n_gdn][draft_cap][H][d_k]
+    float* draft_a = nullptr;             // [n_gdn][draft_cap][H]
+    __nv_bfloat16* draft_x = nullptr;     // [n_gdn][draft_cap][conv_ch]
     // per-kernel timing (kvm_profile_*)
     bool prof = false;
     std::vector<cudaEvent_t> ev;          // 2 per timed launch
@@ -239,6 +264,10 @@ kvm_status check_tail_cu(const kvm_ctx* c, const int32_t* tail_cu, int* total) {
         return fail(KVM_E_CAPACITY, "sum M = %d exceeds max_tail_tokens = %d", *total, c->max_tail);
     return KVM_OK;
 }
+
+// A call that changes what an open draft was made from (caches, states, lengths)
+// ends it.
+void drop_draft(kvm_ctx* c) { c->draft_open = false; }
 
 kvm_status check_layer(const kvm_ctx* c, int layer, int want) {
     if (layer < 0 || layer >= c->n_layers) return fail(KVM_E_INVAL, "layer %d out of range", layer);
@@ -359,11 +388,6 @@ kvm_status plan_spans(const kvm_ctx* c, const int32_t* span_cu, const int32_t* s
 // the last half to one and a half waves are dealt whole, one per block and
 // wave (see tail_attn_tc.cu), and only the rest is cut, each block's share
 // starting from the cost of what it was dealt.
-struct AttnPlan {
-    int n_tiles = 0, n_ctas = 0, waves = 0;
-    std::vector<int> n_qtiles, tile_off;             // per character
-    std::vector<int32_t> cta_tile, cta_k, split_cb;  // [n_ctas + 1], [n_ctas + 1], [number of split tiles]
-};
 
 void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, int grid_cap, bool deal, AttnPlan& pl) {
     pl.n_qtiles.assign(B, 0);
@@ -669,6 +693,7 @@ extern "C" kvm_status kvm_load_prefix(kvm_ctx* c, int32_t b, int32_t live, int64
         CUDA_TRY(cudaMemcpyAsync(c->pos + c->cap_off[b], positions, (size_t)live * 4, cudaMemcpyHostToDevice, s));
         CUDA_TRY(cudaStreamSynchronize(s));
     }
+    drop_draft(c);
     c->live[b] = live;
     c->cursor[b] = cursor;
     c->hpos[b].assign(positions, positions + live);
@@ -745,6 +770,7 @@ extern "C" kvm_status kvm_set_kv(kvm_ctx* c, int32_t layer, int32_t b, const voi
     const int L = c->live[b];
     if (L == 0) return KVM_OK;
     if (!k || !v) return fail(KVM_E_INVAL, "NULL k or v");
+    drop_draft(c);
     return copy_kv(c, layer, b, const_cast<void*>(k), const_cast<void*>(v), true, (cudaStream_t)stream);
 }
 
@@ -774,6 +800,7 @@ extern "C" kvm_status kvm_set_state(kvm_ctx* c, int32_t layer, const float* S, v
     kvm_status st = check_layer(c, layer, KVM_LAYER_GDN);
     if (st) return st;
     if (!S) return fail(KVM_E_INVAL, "NULL state");
+    drop_draft(c);
     const size_t n = (size_t)c->B * c->H * c->dv * c->dk;
     void* dst = c->S + (size_t)c->gdn_idx[layer] * n;
     const void* src = S;
@@ -809,6 +836,7 @@ extern "C" kvm_status kvm_set_conv_weights(kvm_ctx* c, int32_t layer, const floa
     kvm_status st = check_conv_layer(c, layer);
     if (st) return st;
     if (!w) return fail(KVM_E_INVAL, "NULL weights");
+    drop_draft(c);
     const size_t n = (size_t)c->conv_ch * 4;
     CUDA_TRY(cudaMemcpyAsync(c->conv_w + (size_t)c->gdn_idx[layer] * n, w, n * 4, cudaMemcpyDeviceToDevice,
                              (cudaStream_t)stream));
@@ -831,6 +859,7 @@ extern "C" kvm_status kvm_set_conv_state(kvm_ctx* c, int32_t layer, const void* 
     kvm_status st = check_conv_layer(c, layer);
     if (st) return st;
     if (!in) return fail(KVM_E_INVAL, "NULL state");
+    drop_draft(c);
     const int g = c->gdn_idx[layer];
     CUDA_TRY(cudaMemcpyAsync(conv_state_of(c, g, c->conv_par[g]), in, (size_t)c->B * 3 * c->conv_ch * 2,
                              cudaMemcpyDeviceToDevice, (cudaStream_t)stream));
@@ -1111,6 +1140,7 @@ kvm_status do_compact(kvm_ctx* c, const int32_t* span_cu, const int32_t* sbeg, c
     SpanPlan pl;
     kvm_status st = plan_spans(c, span_cu, sbeg, send, pl);
     if (st) return st;
+    drop_draft(c);
     st = launch_compaction(c, pl, s, 0, c->n_attn, true);
     if (st) return st;
     st = launch_gather(c, pl, gather_out, s);
@@ -1119,28 +1149,11 @@ kvm_status do_compact(kvm_ctx* c, const int32_t* span_cu, const int32_t* sbeg, c
     return KVM_OK;
 }
 
-// tail_pos_dev: device positions of the tail tokens (already staged), or
-// null for the true tail p_b + i; tail_pos_host: the same values on the host
-// for validation (null when tail_pos_dev is null).
-kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const void* q, const void* k_new,
-                        const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev = nullptr,
-                        const int32_t* tail_pos_host = nullptr) {
-    kvm_status st = check_layer(c, layer, KVM_LAYER_ATTN);
-    if (st) return st;
-    int total = 0;
-    st = check_tail_cu(c, tail_cu, &total);
-    if (st) return st;
-    for (int b = 0; b < c->B; ++b) {
-        const int m = tail_cu[b + 1] - tail_cu[b];
-        if (c->live[b] + m > c->cap[b])
-            return fail(KVM_E_CAPACITY, "character %d: live %d + tail %d exceeds capacity %d", b, c->live[b], m,
-                        c->cap[b]);
-    }
-    st = check_positions(c, tail_cu, tail_pos_host);
-    if (st) return st;
-    if (total == 0) return KVM_OK;
-    if (!q || !k_new || !v_new || !out) return fail(KVM_E_INVAL, "NULL tensor");
-
+// One attention layer's launches under its partition pl: a tail of `total` tokens
+// at tail_pos_dev (null: p_b + i), or with anc the nodes of a draft.
+kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int total, const AttnPlan& pl, const void* q,
+                            const void* k_new, const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev,
+                            const uint64_t* anc) {
     thread_local static AttnParams p;
     std::memset(&p, 0, sizeof p);
     const int a = c->attn_idx[layer];
@@ -1161,22 +1174,20 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     p.pos = c->pos;
     p.out = static_cast<__nv_bfloat16*>(out);
     p.tail_pos = tail_pos_dev;
+    p.anc = anc;
     p.part_o = c->part_o;
     p.part_ml = c->part_ml;
     p.err = c->err;
     p.diag = c->diag;
     for (int d = 0; d < c->R / 2; ++d) p.inv_freq[d] = c->inv_freq[d];
-    std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) {
         AttnChar& ch = p.ch[b];
         ch.L_prev = c->live[b];
-        ch.M = Ms[b] = tail_cu[b + 1] - tail_cu[b];
+        ch.M = tail_cu[b + 1] - tail_cu[b];
         ch.tail_off = tail_cu[b];
         ch.cap_off = c->cap_off[b];
         ch.p = c->cursor[b];
     }
-    AttnPlan pl;
-    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, p.tok_per_tile, attention_grid_cap(c->num_sms, c->D), true, pl);
     for (int b = 0; b < c->B; ++b) {
         p.ch[b].n_qtiles = pl.n_qtiles[b];
         p.ch[b].tile_off = pl.tile_off[b];
@@ -1215,7 +1226,7 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
             st.n_parts = (int16_t)(c1 - c0 + 1);
             st.slot0 = pl.cta_tile[c0] == t ? 2 * c0 : 2 * c0 + 1;
             st.token0 = tail_cu[b] + tok;
-            st.rows = (int16_t)(std::min(p.tok_per_tile, Ms[b] - tok) * c->g);
+            st.rows = (int16_t)(std::min(p.tok_per_tile, tail_cu[b + 1] - tail_cu[b] - tok) * c->g);
             st.head0 = local / pl.n_qtiles[b] * c->g;
         }
         ps = prof_begin(c, KVM_K_ATTN_COMBINE, s);
@@ -1224,6 +1235,36 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
         LAUNCH_CHECK(c);
     }
     return KVM_OK;
+}
+
+// tail_pos_dev: device positions of the tail tokens (already staged), or
+// null for the true tail p_b + i; tail_pos_host: the same values on the host
+// for validation (null when tail_pos_dev is null).
+kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const void* q, const void* k_new,
+                        const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev = nullptr,
+                        const int32_t* tail_pos_host = nullptr) {
+    kvm_status st = check_layer(c, layer, KVM_LAYER_ATTN);
+    if (st) return st;
+    int total = 0;
+    st = check_tail_cu(c, tail_cu, &total);
+    if (st) return st;
+    for (int b = 0; b < c->B; ++b) {
+        const int m = tail_cu[b + 1] - tail_cu[b];
+        if (c->live[b] + m > c->cap[b])
+            return fail(KVM_E_CAPACITY, "character %d: live %d + tail %d exceeds capacity %d", b, c->live[b], m,
+                        c->cap[b]);
+    }
+    st = check_positions(c, tail_cu, tail_pos_host);
+    if (st) return st;
+    if (total == 0) return KVM_OK;
+    if (!q || !k_new || !v_new || !out) return fail(KVM_E_INVAL, "NULL tensor");
+
+    std::vector<int> Ms(c->B);
+    for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
+    AttnPlan pl;
+    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, pl);
+    drop_draft(c);
+    return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
 }
 
 // Rows of S per eight lanes of the token-by-token delta rule: four (k and q
@@ -1246,6 +1287,7 @@ kvm_status do_gdn(kvm_ctx* c, int layer, const int32_t* tail_cu, const void* q, 
     if (st) return st;
     if (total == 0) return KVM_OK;
     if (!q || !k || !v || !alpha || !beta || !out) return fail(KVM_E_INVAL, "NULL tensor");
+    drop_draft(c);
     int active = 0, longest = 0;
     for (int b = 0; b < c->B; ++b) {
         const int m = tail_cu[b + 1] - tail_cu[b];
@@ -1519,6 +1561,7 @@ extern "C" kvm_status kvm_rerotate_keys(kvm_ctx* c, int32_t b, int32_t live_begi
         if (new_pos[i] < 0) return fail(KVM_E_INVAL, "new position %d is negative", i);
         top = std::max<int64_t>(top, (int64_t)new_pos[i] + 1);
     }
+    drop_draft(c);
     cudaStream_t s = (cudaStream_t)stream;
     kvm_status st = stage_positions(c, new_pos, n, c->reloc_pos_dev, s);
     if (st) return st;
@@ -1628,11 +1671,397 @@ extern "C" kvm_status kvm_advance_at(kvm_ctx* c, const int32_t* tail_cu, const i
             return fail(KVM_E_CAPACITY, "character %d would exceed its capacity", b);
     st = check_positions(c, tail_cu, tail_pos);
     if (st) return st;
+    drop_draft(c);
     do_advance(c, tail_cu, tail_pos);
     return KVM_OK;
 }
 
 extern "C" kvm_status kvm_advance(kvm_ctx* c, const int32_t* tail_cu) { return kvm_advance_at(c, tail_cu, nullptr); }
+
+// ============================================================================
+// drafts
+// ============================================================================
+namespace {
+
+// Release one buffer of alloc_dev's.
+template <typename T>
+void free_dev(kvm_ctx* c, T** p) {
+    for (size_t i = 0; *p && i < c->allocs.size(); ++i) {
+        if (static_cast<char*>(c->allocs[i].base) + kCanary != reinterpret_cast<char*>(*p)) continue;
+        cudaFree(c->allocs[i].base);
+        c->allocs.erase(c->allocs.begin() + i);
+        break;
+    }
+    *p = nullptr;
+}
+
+void free_draft(kvm_ctx* c) {
+    drop_draft(c);
+    c->draft_cap = 0;
+    free_dev(c, &c->draft_anc);
+    free_dev(c, &c->draft_pos);
+    free_dev(c, &c->draft_u);
+    free_dev(c, &c->draft_k);
+    free_dev(c, &c->draft_a);
+    free_dev(c, &c->draft_x);
+}
+
+// Checks that every draft call of a context shares: an open draft, and the
+// context's own device current (its buffers and launches are there).
+kvm_status check_draft(const kvm_ctx* c) {
+    if (!c) return fail(KVM_E_INVAL, "NULL context");
+    if (!c->draft_open)
+        return fail(KVM_E_INVAL, "no draft is open (kvm_draft_begin; a call that changes caches, states or lengths ends it)");
+    int dev = -1;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != c->device) return fail(KVM_E_INVAL, "the context lives on device %d, device %d is current", c->device, dev);
+    return KVM_OK;
+}
+
+bool aligned16(std::initializer_list<const void*> ps) {
+    uintptr_t bits = 0;
+    for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+    return (bits & 15) == 0;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+// The trees of kvm_draft_begin.
+kvm_status check_tree(int B, const int32_t* node_cu, const int32_t* parent) {
+    if (!node_cu) return fail(KVM_E_INVAL, "node_cu is NULL");
+    if (node_cu[0] != 0) return fail(KVM_E_INVAL, "node_cu[0] must be 0");
+    for (int b = 0; b < B; ++b) {
+        const int64_t n = (int64_t)node_cu[b + 1] - node_cu[b];
+        if (n < 0) return fail(KVM_E_INVAL, "node_cu not monotone at character %d", b);
+        if (n > kDraftNodes)
+            return fail(KVM_E_UNSUPPORTED, "character %d: %d nodes, a tree has at most %d", b, (int)n, kDraftNodes);
+    }
+    if (node_cu[B] > 0 && !parent) return fail(KVM_E_INVAL, "parent is NULL");
+    for (int b = 0; b < B; ++b)
+        for (int i = 0; i < node_cu[b + 1] - node_cu[b]; ++i) {
+            const int p = parent[node_cu[b] + i];
+            if (p < -1 || p >= i)
+                return fail(KVM_E_INVAL, "character %d node %d: parent %d, need -1 or a smaller index", b, i, p);
+        }
+    return KVM_OK;
+}
+
+// The paths of kvm_draft_commit in checked trees.
+kvm_status check_path(int B, const int32_t* node_cu, const int32_t* parent, const int32_t* path_cu, const int32_t* path) {
+    if (!path_cu) return fail(KVM_E_INVAL, "path_cu is NULL");
+    if (path_cu[0] != 0) return fail(KVM_E_INVAL, "path_cu[0] must be 0");
+    for (int b = 0; b < B; ++b) {
+        const int64_t d = (int64_t)path_cu[b + 1] - path_cu[b];
+        const int n = node_cu[b + 1] - node_cu[b];
+        if (d < 0) return fail(KVM_E_INVAL, "path_cu not monotone at character %d", b);
+        if (d > n) return fail(KVM_E_INVAL, "character %d: a path of %lld in a tree of %d nodes", b, (long long)d, n);
+    }
+    if (path_cu[B] > 0 && !path) return fail(KVM_E_INVAL, "path is NULL");
+    for (int b = 0; b < B; ++b) {
+        const int n = node_cu[b + 1] - node_cu[b];
+        int before = -1;
+        for (int i = path_cu[b]; i < path_cu[b + 1]; ++i) {
+            if (path[i] < 0 || path[i] >= n || parent[node_cu[b] + path[i]] != before)
+                return fail(KVM_E_INVAL, "character %d: path entry %d (node %d) does not follow node %d", b, i - path_cu[b],
+                            path[i], before);
+            before = path[i];
+        }
+    }
+    return KVM_OK;
+}
+
+kvm_status draft_reserve(kvm_ctx* c, int max_nodes) {
+    if (!c) return fail(KVM_E_INVAL, "NULL context");
+    if (max_nodes <= 0 || max_nodes > c->max_tail)
+        return fail(KVM_E_INVAL, "max_nodes must be in [1, max_tail_tokens = %d]", c->max_tail);
+    if (c->n_gdn > kMaxDraftLayers)
+        return fail(KVM_E_UNSUPPORTED, "drafts take at most %d delta-rule layers", kMaxDraftLayers);
+    int dev = -1;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != c->device) return fail(KVM_E_INVAL, "the context lives on device %d, device %d is current", c->device, dev);
+    max_nodes = std::min(max_nodes, c->B * kDraftNodes);
+    if (max_nodes <= c->draft_cap) return KVM_OK;
+    CUDA_TRY(cudaDeviceSynchronize());               // earlier drafts may still be at work in the old buffers
+    free_draft(c);
+    const size_t n = max_nodes, ln = (size_t)c->n_gdn * n;
+    cudaError_t e = alloc_dev(c, &c->draft_anc, n, "draft_anc");
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_pos, n, "draft_pos");
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_u, ln * c->H * c->dv, "draft_u", false);
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_k, ln * c->H * c->dk, "draft_k", false);
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_a, ln * c->H, "draft_a", false);
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_x, c->conv ? ln * c->conv_ch : 0, "draft_x", false);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) {
+        free_draft(c);
+        return fail(KVM_E_CUDA, "allocation failed: %s", cudaGetErrorString(e));
+    }
+    c->draft_cap = max_nodes;
+    return KVM_OK;
+}
+
+kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent, cudaStream_t s) {
+    if (!c) return fail(KVM_E_INVAL, "NULL context");
+    kvm_status st = check_tree(c->B, node_cu, parent);
+    if (st) return st;
+    const int total = node_cu[c->B];
+    if (total > c->draft_cap)
+        return fail(KVM_E_CAPACITY, "%d nodes, room for %d is reserved (kvm_draft_reserve)", total, c->draft_cap);
+    for (int b = 0; b < c->B; ++b) {
+        const int n = node_cu[b + 1] - node_cu[b];
+        if (c->live[b] + n > c->cap[b])
+            return fail(KVM_E_CAPACITY, "character %d: live %d + %d nodes exceed capacity %d", b, c->live[b], n, c->cap[b]);
+        if (c->cursor[b] + n > INT32_MAX) return fail(KVM_E_CAPACITY, "character %d: position ids overflow", b);
+    }
+    int dev = -1;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != c->device) return fail(KVM_E_INVAL, "the context lives on device %d, device %d is current", c->device, dev);
+    drop_draft(c);
+    c->draft_cu.assign(node_cu, node_cu + c->B + 1);
+    c->draft_parent.assign(parent, parent + total);
+    c->draft_done.assign(c->n_layers, 0);
+    if (total > 0) {
+        if (c->n_attn > 0) {
+            std::vector<int> M(c->B);
+            for (int b = 0; b < c->B; ++b) M[b] = node_cu[b + 1] - node_cu[b];
+            plan_attention(c->B, c->live.data(), M.data(), c->Hkv, kAttnRows / c->g,
+                           attention_grid_cap(c->num_sms, c->D), true, c->draft_plan);
+        }
+        thread_local static DraftTreeParams p;
+        p.n_chars = c->B;
+        std::copy(node_cu, node_cu + c->B + 1, p.cu);
+        std::copy(c->cursor.begin(), c->cursor.end(), p.cursor);
+        std::copy(parent, parent + total, p.parent);
+        p.anc = c->draft_anc;
+        p.pos = c->draft_pos;
+        const int ps = prof_begin(c, KVM_K_DRAFT_TREE, s);
+        launch_draft_tree(p, s);
+        prof_end(c, ps, s);
+        LAUNCH_CHECK(c);
+    }
+    c->draft_open = true;
+    return KVM_OK;
+}
+
+kvm_status draft_attn(kvm_ctx* c, int layer, const void* q, const void* k_new, const void* v_new, void* out, cudaStream_t s) {
+    kvm_status st = check_draft(c);
+    if (st) return st;
+    st = check_layer(c, layer, KVM_LAYER_ATTN);
+    if (st) return st;
+    const int total = c->draft_cu[c->B];
+    if (total > 0) {
+        if (!q || !k_new || !v_new || !out) return fail(KVM_E_INVAL, "NULL tensor");
+        if (!aligned16({q, k_new, v_new, out})) return fail(KVM_E_INVAL, "a tensor is not 16-byte aligned");
+        const size_t nq = (size_t)total * c->Hq * c->D * 2, nk = (size_t)total * c->Hkv * c->D * 2;
+        if (overlap(out, nq, q, nq) || overlap(out, nq, k_new, nk) || overlap(out, nq, v_new, nk))
+            return fail(KVM_E_INVAL, "out overlaps an input");
+        st = launch_attention(c, layer, c->draft_cu.data(), total, c->draft_plan, q, k_new, v_new, out, s, c->draft_pos,
+                              c->draft_anc);
+        if (st) return st;
+    }
+    c->draft_done[layer] = 1;
+    return KVM_OK;
+}
+
+kvm_status draft_gdn(kvm_ctx* c, int layer, const void* q, const void* k, const void* v, const float* alpha,
+                     const float* beta, void* out, cudaStream_t s) {
+    kvm_status st = check_draft(c);
+    if (st) return st;
+    st = check_layer(c, layer, KVM_LAYER_GDN);
+    if (st) return st;
+    const int total = c->draft_cu[c->B];
+    if (total > 0) {
+        if (!q || !k || !v || !alpha || !beta || !out) return fail(KVM_E_INVAL, "NULL tensor");
+        if (!aligned16({q, k, v, alpha, beta, out})) return fail(KVM_E_INVAL, "a tensor is not 16-byte aligned");
+        const size_t rows = (size_t)total * c->H, nv = rows * c->dv * 2, nk = rows * c->dk * 2;
+        if (overlap(out, nv, q, nk) || overlap(out, nv, k, nk) || overlap(out, nv, v, nv) || overlap(out, nv, alpha, rows * 4) ||
+            overlap(out, nv, beta, rows * 4))
+            return fail(KVM_E_INVAL, "out overlaps an input");
+        thread_local static DraftGdnParams p;
+        std::memset(&p, 0, sizeof p);
+        const int g = c->gdn_idx[layer];
+        const size_t at = (size_t)g * c->draft_cap;
+        p.n_chars = c->B;
+        p.H = c->H; p.dk = c->dk; p.dv = c->dv; p.channels = c->conv_ch;
+        std::copy(c->draft_cu.begin(), c->draft_cu.end(), p.cu);
+        p.anc = c->draft_anc;
+        p.q = static_cast<const __nv_bfloat16*>(q);
+        p.k = static_cast<const __nv_bfloat16*>(k);
+        p.v = static_cast<const __nv_bfloat16*>(v);
+        p.alpha = alpha;
+        p.beta = beta;
+        p.out = static_cast<__nv_bfloat16*>(out);
+        p.S = c->S + (size_t)g * c->B * c->H * c->dv * c->dk;
+        p.rec_u = c->draft_u + at * c->H * c->dv;
+        p.rec_k = c->draft_k + at * c->H * c->dk;
+        p.rec_a = c->draft_a + at * c->H;
+        if (c->conv) {
+            p.w = c->conv_w + (size_t)g * c->conv_ch * 4;
+            p.state_in = conv_state_of(c, g, c->conv_par[g]);
+            p.rec_x = c->draft_x + at * c->conv_ch;
+        }
+        int most = 0;
+        for (int b = 0; b < c->B; ++b) most = std::max(most, c->draft_cu[b + 1] - c->draft_cu[b]);
+        const int ps = prof_begin(c, KVM_K_DRAFT_GDN, s);
+        launch_draft_gdn(p, most, s);
+        prof_end(c, ps, s);
+        LAUNCH_CHECK(c);
+    }
+    c->draft_done[layer] = 1;
+    return KVM_OK;
+}
+
+kvm_status draft_verify(kvm_ctx* c, int vocab, int prob_type, const int32_t* tokens, const void* target, const void* draft,
+                        const float* u, const float* u_next, int32_t* path, int32_t* count, int32_t* next, cudaStream_t s) {
+    kvm_status st = check_draft(c);
+    if (st) return st;
+    if (vocab < 1 || vocab > (1 << 24)) return fail(KVM_E_UNSUPPORTED, "vocab must be in [1, 2^24]");
+    if (prob_type != KVM_PROB_F32 && prob_type != KVM_PROB_BF16) return fail(KVM_E_INVAL, "bad probability type %d", prob_type);
+    for (int b = 0; b < c->B; ++b)
+        for (int i = c->draft_cu[b] + 1; i < c->draft_cu[b + 1]; ++i)
+            if (c->draft_parent[i] < 0)
+                return fail(KVM_E_INVAL, "character %d has several roots: a verdict needs one", b);
+    const int total = c->draft_cu[c->B];
+    if (!u_next || !count || !next || (total > 0 && (!tokens || !target || !draft || !u || !path)))
+        return fail(KVM_E_INVAL, "NULL tensor");
+    if (!aligned16({tokens, target, draft, u, u_next, path, count, next}))
+        return fail(KVM_E_INVAL, "a tensor is not 16-byte aligned");
+    thread_local static DraftVerifyParams p;
+    p.n_chars = c->B;
+    p.vocab = vocab;
+    std::copy(c->draft_cu.begin(), c->draft_cu.end(), p.cu);
+    p.anc = c->draft_anc;
+    p.tokens = tokens;
+    p.target = target;
+    p.draft = draft;
+    p.u = u;
+    p.u_next = u_next;
+    p.path = path;
+    p.count = count;
+    p.next = next;
+    p.err = c->err;
+    const int ps = prof_begin(c, KVM_K_DRAFT_VERIFY, s);
+    launch_draft_verify(p, prob_type == KVM_PROB_BF16, c->num_sms, s);
+    prof_end(c, ps, s);
+    LAUNCH_CHECK(c);
+    return KVM_OK;
+}
+
+kvm_status draft_commit(kvm_ctx* c, const int32_t* path_cu, const int32_t* path, cudaStream_t s) {
+    kvm_status st = check_draft(c);
+    if (st) return st;
+    st = check_path(c->B, c->draft_cu.data(), c->draft_parent.data(), path_cu, path);
+    if (st) return st;
+    const int total = path_cu[c->B];
+    if (total > 0)
+        for (int l = 0; l < c->n_layers; ++l)
+            if (!c->draft_done[l]) return fail(KVM_E_INVAL, "layer %d has not run on this draft", l);
+    if (total > 0) {
+        thread_local static DraftCommitParams p;
+        std::memset(&p, 0, offsetof(DraftCommitParams, path));
+        p.n_chars = c->B;
+        p.n_attn = c->n_attn; p.Hkv = c->Hkv; p.D = c->D;
+        p.n_gdn = c->n_gdn; p.H = c->H; p.dk = c->dk; p.dv = c->dv; p.channels = c->conv ? c->conv_ch : 0;
+        p.rec_nodes = c->draft_cap;
+        p.slab_rows = c->T_cap;
+        p.K = c->K;
+        p.V = c->V;
+        p.pos = c->pos;
+        p.S = c->S;
+        p.rec_u = c->draft_u;
+        p.rec_k = c->draft_k;
+        p.rec_a = c->draft_a;
+        p.rec_x = c->draft_x;
+        p.conv_state = c->conv_state;
+        if (c->conv)
+            for (int g = 0; g < c->n_gdn; ++g) p.conv_par[g >> 5] |= (uint32_t)c->conv_par[g] << (g & 31);
+        for (int b = 0; b < c->B; ++b) {
+            p.node0[b] = c->draft_cu[b];
+            p.slot[b] = c->cap_off[b] + c->live[b];
+            p.first_pos[b] = (int32_t)c->cursor[b];
+        }
+        std::copy(path_cu, path_cu + c->B + 1, p.path_cu);
+        std::copy(path, path + total, p.path);
+        const int ps = prof_begin(c, KVM_K_DRAFT_COMMIT, s);
+        launch_draft_commit(p, s);
+        prof_end(c, ps, s);
+        LAUNCH_CHECK(c);
+    }
+    drop_draft(c);
+    do_advance(c, path_cu);
+    return KVM_OK;
+}
+
+// No exception of the host's allocator leaves a C entry point.
+template <typename F>
+kvm_status guarded(F&& f) noexcept {
+    try {
+        return f();
+    } catch (const std::exception&) {
+        g_err.clear();
+        return KVM_E_CAPACITY;
+    }
+}
+}  // namespace
+
+extern "C" kvm_status kvm_plan_draft(int32_t n_chars, const int32_t* node_cu, const int32_t* parent, int32_t* depth,
+                                     uint64_t* ancestors) {
+    return guarded([&]() -> kvm_status {
+        if (n_chars <= 0 || n_chars > kMaxChars) return fail(KVM_E_INVAL, "n_chars must be in [1,%d]", kMaxChars);
+        const kvm_status st = check_tree(n_chars, node_cu, parent);
+        if (st) return st;
+        std::vector<uint64_t> anc(kDraftNodes);
+        for (int b = 0; b < n_chars; ++b)
+            for (int x = node_cu[b]; x < node_cu[b + 1]; ++x) {
+                const int i = x - node_cu[b], p = parent[x];
+                anc[i] = (p >= 0 ? anc[p] : 0) | 1ull << i;
+                if (depth) depth[x] = __builtin_popcountll(anc[i]) - 1;
+                if (ancestors) ancestors[x] = anc[i];
+            }
+        return KVM_OK;
+    });
+}
+
+extern "C" kvm_status kvm_plan_draft_path(int32_t n_chars, const int32_t* node_cu, const int32_t* parent,
+                                          const int32_t* path_cu, const int32_t* path) {
+    return guarded([&]() -> kvm_status {
+        if (n_chars <= 0 || n_chars > kMaxChars) return fail(KVM_E_INVAL, "n_chars must be in [1,%d]", kMaxChars);
+        const kvm_status st = check_tree(n_chars, node_cu, parent);
+        return st ? st : check_path(n_chars, node_cu, parent, path_cu, path);
+    });
+}
+
+extern "C" kvm_status kvm_draft_reserve(kvm_ctx* c, int32_t max_nodes) {
+    return guarded([&] { return draft_reserve(c, max_nodes); });
+}
+
+extern "C" kvm_status kvm_draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent, void* stream) {
+    return guarded([&] { return draft_begin(c, node_cu, parent, (cudaStream_t)stream); });
+}
+
+extern "C" kvm_status kvm_draft_attn(kvm_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                                     void* out, void* stream) {
+    return guarded([&] { return draft_attn(c, layer, q, k_new, v_new, out, (cudaStream_t)stream); });
+}
+
+extern "C" kvm_status kvm_draft_gdn(kvm_ctx* c, int32_t layer, const void* q, const void* k, const void* v,
+                                    const float* alpha, const float* beta, void* out, void* stream) {
+    return guarded([&] { return draft_gdn(c, layer, q, k, v, alpha, beta, out, (cudaStream_t)stream); });
+}
+
+extern "C" kvm_status kvm_draft_verify(kvm_ctx* c, int32_t vocab, int32_t prob_type, const int32_t* tokens,
+                                       const void* target, const void* draft, const float* u, const float* u_next,
+                                       int32_t* path, int32_t* count, int32_t* next, void* stream) {
+    return guarded([&] {
+        return draft_verify(c, vocab, prob_type, tokens, target, draft, u, u_next, path, count, next, (cudaStream_t)stream);
+    });
+}
+
+extern "C" kvm_status kvm_draft_commit(kvm_ctx* c, const int32_t* path_cu, const int32_t* path, void* stream) {
+    return guarded([&] { return draft_commit(c, path_cu, path, (cudaStream_t)stream); });
+}
 
 namespace {
 // NVTX ranges (a tool such as Nsight Systems shows them; without one attached
@@ -1687,6 +2116,7 @@ kvm_status update_round_impl(kvm_ctx* c, const kvm_round* r, void* stream) {
         st = plan_spans_for(c->B, tail_len.data(), r->delim_cu, r->delim_begin, r->delim_end, delim_plan);
         if (st) return st;
     }
+    drop_draft(c);
     const bool host_io = r->io_on_host && total > 0;
     auto sizes = [&](int l, size_t n[6]) {
         const bool attn = c->kind[l] == KVM_LAYER_ATTN;
@@ -1963,6 +2393,7 @@ extern "C" kvm_status kvm_fork(kvm_ctx* dst, const kvm_ctx* src, void* stream) {
                                  cudaMemcpyDeviceToDevice, s));
         dst->conv_par = src->conv_par;
     }
+    drop_draft(dst);
     dst->live = src->live;
     dst->cursor = src->cursor;
     dst->hpos = src->hpos;

@@ -160,6 +160,7 @@ struct AttnParams {
     float* part_ml;               // [2 n_ctas][128][2]: (reference max in log2 units, sum) of a partial
     int32_t* err;
     int32_t* diag;                // first expired wait: block + 1, tag, parity
+    const uint64_t* anc;          // device [sum M]: a draft's ancestor bits (DraftTreeParams), or null: a causal tail
     double inv_freq[kMaxRotaryHalf];
     int32_t cta_tile[kMaxAttnCtas + 1];
     int32_t cta_k[kMaxAttnCtas + 1];
@@ -320,6 +321,93 @@ struct RecurParams {
 };
 // nr: rows of S per eight lanes (1, 2 or 4); 16 nr divides d_v.
 void launch_gdn_recur(const RecurParams& p, int nr, cudaStream_t s);
+
+// ----------------------------------------------------------------------------
+// drafts: trees of guessed tokens behind the live entries (kvm_draft_*)
+// ----------------------------------------------------------------------------
+constexpr int kDraftNodes = 64;               // nodes a character: a node's ancestors are the bits of one word
+constexpr int kMaxDraftNodes = kMaxChars * kDraftNodes;
+constexpr int kMaxDraftLayers = 1024;         // delta-rule layers of a context that drafts
+
+// Writes each node's ancestor word (bit j: node j is the node itself or an
+// ancestor; so its depth is the number of bits less one, and its parent,
+// grandparent, .. are its bits from the highest below its own down) and its
+// position, cursor + depth.
+struct DraftTreeParams {
+    int32_t n_chars;
+    int32_t cu[kMaxChars + 1];
+    int64_t cursor[kMaxChars];
+    int8_t parent[kMaxDraftNodes];            // packed; -1: a root
+    uint64_t* anc;                            // device [sum n]
+    int32_t* pos;                             // device [sum n], or null
+};
+void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s);
+
+// The delta rule over a draft's nodes, and what a commit needs of each: its
+// update u, its key, its decay and, with the convolution, its raw inputs.
+struct DraftGdnParams {
+    int32_t n_chars, H, dk, dv, channels;
+    int32_t cu[kMaxChars + 1];
+    const uint64_t* anc;                      // [sum n]
+    const __nv_bfloat16* q;                   // [sum n][H][d_k] (pre-convolution with w)
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;                   // [sum n][H][d_v]
+    const float* alpha;                       // [sum n][H]
+    const float* beta;
+    __nv_bfloat16* out;                       // [sum n][H][d_v]
+    const float* S;                           // this layer's state [n_chars][H][d_v][d_k]
+    const float* w;                           // [channels][4], or null: no convolution
+    const __nv_bfloat16* state_in;            // [n_chars][3][channels]
+    float* rec_u;                             // [sum n][H][d_v]
+    __nv_bfloat16* rec_k;                     // [sum n][H][d_k]
+    float* rec_a;                             // [sum n][H]
+    __nv_bfloat16* rec_x;                     // [sum n][channels] (with w)
+};
+void launch_draft_gdn(const DraftGdnParams& p, int most, cudaStream_t s);
+
+// The verdict over a draft: the path that the target's probabilities accept and
+// the token after it (see draft_verify.cu).
+struct DraftVerifyParams {
+    int32_t n_chars, vocab;
+    int32_t cu[kMaxChars + 1];
+    const uint64_t* anc;                      // [sum n]
+    const int32_t* tokens;                    // [sum n]
+    const void* target;                       // [sum n][vocab]
+    const void* draft;
+    const float* u;                           // [sum n]
+    const float* u_next;                      // [n_chars]
+    int32_t* path;                            // [sum n]
+    int32_t* count;                           // [n_chars]
+    int32_t* next;                            // [n_chars]
+    int32_t* err;
+};
+void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cudaStream_t s);
+
+// Keeps one path of every character's draft: its keys and values move to the
+// live end, the delta-rule states advance along it.
+struct DraftCommitParams {
+    int32_t n_chars, n_attn, Hkv, D;
+    int32_t n_gdn, H, dk, dv, channels;       // channels: of the convolution, 0 without
+    int32_t nodes;                            // sum n
+    int32_t rec_nodes;                        // nodes a layer's records have room for
+    int64_t slab_rows;
+    __nv_bfloat16* K;                         // [n_attn][Hkv][slab_rows][D]
+    __nv_bfloat16* V;
+    int32_t* pos;                             // [slab_rows]
+    float* S;                                 // [n_gdn][n_chars][H][d_v][d_k]
+    const float* rec_u;                       // [n_gdn][rec_nodes][H][d_v]
+    const __nv_bfloat16* rec_k;
+    const float* rec_a;
+    const __nv_bfloat16* rec_x;               // [n_gdn][rec_nodes][channels]
+    __nv_bfloat16* conv_state;                // [2][n_gdn][n_chars][3][channels]
+    uint32_t conv_par[kMaxDraftLayers / 32];  // bit g: the current buffer of layer g
+    int32_t node0[kMaxChars];                 // the character's first packed node
+    int32_t slot[kMaxChars];                  // slot of its first node: slot offset + live length
+    int32_t first_pos[kMaxChars];             // its cursor
+    int32_t path_cu[kMaxChars + 1];
+    int8_t path[kMaxDraftNodes];              // the accepted nodes' indices, packed
+};
+void launch_draft_commit(const DraftCommitParams& p, cudaStream_t s);
 
 // Bytes of one (chunk, head) record of the delta-rule workspace.
 int64_t gdn_record_bytes(int dk, int dv);

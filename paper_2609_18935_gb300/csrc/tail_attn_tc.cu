@@ -132,8 +132,9 @@ __device__ __forceinline__ Tile decode_tile(const AttnParams& p, int t) {
 }
 
 // DEAL: p.waves > 0 (a kernel of its own: the segment lookup with waves cost
-// 1 % of the time where there are none)
-template <int D, bool DEAL>
+// 1 % of the time where there are none).  TREE: the tail is a draft (p.anc): a
+// row sees the live entries and, of the tail, the nodes of its ancestor word.
+template <int D, bool DEAL, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __grid_constant__ AttnParams p) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -392,7 +393,9 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             const bool has_next = seg + 1 < n_seg;
             const int tok = T.tok0 + r / g;
             const bool row_valid = tok < ch.M;
-            const int lim = ch.L_prev + min(tok, ch.M - 1) + 1;    // keys [0, lim) are visible
+            const int lim = TREE ? ch.L_prev : ch.L_prev + min(tok, ch.M - 1) + 1;    // keys [0, lim) are visible
+            unsigned long long anc = 0;                  // and of a draft the nodes in these bits
+            if constexpr (TREE) anc = p.anc[ch.tail_off + min(tok, ch.M - 1)];
             float mr = -INFINITY;                        // reference max at this group's last tile, log2 units
             float l = 0.f;                               // this group's share of the row sum, relative to it
             auto scale_to = [&](float from, float to) { return from == to ? 1.f : from == -INFINITY ? 0.f : ex2(from - to); };
@@ -410,10 +413,22 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 if (i + 1 == n && has_next) stage_q(tile_of(seg + 1));
                 const int key0 = (k + i) * BN;
                 if (key0 + BN > lim) {
+                    if constexpr (TREE) {
+                        // bit c: key key0 + c is live or an ancestor; a draft has
+                        // at most 64 nodes, so both shifts stay below 64
+                        const int at = key0 - lim;       // node of the tile's first key
+                        const unsigned long long seen = at >= 64 ? 0 : at >= 0 ? anc >> at : (anc << -at) | ((1ull << -at) - 1);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        if (key0 + c >= lim) sa[c] = 0xff800000u;                // -inf
-                        if (key0 + 32 + c >= lim) sb[c] = 0xff800000u;
+                        for (int c = 0; c < 32; ++c) {
+                            if (!((uint32_t)seen >> c & 1u)) sa[c] = 0xff800000u;
+                            if (!((uint32_t)(seen >> 32) >> c & 1u)) sb[c] = 0xff800000u;
+                        }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            if (key0 + c >= lim) sa[c] = 0xff800000u;                // -inf
+                            if (key0 + 32 + c >= lim) sb[c] = 0xff800000u;
+                        }
                     }
                 }
                 float m8[8];
@@ -566,27 +581,35 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
     }
 }
 
-template <int D, bool DEAL>
+template <int D, bool DEAL, bool TREE>
 void launch_tc(const AttnParams& p, cudaStream_t s) {
     using C = Cfg<D>;
     static unsigned long long configured = 0;   // one bit per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(configured >> (dev & 63) & 1ull)) {
-        cudaFuncSetAttribute(tail_attention_tc_kernel<D, DEAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        cudaFuncSetAttribute(tail_attention_tc_kernel<D, DEAL, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(tail_attention_tc_kernel<D, DEAL>, dim3(p.n_ctas), dim3(kThreads), C::SMEM, s, p);
+    launch_pdl(tail_attention_tc_kernel<D, DEAL, TREE>, dim3(p.n_ctas), dim3(kThreads), C::SMEM, s, p);
 }
 
+}  // namespace
+
+namespace {
+template <int D>
+void launch_d(const AttnParams& p, cudaStream_t s) {
+    if (p.anc) p.waves > 0 ? launch_tc<D, true, true>(p, s) : launch_tc<D, false, true>(p, s);
+    else p.waves > 0 ? launch_tc<D, true, false>(p, s) : launch_tc<D, false, false>(p, s);
+}
 }  // namespace
 
 void launch_tail_attention(const AttnParams& p, cudaStream_t s) {
     if (p.n_ctas <= 0) return;
     switch (p.D) {
-        case 64: p.waves > 0 ? launch_tc<64, true>(p, s) : launch_tc<64, false>(p, s); break;
-        case 128: p.waves > 0 ? launch_tc<128, true>(p, s) : launch_tc<128, false>(p, s); break;
-        case 256: p.waves > 0 ? launch_tc<256, true>(p, s) : launch_tc<256, false>(p, s); break;
+        case 64: launch_d<64>(p, s); break;
+        case 128: launch_d<128>(p, s); break;
+        case 256: launch_d<256>(p, s); break;
         default: break;   // rejected on the host
     }
 }

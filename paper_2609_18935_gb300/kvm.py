@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import sys
 
 import numpy as np
 
@@ -20,6 +21,7 @@ LIB_PATH = os.environ.get("KVM_LIB", os.path.join(_PKG, "_build", "libkvm.so"))
 KVM_OK, KVM_E_INVAL, KVM_E_SPAN, KVM_E_CAPACITY, KVM_E_CUDA, KVM_E_DEVICE, KVM_E_UNSUPPORTED = range(7)
 LAYER_GDN, LAYER_ATTN = 0, 1
 PLAN_GDN_FUSED, PLAN_GDN_STATE_CHAIN = 0, 1
+PROB_F32, PROB_BF16 = 0, 1
 
 _ERRNAMES = {1: "KVM_E_INVAL", 2: "KVM_E_SPAN", 3: "KVM_E_CAPACITY", 4: "KVM_E_CUDA",
              5: "KVM_E_DEVICE", 6: "KVM_E_UNSUPPORTED"}
@@ -116,6 +118,16 @@ _SIGS = {
     "kvm_set_plan": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32]),
     "kvm_attn_probe": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_int32, C.c_void_p, C.c_void_p]),
+    "kvm_plan_draft": (C.c_int, [C.c_int32, _HOST, _HOST, C.POINTER(C.c_int32), C.POINTER(C.c_uint64)]),
+    "kvm_plan_draft_path": (C.c_int, [C.c_int32, _HOST, _HOST, _HOST, _HOST]),
+    "kvm_draft_reserve": (C.c_int, [C.c_void_p, C.c_int32]),
+    "kvm_draft_begin": (C.c_int, [C.c_void_p, _HOST, _HOST, C.c_void_p]),
+    "kvm_draft_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "kvm_draft_gdn": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_void_p]),
+    "kvm_draft_verify": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "kvm_draft_commit": (C.c_int, [C.c_void_p, _HOST, _HOST, C.c_void_p]),
     "kvm_effective_group_count": (C.c_int, [C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
     "kvm_total_variation": (C.c_int, [C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                       C.POINTER(C.c_double)]),
@@ -125,9 +137,10 @@ _SIGS = {
 }
 
 # kernel families of kvm_profile_read
-K_COMPACT, K_ROPE_APPEND, K_ATTENTION, K_ATTN_COMBINE, K_GDN, K_GATHER, K_GDN_PREP, K_GDN_CONV = range(8)
+(K_COMPACT, K_ROPE_APPEND, K_ATTENTION, K_ATTN_COMBINE, K_GDN, K_GATHER, K_GDN_PREP, K_GDN_CONV, K_DRAFT_TREE,
+ K_DRAFT_GDN, K_DRAFT_VERIFY, K_DRAFT_COMMIT) = range(12)
 KERNEL_NAMES = ["kv_compact", "rope_append", "tail_attention", "attn_combine", "gdn_chunk_scan", "gather_map",
-                "gdn_chunk_prep", "gdn_conv"]
+                "gdn_chunk_prep", "gdn_conv", "draft_tree", "draft_gdn", "draft_verify", "draft_commit"]
 
 _lib = None
 
@@ -335,6 +348,35 @@ def plan_partition(cost, n_ranks):
     return rank_of, loads
 
 
+def _packed(cu, values, what):
+    """Offsets and packed values of a call, as bytes; their lengths have to fit."""
+    cu, values = _b32(cu), _b32(values)
+    n = int.from_bytes(cu[-4:], sys.byteorder, signed=True)
+    if len(values) != 4 * n:
+        raise ValueError(f"{what} holds {len(values) // 4} entries, its offsets end at {n}")
+    return cu, values, n
+
+
+def plan_draft(node_cu, parent):
+    """kvm_plan_draft: (depth, ancestor word) per node of the given trees; raises
+    KvmError as Context.draft_begin would."""
+    load_library()
+    cu, par, n = _packed(node_cu, parent, "parent")
+    depth, anc = np.zeros(n, np.int32), np.zeros(n, np.uint64)
+    _check(_lib.kvm_plan_draft(len(cu) // 4 - 1, cu, par, _p32(depth), anc.ctypes.data_as(C.POINTER(C.c_uint64))))
+    return depth, anc
+
+
+def plan_draft_path(node_cu, parent, path_cu, path):
+    """kvm_plan_draft_path: raises KvmError where Context.draft_commit would refuse the paths."""
+    load_library()
+    cu, par, _ = _packed(node_cu, parent, "parent")
+    pcu, nodes, _ = _packed(path_cu, path, "path")
+    if len(pcu) != len(cu):
+        raise ValueError("path_cu and node_cu differ in length")
+    _check(_lib.kvm_plan_draft_path(len(cu) // 4 - 1, cu, par, pcu, nodes))
+
+
 def pinned_layer_inputs(inputs):
     """Copy per-layer inputs into one pinned host arena per layer.
 
@@ -379,6 +421,7 @@ class Context:
         h = C.c_void_p()
         _check(lib.kvm_create(C.byref(self.desc), self.n_chars, _p32(caps), int(max_tail_tokens), C.byref(h)))
         self._h = h
+        self._draft_nodes = None
 
     def destroy(self):
         if self._h:
@@ -522,6 +565,71 @@ class Context:
                        _b32(tail_pos) if tail_pos is not None else None,
                        *((_b32(x) for x in delim) if delim is not None else (None, None, None)))
         _check(_lib.kvm_update_round(self._h, C.byref(r), _stream(stream)))
+
+    # ---------------------------------------------------------------- drafts
+    def draft_reserve(self, max_nodes):
+        """kvm_draft_reserve: room for trees of max_nodes nodes, all characters together."""
+        _check(_lib.kvm_draft_reserve(self._h, int(max_nodes)))
+
+    def draft_begin(self, node_cu, parent, stream=None):
+        """kvm_draft_begin: a step's trees (host int32 offsets [n_chars + 1] and packed parents, -1: a root)."""
+        cu, par, n = _packed(node_cu, parent, "parent")
+        if len(cu) != 4 * (self.n_chars + 1):
+            raise ValueError(f"node_cu holds {len(cu) // 4} offsets, need {self.n_chars + 1}")
+        _check(_lib.kvm_draft_begin(self._h, cu, par, _stream(stream)))
+        self._draft_nodes = n
+
+    def _draft_rows(self, **tensors):
+        """Shapes of the nodes' tensors: [nodes][..], checked because the library reads them unseen (with no draft begun
+        it refuses the call itself)."""
+        if self._draft_nodes is None:
+            return
+        for name, (t, rest) in tensors.items():
+            if tuple(t.shape) != (self._draft_nodes, *rest):
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, need {(self._draft_nodes, *rest)}")
+
+    def draft_attn(self, layer, q, k_new, v_new, out, stream=None):
+        """kvm_draft_attn: one attention layer over the open draft; q, out CUDA bf16 [nodes][Hq][D], k_new, v_new
+        [nodes][Hkv][D]."""
+        bf = _torch().bfloat16
+        heads, kv = (self.Hq, self.D), (self.Hkv, self.D)
+        self._draft_rows(q=(q, heads), k_new=(k_new, kv), v_new=(v_new, kv), out=(out, heads))
+        _check(_lib.kvm_draft_attn(self._h, layer, _dptr(q, bf), _dptr(k_new, bf), _dptr(v_new, bf), _dptr(out, bf),
+                                   _stream(stream)))
+
+    def draft_gdn(self, layer, q, k, v, alpha, beta, out, stream=None):
+        """kvm_draft_gdn: one delta-rule layer over the open draft; q, k CUDA bf16 [nodes][H][dk], v, out [nodes][H][dv],
+        alpha, beta fp32 [nodes][H]."""
+        torch = _torch()
+        bf, f = torch.bfloat16, torch.float32
+        key, val = (self.H, self.dk), (self.H, self.dv)
+        self._draft_rows(q=(q, key), k=(k, key), v=(v, val), alpha=(alpha, (self.H,)), beta=(beta, (self.H,)), out=(out, val))
+        _check(_lib.kvm_draft_gdn(self._h, layer, _dptr(q, bf), _dptr(k, bf), _dptr(v, bf), _dptr(alpha, f), _dptr(beta, f),
+                                  _dptr(out, bf), _stream(stream)))
+
+    def draft_verify(self, tokens, target, draft, u, u_next, path, count, next_token, stream=None):
+        """kvm_draft_verify: target, draft CUDA fp32 or bf16 [nodes][vocab]; tokens int32 [nodes], u fp32 [nodes], u_next
+        fp32 [n_chars]; path int32 [nodes], count and next_token int32 [n_chars] are written."""
+        torch = _torch()
+        if target.dim() != 2 or target.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("target must be [nodes][vocab] in float32 or bfloat16")
+        vocab = target.shape[1]
+        one = (self.n_chars,)
+        self._draft_rows(tokens=(tokens, ()), target=(target, (vocab,)), draft=(draft, (vocab,)), u=(u, ()), path=(path, ()))
+        for name, t in (("u_next", u_next), ("count", count), ("next_token", next_token)):
+            if tuple(t.shape) != one:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, need {one}")
+        i, f = torch.int32, torch.float32
+        _check(_lib.kvm_draft_verify(self._h, vocab, PROB_F32 if target.dtype == f else PROB_BF16, _dptr(tokens, i),
+                                     _dptr(target), _dptr(draft, target.dtype), _dptr(u, f), _dptr(u_next, f), _dptr(path, i),
+                                     _dptr(count, i), _dptr(next_token, i), _stream(stream)))
+
+    def draft_commit(self, path_cu, path, stream=None):
+        """kvm_draft_commit: keep one path of each tree (host int32 offsets [n_chars + 1] and packed node indices)."""
+        cu, nodes, _ = _packed(path_cu, path, "path")
+        if len(cu) != 4 * (self.n_chars + 1):
+            raise ValueError(f"path_cu holds {len(cu) // 4} offsets, need {self.n_chars + 1}")
+        _check(_lib.kvm_draft_commit(self._h, cu, nodes, _stream(stream)))
 
     def attn_probe(self, layer, b, q, group_of=None, n_groups=0, stream=None):
         """kvm_attn_probe: the probe distribution over character b's live
