@@ -185,6 +185,7 @@ struct kvm_ctx {
     bool draft_open = false;
     std::vector<int32_t> draft_cu, draft_parent;
     std::vector<char> draft_done;
+    std::vector<int16_t> draft_order;     // characters by decreasing number of nodes
     AttnPlan draft_plan;
     uint64_t* draft_anc = nullptr;
     int32_t* draft_pos = nullptr;
@@ -1822,6 +1823,10 @@ kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent
     c->draft_cu.assign(node_cu, node_cu + c->B + 1);
     c->draft_parent.assign(parent, parent + total);
     c->draft_done.assign(c->n_layers, 0);
+    c->draft_order.resize(c->B);
+    std::iota(c->draft_order.begin(), c->draft_order.end(), (int16_t)0);
+    std::stable_sort(c->draft_order.begin(), c->draft_order.end(),
+                     [&](int a, int b) { return node_cu[a + 1] - node_cu[a] > node_cu[b + 1] - node_cu[b]; });
     if (total > 0) {
         if (c->n_attn > 0) {
             std::vector<int> M(c->B);
@@ -1902,10 +1907,12 @@ kvm_status draft_gdn(kvm_ctx* c, int layer, const void* q, const void* k, const 
             p.state_in = conv_state_of(c, g, c->conv_par[g]);
             p.rec_x = c->draft_x + at * c->conv_ch;
         }
-        int most = 0;
-        for (int b = 0; b < c->B; ++b) most = std::max(most, c->draft_cu[b + 1] - c->draft_cu[b]);
+        p.err = c->err;
+        p.diag = c->diag;
+        for (int b = 0; b < c->B; ++b) p.order[b] = c->draft_order[b];
+        p.most = c->draft_cu[p.order[0] + 1] - c->draft_cu[p.order[0]];
         const int ps = prof_begin(c, KVM_K_DRAFT_GDN, s);
-        launch_draft_gdn(p, most, s);
+        launch_draft_gdn(p, s);
         prof_end(c, ps, s);
         LAUNCH_CHECK(c);
     }

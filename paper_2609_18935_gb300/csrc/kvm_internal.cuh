@@ -362,8 +362,12 @@ struct DraftGdnParams {
     __nv_bfloat16* rec_k;                     // [sum n][H][d_k]
     float* rec_a;                             // [sum n][H]
     __nv_bfloat16* rec_x;                     // [sum n][channels] (with w)
+    int32_t most;                             // nodes of the largest tree
+    int32_t* err;
+    int32_t* diag;                            // first expired wait: block + 1, tag, parity
+    int16_t order[kMaxChars];                 // characters by decreasing number of nodes
 };
-void launch_draft_gdn(const DraftGdnParams& p, int most, cudaStream_t s);
+void launch_draft_gdn(const DraftGdnParams& p, cudaStream_t s);
 
 // The verdict over a draft: the path that the target's probabilities accept and
 // the token after it (see draft_verify.cu).
