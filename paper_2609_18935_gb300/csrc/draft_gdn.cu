@@ -16,14 +16,21 @@
 //    of [K; Q] K^T.  Both products run on the tensor cores (tcgen05, M 128: the
 //    rows of S, of [K; Q]) into TMEM, 3 T columns.
 //  * S is fp32: 64 columns at a time, loaded as whole lines into registers while
-//    the inputs are staged, then split into three bf16 parts (24 bits, so the
-//    product is as exact as its fp32 sums: u enters the states of later steps).
-//  * C_ij = beta_i R_ij (k_i . k_j) and E_ij = R_ij (q_i . k_j), 0 off the paths,
-//    go to shared memory over the consumed parts of S.
-//  * Four warps solve for u, a thread a row of S: 16 nodes at a time, first the
-//    blocks left of the diagonal, then the triangle in registers; the other four
-//    follow with the outputs, one barrier per 16 nodes between them.  fma pairs
-//    (f32x2), coefficients as broadcast 16-byte loads: 64 for 256 multiply-adds.
+//    the inputs are staged, then split into three bf16 parts of eight bits each
+//    (by truncation: two masks and two exact differences, where rounding took
+//    conversions at an eighth of the rate and 2.9 us a block).  u enters the states
+//    of later steps, so all of S's bits take part.
+//  * C_ij = -beta_i R_ij (k_i . k_j) and E_ij = R_ij (q_i . k_j), 0 off the paths,
+//    go to shared memory over the consumed parts of S, in three and two bf16 parts.
+//  * The triangular solve and the outputs: a warp owns 16 rows of S and works
+//    through the nodes 16 at a time, u_I = (1 - C_II)^-1 (rhs_I + sum_{J < I} C_IJ u_J),
+//    o_I = G S q + sum_{J <= I} E_IJ u_J.  These are warp-wide products of 16 x 16 x
+//    16 whose left operand is the previous product's accumulator, so they run on
+//    mma.sync with u in registers: a round through TMEM and shared memory a block
+//    would cost more than the product.  (With u in registers a row a thread and
+//    the coefficients as broadcast loads, 16 bytes a lane, shared memory returned
+//    a coefficient a clock and warp: 9 us at 64 nodes, against 0.8.)  The inverses
+//    of the diagonal blocks are formed in fp32, a column a lane.
 // R_ij = G_i / G_j while no G is small, else products down the path (a decay of 0
 // is one).
 #include "kvm_internal.cuh"
@@ -38,54 +45,152 @@ using namespace ptx;
 constexpr int kThreads = 256;
 constexpr int kRowsA = 128;                      // rows of an A operand
 constexpr int kPartBytes = kRowsA * 128;         // 64 bf16 columns of S
-constexpr int kLdc = kDraftNodes + 4;            // row pitch of C and E: 16-byte rows on all banks
+constexpr int kLdc = kDraftNodes + 8;            // row pitch of C's and E's parts: fragments on all banks
+constexpr int kLdv = kRowsA + 8;                 // row pitch of v
+constexpr int kLdd = 24;                         // row pitch of the inverse diagonal blocks' parts
+constexpr int kLdf = 20;                         // row pitch of the diagonal blocks in fp32
 constexpr float kSmallDecay = 0x1p-40f;
 
 // Shared memory for trees of up to T nodes (a multiple of 16).  [K; Q] comes first:
 // as an A operand it is read up to row 127, past its own 2 T.
 struct Layout {
     int kq, v, s, misc, bytes;
-    __host__ __device__ Layout(int T, int dk) {
-        const int tile = 2 * T * dk * 2, u = T * kRowsA * 4;         // u takes the tile's place
+    __host__ __device__ Layout(int T, int dk, int raw) {       // raw: bytes of a node's unconvolved inputs, or 0
+        const int diag = T / 16 * (16 * kLdf * 4 + 3 * 16 * kLdd * 2), tile = 2 * T * dk * 2;
+        const int parts = 3 * kPartBytes, x = (T + 3) * raw;
         kq = 0;
-        v = kq + (tile > u ? tile : u);
-        s = v + T * kRowsA * 2;
-        misc = s + 3 * kPartBytes;
+        v = (max_(tile, diag) + 1023) / 1024 * 1024;
+        s = (v + T * kLdv * 2 + 1023) / 1024 * 1024;
+        misc = (s + max_(parts, x) + 1023) / 1024 * 1024;
         bytes = misc + 2048;
     }
+    static __host__ __device__ int max_(int a, int b) { return a > b ? a : b; }
 };
-static_assert(2 * kDraftNodes * kLdc * 4 <= 3 * kPartBytes, "C and E take the place of S's parts");
+static_assert(5 * kDraftNodes * kLdc * 2 <= 3 * kPartBytes, "C and E take the place of S's parts");
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* x) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[e]));
-        x[2 * e] = f.x;
-        x[2 * e + 1] = f.y;
-    }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// x -> its bf16 value, x -= that
-__device__ __forceinline__ float take_bf16(float& x) {
-    const float h = __bfloat162float(__float2bfloat16_rn(x));
-    x -= h;
-    return h;
+// The leading eight bits of a and b as a bf16 pair (a low); a and b keep the rest.
+__device__ __forceinline__ uint32_t take_part(float& a, float& b) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    a -= __uint_as_float(x & 0xffff0000u);
+    b -= __uint_as_float(y & 0xffff0000u);
+    return __byte_perm(x, y, 0x7632);
 }
 
-// acc[i] += C[i][0..15] . u[0..15] in pairs (even and odd columns apart)
-__device__ __forceinline__ void block16(f2 (&acc)[16], const float* C, const f2 (&u)[8]) {
+// D (16 x 8, fp32) += A (16 x 16, bf16) B (16 x 8, bf16): lane l holds of D rows
+// l / 4 and l / 4 + 8, columns 2 (l % 4) and the next; A's pairs are two such D
+// side by side, B's are k rows of column l / 4.
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 TMEM lanes x 16 columns, as two such D.
+__device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, float (&d)[2][4]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+    tmem_ld_wait();
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int e = 0; e < 8; ++e) d[e >> 2][e & 3] = __uint_as_float(r[e]);
+}
+// The first N of three parts of a 16 x 16 block, as A operands.
+template <int N>
+__device__ __forceinline__ void split(const float (&d)[2][4], uint32_t (&a)[N][4]) {
+    float x[2][4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(C + i * kLdc + 4 * x);
-            acc[i] = fma2(c.x, u[2 * x], acc[i]);
-            acc[i] = fma2(c.y, u[2 * x + 1], acc[i]);
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][e] = d[t][e];
+#pragma unroll
+    for (int part = 0; part < N; ++part)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            a[part][2 * t] = take_part(x[t][0], x[t][1]);
+            a[part][2 * t + 1] = take_part(x[t][2], x[t][3]);
         }
+}
+// d += (sum of a's parts) B^T, B a 16 x 16 block [column of d][k] in NB parts, the
+// products below 2^-24 (or with two parts 2^-16) of the largest left out.
+template <int NA, int NB>
+__device__ __forceinline__ void block_mma(float (&d)[2][4], const uint32_t (&a)[NA][4], const __nv_bfloat16* B, int pitch, int part_step) {
+    constexpr int LAST = NB - 1;                 // parts i of a and j of B with i + j <= LAST
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const uint32_t* b = reinterpret_cast<const uint32_t*>(B + j * part_step + (8 * t + (lane >> 2)) * pitch) + (lane & 3);
+            const uint32_t b0 = b[0], b1 = b[4];
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+                if (i + j <= LAST) mma16(d[t], a[i], b0, b1);
+        }
+}
+
+// The convolution, SiLU and (norm) the scaling to unit length of one part of the
+// staged raw rows [3 carried + nodes][pitch bytes]: four channels a lane, `per`
+// lanes a node (8, 16 or 32; lanes past dim / 4 idle), the taps in registers.
+template <typename Put>
+__device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim, const float* w, bool norm, int n,
+                                          const uint64_t* anc, Put put) {
+    const int per = dim <= 32 ? 8 : dim <= 64 ? 16 : 32;
+    const int lane = threadIdx.x % per, c = 4 * lane;
+    const bool act = c < dim;
+    float4 tap[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tap[e] = act ? *(reinterpret_cast<const float4*>(w) + c + e) : make_float4(0, 0, 0, 0);
+    for (int i0 = 0; i0 < n; i0 += kThreads / per) {
+        const int i = i0 + threadIdx.x / per;
+        float y[4] = {};
+        float sq = 0.f;
+        if (i < n && act) {
+            // tap 3 is the node, 2 its parent, .. and then the carried inputs from the last back
+            uint64_t m = anc[i];
+            const int up = __popcll(m);
+            uint2 x[4];
+#pragma unroll
+            for (int t = 3; t >= 0; --t) {
+                const int a = m ? 63 - __clzll(m) : -1;
+                m &= ~(a >= 0 ? 1ull << a : 0ull);
+                x[t] = *reinterpret_cast<const uint2*>(raw + (a >= 0 ? 3 + a : t + up - 1) * pitch + 2 * c);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[t].x));
+                const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[t].y));
+                const float f[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float tw = t == 0 ? tap[e].x : t == 1 ? tap[e].y : t == 2 ? tap[e].z : tap[e].w;
+                    y[e] = fmaf(tw, f[e], y[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float2 z = silu2(pack2(y[e], y[e + 1]));
+                y[e] = z.x;
+                y[e + 1] = z.y;
+                sq = fmaf(z.x, z.x, fmaf(z.y, z.y, sq));
+            }
+        }
+        if (norm) {                                  // whole warps run the loop
+            for (int o = per / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            const float inv = sq > 0.f ? rsqrtf(sq) : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= inv;
+        }
+        // rounded to bf16, the operands' type, as after the convolution of a tail
+        if (i < n && act) put(i, c, make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])));
+    }
 }
 
 template <int DK, bool CONV>
@@ -95,10 +200,12 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     const int b = p.order[blockIdx.y], h = blockIdx.x;
     const int n0 = p.cu[b], n = p.cu[b + 1] - n0;
     if (n <= 0) return;
-    const Layout at((p.most + 15) / 16 * 16, DK);
+    const int H = p.H, dv = p.dv, hk = H * DK;
+    const int pitch = CONV ? (2 * DK + dv) * 2 : 0;
+    const Layout at((p.most + 15) / 16 * 16, DK, pitch);
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
-    const int T = (n + 15) / 16 * 16;
+    const int T = (n + 15) / 16 * 16, NB = T / 16;
     const uint32_t region = 2 * T * 128;             // bytes of 64 columns of [K; Q]
     uint64_t* anc = reinterpret_cast<uint64_t*>(smem + at.misc);           // [64]
     float* al = reinterpret_cast<float*>(smem + at.misc + 512);            // [64] each
@@ -109,13 +216,14 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     uint32_t* slot = reinterpret_cast<uint32_t*>(smem + at.misc + 1552);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + at.misc + 1556);
     int* small = reinterpret_cast<int*>(smem + at.misc + 1560);
-    float* Cm = reinterpret_cast<float*>(smem + at.s);
-    float* Em = Cm + kDraftNodes * kLdc;
-    float* U = reinterpret_cast<float*>(smem + at.kq);                     // [T][128]
-    __nv_bfloat16* vs = reinterpret_cast<__nv_bfloat16*>(smem + at.v);     // [T][128]
+    constexpr int kPart = kDraftNodes * kLdc;        // elements of a part of C or E
+    __nv_bfloat16* Cp = reinterpret_cast<__nv_bfloat16*>(smem + at.s);     // C: three parts, blocks left of the diagonal
+    __nv_bfloat16* Ep = Cp + 3 * kPart;                                    // E: two
+    float* Cd = reinterpret_cast<float*>(smem + at.kq);                    // C's diagonal blocks [NB][16][kLdf]
+    __nv_bfloat16* Dp = reinterpret_cast<__nv_bfloat16*>(Cd + NB * 16 * kLdf);   // their inverses [NB][three parts][16][kLdd]
+    __nv_bfloat16* vs = reinterpret_cast<__nv_bfloat16*>(smem + at.v);     // [T][kLdv]
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int H = p.H, dv = p.dv, hk = H * DK;
     uint32_t cols = 32;                              // TMEM: S [K; Q]^T, then [K; Q] K^T
     while ((int)cols < 3 * T) cols *= 2;
     if (tid == 0) {
@@ -132,7 +240,35 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     grid_dependency_wait();
     grid_dependents_launch();
 
-    // ---- loads: S (in registers), the nodes' words and gates
+    // ---- loads: the inputs (asynchronously), S into registers, the nodes' words and gates
+    {
+        const __nv_bfloat16* kg = p.k + (int64_t)n0 * hk + h * DK;
+        const __nv_bfloat16* qg = p.q + (int64_t)n0 * hk + h * DK;
+        const __nv_bfloat16* vg = p.v + ((int64_t)n0 * H + h) * dv;
+        if constexpr (CONV) {
+            // raw rows q | k | v, three carried ones first
+            const int per = pitch / 16;
+            for (int e = tid; e < (n + 3) * per; e += kThreads) {
+                const int i = e / per, x = e % per, c = 8 * (x < GK ? x : x < 2 * GK ? x - GK : x - 2 * GK);
+                const void* src;
+                if (i < 3)
+                    src = p.state_in + ((int64_t)b * 3 + i) * p.channels + (x < GK ? h * DK : x < 2 * GK ? hk + h * DK : 2 * hk + h * dv) + c;
+                else
+                    src = x < 2 * GK ? (x < GK ? qg : kg) + (int64_t)(i - 3) * hk + c : vg + (int64_t)(i - 3) * H * dv + c;
+                cp_async16(base + at.s + i * pitch + 16 * x, src);
+            }
+        } else {
+            for (int e = tid; e < 2 * n * GK; e += kThreads) {
+                const int row = e / GK, c = 8 * (e % GK);
+                const bool is_k = row < n;
+                const int i = is_k ? row : row - n;
+                cp_async16(base + at.kq + sw128_off16(is_k ? i : T + i, c, 2 * T), (is_k ? kg : qg) + (int64_t)i * hk + c);
+            }
+            const int gv = dv / 8;
+            for (int e = tid; e < n * gv; e += kThreads)
+                cp_async16(base + at.v + ((e / gv) * kLdv + 8 * (e % gv)) * 2, vg + (int64_t)(e / gv) * H * dv + 8 * (e % gv));
+        }
+    }
     const float* Sg = p.S + ((int64_t)b * H + h) * dv * DK;
     float4 s[HALVES][8];
 #pragma unroll
@@ -149,73 +285,31 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         be[tid] = p.beta[(int64_t)(n0 + tid) * H + h];
         p.rec_a[(int64_t)(n0 + tid) * H + h] = a;
     }
+    cp_async_wait();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *slot;
     const uint32_t tg = tmem + 2 * T;
 
-    // ---- stage k, q, v, eight channels a piece: k rows, then q rows, then v rows
-    {
-        const int nk = n * GK, all = 2 * nk + n * (dv / 8);
-        for (int e0 = 0; e0 < all; e0 += kThreads) {
-            const int e = e0 + tid;
-            const bool act = e < all, is_k = e < nk, is_v = e >= 2 * nk;
-            const int x = is_k ? e : is_v ? e - 2 * nk : e - nk;
-            const int per = is_v ? dv / 8 : GK;
-            const int i = act ? x / per : 0, c = act ? 8 * (x % per) : 0;
-            const __nv_bfloat16* in = (is_v ? p.v : is_k ? p.k : p.q) + (is_v ? h * dv : h * DK) + c;
-            const int64_t stride = is_v ? (int64_t)H * dv : hk;
-            uint4 val = *reinterpret_cast<const uint4*>(in + (int64_t)(n0 + i) * stride);
-            if constexpr (CONV) {
-                // taps 3, 2, .. are the node, its parent, .. and then the carried inputs from the last back
-                const int ch = (is_v ? 2 * hk + h * dv : is_k ? hk + h * DK : h * DK) + c;
-                if (act) *reinterpret_cast<uint4*>(p.rec_x + (int64_t)(n0 + i) * p.channels + ch) = val;
-                unsigned long long m = anc[i];
-                const int up = __popcll(m);
-                uint4 r[4];
-                r[3] = val;
-                m &= ~(1ull << i);
-#pragma unroll
-                for (int t = 2; t >= 0; --t) {
-                    const int a = m ? 63 - __clzll(m) : -1;
-                    m &= ~(a >= 0 ? 1ull << a : 0ull);
-                    r[t] = *reinterpret_cast<const uint4*>(
-                        a >= 0 ? in + (int64_t)(n0 + a) * stride : p.state_in + ((int64_t)b * 3 + t + up - 1) * p.channels + ch);
-                }
-                float y[8] = {};
-                float f[4][8];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) unpack8(r[t], f[t]);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float4 w = *(reinterpret_cast<const float4*>(p.w) + ch + q);
-                    y[q] = fmaf(w.w, f[3][q], fmaf(w.z, f[2][q], fmaf(w.y, f[1][q], w.x * f[0][q])));
-                }
-                float sq = 0.f;
-#pragma unroll
-                for (int q = 0; q < 8; q += 2) {
-                    const float2 z = silu2(pack2(y[q], y[q + 1]));
-                    y[q] = z.x;
-                    y[q + 1] = z.y;
-                    sq = fmaf(z.x, z.x, fmaf(z.y, z.y, sq));
-                }
-                // a k row's GK lanes are neighbours (whole warps run this loop)
-#pragma unroll
-                for (int o = GK / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                const float inv = !is_k ? 1.f : sq > 0.f ? rsqrtf(sq) : 0.f;
-                // rounded to bf16, the operands' type, as after the convolution of a tail
-                val = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                                 pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
-            }
-            if (!act) continue;
-            if (is_v) {
-                *reinterpret_cast<uint4*>(vs + i * kRowsA + c) = val;
-            } else {
-                *reinterpret_cast<uint4*>(smem + at.kq + sw128_off16(is_k ? i : T + i, c, 2 * T)) = val;
-                if (is_k) *reinterpret_cast<uint4*>(p.rec_k + ((int64_t)(n0 + i) * H + h) * DK + c) = val;
-            }
+    if constexpr (CONV) {
+        const uint8_t* raw = smem + at.s;
+        const int per = pitch / 16;
+        for (int e = tid; e < n * per; e += kThreads) {                    // what a commit carries on
+            const int i = e / per, x = e % per, c = 8 * (x < GK ? x : x < 2 * GK ? x - GK : x - 2 * GK);
+            *reinterpret_cast<uint4*>(p.rec_x + (int64_t)(n0 + i) * p.channels + (x < GK ? h * DK : x < 2 * GK ? hk + h * DK : 2 * hk + h * dv) + c) =
+                *reinterpret_cast<const uint4*>(raw + (3 + i) * pitch + 16 * x);
         }
+        conv_part(raw, pitch, DK, p.w + (int64_t)(h * DK) * 4, false, n, anc, [&](int i, int c, uint2 y) {
+            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(T + i, c, 2 * T)) = y;
+        });
+        conv_part(raw + 2 * DK, pitch, DK, p.w + (int64_t)(hk + h * DK) * 4, true, n, anc, [&](int i, int c, uint2 y) {
+            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(i, c, 2 * T)) = y;
+        });
+        conv_part(raw + 4 * DK, pitch, dv, p.w + (int64_t)(2 * hk + h * dv) * 4, false, n, anc, [&](int i, int c, uint2 y) {
+            *reinterpret_cast<uint2*>(vs + i * kLdv + c) = y;
+        });
+        __syncthreads();                             // the raw rows make room for S's parts
     }
     // ---- the products, 64 columns of S at a time
     bool ok = true;
@@ -229,8 +323,8 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
             float4 v = s[x][e];
 #pragma unroll
             for (int part = 0; part < 3; ++part) {
-                const float a = take_bf16(v.x), c = take_bf16(v.y), d = take_bf16(v.z), f = take_bf16(v.w);
-                *reinterpret_cast<uint2*>(smem + at.s + part * kPartBytes + o) = make_uint2(pack_bf16(a, c), pack_bf16(d, f));
+                const uint32_t lo = take_part(v.x, v.y), hi = take_part(v.z, v.w);
+                *reinterpret_cast<uint2*>(smem + at.s + part * kPartBytes + o) = make_uint2(lo, hi);
             }
         }
         fence_proxy_async_smem();
@@ -241,17 +335,22 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
             const uint64_t sd = smem_desc_sw128(base + at.s, 16, 1024);
             const uint32_t id_s = idesc_bf16_f32(kRowsA, 2 * T, false), id_g = idesc_bf16_f32(kRowsA, T, false);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                mma_bf16(tg, kq + 2 * ks, kq + 2 * ks, id_g, (x > 0 || ks > 0) ? 1u : 0u);
-#pragma unroll
             for (int part = 0; part < 3; ++part)
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks)
                     mma_bf16(tmem, sd + ((part * kPartBytes) >> 4) + 2 * ks, kq + 2 * ks, id_s, (x > 0 || part > 0 || ks > 0) ? 1u : 0u);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                mma_bf16(tg, kq + 2 * ks, kq + 2 * ks, id_g, (x > 0 || ks > 0) ? 1u : 0u);
             mma_commit(bar + 8 * x);
         }
     }
-    // ---- decays from the root, while the products run
+    // ---- while the products run: the keys' record, and the decays from the root
+    for (int e = tid; e < n * GK; e += kThreads) {
+        const int i = e / GK, c = 8 * (e % GK);
+        *reinterpret_cast<uint4*>(p.rec_k + ((int64_t)(n0 + i) * H + h) * DK + c) =
+            *reinterpret_cast<const uint4*>(smem + at.kq + sw128_off16(i, c, 2 * T));
+    }
     if (tid < kDraftNodes) {
         float g = 1.f;
         if (tid < n) {
@@ -265,117 +364,127 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     ok = ok && mbar_wait(bar + 8 * (HALVES - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x62);
     ok = __syncthreads_and(ok);
     tc_fence_after();
-    const int quarter = warp & 3, half = warp >> 2;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     if (ok) {
         // ---- C and E: lane l of the product holds k row l, or q row l - T; the two warps of a quarter take 16 columns in turn
-        const int l = quarter * 32 + lane;
+        const int l = (warp & 3) * 32 + lane;
         const bool is_c = l < T, real = l < 2 * T && (is_c ? l : l - T) < n;
-        const int i = is_c ? l : l - T;
-        float* row = (is_c ? Cm : Em) + i * kLdc;
+        const int i = is_c ? l : l - T, I = i / 16;
         const bool exact = *small != 0;
         uint64_t m = real ? anc[i] : 0;
         if (is_c) m &= ~(1ull << i);                 // C is strict
-        const float scale = real ? (is_c ? be[i] : 1.f) : 0.f;
-        for (int c0 = 16 * half; c0 < T; c0 += 32) {
+        const float scale = real ? (is_c ? -be[i] : 1.f) * (exact ? 1.f : G[i]) : 0.f;
+        for (int J = warp >> 2; J < NB; J += 2) {
             uint32_t g[16];
-            tmem_ld16(lanes + 2 * T + c0, g);
+            tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T + 16 * J, g);
             tmem_ld_wait();
-            if (l >= 2 * T) continue;
+            if (l >= 2 * T || J > I) continue;
+            float y[16];
+            if (!exact) {
 #pragma unroll
-            for (int c = 0; c < 16; c += 4) {
-                float y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = c0 + c + e;
-                    float R = scale;
-                    if (!exact && real) R *= G[i] * rG[j];
-                    y[e] = (m >> j & 1) ? R * __uint_as_float(g[c + e]) : 0.f;
+                for (int c = 0; c < 16; ++c)
+                    y[c] = (m >> (16 * J + c) & 1) ? scale * rG[16 * J + c] * __uint_as_float(g[c]) : 0.f;
+            } else {
+                // some decay is small: the product down the path, which reaches this block's nodes from the largest down
+                float R = scale;
+                for (uint64_t a = real ? anc[i] >> (16 * J + 15) >> 1 : 0; a;) {
+                    const int j = 63 - __clzll((long long)a);
+                    a &= ~(1ull << j);
+                    R *= al[16 * J + 16 + j];
                 }
-                *reinterpret_cast<float4*>(row + c0 + c) = make_float4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+                for (int c = 15; c >= 0; --c) {
+                    y[c] = (m >> (16 * J + c) & 1) ? R * __uint_as_float(g[c]) : 0.f;
+                    if (real && (anc[i] >> (16 * J + c) & 1)) R *= al[16 * J + c];
+                }
+            }
+            if (is_c && J == I) {
+                float* row = Cd + (I * 16 + (i & 15)) * kLdf;
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(row + c) = make_float4(y[c], y[c + 1], y[c + 2], y[c + 3]);
+            } else {
+                __nv_bfloat16* row = (is_c ? Cp : Ep) + i * kLdc + 16 * J;
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    if (part == 2 && !is_c) break;
+                    uint32_t w[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) w[c] = take_part(y[2 * c], y[2 * c + 1]);
+                    uint4* dst = reinterpret_cast<uint4*>(row + part * kPart);
+                    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                }
             }
         }
     }
     __syncthreads();
-    if (ok && *small != 0) {
-        // some decay is small: the products down each path, node by node
-        if (tid < 2 * T) {
-            const bool is_c = tid < T;
-            const int i = is_c ? tid : tid - T;
-            float* row = (is_c ? Cm : Em) + i * kLdc;
-            float R = 1.f;
-            for (uint64_t m = i < n ? anc[i] : 0; m;) {
-                const int j = 63 - __clzll((long long)m);
-                m &= ~(1ull << j);
-                row[j] *= R;
-                R *= al[j];
-            }
+    if (ok && warp < NB) {
+        // ---- (1 - C_II)^-1, block `warp`: column `lane` by forward substitution
+        const int j = lane & 15;
+        const float* C = Cd + warp * 16 * kLdf;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float t[2] = {i == j ? 1.f : 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < i; ++m) t[m & 1] = fmaf(C[i * kLdf + m], x[m], t[m & 1]);
+            x[i] = t[0] + t[1];
         }
-        __syncthreads();
+        if (lane < 16) {
+            __nv_bfloat16* D = Dp + warp * 3 * 16 * kLdd + j;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    const uint32_t w = take_part(x[i], x[i + 1]);
+                    D[(part * 16 + i) * kLdd] = __ushort_as_bfloat16((unsigned short)w);
+                    D[(part * 16 + i + 1) * kLdd] = __ushort_as_bfloat16((unsigned short)(w >> 16));
+                }
+        }
     }
+    __syncthreads();
     if (ok) {
-        const int r = quarter * 32 + lane;           // row of S
-        const int NB = T / 16;
-        if (half == 0) {
-            // ---- u
-            for (int I = 0; I < NB; ++I) {
-                uint32_t a[16];
-                tmem_ld16(lanes + 16 * I, a);
-                f2 acc[16] = {};
-                for (int J = 0; J < I; ++J) {
-                    f2 u[8];
+        // ---- u and the outputs: this warp's rows of S are TMEM lanes 32 (warp % 4) + 16 (warp / 4) ..
+        const int r0 = (warp & 3) * 32 + (warp >> 2) * 16;
+        const uint32_t lanes = tmem + ((uint32_t)r0 << 16);
+        const int row = r0 + (lane >> 2), col = 2 * (lane & 3);
+        uint32_t u[4][3][4];                         // the parts of each block's u
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) u[x] = pack2(U[(16 * J + 2 * x) * kRowsA + r], U[(16 * J + 2 * x + 1) * kRowsA + r]);
-                    block16(acc, Cm + 16 * I * kLdc + 16 * J, u);
-                }
-                tmem_ld_wait();
-                float u[16];
+        for (int I = 0; I < 4; ++I) {
+            if (I >= NB) break;
+            float x[2][4], o[2][4];
+            tmem_ld_16x16(lanes + 16 * I, x);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int node = 16 * I + i;
-                    const float2 t = unpack2(acc[i]);
-                    const float v = __bfloat162float(vs[node * kRowsA + r]);
-                    const float x = be[node] * (v - G[node] * __uint_as_float(a[i])) - (t.x + t.y);
-                    u[i] = node < n ? x : 0.f;       // a padding row holds anything
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int node = 16 * I + 8 * t + col + (e & 1), r = row + 8 * (e >> 1);
+                    const float v = __bfloat162float(vs[node * kLdv + r]);
+                    x[t][e] = node < n ? be[node] * (v - G[node] * x[t][e]) : 0.f;      // a padding row holds anything
                 }
 #pragma unroll
-                for (int i = 1; i < 16; ++i)
+            for (int J = 0; J < I; ++J) block_mma<3, 3>(x, u[J], Cp + 16 * I * kLdc + 16 * J, kLdc, kPart);
+            split(x, u[I]);
+            float y[2][4] = {};
+            block_mma<3, 3>(y, u[I], Dp + I * 3 * 16 * kLdd, kLdd, 16 * kLdd);
+            split(y, u[I]);
+            tmem_ld_16x16(lanes + T + 16 * I, o);
 #pragma unroll
-                    for (int j = 0; j < i; ++j) u[i] = fmaf(-Cm[(16 * I + i) * kLdc + 16 * I + j], u[j], u[i]);
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) U[(16 * I + i) * kRowsA + r] = u[i];
-                named_bar_arrive(1 + I, kThreads);
-                if (r < dv) {
-                    float* rec = p.rec_u + ((int64_t)(n0 + 16 * I) * H + h) * dv + r;
+                for (int e = 0; e < 4; ++e) o[t][e] *= G[16 * I + 8 * t + col + (e & 1)];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (16 * I + i < n) rec[(int64_t)i * H * dv] = u[i];
-                }
+            for (int J = 0; J <= I; ++J) {
+                const uint32_t (&a)[2][4] = *reinterpret_cast<const uint32_t (*)[2][4]>(&u[J]);
+                block_mma<2, 2>(o, a, Ep + 16 * I * kLdc + 16 * J, kLdc, kPart);
             }
-        } else {
-            // ---- outputs
-            for (int I = 0; I < NB; ++I) {
-                uint32_t a[16];
-                tmem_ld16(lanes + T + 16 * I, a);
-                f2 acc[16] = {};
-                for (int J = 0; J <= I; ++J) {
-                    if (J == I) named_bar_sync(1 + I, kThreads);
-                    f2 u[8];
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) u[x] = pack2(U[(16 * J + 2 * x) * kRowsA + r], U[(16 * J + 2 * x + 1) * kRowsA + r]);
-                    block16(acc, Em + 16 * I * kLdc + 16 * J, u);
-                }
-                tmem_ld_wait();
-                if (r < dv) {
-                    __nv_bfloat16* out = p.out + ((int64_t)(n0 + 16 * I) * H + h) * dv + r;
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float2 t = unpack2(acc[i]);
-                        if (16 * I + i < n)
-                            out[(int64_t)i * H * dv] = __float2bfloat16_rn(fmaf(G[16 * I + i], __uint_as_float(a[i]), t.x + t.y));
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int node = 16 * I + 8 * t + col + (e & 1), r = row + 8 * (e >> 1);
+                    vs[node * kLdv + r] = __float2bfloat16_rn(o[t][e]);                 // in v's place, read by this lane alone
+                    if (node < n && r < dv) p.rec_u[((int64_t)(n0 + node) * H + h) * dv + r] = y[t][e];
                 }
-            }
         }
     } else if (*abort_flag) {
         // what was issued completes before TMEM and shared memory are released
@@ -384,6 +493,12 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     }
     tc_fence_before();
     __syncthreads();
+    if (ok) {
+        const int gv = dv / 8;
+        for (int e = tid; e < n * gv; e += kThreads)
+            *reinterpret_cast<uint4*>(p.out + ((int64_t)(n0 + e / gv) * H + h) * dv + 8 * (e % gv)) =
+                *reinterpret_cast<const uint4*>(vs + (e / gv) * kLdv + 8 * (e % gv));
+    }
     if (warp == 0) {
         tc_fence_after();
         tmem_dealloc(tmem, cols);
@@ -392,14 +507,16 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
 
 template <int DK, bool CONV>
 void launch(const DraftGdnParams& p, cudaStream_t s) {
+    const int pitch = CONV ? (2 * DK + p.dv) * 2 : 0;
     static unsigned long long configured = 0;    // one bit per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(configured >> (dev & 63) & 1ull)) {
-        cudaFuncSetAttribute(draft_gdn_kernel<DK, CONV>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout(kDraftNodes, DK).bytes + 1024);
+        cudaFuncSetAttribute(draft_gdn_kernel<DK, CONV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             Layout(kDraftNodes, DK, CONV ? (2 * DK + 128) * 2 : 0).bytes + 1024);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(draft_gdn_kernel<DK, CONV>, dim3(p.H, p.n_chars), dim3(kThreads), Layout((p.most + 15) / 16 * 16, DK).bytes + 1024, s, p);
+    launch_pdl(draft_gdn_kernel<DK, CONV>, dim3(p.H, p.n_chars), dim3(kThreads), Layout((p.most + 15) / 16 * 16, DK, pitch).bytes + 1024, s, p);
 }
 
 }  // namespace
