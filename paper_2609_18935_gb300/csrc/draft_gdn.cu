@@ -102,6 +102,16 @@ __device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, float (&d)[2][4]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e >> 2][e & 3] = __uint_as_float(r[e]);
 }
+// d += lo, lo = 0
+__device__ __forceinline__ void join(float (&d)[2][4], float (&lo)[2][4]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            d[t][e] += lo[t][e];
+            lo[t][e] = 0.f;
+        }
+}
 // The first N of three parts of a 16 x 16 block, as A operands.
 template <int N>
 __device__ __forceinline__ void split(const float (&d)[2][4], uint32_t (&a)[N][4]) {
@@ -119,77 +129,95 @@ __device__ __forceinline__ void split(const float (&d)[2][4], uint32_t (&a)[N][4
         }
 }
 // d += (sum of a's parts) B^T, B a 16 x 16 block [column of d][k] in NB parts, the
-// products below 2^-24 (or with two parts 2^-16) of the largest left out.
+// products below 2^-24 (or with two parts 2^-16) of the largest left out.  Small
+// products are summed apart (lo): four chains of dependent products instead of one.
 template <int NA, int NB>
-__device__ __forceinline__ void block_mma(float (&d)[2][4], const uint32_t (&a)[NA][4], const __nv_bfloat16* B, int pitch, int part_step) {
+__device__ __forceinline__ void block_mma(float (&d)[2][4], float (&lo)[2][4], const uint32_t (&a)[NA][4], const __nv_bfloat16* B,
+                                          int pitch, int part_step) {
     constexpr int LAST = NB - 1;                 // parts i of a and j of B with i + j <= LAST
     const int lane = threadIdx.x & 31;
+    const uint32_t* b = reinterpret_cast<const uint32_t*>(B + (lane >> 2) * pitch) + (lane & 3);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int j = 0; j < NB; ++j) {
+        uint32_t f[2][2];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const uint32_t* b = reinterpret_cast<const uint32_t*>(B + j * part_step + (8 * t + (lane >> 2)) * pitch) + (lane & 3);
-            const uint32_t b0 = b[0], b1 = b[4];
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-                if (i + j <= LAST) mma16(d[t], a[i], b0, b1);
+        for (int t = 0; t < 2; ++t) {
+            f[t][0] = b[(j * part_step + 8 * t * pitch) / 2];
+            f[t][1] = b[(j * part_step + 8 * t * pitch) / 2 + 4];
         }
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                if (i + j <= LAST) mma16(i + j == 0 ? d[t] : lo[t], a[i], f[t][0], f[t][1]);
+    }
 }
 
 // The convolution, SiLU and (norm) the scaling to unit length of one part of the
 // staged raw rows [3 carried + nodes][pitch bytes]: four channels a lane, `per`
-// lanes a node (8, 16 or 32; lanes past dim / 4 idle), the taps in registers.
+// lanes a node (8, 16 or 32; lanes past dim / 4 idle), the taps in registers, four
+// nodes a thread at a time.  taps: per node the staged rows of its four taps, a
+// byte each.
+constexpr int kAhead = 4;
+// x / (1 + e^-x) with approximate exponential and reciprocal: within 2^-21, and the
+// result is rounded to eight bits (from -88.7 down, where it is below 2^-121, 0).
+__device__ __forceinline__ float silu(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
+    return x * r;
+}
+__device__ __forceinline__ int conv_lanes(int dim) { return dim <= 32 ? 8 : dim <= 64 ? 16 : 32; }
+__device__ __forceinline__ void conv_taps(float4 (&tap)[4], int dim, const float* w) {
+    const int c = 4 * (threadIdx.x % conv_lanes(dim));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tap[e] = c < dim ? *(reinterpret_cast<const float4*>(w) + c + e) : make_float4(0, 0, 0, 0);
+}
 template <typename Put>
-__device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim, const float* w, bool norm, int n,
-                                          const uint64_t* anc, Put put) {
-    const int per = dim <= 32 ? 8 : dim <= 64 ? 16 : 32;
-    const int lane = threadIdx.x % per, c = 4 * lane;
+__device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim, const float4 (&tap)[4], bool norm, int n,
+                                          const uint32_t* taps, Put put) {
+    const int per = conv_lanes(dim);
+    const int lane = threadIdx.x % per, c = 4 * lane, step = kThreads / per;
     const bool act = c < dim;
-    float4 tap[4];
+    raw += act ? 2 * c : 0;
+    for (int i0 = threadIdx.x / per; i0 - (int)threadIdx.x / per < n; i0 += kAhead * step) {
+        uint2 x[kAhead][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) tap[e] = act ? *(reinterpret_cast<const float4*>(w) + c + e) : make_float4(0, 0, 0, 0);
-    for (int i0 = 0; i0 < n; i0 += kThreads / per) {
-        const int i = i0 + threadIdx.x / per;
-        float y[4] = {};
-        float sq = 0.f;
-        if (i < n && act) {
-            // tap 3 is the node, 2 its parent, .. and then the carried inputs from the last back
-            uint64_t m = anc[i];
-            const int up = __popcll(m);
-            uint2 x[4];
+        for (int a = 0; a < kAhead; ++a) {
+            const uint32_t rows = taps[min(i0 + a * step, n - 1)];
 #pragma unroll
-            for (int t = 3; t >= 0; --t) {
-                const int a = m ? 63 - __clzll(m) : -1;
-                m &= ~(a >= 0 ? 1ull << a : 0ull);
-                x[t] = *reinterpret_cast<const uint2*>(raw + (a >= 0 ? 3 + a : t + up - 1) * pitch + 2 * c);
-            }
+            for (int t = 0; t < 4; ++t) x[a][t] = *reinterpret_cast<const uint2*>(raw + (rows >> (8 * t) & 255) * pitch);
+        }
+        float y[kAhead][4], sq[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            f2 lo = 0, hi = 0;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[t].x));
-                const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[t].y));
-                const float f[4] = {lo.x, lo.y, hi.x, hi.y};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float tw = t == 0 ? tap[e].x : t == 1 ? tap[e].y : t == 2 ? tap[e].z : tap[e].w;
-                    y[e] = fmaf(tw, f[e], y[e]);
-                }
+                const float2 l = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[a][t].x));
+                const float2 h = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[a][t].y));
+                auto at = [&](const float4& f) { return t == 0 ? f.x : t == 1 ? f.y : t == 2 ? f.z : f.w; };
+                lo = fma2(pack2(at(tap[0]), at(tap[1])), pack2(l.x, l.y), lo);
+                hi = fma2(pack2(at(tap[2]), at(tap[3])), pack2(h.x, h.y), hi);
             }
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                const float2 z = silu2(pack2(y[e], y[e + 1]));
-                y[e] = z.x;
-                y[e + 1] = z.y;
-                sq = fmaf(z.x, z.x, fmaf(z.y, z.y, sq));
-            }
+            const float2 l = unpack2(lo), h = unpack2(hi);
+            y[a][0] = silu(l.x); y[a][1] = silu(l.y); y[a][2] = silu(h.x); y[a][3] = silu(h.y);
+            sq[a] = act ? fmaf(y[a][0], y[a][0], fmaf(y[a][1], y[a][1], fmaf(y[a][2], y[a][2], y[a][3] * y[a][3]))) : 0.f;
         }
         if (norm) {                                  // whole warps run the loop
-            for (int o = per / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-            const float inv = sq > 0.f ? rsqrtf(sq) : 0.f;
+            for (int o = per / 2; o > 0; o >>= 1)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] *= inv;
+                for (int a = 0; a < kAhead; ++a) sq[a] += __shfl_xor_sync(0xffffffffu, sq[a], o);
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const float inv = sq[a] > 0.f ? rsqrtf(sq[a]) : 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[a][e] *= inv;
+            }
         }
         // rounded to bf16, the operands' type, as after the convolution of a tail
-        if (i < n && act) put(i, c, make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])));
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (act && i0 + a * step < n) put(i0 + a * step, c, make_uint2(pack_bf16(y[a][0], y[a][1]), pack_bf16(y[a][2], y[a][3])));
     }
 }
 
@@ -212,10 +240,11 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     float* be = al + kDraftNodes;
     float* G = be + kDraftNodes;
     float* rG = G + kDraftNodes;
-    const uint32_t bar = base + at.misc + 1536;                            // two barriers, one per half of S
-    uint32_t* slot = reinterpret_cast<uint32_t*>(smem + at.misc + 1552);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + at.misc + 1556);
-    int* small = reinterpret_cast<int*>(smem + at.misc + 1560);
+    const uint32_t bar = base + at.misc + 1536;                            // one barrier per half of S, one of the raw rows
+    uint32_t* slot = reinterpret_cast<uint32_t*>(smem + at.misc + 1560);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + at.misc + 1564);
+    int* small = reinterpret_cast<int*>(smem + at.misc + 1568);
+    uint32_t* taps = reinterpret_cast<uint32_t*>(smem + at.misc + 1572);   // [64]
     constexpr int kPart = kDraftNodes * kLdc;        // elements of a part of C or E
     __nv_bfloat16* Cp = reinterpret_cast<__nv_bfloat16*>(smem + at.s);     // C: three parts, blocks left of the diagonal
     __nv_bfloat16* Ep = Cp + 3 * kPart;                                    // E: two
@@ -229,14 +258,14 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     if (tid == 0) {
         *abort_flag = 0;
         *small = 0;
-        mbar_init(bar, 1);
-        mbar_init(bar + 8, 1);
+        for (int x = 0; x < 3; ++x) mbar_init(bar + 8 * x, 1);
         fence_mbar_init();
     }
     if (warp == 0) {
         tmem_alloc(smem_u32(slot), cols);
         tmem_relinquish();
     }
+    if constexpr (CONV) __syncthreads();             // the barrier that the raw rows arrive at
     grid_dependency_wait();
     grid_dependents_launch();
 
@@ -246,16 +275,17 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         const __nv_bfloat16* qg = p.q + (int64_t)n0 * hk + h * DK;
         const __nv_bfloat16* vg = p.v + ((int64_t)n0 * H + h) * dv;
         if constexpr (CONV) {
-            // raw rows q | k | v, three carried ones first
-            const int per = pitch / 16;
-            for (int e = tid; e < (n + 3) * per; e += kThreads) {
-                const int i = e / per, x = e % per, c = 8 * (x < GK ? x : x < 2 * GK ? x - GK : x - 2 * GK);
-                const void* src;
-                if (i < 3)
-                    src = p.state_in + ((int64_t)b * 3 + i) * p.channels + (x < GK ? h * DK : x < 2 * GK ? hk + h * DK : 2 * hk + h * dv) + c;
-                else
-                    src = x < 2 * GK ? (x < GK ? qg : kg) + (int64_t)(i - 3) * hk + c : vg + (int64_t)(i - 3) * H * dv + c;
-                cp_async16(base + at.s + i * pitch + 16 * x, src);
+            // raw rows q | k | v, three carried ones first: a thread's bulk copies a row
+            if (tid == 0) mbar_arrive_expect_tx(bar + 16, (uint32_t)((n + 3) * pitch));
+            __syncwarp();
+            if (tid < n + 3) {
+                const __nv_bfloat16* st = p.state_in + ((int64_t)b * 3 + tid) * p.channels;
+                const bool old = tid < 3;
+                const int i = tid - 3;
+                const uint32_t dst = base + at.s + tid * pitch;
+                bulk_load(dst, old ? st + h * DK : qg + (int64_t)i * hk, DK * 2, bar + 16);
+                bulk_load(dst + 2 * DK, old ? st + hk + h * DK : kg + (int64_t)i * hk, DK * 2, bar + 16);
+                bulk_load(dst + 4 * DK, old ? st + 2 * hk + h * dv : vg + (int64_t)i * H * dv, dv * 2, bar + 16);
             }
         } else {
             for (int e = tid; e < 2 * n * GK; e += kThreads) {
@@ -264,22 +294,47 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                 const int i = is_k ? row : row - n;
                 cp_async16(base + at.kq + sw128_off16(is_k ? i : T + i, c, 2 * T), (is_k ? kg : qg) + (int64_t)i * hk + c);
             }
-            const int gv = dv / 8;
-            for (int e = tid; e < n * gv; e += kThreads)
-                cp_async16(base + at.v + ((e / gv) * kLdv + 8 * (e % gv)) * 2, vg + (int64_t)(e / gv) * H * dv + 8 * (e % gv));
+            if ((tid & 15) * 8 < dv)
+                for (int i = tid >> 4; i < n; i += kThreads / 16)
+                    cp_async16(base + at.v + (i * kLdv + 8 * (tid & 15)) * 2, vg + (int64_t)i * H * dv + 8 * (tid & 15));
         }
     }
     const float* Sg = p.S + ((int64_t)b * H + h) * dv * DK;
     float4 s[HALVES][8];
+    auto load_s = [&]() {
 #pragma unroll
-    for (int x = 0; x < HALVES; ++x)
+        for (int x = 0; x < HALVES; ++x)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
-            s[x][e] = row < dv ? *reinterpret_cast<const float4*>(Sg + (int64_t)row * DK + 64 * x + 4 * c4) : make_float4(0, 0, 0, 0);
-        }
+            for (int e = 0; e < 8; ++e) {
+                const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
+                s[x][e] = row < dv ? *reinterpret_cast<const float4*>(Sg + (int64_t)row * DK + 64 * x + 4 * c4) : make_float4(0, 0, 0, 0);
+            }
+    };
+    // the convolution needs the registers: there S comes after it, from L2
+    float4 tk[4], tq[4], tv[4];
+    if constexpr (CONV) {
+        for (int e = tid * 32; e < dv * DK; e += kThreads * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(Sg + e));
+        conv_taps(tk, DK, p.w + (int64_t)(hk + h * DK) * 4);
+        conv_taps(tq, DK, p.w + (int64_t)(h * DK) * 4);
+        conv_taps(tv, dv, p.w + (int64_t)(2 * hk + h * dv) * 4);
+    } else {
+        load_s();
+    }
     if (tid < n) {
-        anc[tid] = p.anc[n0 + tid];
+        const uint64_t own = p.anc[n0 + tid];
+        anc[tid] = own;
+        if constexpr (CONV) {
+            // staged rows of the taps: 3 is the node, 2 its parent, .. and then the carried inputs from the last back
+            uint64_t m = own;
+            uint32_t rows = 0;
+#pragma unroll
+            for (int t = 3; t >= 0; --t) {
+                const int a = m ? 63 - __clzll((long long)m) : -1;
+                m &= ~(a >= 0 ? 1ull << a : 0ull);
+                rows |= (uint32_t)(a >= 0 ? 3 + a : t + __popcll(own) - 1) << (8 * t);
+            }
+            taps[tid] = rows;
+        }
         const float a = p.alpha[(int64_t)(n0 + tid) * H + h];
         al[tid] = a;
         be[tid] = p.beta[(int64_t)(n0 + tid) * H + h];
@@ -291,31 +346,36 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = *slot;
     const uint32_t tg = tmem + 2 * T;
+    bool ok = true;
 
     if constexpr (CONV) {
         const uint8_t* raw = smem + at.s;
-        const int per = pitch / 16;
-        for (int e = tid; e < n * per; e += kThreads) {                    // what a commit carries on
-            const int i = e / per, x = e % per, c = 8 * (x < GK ? x : x < 2 * GK ? x - GK : x - 2 * GK);
-            *reinterpret_cast<uint4*>(p.rec_x + (int64_t)(n0 + i) * p.channels + (x < GK ? h * DK : x < 2 * GK ? hk + h * DK : 2 * hk + h * dv) + c) =
-                *reinterpret_cast<const uint4*>(raw + (3 + i) * pitch + 16 * x);
+        ok = mbar_wait(bar + 16, 0, abort_flag, p.err, kErrWait, p.diag, 0x60);
+        if (tid < n && ok) {                         // what a commit carries on
+            __nv_bfloat16* rec = p.rec_x + (int64_t)(n0 + tid) * p.channels;
+            const uint32_t src = base + at.s + (3 + tid) * pitch;
+            bulk_store(rec + h * DK, src, DK * 2);
+            bulk_store(rec + hk + h * DK, src + 2 * DK, DK * 2);
+            bulk_store(rec + 2 * hk + h * dv, src + 4 * DK, dv * 2);
+            bulk_commit();
         }
-        conv_part(raw, pitch, DK, p.w + (int64_t)(h * DK) * 4, false, n, anc, [&](int i, int c, uint2 y) {
-            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(T + i, c, 2 * T)) = y;
-        });
-        conv_part(raw + 2 * DK, pitch, DK, p.w + (int64_t)(hk + h * DK) * 4, true, n, anc, [&](int i, int c, uint2 y) {
+        conv_part(raw + 2 * DK, pitch, DK, tk, true, n, taps, [&](int i, int c, uint2 y) {
             *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(i, c, 2 * T)) = y;
         });
-        conv_part(raw + 4 * DK, pitch, dv, p.w + (int64_t)(2 * hk + h * dv) * 4, false, n, anc, [&](int i, int c, uint2 y) {
+        conv_part(raw, pitch, DK, tq, false, n, taps, [&](int i, int c, uint2 y) {
+            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(T + i, c, 2 * T)) = y;
+        });
+        conv_part(raw + 4 * DK, pitch, dv, tv, false, n, taps, [&](int i, int c, uint2 y) {
             *reinterpret_cast<uint2*>(vs + i * kLdv + c) = y;
         });
-        __syncthreads();                             // the raw rows make room for S's parts
+        load_s();
+        if (tid < n) bulk_wait_read();
+        ok = __syncthreads_and(ok);                  // the raw rows make room for S's parts
     }
     // ---- the products, 64 columns of S at a time
-    bool ok = true;
 #pragma unroll
     for (int x = 0; x < HALVES; ++x) {
-        if (x > 0) ok = mbar_wait(bar + 8 * (x - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x61);   // the parts are consumed
+        if (x > 0) ok = ok && mbar_wait(bar + 8 * (x - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x61);   // the parts are consumed
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
@@ -351,15 +411,42 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         *reinterpret_cast<uint4*>(p.rec_k + ((int64_t)(n0 + i) * H + h) * DK + c) =
             *reinterpret_cast<const uint4*>(smem + at.kq + sw128_off16(i, c, 2 * T));
     }
-    if (tid < kDraftNodes) {
-        float g = 1.f;
-        if (tid < n) {
-            for (uint64_t m = anc[tid]; m; m &= m - 1) g *= al[__ffsll((long long)m) - 1];   // root first
-            if (!(g >= kSmallDecay)) *small = 1;
+    if (warp == 1) {
+        // products up the tree by doubling: g holds the nodes from i up to before `up`
+        float g[2];
+        int up[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int i = lane + 32 * x;
+            const uint64_t m = i < n ? anc[i] & ~(1ull << i) : 0;
+            g[x] = i < n ? al[i] : 1.f;
+            up[x] = m ? 63 - __clzll((long long)m) : -1;
         }
-        G[tid] = g;
-        rG[tid] = 1.f / g;
-        if (tid >= n) be[tid] = 0.f;
+        while (__any_sync(0xffffffffu, up[0] >= 0 || up[1] >= 0)) {
+            float t[2];
+            int w[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int from = up[x] & 31;
+                const float a = __shfl_sync(0xffffffffu, g[0], from), c = __shfl_sync(0xffffffffu, g[1], from);
+                const int d = __shfl_sync(0xffffffffu, up[0], from), e = __shfl_sync(0xffffffffu, up[1], from);
+                t[x] = up[x] < 0 ? 1.f : up[x] < 32 ? a : c;
+                w[x] = up[x] < 0 ? -1 : up[x] < 32 ? d : e;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                g[x] *= t[x];
+                up[x] = w[x];
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int i = lane + 32 * x;
+            if (i < n && !(g[x] >= kSmallDecay)) *small = 1;
+            G[i] = g[x];
+            rG[i] = 1.f / g[x];
+            if (i >= n) be[i] = 0.f;
+        }
     }
     ok = ok && mbar_wait(bar + 8 * (HALVES - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x62);
     ok = __syncthreads_and(ok);
@@ -451,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
 #pragma unroll
         for (int I = 0; I < 4; ++I) {
             if (I >= NB) break;
-            float x[2][4], o[2][4];
+            float x[2][4], o[2][4], lo[2][4] = {};
             tmem_ld_16x16(lanes + 16 * I, x);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -462,10 +549,12 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                     x[t][e] = node < n ? be[node] * (v - G[node] * x[t][e]) : 0.f;      // a padding row holds anything
                 }
 #pragma unroll
-            for (int J = 0; J < I; ++J) block_mma<3, 3>(x, u[J], Cp + 16 * I * kLdc + 16 * J, kLdc, kPart);
+            for (int J = 0; J < I; ++J) block_mma<3, 3>(x, lo, u[J], Cp + 16 * I * kLdc + 16 * J, kLdc, kPart);
+            join(x, lo);
             split(x, u[I]);
             float y[2][4] = {};
-            block_mma<3, 3>(y, u[I], Dp + I * 3 * 16 * kLdd, kLdd, 16 * kLdd);
+            block_mma<3, 3>(y, lo, u[I], Dp + I * 3 * 16 * kLdd, kLdd, 16 * kLdd);
+            join(y, lo);
             split(y, u[I]);
             tmem_ld_16x16(lanes + T + 16 * I, o);
 #pragma unroll
@@ -475,8 +564,9 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
 #pragma unroll
             for (int J = 0; J <= I; ++J) {
                 const uint32_t (&a)[2][4] = *reinterpret_cast<const uint32_t (*)[2][4]>(&u[J]);
-                block_mma<2, 2>(o, a, Ep + 16 * I * kLdc + 16 * J, kLdc, kPart);
+                block_mma<2, 2>(o, lo, a, Ep + 16 * I * kLdc + 16 * J, kLdc, kPart);
             }
+            join(o, lo);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -494,10 +584,13 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     tc_fence_before();
     __syncthreads();
     if (ok) {
-        const int gv = dv / 8;
-        for (int e = tid; e < n * gv; e += kThreads)
-            *reinterpret_cast<uint4*>(p.out + ((int64_t)(n0 + e / gv) * H + h) * dv + 8 * (e % gv)) =
-                *reinterpret_cast<const uint4*>(vs + (e / gv) * kLdv + 8 * (e % gv));
+        const int c = 8 * (tid & 15);
+        if (c < dv)
+            for (int i = tid >> 4; i < n; i += kThreads / 16)
+                *reinterpret_cast<uint4*>(p.out + ((int64_t)(n0 + i) * H + h) * dv + c) = *reinterpret_cast<const uint4*>(vs + i * kLdv + c);
+    }
+    if constexpr (CONV) {
+        if (tid < n) bulk_wait_all();
     }
     if (warp == 0) {
         tc_fence_after();

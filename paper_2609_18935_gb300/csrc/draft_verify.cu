@@ -17,10 +17,12 @@
 //
 // Sums decide between neighbouring tokens, so they are carried in pairs of fp32
 // (the error-free sum and product; Dekker, "A floating-point technique for
-// extending the available precision", 1971) and joined in 64 bits: about 2^-46
+// extending the available precision", 1971): about 2^-46
 // relative, where a sum in 32 bits would move the draw by many tokens of a large
-// vocabulary, and the 64-bit pipe (two results a cycle and SM) would bound the pass.
+// vocabulary, and the 64-bit pipe gives two results a cycle and SM: with the few
+// scalars of the walk alone in 64 bits, in every thread, a verdict took twice as long.
 #include "kvm_internal.cuh"
+#include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
 
 namespace kvm {
@@ -28,67 +30,94 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;              // 8 is what every launch may ask for, 16 a kernel that opts in
 
 // hi + lo
 struct Pair {
     float hi, lo;
 };
+// Two of them side by side (packed fp32).
+struct Pairs {
+    f2 hi, lo;
+};
 
 __device__ __forceinline__ float probability(float x) {       // what is not a finite positive number counts as 0
-    return x > 0.f && x <= 3.402823466e38f ? x : 0.f;
+    return __float_as_uint(x) < 0x7f800000u ? x : 0.f;
 }
 
-// max(p - c q, 0)
-__device__ __forceinline__ Pair weight(float p, float q, float ch, float cl) {
-    p = probability(p);
-    q = probability(q);
-    const float m = -ch * q, e = fmaf(-ch, q, -m);             // -c q = m + e - cl q
-    const float s = p + m;
-    const float bv = s - p, av = s - bv;
-    const float lo = ((p - av) + (m - bv)) + fmaf(-cl, q, e);
-    return s + lo > 0.f ? Pair{s, lo} : Pair{0.f, 0.f};
+// max(p - c q, 0) of two elements; c = ch + cl
+__device__ __forceinline__ Pairs weights(f2 p, f2 q, f2 ch, f2 nch, f2 ncl) {
+    const f2 m = mul2(nch, q), e = fma2(ch, q, m);             // -c q = m - e + ncl q
+    const f2 s = add2(p, m);
+    const f2 bv = sub2(s, p), av = sub2(s, bv);
+    const f2 lo = fma2(ncl, q, sub2(add2(sub2(p, av), sub2(m, bv)), e));
+    const float2 t = unpack2(add2(s, lo)), x = unpack2(s), y = unpack2(lo);
+    return {pack2(t.x > 0.f ? x.x : 0.f, t.y > 0.f ? x.y : 0.f), pack2(t.x > 0.f ? y.x : 0.f, t.y > 0.f ? y.y : 0.f)};
 }
 
-__device__ __forceinline__ void add(Pair& a, const Pair& x) {
-    const float s = a.hi + x.hi;
-    const float bv = s - a.hi, av = s - bv;
-    a.lo += ((a.hi - av) + (x.hi - bv)) + x.lo;
+__device__ __forceinline__ void add(Pairs& a, const Pairs& x) {
+    const f2 s = add2(a.hi, x.hi);
+    const f2 bv = sub2(s, a.hi), av = sub2(s, bv);
+    a.lo = add2(a.lo, add2(add2(sub2(a.hi, av), sub2(x.hi, bv)), x.lo));
     a.hi = s;
 }
+__device__ __forceinline__ Pair add(Pair a, Pair x) {
+    const float s = a.hi + x.hi;
+    const float bv = s - a.hi, av = s - bv;
+    const float lo = ((a.hi - av) + (x.hi - bv)) + (a.lo + x.lo);
+    const float hi = s + lo;                                   // kept normalised: lo below an ulp of hi
+    return {hi, lo - (hi - s)};
+}
+__device__ __forceinline__ Pair sub(Pair a, Pair x) { return add(a, {-x.hi, -x.lo}); }
+__device__ __forceinline__ Pair mul(Pair a, float x) {
+    const float h = a.hi * x, l = fmaf(a.hi, x, -h) + a.lo * x;
+    const float hi = h + l;
+    return {hi, l - (hi - h)};
+}
+__device__ __forceinline__ Pair mul(Pair a, Pair x) {
+    const float h = a.hi * x.hi, l = fmaf(a.hi, x.hi, -h) + (a.hi * x.lo + a.lo * x.hi);
+    const float hi = h + l;
+    return {hi, l - (hi - h)};
+}
+__device__ __forceinline__ bool positive(Pair a) { return a.hi > 0.f; }          // of a normalised one
+__device__ __forceinline__ bool less(Pair a, Pair x) { return positive(sub(x, a)); }
+__device__ __forceinline__ Pair shuffle_xor(Pair a, int o) {
+    return {__shfl_xor_sync(0xffffffffu, a.hi, o), __shfl_xor_sync(0xffffffffu, a.lo, o)};
+}
+// Every lane gets the sum in the same bits: a sum of two does not depend on their order.
+__device__ __forceinline__ Pair warp_sum(Pair a) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a = add(a, shuffle_xor(a, o));
+    return a;
+}
 
-// Four neighbouring values of a row from virtual place y (a multiple of 4): place
-// y holds element y - m, so that places on the vector grid lie on it in memory too.
+// Four neighbouring values of a row from virtual place y (a multiple of 4), as
+// probabilities: place y holds element y - m, so that places on the vector grid lie
+// on it in memory too.
 template <typename T>
-__device__ __forceinline__ void load4(const T* row, int y, int m, int end, float* x) {
+__device__ __forceinline__ void load4(const T* row, int y, int m, int end, float (&x)[4]) {
     if (y >= m && y + 4 <= end) {
         if constexpr (sizeof(T) == 4) {
             const float4 v = *reinterpret_cast<const float4*>(row + (y - m));
             x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
         } else {
             const uint2 v = *reinterpret_cast<const uint2*>(row + (y - m));
-            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x));
-            const float2 c = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
-            x[0] = a.x; x[1] = a.y; x[2] = c.x; x[3] = c.y;
+            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
         }
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = y + e >= m && y + e < end ? (float)row[y + e - m] : 0.f;
     }
-}
-
-__device__ __forceinline__ double warp_sum(double x) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
+    for (int e = 0; e < 4; ++e) x[e] = probability(x[e]);
 }
 
-__device__ __forceinline__ double ld_cluster(const double* mine, uint32_t rank) {
+// Writes v over the neighbour's copy of *mine, in block `rank` of the cluster.
+__device__ __forceinline__ void st_cluster(const Pair* mine, uint32_t rank, Pair v) {
     uint32_t addr;
-    double v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(ptx::smem_u32(mine)), "r"(rank));
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.hi), "f"(v.lo) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -96,9 +125,11 @@ __device__ __forceinline__ void cluster_sync() {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_constant__ DraftVerifyParams p) {
-    __shared__ double sums[2][kWarps];               // each warp's sum of its range, two passes deep
+    __shared__ Pair sums[kWarps];                    // this block's warps' sums of their ranges
+    __shared__ Pair parts[2][kMaxCluster];           // every block's sum, two passes deep
     __shared__ float pt[kDraftNodes], qt[kDraftNodes], us[kDraftNodes];
-    __shared__ int par[kDraftNodes], path[kDraftNodes];
+    __shared__ int path[kDraftNodes];
+    __shared__ unsigned long long kids[kDraftNodes];               // each node's children
     uint32_t rank, blocks;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
@@ -114,10 +145,12 @@ __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_con
         if (rank == 0 && tid == 0) { p.count[b] = 0; p.next[b] = -1; }
         return;
     }
+    if (tid < kDraftNodes) kids[tid] = 0;
+    __syncthreads();
     if (tid < n) {
         const unsigned long long up = p.anc[n0 + tid] & ~(1ull << tid);
         const int pa = up ? 63 - __clzll(up) : -1;
-        par[tid] = pa;
+        if (pa >= 0) atomicOr(kids + pa, 1ull << tid);
         us[tid] = p.u[n0 + tid];
         float x = 0.f, y = 0.f;
         if (pa >= 0) {
@@ -136,30 +169,42 @@ __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_con
 
     const int gw = rank * kWarps + warp, n_gw = blocks * kWarps;
     int cur = 0, count = 1, pass = 0;
-    double c = 0.0, Z = 1.0;
+    Pair c{0.f, 0.f}, Z{1.f, 0.f};
     if (tid == 0) path[0] = 0;
     // this warp's part of the current row, and the sum over all of max(p - c q, 0)
     int m = 0, end = 0, per = 0;
     const T *rp = nullptr, *rq = nullptr;
+    f2 ch2 = 0, nch2 = 0, ncl2 = 0;
+    auto set_c = [&]() {
+        ch2 = pack2(c.hi, c.hi);
+        nch2 = pack2(-c.hi, -c.hi);
+        ncl2 = pack2(-c.lo, -c.lo);
+    };
     auto row_sum = [&]() {
-        const float ch = (float)c, cl = (float)(c - (double)ch);
-        Pair acc{0.f, 0.f};
+        set_c();
+        Pairs acc{0, 0};                             // four zeros
         const int y1 = min(end, (gw + 1) * per);
 #pragma unroll 4
         for (int y = gw * per + 4 * lane; y < y1; y += 128) {
             float a[4], d[4];
             load4(rp, y, m, end, a);
             load4(rq, y, m, end, d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) add(acc, weight(a[e], d[e], ch, cl));
+            add(acc, weights(pack2(a[0], a[1]), pack2(d[0], d[1]), ch2, nch2, ncl2));
+            add(acc, weights(pack2(a[2], a[3]), pack2(d[2], d[3]), ch2, nch2, ncl2));
         }
-        const double mine = warp_sum((double)acc.hi + (double)acc.lo);
-        if (lane == 0) sums[pass & 1][warp] = mine;
-        cluster_sync();
-        double z = 0.0;
-        for (int g = lane; g < n_gw; g += 32) z += ld_cluster(&sums[pass & 1][g % kWarps], g / kWarps);
-        ++pass;
-        return warp_sum(z);                          // the same order in every warp
+        const float2 hi = unpack2(acc.hi), lo = unpack2(acc.lo);
+        const Pair mine = warp_sum(add(Pair{hi.x, lo.x}, Pair{hi.y, lo.y}));
+        if (lane == 0) sums[warp] = mine;
+        __syncthreads();
+        Pair* all = parts[pass++ & 1];
+        if (warp == 0) {
+            const Pair z = warp_sum(lane < kWarps ? sums[lane] : Pair{0.f, 0.f});
+            if (blocks == 1) { if (lane == 0) all[0] = z; }
+            else if (lane < blocks) st_cluster(all + rank, lane, z);
+        }
+        if (blocks == 1) __syncthreads();
+        else cluster_sync();
+        return warp_sum(lane < blocks ? all[lane] : Pair{0.f, 0.f});   // the same order in every warp
     };
     for (;;) {
         const int64_t at = (int64_t)(n0 + cur) * V;
@@ -168,15 +213,15 @@ __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_con
         per = ((end + n_gw - 1) / n_gw + 127) / 128 * 128;
         rp = target + at;
         rq = draft + at;
-        c = 0.0;
-        Z = 1.0;
+        c = {0.f, 0.f};
+        Z = {1.f, 0.f};
         int taken = -1;
-        for (int i = cur + 1; i < n; ++i) {
-            if (par[i] != cur) continue;
-            const double q = qt[i], w = (double)pt[i] - c * q;
-            if ((double)us[i] * q * Z < (w > 0.0 ? w : 0.0)) { taken = i; break; }
-            if (Z == 0.0) break;                     // nothing is left of p: no other guess can be accepted
-            c = c == 0.0 ? 1.0 : c + Z;
+        for (unsigned long long m = kids[cur]; m; m &= m - 1) {
+            const int i = __ffsll((long long)m) - 1;
+            const Pair w = sub({pt[i], 0.f}, mul(c, qt[i]));
+            if (positive(w) && less(mul(mul(Z, qt[i]), us[i]), w)) { taken = i; break; }
+            if (!positive(Z)) break;                 // nothing is left of p: no other guess can be accepted
+            c = positive(c) ? add(c, Z) : Pair{1.f, 0.f};
             Z = row_sum();
         }
         if (taken < 0) break;
@@ -185,35 +230,36 @@ __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_con
         ++count;
     }
     // ---- the next token, from what is left of the last node's row (all of it where nothing is)
-    if (c == 0.0 || Z == 0.0) {
-        c = 0.0;
+    if (!positive(c) || !positive(Z)) {
+        c = {0.f, 0.f};
         Z = row_sum();
     }
-    const double T0 = (double)p.u_next[b] * Z;
-    const double* last = sums[(pass - 1) & 1];
-    // the last warp range with something in it whose running sum before it is <= T0
-    int found = -1;
-    double before = 0.0, base = 0.0;
-    for (int g0 = 0; g0 < n_gw; g0 += 32) {
-        const int g = g0 + lane;
-        const double x = g < n_gw ? ld_cluster(last + g % kWarps, g / kWarps) : 0.0;
-        double inc = x;
+    const Pair T0 = mul(Z, p.u_next[b]);
+    // running sum of x over the lanes before this one
+    auto before_lane = [&](Pair x) {
+        Pair inc = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const double t = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += t;
+            const Pair t{__shfl_up_sync(0xffffffffu, inc.hi, o), __shfl_up_sync(0xffffffffu, inc.lo, o)};
+            if (lane >= o) inc = add(t, inc);
         }
-        const double pre = base + (inc - x);
-        const unsigned hit = __ballot_sync(0xffffffffu, x > 0.0 && pre <= T0);
-        if (hit) {
-            const int l = 31 - __clz(hit);
-            found = g0 + l;
-            before = __shfl_sync(0xffffffffu, pre, l);
-        }
-        base += __shfl_sync(0xffffffffu, inc, 31);
-    }
+        const Pair t{__shfl_up_sync(0xffffffffu, inc.hi, 1), __shfl_up_sync(0xffffffffu, inc.lo, 1)};
+        return lane ? t : Pair{0.f, 0.f};
+    };
+    const Pair* last = parts[(pass - 1) & 1];
+    // the last of n_of sums with something in it whose running sum, on top of `base`, before it is <= T0; that running sum
+    auto find = [&](const Pair* of, int n_of, Pair& base) {
+        const Pair x = lane < n_of ? of[lane] : Pair{0.f, 0.f};
+        const Pair pre = add(base, before_lane(x));
+        const unsigned hit = __ballot_sync(0xffffffffu, positive(x) && !less(T0, pre));
+        const int l = 31 - __clz(hit);               // -1 where there is none
+        base = {__shfl_sync(0xffffffffu, pre.hi, l & 31), __shfl_sync(0xffffffffu, pre.lo, l & 31)};
+        return l;
+    };
+    Pair before{0.f, 0.f};
+    const int block = find(last, blocks, before);
+    const int found = block == (int)rank ? (int)rank * kWarps + find(sums, kWarps, before) : -1;
     if (found == gw) {
-        const float ch = (float)c, cl = (float)(c - (double)ch);
         const int y1 = min(end, (gw + 1) * per);
         int best = -1;
         for (int y0 = gw * per; y0 < y1; y0 += 128) {
@@ -223,45 +269,48 @@ __global__ void __launch_bounds__(kThreads) draft_verify_kernel(const __grid_con
                 load4(rp, y, m, end, a);
                 load4(rq, y, m, end, d);
             }
-            double w[4], x = 0.0;
+            Pair w[4], x{0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const Pairs v = weights(pack2(a[e], a[e + 1]), pack2(d[e], d[e + 1]), ch2, nch2, ncl2);
+                const float2 hi = unpack2(v.hi), lo = unpack2(v.lo);
+                w[e] = add(Pair{0.f, 0.f}, Pair{hi.x, lo.x});
+                w[e + 1] = add(Pair{0.f, 0.f}, Pair{hi.y, lo.y});
+                x = add(add(x, w[e]), w[e + 1]);
+            }
+            Pair pre = add(before, before_lane(x));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const Pair v = weight(a[e], d[e], ch, cl);
-                w[e] = (double)v.hi + (double)v.lo;
-                x += w[e];
+                if (positive(w[e]) && !less(T0, pre)) best = y + e - m;
+                pre = add(pre, w[e]);
             }
-            double inc = x;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += t;
-            }
-            double pre = before + (inc - x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (w[e] > 0.0 && pre <= T0) best = y + e - m;
-                pre += w[e];
-            }
-            before += __shfl_sync(0xffffffffu, inc, 31);
+            before = {__shfl_sync(0xffffffffu, pre.hi, 31), __shfl_sync(0xffffffffu, pre.lo, 31)};
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
         if (lane == 0) p.next[b] = best;
     }
     if (rank == 0) {
-        if (found < 0 && tid == 0) p.next[b] = -1;   // the row holds no positive number
+        if (block < 0 && tid == 0) p.next[b] = -1;   // the row holds no positive number
         __syncthreads();
         if (tid < n) p.path[n0 + tid] = tid < count ? path[tid] : -1;
         if (tid == 0) p.count[b] = count;
     }
-    cluster_sync();                                  // no block leaves while another may read its sums
+    if (blocks > 1) cluster_sync();                  // no block leaves while another may still write to it
 }
 
 }  // namespace
 
-void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cudaStream_t s) {
-    int blocks = 1;
-    while (blocks < kMaxCluster && blocks * kThreads * 8 < p.vocab && 2 * blocks * p.n_chars <= 2 * num_sms) blocks *= 2;
+namespace {
+template <typename T>
+void launch(const DraftVerifyParams& p, int blocks, cudaStream_t s) {
+    static unsigned long long configured = 0;    // one bit per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!(configured >> (dev & 63) & 1ull)) {
+        cudaFuncSetAttribute(draft_verify_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        configured |= 1ull << (dev & 63);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks, p.n_chars);
     cfg.blockDim = dim3(kThreads);
@@ -275,8 +324,14 @@ void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cud
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    if (bf16) cudaLaunchKernelEx(&cfg, draft_verify_kernel<__nv_bfloat16>, p);
-    else cudaLaunchKernelEx(&cfg, draft_verify_kernel<float>, p);
+    cudaLaunchKernelEx(&cfg, draft_verify_kernel<T>, p);
+}
+}  // namespace
+
+void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cudaStream_t s) {
+    int blocks = 1;
+    while (blocks < kMaxCluster && blocks * kThreads * 4 < p.vocab && 2 * blocks * p.n_chars <= 2 * num_sms) blocks *= 2;
+    bf16 ? launch<__nv_bfloat16>(p, blocks, s) : launch<float>(p, blocks, s);
 }
 
 }  // namespace kvm
