@@ -579,50 +579,48 @@ class Context:
         _check(_lib.kvm_draft_begin(self._h, cu, par, _stream(stream)))
         self._draft_nodes = n
 
-    def _draft_rows(self, **tensors):
-        """Shapes of the nodes' tensors: [nodes][..], checked because the library reads them unseen (with no draft begun
-        it refuses the call itself)."""
-        if self._draft_nodes is None:
-            return
-        for name, (t, rest) in tensors.items():
-            if tuple(t.shape) != (self._draft_nodes, *rest):
-                raise ValueError(f"{name} has shape {tuple(t.shape)}, need {(self._draft_nodes, *rest)}")
+    def _draft_ptr(self, name, t, dtype, rest) -> int:
+        """Address of one of an open draft's tensors, [nodes][rest..]: shapes are checked because the library reads them
+        unseen (with no draft begun it refuses the call itself)."""
+        n = self._draft_nodes
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.shape == (n, *rest)):
+            return t.data_ptr()
+        _dptr(t, dtype)
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, need {(n, *rest)}")
 
     def draft_attn(self, layer, q, k_new, v_new, out, stream=None):
         """kvm_draft_attn: one attention layer over the open draft; q, out CUDA bf16 [nodes][Hq][D], k_new, v_new
         [nodes][Hkv][D]."""
-        bf = _torch().bfloat16
+        bf, ptr = _torch().bfloat16, self._draft_ptr
         heads, kv = (self.Hq, self.D), (self.Hkv, self.D)
-        self._draft_rows(q=(q, heads), k_new=(k_new, kv), v_new=(v_new, kv), out=(out, heads))
-        _check(_lib.kvm_draft_attn(self._h, layer, _dptr(q, bf), _dptr(k_new, bf), _dptr(v_new, bf), _dptr(out, bf),
-                                   _stream(stream)))
+        _check(_lib.kvm_draft_attn(self._h, layer, ptr("q", q, bf, heads), ptr("k_new", k_new, bf, kv),
+                                   ptr("v_new", v_new, bf, kv), ptr("out", out, bf, heads), _stream(stream)))
 
     def draft_gdn(self, layer, q, k, v, alpha, beta, out, stream=None):
         """kvm_draft_gdn: one delta-rule layer over the open draft; q, k CUDA bf16 [nodes][H][dk], v, out [nodes][H][dv],
         alpha, beta fp32 [nodes][H]."""
-        torch = _torch()
+        torch, ptr = _torch(), self._draft_ptr
         bf, f = torch.bfloat16, torch.float32
-        key, val = (self.H, self.dk), (self.H, self.dv)
-        self._draft_rows(q=(q, key), k=(k, key), v=(v, val), alpha=(alpha, (self.H,)), beta=(beta, (self.H,)), out=(out, val))
-        _check(_lib.kvm_draft_gdn(self._h, layer, _dptr(q, bf), _dptr(k, bf), _dptr(v, bf), _dptr(alpha, f), _dptr(beta, f),
-                                  _dptr(out, bf), _stream(stream)))
+        key, val, gate = (self.H, self.dk), (self.H, self.dv), (self.H,)
+        _check(_lib.kvm_draft_gdn(self._h, layer, ptr("q", q, bf, key), ptr("k", k, bf, key), ptr("v", v, bf, val),
+                                  ptr("alpha", alpha, f, gate), ptr("beta", beta, f, gate), ptr("out", out, bf, val),
+                                  _stream(stream)))
 
     def draft_verify(self, tokens, target, draft, u, u_next, path, count, next_token, stream=None):
         """kvm_draft_verify: target, draft CUDA fp32 or bf16 [nodes][vocab]; tokens int32 [nodes], u fp32 [nodes], u_next
         fp32 [n_chars]; path int32 [nodes], count and next_token int32 [n_chars] are written."""
-        torch = _torch()
-        if target.dim() != 2 or target.dtype not in (torch.float32, torch.bfloat16):
+        torch, ptr = _torch(), self._draft_ptr
+        i, f, t = torch.int32, torch.float32, target.dtype
+        if target.dim() != 2 or (t is not f and t is not torch.bfloat16):
             raise ValueError("target must be [nodes][vocab] in float32 or bfloat16")
-        vocab = target.shape[1]
-        one = (self.n_chars,)
-        self._draft_rows(tokens=(tokens, ()), target=(target, (vocab,)), draft=(draft, (vocab,)), u=(u, ()), path=(path, ()))
-        for name, t in (("u_next", u_next), ("count", count), ("next_token", next_token)):
-            if tuple(t.shape) != one:
-                raise ValueError(f"{name} has shape {tuple(t.shape)}, need {one}")
-        i, f = torch.int32, torch.float32
-        _check(_lib.kvm_draft_verify(self._h, vocab, PROB_F32 if target.dtype == f else PROB_BF16, _dptr(tokens, i),
-                                     _dptr(target), _dptr(draft, target.dtype), _dptr(u, f), _dptr(u_next, f), _dptr(path, i),
-                                     _dptr(count, i), _dptr(next_token, i), _stream(stream)))
+        row, one = (target.shape[1],), (self.n_chars,)
+        for name, x in (("u_next", u_next), ("count", count), ("next_token", next_token)):
+            if x.shape != one:
+                raise ValueError(f"{name} has shape {tuple(x.shape)}, need {one}")
+        _check(_lib.kvm_draft_verify(self._h, row[0], PROB_F32 if t is f else PROB_BF16, ptr("tokens", tokens, i, ()),
+                                     ptr("target", target, t, row), ptr("draft", draft, t, row), ptr("u", u, f, ()),
+                                     _dptr(u_next, f), ptr("path", path, i, ()), _dptr(count, i), _dptr(next_token, i),
+                                     _stream(stream)))
 
     def draft_commit(self, path_cu, path, stream=None):
         """kvm_draft_commit: keep one path of each tree (host int32 offsets [n_chars + 1] and packed node indices)."""
