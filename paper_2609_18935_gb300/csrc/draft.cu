@@ -1,8 +1,11 @@
 // Drafts: a tree of guessed tokens behind each character's live entries, and
 // the commit of one of its paths (kvm_draft_begin, kvm_draft_commit).
 //
-//  draft_tree   : each node's ancestors as the bits of one word, and its
-//                 position, cursor + depth.  Once a step, for every layer.
+//  draft_tree   : each node's ancestors as the bits of one word, its position,
+//                 cursor + depth, and the cosines and sines of its rotary angles.
+//                 Once a step, for every layer.
+//  draft_append : an attention layer's keys (rotated) and values of the nodes to
+//                 the slots behind the live entries.
 //  draft_commit : one launch for every layer.  The nodes of a path are the
 //                 character's next tokens:
 //                 * attention caches: the path's key and value rows move from
@@ -24,16 +27,79 @@
 namespace kvm {
 namespace {
 
-__global__ void __launch_bounds__(kDraftNodes) draft_tree_kernel(const __grid_constant__ DraftTreeParams p) {
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr int kTreeNodes = 8;                // nodes a block of the tree kernel
+
+// grid (n_chars, ceil(most / kTreeNodes))
+__global__ void __launch_bounds__(256) draft_tree_kernel(const __grid_constant__ DraftTreeParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
-    const int b = blockIdx.x, i = threadIdx.x;
-    const int n0 = p.cu[b];
-    if (i >= p.cu[b + 1] - n0) return;
-    uint64_t anc = 0;
-    for (int j = i; j >= 0; j = p.parent[n0 + j]) anc |= 1ull << j;   // parents have smaller indices (checked on the host)
-    p.anc[n0 + i] = anc;
-    if (p.pos) p.pos[n0 + i] = (int32_t)(p.cursor[b] + __popcll(anc) - 1);
+    const int b = blockIdx.x, i0 = blockIdx.y * kTreeNodes, n0 = p.cu[b];
+    const int n = min(kTreeNodes, p.cu[b + 1] - n0 - i0);
+    __shared__ int depth[kTreeNodes];
+    if ((int)threadIdx.x < n) {
+        const int i = i0 + threadIdx.x;
+        uint64_t anc = 0;
+        for (int j = i; j >= 0; j = p.parent[n0 + j]) anc |= 1ull << j;   // parents have smaller indices (checked on the host)
+        p.anc[n0 + i] = anc;
+        depth[threadIdx.x] = __popcll(anc) - 1;
+        p.pos[n0 + i] = (int32_t)(p.cursor[b] + depth[threadIdx.x]);
+    }
+    __syncthreads();
+    const int half = p.R / 2;
+    for (int e = threadIdx.x; e < n * half; e += blockDim.x) {
+        const int x = e / half, d = e % half;
+        // formed and reduced in 64 bits: positions far beyond the live length stay exact
+        const double ang = (double)(p.cursor[b] + depth[x]) * p.inv_freq[d];
+        const double r = fma(-rint(ang * (1.0 / kTwoPi)), kTwoPi, ang);
+        float2 t;
+        sincosf((float)r, &t.y, &t.x);
+        p.turn[(int64_t)(n0 + i0 + x) * half + d] = t;
+    }
+}
+
+// A block a node, a thread eight elements of a key or value row, those of a rotary
+// pair (i, i + R / 2) together: the attention that follows rotates q itself and
+// waits for this kernel only where it reads the nodes' rows.
+__global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant__ AttnParams p) {
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int n = blockIdx.x;
+    int lo = 0, hi = p.n_chars - 1;              // last b with tail_off <= n owns node n
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.ch[mid].tail_off <= n) lo = mid; else hi = mid - 1;
+    }
+    const AttnChar& c = p.ch[lo];
+    const int i = n - c.tail_off;
+    if (i < 0 || i >= c.M) { if (threadIdx.x == 0) atomicOr(p.err, kErrBounds); return; }
+    const int64_t slot = c.cap_off + c.L_prev + i;
+    const int D = p.D, half = p.R / 2, rot = half / 8, per = D / 8, keys = p.Hkv * (per - rot);
+    for (int e = threadIdx.x; e < keys + p.Hkv * per; e += blockDim.x) {
+        const bool is_v = e >= keys;
+        const int x = is_v ? e - keys : e, pieces = is_v ? per : per - rot, h = x / pieces, g = x % pieces;
+        const bool turned = !is_v && g < rot;
+        const int d = 8 * (is_v || turned ? g : g + rot);            // past the pairs' second halves
+        const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + ((int64_t)n * p.Hkv + h) * D + d;
+        __nv_bfloat16* dst = (is_v ? p.V : p.K) + ((int64_t)h * p.slab_rows + slot) * D + d;
+        uint4 a = *reinterpret_cast<const uint4*>(src);
+        if (turned) {
+            uint4 y = *reinterpret_cast<const uint4*>(src + half);
+            const float4* t = reinterpret_cast<const float4*>(p.turn + (int64_t)n * half + d);
+            __nv_bfloat162* u = reinterpret_cast<__nv_bfloat162*>(&a);
+            __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&y);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 cs = t[q];              // (cos, sin) of two dims
+                const float2 f = __bfloat1622float2(u[q]), s = __bfloat1622float2(w[q]);
+                u[q] = __floats2bfloat162_rn(f.x * cs.x - s.x * cs.y, f.y * cs.z - s.y * cs.w);
+                w[q] = __floats2bfloat162_rn(s.x * cs.x + f.x * cs.y, s.y * cs.z + f.y * cs.w);
+            }
+            *reinterpret_cast<uint4*>(dst + half) = y;
+        }
+        *reinterpret_cast<uint4*>(dst) = a;
+    }
+    if (threadIdx.x == 0) p.pos[slot] = p.tail_pos[n];
 }
 
 constexpr int kThreads = 128;
@@ -180,7 +246,11 @@ __global__ void __launch_bounds__(kThreads) draft_commit_kernel(const __grid_con
 }  // namespace
 
 void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s) {
-    launch_pdl(draft_tree_kernel, dim3(p.n_chars), dim3(kDraftNodes), 0, s, p);
+    launch_pdl(draft_tree_kernel, dim3(p.n_chars, (p.most + kTreeNodes - 1) / kTreeNodes), dim3(256), 0, s, p);
+}
+
+void launch_draft_append(const AttnParams& p, int nodes, cudaStream_t s) {
+    launch_pdl(draft_append_kernel, dim3(nodes), dim3(128), 0, s, p);
 }
 
 void launch_draft_commit(const DraftCommitParams& p, cudaStream_t s) {

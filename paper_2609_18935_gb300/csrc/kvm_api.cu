@@ -189,6 +189,7 @@ struct kvm_ctx {
     AttnPlan draft_plan;
     uint64_t* draft_anc = nullptr;
     int32_t* draft_pos = nullptr;
+    float2* draft_turn = nullptr;         // [draft_cap][R / 2] (cos, sin)
     float* draft_u = nullptr;             // [n_gdn][draft_cap][H][d_v]
     __nv_bfloat16* draft_k = nullptr;     // [n_gdn][draft_cap][H][d_k]
     float* draft_a = nullptr;             // [n_gdn][draft_cap][H]
@@ -1176,6 +1177,9 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     p.out = static_cast<__nv_bfloat16*>(out);
     p.tail_pos = tail_pos_dev;
     p.anc = anc;
+    // a draft's q is rotated in the attention where a rotary pair's elements lie whole
+    // 32-byte steps apart; else as a tail's, before it
+    p.turn = anc && c->R % 32 == 0 ? c->draft_turn : nullptr;
     p.part_o = c->part_o;
     p.part_ml = c->part_ml;
     p.err = c->err;
@@ -1200,7 +1204,8 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
     int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
-    launch_rope_append(p, total, s);
+    if (p.turn) launch_draft_append(p, total, s);
+    else launch_rope_append(p, total, s);
     prof_end(c, ps, s);
     LAUNCH_CHECK(c);
     ps = prof_begin(c, KVM_K_ATTENTION, s);
@@ -1211,6 +1216,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
         thread_local static CombineParams cp;
         cp.Hq = c->Hq; cp.D = c->D; cp.g = c->g;
         cp.n_split_tiles = (int)pl.split_cb.size();
+        cp.draft = anc != nullptr;
         cp.part_o = c->part_o;
         cp.part_ml = c->part_ml;
         cp.out = p.out;
@@ -1701,6 +1707,7 @@ void free_draft(kvm_ctx* c) {
     c->draft_cap = 0;
     free_dev(c, &c->draft_anc);
     free_dev(c, &c->draft_pos);
+    free_dev(c, &c->draft_turn);
     free_dev(c, &c->draft_u);
     free_dev(c, &c->draft_k);
     free_dev(c, &c->draft_a);
@@ -1790,6 +1797,7 @@ kvm_status draft_reserve(kvm_ctx* c, int max_nodes) {
     const size_t n = max_nodes, ln = (size_t)c->n_gdn * n;
     cudaError_t e = alloc_dev(c, &c->draft_anc, n, "draft_anc");
     if (e == cudaSuccess) e = alloc_dev(c, &c->draft_pos, n, "draft_pos");
+    if (e == cudaSuccess) e = alloc_dev(c, &c->draft_turn, n * std::max(1, c->R / 2), "draft_turn");   // p.turn is set without rotary dims too
     if (e == cudaSuccess) e = alloc_dev(c, &c->draft_u, ln * c->H * c->dv, "draft_u", false);
     if (e == cudaSuccess) e = alloc_dev(c, &c->draft_k, ln * c->H * c->dk, "draft_k", false);
     if (e == cudaSuccess) e = alloc_dev(c, &c->draft_a, ln * c->H, "draft_a", false);
@@ -1841,6 +1849,10 @@ kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent
         std::copy(parent, parent + total, p.parent);
         p.anc = c->draft_anc;
         p.pos = c->draft_pos;
+        p.turn = c->draft_turn;
+        p.R = c->R;
+        p.most = c->draft_cu[c->draft_order[0] + 1] - c->draft_cu[c->draft_order[0]];
+        std::copy(c->inv_freq, c->inv_freq + kMaxRotaryHalf, p.inv_freq);
         const int ps = prof_begin(c, KVM_K_DRAFT_TREE, s);
         launch_draft_tree(p, s);
         prof_end(c, ps, s);

@@ -161,6 +161,7 @@ struct AttnParams {
     int32_t* err;
     int32_t* diag;                // first expired wait: block + 1, tag, parity
     const uint64_t* anc;          // device [sum M]: a draft's ancestor bits (DraftTreeParams), or null: a causal tail
+    const float2* turn;           // of a draft: (cos, sin) [sum M][R / 2], with which the attention rotates q itself; or null
     double inv_freq[kMaxRotaryHalf];
     int32_t cta_tile[kMaxAttnCtas + 1];
     int32_t cta_k[kMaxAttnCtas + 1];
@@ -179,6 +180,7 @@ struct SplitTile {
 struct CombineParams {
     int32_t Hq, D, g;
     int32_t n_split_tiles;
+    int32_t draft;                // tiles of a draft: few, often full, in many parts
     const float* part_o;          // as in AttnParams
     const float* part_ml;
     __nv_bfloat16* out;           // [sum M][Hq][D]
@@ -339,9 +341,14 @@ struct DraftTreeParams {
     int64_t cursor[kMaxChars];
     int8_t parent[kMaxDraftNodes];            // packed; -1: a root
     uint64_t* anc;                            // device [sum n]
-    int32_t* pos;                             // device [sum n], or null
+    int32_t* pos;                             // device [sum n]
+    float2* turn;                             // device [sum n][R / 2]: (cos, sin) of each node's rotary angles
+    int32_t R, most;                          // rotary dims; nodes of the largest tree
+    double inv_freq[kMaxRotaryHalf];
 };
 void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s);
+// Keys and values of a draft's nodes to their slots (R a multiple of 16; p.turn).
+void launch_draft_append(const AttnParams& p, int nodes, cudaStream_t s);
 
 // The delta rule over a draft's nodes, and what a commit needs of each: its
 // update u, its key, its decay and, with the convolution, its raw inputs.

@@ -254,6 +254,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 
+// 16 lanes x 8 columns: thread t holds row t / 4, columns 2 (t % 4) and the next
+// (a, b), and the same of row t / 4 + 8 (c, d).
+__device__ __forceinline__ void tmem_st_16x8(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
+}
+
 // 32 lanes x W (16 or 32) consecutive 32-bit columns.
 template <int W>
 __device__ __forceinline__ void tmem_ldw(uint32_t taddr, uint32_t (&r)[W]) {

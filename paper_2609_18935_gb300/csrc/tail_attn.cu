@@ -431,6 +431,20 @@ void launch_attn_combine(const CombineParams& p, cudaStream_t s) {
         parts = max(parts, (int)p.tile[x].n_parts);
     }
     const int part_blocks = (rows * (p.D / 4) + 31) / 32;
+    if (p.draft) {
+        // up to a warp for two parts, while all of them are resident at once
+        const int64_t blocks = (int64_t)p.n_split_tiles * part_blocks, room = 64 * (int64_t)sms;
+        int lanes = 2;
+        while (lanes < 16 && 2 * lanes < parts && 2 * lanes * blocks <= room) lanes *= 2;
+        if (lanes * blocks <= room) {
+            const dim3 grid(p.n_split_tiles, part_blocks), block(32 * lanes);
+            if (lanes == 2) launch_pdl(attn_combine_parts_kernel<2>, grid, block, 0, s, p);
+            else if (lanes == 4) launch_pdl(attn_combine_parts_kernel<4>, grid, block, 0, s, p);
+            else if (lanes == 8) launch_pdl(attn_combine_parts_kernel<8>, grid, block, 0, s, p);
+            else launch_pdl(attn_combine_parts_kernel<16>, grid, block, 0, s, p);
+            return;
+        }
+    }
     if (rows <= 32 && (int64_t)p.n_split_tiles * part_blocks <= 8 * (int64_t)sms) {
         const dim3 grid(p.n_split_tiles, part_blocks);
         if (parts <= 8) launch_pdl(attn_combine_parts_kernel<4>, grid, dim3(32 * 4), 0, s, p);

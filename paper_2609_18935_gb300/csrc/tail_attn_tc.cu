@@ -131,6 +131,68 @@ __device__ __forceinline__ Tile decode_tile(const AttnParams& p, int t) {
     return r;
 }
 
+// Rows of a draft's Q tile into TMEM, 16 lanes x 8 columns (a k step of the MMA) at
+// a time, eight rows of 32 bytes a load: with a row a thread every load touched 32
+// lines and the block's 64 KB took 2.3 us against 1.1.  The two warps of a quarter
+// take the steps in turn.  With p.turn the caller's q is rotated here (R is a
+// multiple of 32: a pair's elements are in the same place of steps R / 32 apart),
+// and nothing of the previous grid, which only appends the nodes' keys and values,
+// is read: the kernel before that one has completed before this one could start.
+template <int D>
+__device__ __forceinline__ void stage_q_tree(const AttnParams& p, const Tile& T, int quarter, int grp, int lane, uint32_t tq) {
+    const AttnChar& ch = p.ch[T.b];
+    const int j = lane & 3, half = p.R / 2;
+    if (!p.turn) grid_dependency_wait();                   // q_rot comes from the previous grid
+    const __nv_bfloat16* q = p.turn ? p.q : p.q_rot;
+#pragma unroll 1
+    for (int hf = 0; hf < 2; ++hf) {
+        const uint2* src[2];
+        const float4* turn[2];
+        bool real[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int r = quarter * 32 + hf * 16 + 8 * x + (lane >> 2), tok = T.tok0 + r / p.g;
+            real[x] = tok < ch.M;
+            const int64_t n = ch.tail_off + (real[x] ? tok : 0);
+            src[x] = reinterpret_cast<const uint2*>(q + (n * p.Hq + T.kvh * p.g + r % p.g) * D) + j;
+            turn[x] = reinterpret_cast<const float4*>(p.turn + n * half) + 2 * j;
+        }
+        uint2 v[D / 32][2];
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) v[k][x] = src[x][4 * (2 * k + grp)];
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const int c = 2 * k + grp;                     // step: elements 16 c + 4 j .. + 3 are this thread's
+            if (p.turn && 16 * c < p.R) {
+                const bool first = 16 * c < half;
+                const int at = first ? 16 * c : 16 * c - half;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint2 o = src[x][4 * (first ? c + p.R / 32 : c - p.R / 32)];
+                    const float4 t0 = turn[x][at / 2], t1 = turn[x][at / 2 + 1];
+                    const uint32_t a[2] = {v[k][x].x, v[k][x].y}, b[2] = {o.x, o.y};
+                    uint32_t w[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float4 t = e ? t1 : t0;      // (cos, sin) of two dims
+                        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a[e]));
+                        const float2 s = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b[e]));
+                        // the forms that rope_append rotates a tail in
+                        const __nv_bfloat162 h = first ? __floats2bfloat162_rn(f.x * t.x - s.x * t.y, f.y * t.z - s.y * t.w)
+                                                       : __floats2bfloat162_rn(f.x * t.x + s.x * t.y, f.y * t.z + s.y * t.w);
+                        w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                    v[k][x] = make_uint2(w[0], w[1]);
+                }
+            }
+            const uint2 a = real[0] ? v[k][0] : make_uint2(0, 0), b = real[1] ? v[k][1] : make_uint2(0, 0);
+            tmem_st_16x8(tq + ((uint32_t)(hf * 16) << 16) + 8 * c, a.x, a.y, b.x, b.y);
+        }
+    }
+}
+
 // DEAL: p.waves > 0 (a kernel of its own: the segment lookup with waves cost
 // 1 % of the time where there are none).  TREE: the tail is a draft (p.anc): a
 // row sees the live entries and, of the tail, the nodes of its ancestor word.
@@ -353,6 +415,13 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
         // Q tile of query tile t into TMEM: this thread's half of row r (D / 2
         // bf16 = D / 4 columns); rows past the character's tail are zero
         auto stage_q = [&](int t) {
+            if constexpr (TREE) {
+                stage_q_tree<D>(p, decode_tile(p, t), quarter, grp, lane, tmem + lane_off + C::TMEM_Q);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(bar(Q_FULL));
+                return;
+            }
             grid_dependency_wait();                        // q_rot comes from the previous grid
             const Tile T = decode_tile(p, t);
             const AttnChar& ch = p.ch[T.b];

@@ -192,7 +192,10 @@ def test_a_node_outside_the_path_changes_nothing(d):
 
 
 def test_a_chain_equals_a_tail():
-    """The same launches and arithmetic: bit for bit what the tail call gives, and the tail's rows after a commit."""
+    """What the tail call gives, and after a commit its rows and positions bit for bit.  Where blocks share a query tile their
+    parts are the same but merged in another order: each side's fp32 sum of at most 32 parts is within 64 * 2^-24 = 2^-18 of the
+    sum of the parts' sizes, sum_j p_j |v_j| <= max |v|, and each is rounded to bf16 once, by at most 2^-8 of its value; so two
+    outputs a, b differ by at most 2^-8 (|a| + |b|) + 2^-17 max |v|.  A tile of one block alone is the same bit for bit."""
     import torch
     for live, n in ((50, 7), (3000, 64), (0, 1)):
         a, b = Attn(16, 2, 256, 64, [live], seed=41), Attn(16, 2, 256, 64, [live], seed=41)
@@ -203,7 +206,10 @@ def test_a_chain_equals_a_tail():
         cu = np.array([0, n], np.int32)
         b.ctx.tail_attn_prefill(0, cu, q, k, v, ref)
         b.ctx.advance(cu)
-        assert torch.equal(out.view(torch.int16), ref.view(torch.int16))
+        if live < 256:
+            assert torch.equal(out.view(torch.int16), ref.view(torch.int16))
+        x, y, most = out.double(), ref.double(), max(float(v.abs().max()), float(np.abs(a.caches[0].V).max(initial=0.0)))
+        assert bool(((x - y).abs() <= 2.0 ** -8 * (x.abs() + y.abs()) + 2.0 ** -17 * most).all())
         a.ctx.draft_commit(cu, np.arange(n))
         assert a.ctx.get_live(0) == b.ctx.get_live(0)
         for s, t in zip((*a.ctx.get_kv(0, 0), a.ctx.get_positions(0)), (*b.ctx.get_kv(0, 0), b.ctx.get_positions(0))):
