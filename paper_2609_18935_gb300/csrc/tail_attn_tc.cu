@@ -140,59 +140,79 @@ __device__ __forceinline__ Tile decode_tile(const AttnParams& p, int t) {
 // is read: the kernel before that one has completed before this one could start.
 template <int D>
 __device__ __forceinline__ void stage_q_tree(const AttnParams& p, const Tile& T, int quarter, int grp, int lane, uint32_t tq) {
+    constexpr int HALVES = 2;                              // of a warp's 32 rows
+    if (!p.turn) grid_dependency_wait();                   // q_rot comes from the previous grid
     const AttnChar& ch = p.ch[T.b];
     const int j = lane & 3, half = p.R / 2;
-    if (!p.turn) grid_dependency_wait();                   // q_rot comes from the previous grid
     const __nv_bfloat16* q = p.turn ? p.q : p.q_rot;
-#pragma unroll 1
-    for (int hf = 0; hf < 2; ++hf) {
-        const uint2* src[2];
-        const float4* turn[2];
-        bool real[2];
+    const uint2* src[HALVES][2];
+    const float4* turn[HALVES][2];
+    bool real[HALVES][2];
+    uint2 v[HALVES][D / 32][2];
+#pragma unroll
+    for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int r = quarter * 32 + hf * 16 + 8 * x + (lane >> 2), tok = T.tok0 + r / p.g;
-            real[x] = tok < ch.M;
-            const int64_t n = ch.tail_off + (real[x] ? tok : 0);
-            src[x] = reinterpret_cast<const uint2*>(q + (n * p.Hq + T.kvh * p.g + r % p.g) * D) + j;
-            turn[x] = reinterpret_cast<const float4*>(p.turn + n * half) + 2 * j;
+            real[hf][x] = tok < ch.M;
+            const int64_t n = ch.tail_off + (real[hf][x] ? tok : 0);
+            src[hf][x] = reinterpret_cast<const uint2*>(q + (n * p.Hq + T.kvh * p.g + r % p.g) * D) + j;
+            turn[hf][x] = reinterpret_cast<const float4*>(p.turn + n * half) + 2 * j;
         }
-        uint2 v[D / 32][2];
+    // a rotary step's other half and angles, loaded a step ahead of their use
+    uint2 o[HALVES][2];
+    float4 t[HALVES][2][2];
+    auto fetch = [&](int c) {
+        if (!p.turn || 16 * c >= p.R) return;
+        const bool first = 16 * c < half;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
+        for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) v[k][x] = src[x][4 * (2 * k + grp)];
+            for (int x = 0; x < 2; ++x) {
+                o[hf][x] = src[hf][x][4 * (first ? c + p.R / 32 : c - p.R / 32)];
+                t[hf][x][0] = turn[hf][x][(first ? 16 * c : 16 * c - half) / 2];
+                t[hf][x][1] = turn[hf][x][(first ? 16 * c : 16 * c - half) / 2 + 1];
+            }
+    };
+    fetch(grp);
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const int c = 2 * k + grp;                     // step: elements 16 c + 4 j .. + 3 are this thread's
-            if (p.turn && 16 * c < p.R) {
-                const bool first = 16 * c < half;
-                const int at = first ? 16 * c : 16 * c - half;
+    for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) v[hf][k][x] = src[hf][x][4 * (2 * k + grp)];
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+        const int c = 2 * k + grp;                         // step: elements 16 c + 4 j .. + 3 are this thread's
+        if (p.turn && 16 * c < p.R) {
+            const bool first = 16 * c < half;
+#pragma unroll
+            for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const uint2 o = src[x][4 * (first ? c + p.R / 32 : c - p.R / 32)];
-                    const float4 t0 = turn[x][at / 2], t1 = turn[x][at / 2 + 1];
-                    const uint32_t a[2] = {v[k][x].x, v[k][x].y}, b[2] = {o.x, o.y};
+                    const uint32_t a[2] = {v[hf][k][x].x, v[hf][k][x].y}, b[2] = {o[hf][x].x, o[hf][x].y};
                     uint32_t w[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float4 t = e ? t1 : t0;      // (cos, sin) of two dims
+                        const float4 cs = t[hf][x][e];     // (cos, sin) of two dims
                         const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&a[e]));
                         const float2 s = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b[e]));
                         // the forms that rope_append rotates a tail in
-                        const __nv_bfloat162 h = first ? __floats2bfloat162_rn(f.x * t.x - s.x * t.y, f.y * t.z - s.y * t.w)
-                                                       : __floats2bfloat162_rn(f.x * t.x + s.x * t.y, f.y * t.z + s.y * t.w);
+                        const __nv_bfloat162 h = first ? __floats2bfloat162_rn(f.x * cs.x - s.x * cs.y, f.y * cs.z - s.y * cs.w)
+                                                       : __floats2bfloat162_rn(f.x * cs.x + s.x * cs.y, f.y * cs.z + s.y * cs.w);
                         w[e] = *reinterpret_cast<const uint32_t*>(&h);
                     }
-                    v[k][x] = make_uint2(w[0], w[1]);
+                    v[hf][k][x] = make_uint2(w[0], w[1]);
                 }
-            }
-            const uint2 a = real[0] ? v[k][0] : make_uint2(0, 0), b = real[1] ? v[k][1] : make_uint2(0, 0);
+            if (k + 1 < D / 32) fetch(c + 2);
+        }
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf) {
+            const uint2 a = real[hf][0] ? v[hf][k][0] : make_uint2(0, 0), b = real[hf][1] ? v[hf][k][1] : make_uint2(0, 0);
             tmem_st_16x8(tq + ((uint32_t)(hf * 16) << 16) + 8 * c, a.x, a.y, b.x, b.y);
         }
     }
 }
-
 // DEAL: p.waves > 0 (a kernel of its own: the segment lookup with waves cost
 // 1 % of the time where there are none).  TREE: the tail is a draft (p.anc): a
 // row sees the live entries and, of the tail, the nodes of its ancestor word.
@@ -297,7 +317,9 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                         waited = true;
                     }
                     const int st = j % STAGES;
-                    if (j >= STAGES)
+                    // a draft's blocks have few units: their first Q and K tiles come before the rings fill up
+                    if (TREE && j == (is_k ? 1 : 0)) ok = mbar_wait(bar(Q_FULL), 0, abort_flag, p.err, kErrWait, p.diag, 0x14);
+                    if (ok && j >= STAGES)
                         ok = mbar_wait(bar(empty + st), (j / STAGES - 1) & 1, abort_flag, p.err, kErrWait, p.diag,
                                        (is_k ? 0x12 : 0x13) + 256 * j);
                     if (!ok) break;
@@ -479,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 tc_fence_before();
                 mbar_arrive(bar(S_EMPTY + grp));
                 // the segment's last S has landed, so no MMA reads Q any more
-                if (i + 1 == n && has_next) stage_q(tile_of(seg + 1));
+                if (!TREE && i + 1 == n && has_next) stage_q(tile_of(seg + 1));
                 const int key0 = (k + i) * BN;
                 if (key0 + BN > lim) {
                     if constexpr (TREE) {
@@ -563,9 +585,11 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 mr = mn;
             }
             // the group without the segment's last tile stages its half of the
-            // next Q too (the tile's S buffer is not filled again before that)
-            if (has_next && ((j + n - 1) & 1) != grp) {
-                wait_all(S_FULL + (grp ^ 1), ((j + n - 1) >> 1) & 1, 0x35 + 256 * j);
+            // next Q too (the tile's S buffer is not filled again before that); a
+            // draft's Q, which takes more registers to stage, both groups here
+            const bool other = ((j + n - 1) & 1) != grp;
+            if (has_next && (TREE || other)) {
+                if (other) wait_all(S_FULL + (grp ^ 1), ((j + n - 1) >> 1) & 1, 0x35 + 256 * j);
                 tc_fence_after();
                 stage_q(tile_of(seg + 1));
             }
