@@ -391,7 +391,21 @@ kvm_status plan_spans(const kvm_ctx* c, const int32_t* span_cu, const int32_t* s
 // wave (see tail_attn_tc.cu), and only the rest is cut, each block's share
 // starting from the cost of what it was dealt.
 
-void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, int grid_cap, bool deal, AttnPlan& pl) {
+struct PlanCost {
+    int min_units;                                   // smallest share of a block
+    double segment;                                  // extra cost of a segment, in units
+};
+constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
+// A draft has few query tiles with long key lists: what a segment costs beside its
+// units (its parts' stores and their merge) weighs more, and where the cache bounds
+// the time even cuts matter less.  32 characters of up to 16K live entries and 24
+// nodes, us a layer with 8 | 12 | 24 | 40: 113 | 107 | 106 | 102 (8K, 64 nodes: 102 | 100 | 98
+// | 100).  Three units at least: one character's 4 nodes over 8K 14.0 with four, 13.7
+// with three, 14.4 with two.
+constexpr PlanCost kDraftCost{3, 32.0};
+
+void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, int grid_cap, bool deal, const PlanCost& cost_of,
+                    AttnPlan& pl) {
     pl.n_qtiles.assign(B, 0);
     pl.tile_off.assign(B, 0);
     std::vector<int> nk_of;
@@ -420,7 +434,7 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
         pl.split_cb.clear();
         return;
     }
-    const int G = (int)std::max<int64_t>(1, std::min<int64_t>(grid_cap, units / kMinUnitsPerCta));
+    const int G = (int)std::max<int64_t>(1, std::min<int64_t>(grid_cap, units / cost_of.min_units));
     pl.n_ctas = G;
     pl.cta_tile.assign(G + 1, 0);
     pl.cta_k.assign(G + 1, 0);
@@ -429,11 +443,11 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
     if (deal && G == grid_cap) {
         // another wave while no block passes its even share of all the work
         // (the ranges level the rest): tiles of very uneven length are cut
-        const double share = ((double)units + kSegmentCost * tiles) / G;
+        const double share = ((double)units + cost_of.segment * tiles) / G;
         for (std::vector<double> next = load; (pl.waves + 1) * G + G / 2 <= tiles; ++pl.waves) {
             double most = 0.0;
             for (int cc = 0; cc < G; ++cc) {
-                next[cc] += kSegmentCost + nk_of[pl.waves * G + ((pl.waves & 1) ? G - 1 - cc : cc)];
+                next[cc] += cost_of.segment + nk_of[pl.waves * G + ((pl.waves & 1) ? G - 1 - cc : cc)];
                 most = std::max(most, next[cc]);
             }
             if (most > share) break;
@@ -441,7 +455,7 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
         }
     }
     const int first = pl.waves * G;                           // first tile that is not dealt
-    auto start_cost = [&](int block) { return (block < G ? load[block] : 0.0) + kSegmentCost; };
+    auto start_cost = [&](int block) { return (block < G ? load[block] : 0.0) + cost_of.segment; };
     // blocks needed to cover everything with ranges of cost <= target; the
     // cut points go to cta_tile / cta_k when `emit`
     auto cover = [&](double target, bool emit) -> int {
@@ -450,7 +464,7 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
         if (emit) { pl.cta_tile[0] = first; pl.cta_k[0] = 0; }
         for (int t = first; t < (int)nk_of.size(); ++t) {
             int k = 0;
-            if (t > first) cost += kSegmentCost;              // entering a new query tile
+            if (t > first) cost += cost_of.segment;              // entering a new query tile
             while (k < nk_of[t]) {
                 const double room = target - cost;
                 const int take = room >= nk_of[t] - k ? nk_of[t] - k : std::max(0, (int)room);
@@ -471,7 +485,7 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
         }
         return blocks;
     };
-    double lo = (double)units / G, hi = (double)units / G + 2.0 * kSegmentCost * (1 + tiles / G) + 1.0;
+    double lo = (double)units / G, hi = (double)units / G + 2.0 * cost_of.segment * (1 + tiles / G) + 1.0;
     while (cover(hi, false) > G) hi *= 2;
     for (int it = 0; it < 40 && hi - lo > 0.25; ++it) {
         const double mid = 0.5 * (lo + hi);
@@ -920,7 +934,7 @@ kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_
         if (L[b] < 0) return fail(KVM_E_INVAL, "negative live length at character %d", b);
     }
     AttnPlan pl;
-    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, pl);
+    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, kTailCost, pl);
     if (n_waves) *n_waves = pl.waves;
     *n_blocks = pl.n_ctas;
     *n_tiles = pl.n_tiles;
@@ -1269,7 +1283,7 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
     AttnPlan pl;
-    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, pl);
+    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, kTailCost, pl);
     drop_draft(c);
     return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
 }
@@ -1840,7 +1854,7 @@ kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent
             std::vector<int> M(c->B);
             for (int b = 0; b < c->B; ++b) M[b] = node_cu[b + 1] - node_cu[b];
             plan_attention(c->B, c->live.data(), M.data(), c->Hkv, kAttnRows / c->g,
-                           attention_grid_cap(c->num_sms, c->D), true, c->draft_plan);
+                           attention_grid_cap(c->num_sms, c->D), true, kDraftCost, c->draft_plan);
         }
         thread_local static DraftTreeParams p;
         p.n_chars = c->B;
