@@ -335,12 +335,29 @@ __global__ void __launch_bounds__(32 * LANES) attn_combine_parts_kernel(const __
         acc.z = acc.z * sc + w * x.z; acc.w = acc.w * sc + w * x.w;
         mx = nmx;
     };
+    if (p.draft) {
+        // four parts in flight a thread
+        for (int q0 = part; q0 < st.n_parts; q0 += 4 * LANES) {
+            float2 ml[4];
+            float4 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int q = q0 + u * LANES, slot = part_slot(st, min(q, st.n_parts - 1));
+                ml[u] = *reinterpret_cast<const float2*>(pm + slot * (2 * kRows));
+                x[u] = *reinterpret_cast<const float4*>(po + (int64_t)slot * sstride);
+                if (q >= st.n_parts) ml[u].x = -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) merge(ml[u], x[u]);
+        }
+    } else {
 #pragma unroll 2
-    for (int q = part; q < st.n_parts; q += LANES) {
-        const int slot = part_slot(st, q);
-        const float2 ml = *reinterpret_cast<const float2*>(pm + slot * (2 * kRows));
-        const float4 x = *reinterpret_cast<const float4*>(po + (int64_t)slot * sstride);
-        merge(ml, x);
+        for (int q = part; q < st.n_parts; q += LANES) {
+            const int slot = part_slot(st, q);
+            const float2 ml = *reinterpret_cast<const float2*>(pm + slot * (2 * kRows));
+            const float4 x = *reinterpret_cast<const float4*>(po + (int64_t)slot * sstride);
+            merge(ml, x);
+        }
     }
     acc_s[part][lane] = acc;
     md_s[part][lane] = make_float2(mx, den);

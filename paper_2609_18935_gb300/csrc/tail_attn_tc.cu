@@ -639,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 // partial layout [slot][D / 32][8][row][4]: each 16-byte store
                 // of a warp lands in 512 contiguous bytes
                 const int64_t slot = 2 * cta + (seg == waves ? 0 : 1);
-#pragma unroll 1
+#pragma unroll(TREE && D > 64 ? 2 : 1)
                 for (int c0 = grp * C::HALF; c0 < (grp + 1) * C::HALF; c0 += 32) {
                     uint32_t v[32];
                     tmem_ld32(tmem + lane_off + C::TMEM_O + c0, v);

@@ -192,10 +192,10 @@ def test_a_node_outside_the_path_changes_nothing(d):
 
 
 def test_a_chain_equals_a_tail():
-    """What the tail call gives, and after a commit its rows and positions bit for bit.  Where blocks share a query tile their
-    parts are the same but merged in another order: each side's fp32 sum of at most 32 parts is within 64 * 2^-24 = 2^-18 of the
-    sum of the parts' sizes, sum_j p_j |v_j| <= max |v|, and each is rounded to bf16 once, by at most 2^-8 of its value; so two
-    outputs a, b differ by at most 2^-8 (|a| + |b|) + 2^-17 max |v|.  A tile of one block alone is the same bit for bit."""
+    """What the tail call gives, and after a commit its rows and positions bit for bit.  A tile of one block alone is the same bit
+    for bit too.  Where several blocks share a tile, the two calls cut its keys at other places: a part's weights are rounded to
+    bf16 relative to the part's own largest score, so each side has roundings of its own, of at most the size that the bound on
+    either against the oracle counts (2^-8 of sum p |v|); both are held to that bound."""
     import torch
     for live, n in ((50, 7), (3000, 64), (0, 1)):
         a, b = Attn(16, 2, 256, 64, [live], seed=41), Attn(16, 2, 256, 64, [live], seed=41)
@@ -208,8 +208,9 @@ def test_a_chain_equals_a_tail():
         b.ctx.advance(cu)
         if live < 256:
             assert torch.equal(out.view(torch.int16), ref.view(torch.int16))
-        x, y, most = out.double(), ref.double(), max(float(v.abs().max()), float(np.abs(a.caches[0].V).max(initial=0.0)))
-        assert bool(((x - y).abs() <= 2.0 ** -8 * (x.abs() + y.abs()) + 2.0 ** -17 * most).all())
+        else:
+            for got in (out, ref):
+                a.check([tree("chain", n)], x, got)
         a.ctx.draft_commit(cu, np.arange(n))
         assert a.ctx.get_live(0) == b.ctx.get_live(0)
         for s, t in zip((*a.ctx.get_kv(0, 0), a.ctx.get_positions(0)), (*b.ctx.get_kv(0, 0), b.ctx.get_positions(0))):
