@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(256) draft_tree_kernel(const __grid_constant__
         p.anc[n0 + i] = anc;
         depth[threadIdx.x] = __popcll(anc) - 1;
         p.pos[n0 + i] = (int32_t)(p.cursor[b] + depth[threadIdx.x]);
+        p.slot[n0 + i] = p.slot0[b] + i;
     }
     __syncthreads();
     const int half = p.R / 2;
@@ -61,19 +62,11 @@ __global__ void __launch_bounds__(256) draft_tree_kernel(const __grid_constant__
 // A block a node, a thread eight elements of a key or value row, those of a rotary
 // pair (i, i + R / 2) together: the attention that follows rotates q itself and
 // waits for this kernel only where it reads the nodes' rows.
-__global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant__ DraftAppendParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
     const int n = blockIdx.x;
-    int lo = 0, hi = p.n_chars - 1;              // last b with tail_off <= n owns node n
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.ch[mid].tail_off <= n) lo = mid; else hi = mid - 1;
-    }
-    const AttnChar& c = p.ch[lo];
-    const int i = n - c.tail_off;
-    if (i < 0 || i >= c.M) { if (threadIdx.x == 0) atomicOr(p.err, kErrBounds); return; }
-    const int64_t slot = c.cap_off + c.L_prev + i;
+    const int64_t slot = p.slot[n];
     const int D = p.D, half = p.R / 2, rot = half / 8, per = D / 8, keys = p.Hkv * (per - rot);
     for (int e = threadIdx.x; e < keys + p.Hkv * per; e += blockDim.x) {
         const bool is_v = e >= keys;
@@ -99,7 +92,7 @@ __global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant
         }
         *reinterpret_cast<uint4*>(dst) = a;
     }
-    if (threadIdx.x == 0) p.pos[slot] = p.tail_pos[n];
+    if (threadIdx.x == 0) p.cache_pos[slot] = p.pos[n];
 }
 
 constexpr int kThreads = 128;
@@ -249,8 +242,8 @@ void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s) {
     launch_pdl(draft_tree_kernel, dim3(p.n_chars, (p.most + kTreeNodes - 1) / kTreeNodes), dim3(256), 0, s, p);
 }
 
-void launch_draft_append(const AttnParams& p, int nodes, cudaStream_t s) {
-    launch_pdl(draft_append_kernel, dim3(nodes), dim3(128), 0, s, p);
+void launch_draft_append(const DraftAppendParams& p, cudaStream_t s) {
+    launch_pdl(draft_append_kernel, dim3(p.nodes), dim3(128), 0, s, p);
 }
 
 void launch_draft_commit(const DraftCommitParams& p, cudaStream_t s) {

@@ -15,8 +15,9 @@
 //    of the B operand of S [K; Q]^T and, itself against its K rows, both operands
 //    of [K; Q] K^T.  Both products run on the tensor cores (tcgen05, M 128: the
 //    rows of S, of [K; Q]) into TMEM, 3 T columns.
-//  * S is fp32: 64 columns at a time, loaded as whole lines into registers while
-//    the inputs are staged, then split into three bf16 parts of eight bits each
+//  * S is fp32: 64 columns at a time (side by side where that costs no block an
+//    SM, so that the second half is split while the first one's products run),
+//    loaded as whole lines into registers while the inputs are staged, then split into three bf16 parts of eight bits each
 //    (by truncation: two masks and two exact differences, where rounding took
 //    conversions at an eighth of the rate and 2.9 us a block).  u enters the states
 //    of later steps, so all of S's bits take part.
@@ -33,6 +34,8 @@
 //    of the diagonal blocks are formed in fp32, a column a lane.
 // R_ij = G_i / G_j while no G is small, else products down the path (a decay of 0
 // is one).
+#include <type_traits>
+
 #include "kvm_internal.cuh"
 #include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
@@ -54,15 +57,17 @@ constexpr float kSmallDecay = 0x1p-40f;
 // Shared memory for trees of up to T nodes (a multiple of 16).  [K; Q] comes first:
 // as an A operand it is read up to row 127, past its own 2 T.
 struct Layout {
-    int kq, v, s, misc, bytes;
-    __host__ __device__ Layout(int T, int dk, int raw) {       // raw: bytes of a node's unconvolved inputs, or 0
+    int kq, v, s, misc, w, bytes;
+    // raw: bytes of a node's unconvolved inputs, or 0; wide: both halves of S side by side
+    __host__ __device__ Layout(int T, int dk, int raw, bool wide) {
         const int diag = T / 16 * (16 * kLdf * 4 + 3 * 16 * kLdd * 2), tile = 2 * T * dk * 2;
-        const int parts = 3 * kPartBytes, x = (T + 3) * raw;
+        const int parts = 3 * kPartBytes * (wide ? dk / 64 : 1), x = (T + 3) * raw;
         kq = 0;
         v = (max_(tile, diag) + 1023) / 1024 * 1024;
         s = (v + T * kLdv * 2 + 1023) / 1024 * 1024;
         misc = (s + max_(parts, x) + 1023) / 1024 * 1024;
-        bytes = misc + 2048;
+        w = misc + 2048;                         // the convolution's taps, 16 bytes a channel (raw: 2 bytes a channel)
+        bytes = w + 8 * raw;
     }
     static __host__ __device__ int max_(int a, int b) { return a > b ? a : b; }
 };
@@ -89,18 +94,14 @@ __device__ __forceinline__ uint32_t take_part(float& a, float& b) {
 // l / 4 and l / 4 + 8, columns 2 (l % 4) and the next; A's pairs are two such D
 // side by side, B's are k rows of column l / 4.
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 16 TMEM lanes x 16 columns, as two such D.
-__device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, float (&d)[2][4]) {
-    uint32_t r[8];
+// 16 TMEM lanes x 16 columns, as two such D (to be waited for).
+__device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
-    tmem_ld_wait();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) d[e >> 2][e & 3] = __uint_as_float(r[e]);
 }
 // d += lo, lo = 0
 __device__ __forceinline__ void join(float (&d)[2][4], float (&lo)[2][4]) {
@@ -153,12 +154,6 @@ __device__ __forceinline__ void block_mma(float (&d)[2][4], float (&lo)[2][4], c
     }
 }
 
-// The convolution, SiLU and (norm) the scaling to unit length of one part of the
-// staged raw rows [3 carried + nodes][pitch bytes]: four channels a lane, `per`
-// lanes a node (8, 16 or 32; lanes past dim / 4 idle), the taps in registers, four
-// nodes a thread at a time.  taps: per node the staged rows of its four taps, a
-// byte each.
-constexpr int kAhead = 4;
 // x / (1 + e^-x) with approximate exponential and reciprocal: within 2^-21, and the
 // result is rounded to eight bits (from -88.7 down, where it is below 2^-121, 0).
 __device__ __forceinline__ float silu(float x) {
@@ -166,58 +161,74 @@ __device__ __forceinline__ float silu(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
     return x * r;
 }
-__device__ __forceinline__ int conv_lanes(int dim) { return dim <= 32 ? 8 : dim <= 64 ? 16 : 32; }
-__device__ __forceinline__ void conv_taps(float4 (&tap)[4], int dim, const float* w) {
-    const int c = 4 * (threadIdx.x % conv_lanes(dim));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) tap[e] = c < dim ? *(reinterpret_cast<const float4*>(w) + c + e) : make_float4(0, 0, 0, 0);
-}
+// Place of channel e's taps in shared memory: lanes read octets of channels, 128
+// bytes apart.
+__device__ __forceinline__ int tap_slot(int e) { return (e & ~7) | ((e ^ e >> 3) & 7); }
+// The convolution, SiLU and (norm) the scaling to unit length of one part of the
+// staged raw rows [3 carried + nodes][pitch bytes], for put(node, channel, eight
+// outputs): eight channels a lane, their taps in registers, two nodes a thread at a
+// time.  rows: per node the staged rows of its four taps, a byte each.
 template <typename Put>
-__device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim, const float4 (&tap)[4], bool norm, int n,
-                                          const uint32_t* taps, Put put) {
-    const int per = conv_lanes(dim);
-    const int lane = threadIdx.x % per, c = 4 * lane, step = kThreads / per;
+__device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim, const float4* w, bool norm, int n, const uint32_t* rows,
+                                          Put put) {
+    constexpr int AHEAD = 2;
+    const int per = dim <= 32 ? 4 : dim <= 64 ? 8 : 16;        // lanes a node; those past dim / 8 idle
+    const int c = 8 * (threadIdx.x % per), first = threadIdx.x / per, step = kThreads / per;
     const bool act = c < dim;
-    raw += act ? 2 * c : 0;
-    for (int i0 = threadIdx.x / per; i0 - (int)threadIdx.x / per < n; i0 += kAhead * step) {
-        uint2 x[kAhead][4];
+    if (act) { raw += 2 * c; w += c; }
+    f2 tap[4][4];                                              // [tap][channel pair]
+    const int turn = act ? threadIdx.x % per & 7 : 0;          // the channels of an octet lie turned (tap_slot): neighbours on other banks
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const uint32_t rows = taps[min(i0 + a * step, n - 1)];
+    for (int e = 0; e < 4; ++e) {
+        const float4 f = w[2 * e ^ turn], g = w[(2 * e + 1) ^ turn];
+        tap[0][e] = pack2(f.x, g.x); tap[1][e] = pack2(f.y, g.y); tap[2][e] = pack2(f.z, g.z); tap[3][e] = pack2(f.w, g.w);
+    }
+#pragma unroll 1
+    for (int i0 = first; i0 - first < n; i0 += AHEAD * step) {
+        uint4 x[AHEAD][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) x[a][t] = *reinterpret_cast<const uint2*>(raw + (rows >> (8 * t) & 255) * pitch);
+        for (int a = 0; a < AHEAD; ++a) {
+            const uint32_t r = rows[min(i0 + a * step, n - 1)];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[a][t] = *reinterpret_cast<const uint4*>(raw + (r >> (8 * t) & 255) * pitch);
         }
-        float y[kAhead][4], sq[kAhead];
+        float y[AHEAD][8], sq[AHEAD];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            f2 lo = 0, hi = 0;
+        for (int a = 0; a < AHEAD; ++a) {
+            f2 acc[4] = {};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const float2 l = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[a][t].x));
-                const float2 h = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[a][t].y));
-                auto at = [&](const float4& f) { return t == 0 ? f.x : t == 1 ? f.y : t == 2 ? f.z : f.w; };
-                lo = fma2(pack2(at(tap[0]), at(tap[1])), pack2(l.x, l.y), lo);
-                hi = fma2(pack2(at(tap[2]), at(tap[3])), pack2(h.x, h.y), hi);
+                const uint32_t* u = reinterpret_cast<const uint32_t*>(&x[a][t]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[e] = fma2(tap[t][e], pack2(__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xffff0000u)), acc[e]);
             }
-            const float2 l = unpack2(lo), h = unpack2(hi);
-            y[a][0] = silu(l.x); y[a][1] = silu(l.y); y[a][2] = silu(h.x); y[a][3] = silu(h.y);
-            sq[a] = act ? fmaf(y[a][0], y[a][0], fmaf(y[a][1], y[a][1], fmaf(y[a][2], y[a][2], y[a][3] * y[a][3]))) : 0.f;
+            sq[a] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 v = unpack2(acc[e]);
+                y[a][2 * e] = silu(v.x);
+                y[a][2 * e + 1] = silu(v.y);
+                sq[a] = fmaf(y[a][2 * e], y[a][2 * e], fmaf(y[a][2 * e + 1], y[a][2 * e + 1], sq[a]));
+            }
         }
-        if (norm) {                                  // whole warps run the loop
+        if (norm) {                                            // whole warps run the loop
             for (int o = per / 2; o > 0; o >>= 1)
 #pragma unroll
-                for (int a = 0; a < kAhead; ++a) sq[a] += __shfl_xor_sync(0xffffffffu, sq[a], o);
+                for (int a = 0; a < AHEAD; ++a) sq[a] += __shfl_xor_sync(0xffffffffu, sq[a], o);
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
+            for (int a = 0; a < AHEAD; ++a) {
                 const float inv = sq[a] > 0.f ? rsqrtf(sq[a]) : 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[a][e] *= inv;
+                for (int e = 0; e < 8; ++e) y[a][e] *= inv;
             }
         }
         // rounded to bf16, the operands' type, as after the convolution of a tail
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (act && i0 + a * step < n) put(i0 + a * step, c, make_uint2(pack_bf16(y[a][0], y[a][1]), pack_bf16(y[a][2], y[a][3])));
+        for (int a = 0; a < AHEAD; ++a)
+            if (act && i0 + a * step < n)
+                put(i0 + a * step, c, make_uint4(pack_bf16(y[a][0], y[a][1]), pack_bf16(y[a][2], y[a][3]), pack_bf16(y[a][4], y[a][5]),
+                                                 pack_bf16(y[a][6], y[a][7])));
     }
 }
 
@@ -230,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     if (n <= 0) return;
     const int H = p.H, dv = p.dv, hk = H * DK;
     const int pitch = CONV ? (2 * DK + dv) * 2 : 0;
-    const Layout at((p.most + 15) / 16 * 16, DK, pitch);
+    const Layout at((p.most + 15) / 16 * 16, DK, pitch, p.wide);
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
     const int T = (n + 15) / 16 * 16, NB = T / 16;
@@ -240,11 +251,11 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     float* be = al + kDraftNodes;
     float* G = be + kDraftNodes;
     float* rG = G + kDraftNodes;
-    const uint32_t bar = base + at.misc + 1536;                            // one barrier per half of S, one of the raw rows
+    const uint32_t bar = base + at.misc + 1536;                            // one barrier per half of S
     uint32_t* slot = reinterpret_cast<uint32_t*>(smem + at.misc + 1560);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + at.misc + 1564);
     int* small = reinterpret_cast<int*>(smem + at.misc + 1568);
-    uint32_t* taps = reinterpret_cast<uint32_t*>(smem + at.misc + 1572);   // [64]
+    uint32_t* rows = reinterpret_cast<uint32_t*>(smem + at.misc + 1572);   // [64] staged rows of each node's taps
     constexpr int kPart = kDraftNodes * kLdc;        // elements of a part of C or E
     __nv_bfloat16* Cp = reinterpret_cast<__nv_bfloat16*>(smem + at.s);     // C: three parts, blocks left of the diagonal
     __nv_bfloat16* Ep = Cp + 3 * kPart;                                    // E: two
@@ -258,14 +269,13 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     if (tid == 0) {
         *abort_flag = 0;
         *small = 0;
-        for (int x = 0; x < 3; ++x) mbar_init(bar + 8 * x, 1);
+        for (int x = 0; x < 2; ++x) mbar_init(bar + 8 * x, 1);
         fence_mbar_init();
     }
     if (warp == 0) {
         tmem_alloc(smem_u32(slot), cols);
         tmem_relinquish();
     }
-    if constexpr (CONV) __syncthreads();             // the barrier that the raw rows arrive at
     grid_dependency_wait();
     grid_dependents_launch();
 
@@ -275,18 +285,25 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         const __nv_bfloat16* qg = p.q + (int64_t)n0 * hk + h * DK;
         const __nv_bfloat16* vg = p.v + ((int64_t)n0 * H + h) * dv;
         if constexpr (CONV) {
-            // raw rows q | k | v, three carried ones first: a thread's bulk copies a row
-            if (tid == 0) mbar_arrive_expect_tx(bar + 16, (uint32_t)((n + 3) * pitch));
-            __syncwarp();
-            if (tid < n + 3) {
-                const __nv_bfloat16* st = p.state_in + ((int64_t)b * 3 + tid) * p.channels;
-                const bool old = tid < 3;
-                const int i = tid - 3;
-                const uint32_t dst = base + at.s + tid * pitch;
-                bulk_load(dst, old ? st + h * DK : qg + (int64_t)i * hk, DK * 2, bar + 16);
-                bulk_load(dst + 2 * DK, old ? st + hk + h * DK : kg + (int64_t)i * hk, DK * 2, bar + 16);
-                bulk_load(dst + 4 * DK, old ? st + 2 * hk + h * dv : vg + (int64_t)i * H * dv, dv * 2, bar + 16);
+            // raw rows q | k | v, three carried ones first, a warp a row (as bulk copies, three a row, they took 4K cycles to
+            // issue at 64 nodes), and the taps in the same order
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int x = lane + 32 * u;
+                if (x >= pitch / 16) break;
+                const bool is_q = x < GK, is_v = x >= 2 * GK;
+                const int c = 8 * (is_q ? x : is_v ? x - 2 * GK : x - GK);
+                const __nv_bfloat16* src = (is_v ? vg : is_q ? qg : kg) + c;
+                const int64_t stride = is_v ? H * dv : hk;
+                const uint32_t dst = base + at.s + 16 * x;
+                if (warp < 3)
+                    cp_async16(dst + warp * pitch, p.state_in + ((int64_t)b * 3 + warp) * p.channels +
+                                                       (is_q ? h * DK : is_v ? 2 * hk + h * dv : hk + h * DK) + c);
+                for (int i = warp; i < n; i += kThreads / 32) cp_async16(dst + (3 + i) * pitch, src + i * stride);
             }
+            for (int e = tid; e < 2 * DK + dv; e += kThreads)
+                cp_async16(base + at.w + 16 * tap_slot(e),
+                           p.w + (int64_t)(e < DK ? h * DK + e : e < 2 * DK ? hk + h * DK + e - DK : 2 * hk + h * dv + e - 2 * DK) * 4);
         } else {
             for (int e = tid; e < 2 * n * GK; e += kThreads) {
                 const int row = e / GK, c = 8 * (e % GK);
@@ -301,24 +318,22 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     }
     const float* Sg = p.S + ((int64_t)b * H + h) * dv * DK;
     float4 s[HALVES][8];
-    auto load_s = [&]() {
+    auto load_s = [&](auto half) {
+        constexpr int x = decltype(half)::value;
 #pragma unroll
-        for (int x = 0; x < HALVES; ++x)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
-                s[x][e] = row < dv ? *reinterpret_cast<const float4*>(Sg + (int64_t)row * DK + 64 * x + 4 * c4) : make_float4(0, 0, 0, 0);
-            }
+        for (int e = 0; e < 8; ++e) {
+            const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
+            s[x][e] = row < dv ? *reinterpret_cast<const float4*>(Sg + (int64_t)row * DK + 64 * x + 4 * c4) : make_float4(0, 0, 0, 0);
+        }
     };
+    using First = std::integral_constant<int, 0>;
+    using Last = std::integral_constant<int, HALVES - 1>;
     // the convolution needs the registers: there S comes after it, from L2
-    float4 tk[4], tq[4], tv[4];
     if constexpr (CONV) {
         for (int e = tid * 32; e < dv * DK; e += kThreads * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(Sg + e));
-        conv_taps(tk, DK, p.w + (int64_t)(hk + h * DK) * 4);
-        conv_taps(tq, DK, p.w + (int64_t)(h * DK) * 4);
-        conv_taps(tv, dv, p.w + (int64_t)(2 * hk + h * dv) * 4);
     } else {
-        load_s();
+        load_s(First());
+        if (HALVES > 1) load_s(Last());
     }
     if (tid < n) {
         const uint64_t own = p.anc[n0 + tid];
@@ -326,14 +341,14 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         if constexpr (CONV) {
             // staged rows of the taps: 3 is the node, 2 its parent, .. and then the carried inputs from the last back
             uint64_t m = own;
-            uint32_t rows = 0;
+            uint32_t r = 0;
 #pragma unroll
             for (int t = 3; t >= 0; --t) {
                 const int a = m ? 63 - __clzll((long long)m) : -1;
                 m &= ~(a >= 0 ? 1ull << a : 0ull);
-                rows |= (uint32_t)(a >= 0 ? 3 + a : t + __popcll(own) - 1) << (8 * t);
+                r |= (uint32_t)(a >= 0 ? 3 + a : t + __popcll(own) - 1) << (8 * t);
             }
-            taps[tid] = rows;
+            rows[tid] = r;
         }
         const float a = p.alpha[(int64_t)(n0 + tid) * H + h];
         al[tid] = a;
@@ -350,41 +365,39 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
 
     if constexpr (CONV) {
         const uint8_t* raw = smem + at.s;
-        ok = mbar_wait(bar + 16, 0, abort_flag, p.err, kErrWait, p.diag, 0x60);
-        if (tid < n && ok) {                         // what a commit carries on
-            __nv_bfloat16* rec = p.rec_x + (int64_t)(n0 + tid) * p.channels;
-            const uint32_t src = base + at.s + (3 + tid) * pitch;
-            bulk_store(rec + h * DK, src, DK * 2);
-            bulk_store(rec + hk + h * DK, src + 2 * DK, DK * 2);
-            bulk_store(rec + 2 * hk + h * dv, src + 4 * DK, dv * 2);
-            bulk_commit();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {                // what a commit carries on
+            const int x = lane + 32 * u;
+            if (x >= pitch / 16) break;
+            __nv_bfloat16* rec = p.rec_x + (int64_t)n0 * p.channels +
+                                 (x < GK ? h * DK + 8 * x : x < 2 * GK ? hk + h * DK + 8 * (x - GK) : 2 * hk + h * dv + 8 * (x - 2 * GK));
+            for (int i = warp; i < n; i += kThreads / 32)
+                *reinterpret_cast<uint4*>(rec + (int64_t)i * p.channels) = *reinterpret_cast<const uint4*>(raw + (3 + i) * pitch + 16 * x);
         }
-        conv_part(raw + 2 * DK, pitch, DK, tk, true, n, taps, [&](int i, int c, uint2 y) {
-            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(i, c, 2 * T)) = y;
-        });
-        conv_part(raw, pitch, DK, tq, false, n, taps, [&](int i, int c, uint2 y) {
-            *reinterpret_cast<uint2*>(smem + at.kq + sw128_off16(T + i, c, 2 * T)) = y;
-        });
-        conv_part(raw + 4 * DK, pitch, dv, tv, false, n, taps, [&](int i, int c, uint2 y) {
-            *reinterpret_cast<uint2*>(vs + i * kLdv + c) = y;
-        });
-        load_s();
-        if (tid < n) bulk_wait_read();
-        ok = __syncthreads_and(ok);                  // the raw rows make room for S's parts
+        const float4* w = reinterpret_cast<const float4*>(smem + at.w);
+#pragma unroll 1
+        for (int part = 0; part < 3; ++part)         // q, k, v: one copy of the code
+            conv_part(raw + 2 * DK * part, pitch, part == 2 ? dv : DK, w + DK * part, part == 1, n, rows, [&](int i, int c, uint4 y) {
+                uint8_t* dst = part == 2 ? smem + at.v + (i * kLdv + c) * 2 : smem + at.kq + sw128_off16(part == 1 ? i : T + i, c, 2 * T);
+                *reinterpret_cast<uint4*>(dst) = y;
+            });
+        load_s(First());
+        if (HALVES > 1) load_s(Last());
+        __syncthreads();                             // the raw rows make room for S's parts
     }
     // ---- the products, 64 columns of S at a time
 #pragma unroll
     for (int x = 0; x < HALVES; ++x) {
-        if (x > 0) ok = ok && mbar_wait(bar + 8 * (x - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x61);   // the parts are consumed
+        if (x > 0 && !p.wide) ok = ok && mbar_wait(bar + 8 * (x - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x61);   // the parts are consumed
+        const int s0 = at.s + (p.wide ? 3 * x * kPartBytes : 0);
+        uint8_t* dst = smem + s0 + sw128_off16(tid >> 4, 4 * (tid & 15), kRowsA);       // and every 16 rows on (two of the swizzle's periods)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int row = (tid + e * kThreads) >> 4, c4 = tid & 15;
-            const uint32_t o = sw128_off16(row, 4 * c4, kRowsA);
             float4 v = s[x][e];
 #pragma unroll
             for (int part = 0; part < 3; ++part) {
                 const uint32_t lo = take_part(v.x, v.y), hi = take_part(v.z, v.w);
-                *reinterpret_cast<uint2*>(smem + at.s + part * kPartBytes + o) = make_uint2(lo, hi);
+                *reinterpret_cast<uint2*>(dst + part * kPartBytes + e * (16 * 128)) = make_uint2(lo, hi);
             }
         }
         fence_proxy_async_smem();
@@ -392,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         if (tid == 0 && ok) {
             tc_fence_after();
             const uint64_t kq = smem_desc_sw128(base + at.kq + x * region, 16, 1024);
-            const uint64_t sd = smem_desc_sw128(base + at.s, 16, 1024);
+            const uint64_t sd = smem_desc_sw128(base + s0, 16, 1024);
             const uint32_t id_s = idesc_bf16_f32(kRowsA, 2 * T, false), id_g = idesc_bf16_f32(kRowsA, T, false);
 #pragma unroll
             for (int part = 0; part < 3; ++part)
@@ -465,11 +478,12 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
             tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T + 16 * J, g);
             tmem_ld_wait();
             if (l >= 2 * T || J > I) continue;
+            const uint32_t bits = (uint32_t)(m >> (16 * J)) & 0xffffu;
             float y[16];
             if (!exact) {
 #pragma unroll
                 for (int c = 0; c < 16; ++c)
-                    y[c] = (m >> (16 * J + c) & 1) ? scale * rG[16 * J + c] * __uint_as_float(g[c]) : 0.f;
+                    y[c] = (bits >> c & 1) ? scale * rG[16 * J + c] * __uint_as_float(g[c]) : 0.f;
             } else {
                 // some decay is small: the product down the path, which reaches this block's nodes from the largest down
                 float R = scale;
@@ -480,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                 }
 #pragma unroll
                 for (int c = 15; c >= 0; --c) {
-                    y[c] = (m >> (16 * J + c) & 1) ? R * __uint_as_float(g[c]) : 0.f;
+                    y[c] = (bits >> c & 1) ? R * __uint_as_float(g[c]) : 0.f;
                     if (real && (anc[i] >> (16 * J + c) & 1)) R *= al[16 * J + c];
                 }
             }
@@ -513,7 +527,13 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         for (int i = 0; i < 16; ++i) {
             float t[2] = {i == j ? 1.f : 0.f, 0.f};
 #pragma unroll
-            for (int m = 0; m < i; ++m) t[m & 1] = fmaf(C[i * kLdf + m], x[m], t[m & 1]);
+            for (int m = 0; m < i; m += 4) {
+                const float4 c = *reinterpret_cast<const float4*>(C + i * kLdf + m);    // 0 on and right of the diagonal
+                t[0] = fmaf(c.x, x[m], t[0]);
+                if (m + 1 < i) t[1] = fmaf(c.y, x[m + 1], t[1]);
+                if (m + 2 < i) t[0] = fmaf(c.z, x[m + 2], t[0]);
+                if (m + 3 < i) t[1] = fmaf(c.w, x[m + 3], t[1]);
+            }
             x[i] = t[0] + t[1];
         }
         if (lane < 16) {
@@ -535,19 +555,28 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         const uint32_t lanes = tmem + ((uint32_t)r0 << 16);
         const int row = r0 + (lane >> 2), col = 2 * (lane & 3);
         uint32_t u[4][3][4];                         // the parts of each block's u
+        uint32_t xa[8], oa[8];                       // S k and S q of the next 16 nodes
+        tmem_ld_16x16(lanes, xa);
+        tmem_ld_16x16(lanes + T, oa);
 #pragma unroll
         for (int I = 0; I < 4; ++I) {
             if (I >= NB) break;
             float x[2][4], o[2][4], lo[2][4] = {};
-            tmem_ld_16x16(lanes + 16 * I, x);
+            tmem_ld_wait();
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int node = 16 * I + 8 * t + col + (e & 1), r = row + 8 * (e >> 1);
-                    const float v = __bfloat162float(vs[node * kLdv + r]);
-                    x[t][e] = node < n ? be[node] * (v - G[node] * x[t][e]) : 0.f;      // a padding row holds anything
+                    const float v = __bfloat162float(vs[node * kLdv + r]), gn = G[node];
+                    const float sk = __uint_as_float(xa[4 * t + e]), sq = __uint_as_float(oa[4 * t + e]);
+                    x[t][e] = node < n ? be[node] * (v - gn * sk) : 0.f;                 // a padding row holds anything
+                    o[t][e] = gn * sq;
                 }
+            if (I + 1 < NB) {
+                tmem_ld_16x16(lanes + 16 * (I + 1), xa);
+                tmem_ld_16x16(lanes + T + 16 * (I + 1), oa);
+            }
 #pragma unroll
             for (int J = 0; J < I; ++J) block_mma<3, 3>(x, lo, u[J], Cp + 16 * I * kLdc + 16 * J, kLdc, kPart);
             join(x, lo);
@@ -556,11 +585,6 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
             block_mma<3, 3>(y, lo, u[I], Dp + I * 3 * 16 * kLdd, kLdd, 16 * kLdd);
             join(y, lo);
             split(y, u[I]);
-            tmem_ld_16x16(lanes + T + 16 * I, o);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[t][e] *= G[16 * I + 8 * t + col + (e & 1)];
 #pragma unroll
             for (int J = 0; J <= I; ++J) {
                 const uint32_t (&a)[2][4] = *reinterpret_cast<const uint32_t (*)[2][4]>(&u[J]);
@@ -589,9 +613,6 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
             for (int i = tid >> 4; i < n; i += kThreads / 16)
                 *reinterpret_cast<uint4*>(p.out + ((int64_t)(n0 + i) * H + h) * dv + c) = *reinterpret_cast<const uint4*>(vs + i * kLdv + c);
     }
-    if constexpr (CONV) {
-        if (tid < n) bulk_wait_all();
-    }
     if (warp == 0) {
         tc_fence_after();
         tmem_dealloc(tmem, cols);
@@ -606,10 +627,10 @@ void launch(const DraftGdnParams& p, cudaStream_t s) {
     cudaGetDevice(&dev);
     if (!(configured >> (dev & 63) & 1ull)) {
         cudaFuncSetAttribute(draft_gdn_kernel<DK, CONV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             Layout(kDraftNodes, DK, CONV ? (2 * DK + 128) * 2 : 0).bytes + 1024);
+                             Layout(kDraftNodes, DK, CONV ? (2 * DK + 128) * 2 : 0, true).bytes + 1024);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(draft_gdn_kernel<DK, CONV>, dim3(p.H, p.n_chars), dim3(kThreads), Layout((p.most + 15) / 16 * 16, DK, pitch).bytes + 1024, s, p);
+    launch_pdl(draft_gdn_kernel<DK, CONV>, dim3(p.H, p.n_chars), dim3(kThreads), Layout((p.most + 15) / 16 * 16, DK, pitch, p.wide).bytes + 1024, s, p);
 }
 
 }  // namespace

@@ -340,15 +340,29 @@ struct DraftTreeParams {
     int32_t cu[kMaxChars + 1];
     int64_t cursor[kMaxChars];
     int8_t parent[kMaxDraftNodes];            // packed; -1: a root
+    int32_t slot0[kMaxChars];                 // slot of the character's first node: slot offset + live length
     uint64_t* anc;                            // device [sum n]
     int32_t* pos;                             // device [sum n]
+    int32_t* slot;                            // device [sum n]: the node's cache slot
     float2* turn;                             // device [sum n][R / 2]: (cos, sin) of each node's rotary angles
     int32_t R, most;                          // rotary dims; nodes of the largest tree
     double inv_freq[kMaxRotaryHalf];
 };
 void launch_draft_tree(const DraftTreeParams& p, cudaStream_t s);
-// Keys and values of a draft's nodes to their slots (R a multiple of 16; p.turn).
-void launch_draft_append(const AttnParams& p, int nodes, cudaStream_t s);
+// Keys and values of a draft's nodes to their slots (R a multiple of 16).
+struct DraftAppendParams {
+    int32_t nodes, Hkv, D, R;
+    int64_t slab_rows;
+    const __nv_bfloat16* k_new;               // [sum n][Hkv][D]
+    const __nv_bfloat16* v_new;
+    __nv_bfloat16* K;                         // this layer's slabs [Hkv][slab_rows][D]
+    __nv_bfloat16* V;
+    int32_t* cache_pos;                       // [slab_rows]
+    const int32_t* pos;                       // as the tree kernel left them
+    const int32_t* slot;
+    const float2* turn;
+};
+void launch_draft_append(const DraftAppendParams& p, cudaStream_t s);
 
 // The delta rule over a draft's nodes, and what a commit needs of each: its
 // update u, its key, its decay and, with the convolution, its raw inputs.
@@ -370,6 +384,7 @@ struct DraftGdnParams {
     float* rec_a;                             // [sum n][H]
     __nv_bfloat16* rec_x;                     // [sum n][channels] (with w)
     int32_t most;                             // nodes of the largest tree
+    int32_t wide;                             // both halves of S in shared memory at once
     int32_t* err;
     int32_t* diag;                            // first expired wait: block + 1, tag, parity
     int16_t order[kMaxChars];                 // characters by decreasing number of nodes
