@@ -111,21 +111,25 @@ __device__ __forceinline__ void load4(const T* row, int y, int m, int end, float
     for (int e = 0; e < 4; ++e) x[e] = probability(x[e]);
 }
 
-// Writes v over the neighbour's copy of *mine, in block `rank` of the cluster.
-__device__ __forceinline__ void st_cluster(const Pair* mine, uint32_t rank, Pair v) {
-    uint32_t addr;
+// Writes v over the neighbour's copy of *mine, in block `rank` of the cluster, and
+// counts its eight bytes in at that block's copy of the barrier.
+__device__ __forceinline__ void st_cluster(const Pair* mine, uint32_t bar, uint32_t rank, Pair v) {
+    uint32_t addr, at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(ptx::smem_u32(mine)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.hi), "f"(v.lo) : "memory");
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                 ::"r"(addr), "f"(v.hi), "f"(v.lo), "r"(at) : "memory");
 }
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_constant__ DraftVerifyParams p) {
     constexpr int kWarps = THREADS / 32;
     __shared__ Pair sums[kWarps];                    // this block's warps' sums of their ranges
     __shared__ Pair parts[2][kMaxCluster];           // every block's sum, two passes deep
+    __shared__ __align__(8) uint64_t arrived[2];     // and their barriers: a phase is all blocks' sums of a pass
+    __shared__ int abort_word;
     __shared__ float pt[kDraftNodes], qt[kDraftNodes], us[kDraftNodes];
     __shared__ int path[kDraftNodes];
     __shared__ unsigned long long kids[kDraftNodes];               // each node's children
@@ -140,7 +144,18 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     const T* draft = static_cast<const T*>(p.draft);
     grid_dependency_wait();
     grid_dependents_launch();
+    volatile int* abort_flag = &abort_word;
+    const uint32_t bar = ptx::smem_u32(arrived);
+    if (tid == 0) {
+        *abort_flag = 0;
+        ptx::mbar_init(bar, 1);
+        ptx::mbar_init(bar + 8, 1);
+        ptx::fence_mbar_init();
+    }
+    __syncwarp();
+    if (blocks > 1) cluster_arrive();                // the neighbours' barriers stand before the first sum arrives: waited for below
     if (n <= 0) {                                    // uniform over the cluster
+        if (blocks > 1) cluster_wait();
         if (rank == 0 && tid == 0) { p.count[b] = 0; p.next[b] = -1; }
         return;
     }
@@ -165,6 +180,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         qt[tid] = probability(y);
     }
     __syncthreads();
+    if (blocks > 1) cluster_wait();
 
     const int gw = rank * kWarps + warp, n_gw = blocks * kWarps;
     int cur = 0, count = 1, pass = 0;
@@ -173,6 +189,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     // this warp's part of the current row, and the sum over all of max(p - c q, 0)
     int m = 0, end = 0, per = 0;
     const T *rp = nullptr, *rq = nullptr;
+    bool lost = false;
     f2 ch2 = 0, nch2 = 0, ncl2 = 0;
     auto set_c = [&]() {
         ch2 = pack2(c.hi, c.hi);
@@ -195,14 +212,23 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         const Pair mine = warp_sum(add(Pair{hi.x, lo.x}, Pair{hi.y, lo.y}));
         if (lane == 0) sums[warp] = mine;
         __syncthreads();
-        Pair* all = parts[pass++ & 1];
+        Pair* all = parts[pass & 1];
         if (warp == 0) {
             const Pair z = warp_sum(lane < kWarps ? sums[lane] : Pair{0.f, 0.f});
-            if (blocks == 1) { if (lane == 0) all[0] = z; }
-            else if (lane < blocks) st_cluster(all + rank, lane, z);
+            if (blocks == 1) {
+                if (lane == 0) all[0] = z;
+            } else {
+                if (lane == 0) ptx::mbar_arrive_expect_tx(bar + 8 * (pass & 1), blocks * sizeof(Pair));
+                if (lane < blocks) st_cluster(all + rank, bar + 8 * (pass & 1), lane, z);
+            }
         }
+        // A block sends its sum of pass k + 2, over that of pass k, once it has all
+        // sums of pass k + 1, so every block has read those of pass k by then.
+        // An expired wait ends the walk of the whole block, and by its missing sums the
+        // others'.
         if (blocks == 1) __syncthreads();
-        else cluster_sync();
+        else lost = __syncthreads_or(!ptx::mbar_wait(bar + 8 * (pass & 1), pass >> 1 & 1, abort_flag, p.err, kErrWait, p.diag, 0x71));
+        ++pass;
         return warp_sum(lane < blocks ? all[lane] : Pair{0.f, 0.f});   // the same order in every warp
     };
     for (;;) {
@@ -222,14 +248,15 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
             if (!positive(Z)) break;                 // nothing is left of p: no other guess can be accepted
             c = positive(c) ? add(c, Z) : Pair{1.f, 0.f};
             Z = row_sum();
+            if (lost) break;
         }
-        if (taken < 0) break;
+        if (taken < 0 || lost) break;
         cur = taken;
         if (tid == 0) path[count] = cur;
         ++count;
     }
     // ---- the next token, from what is left of the last node's row (all of it where nothing is)
-    if (!positive(c) || !positive(Z)) {
+    if (!lost && (!positive(c) || !positive(Z))) {
         c = {0.f, 0.f};
         Z = row_sum();
     }
@@ -257,7 +284,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     };
     Pair before{0.f, 0.f};
     const int block = find(last, blocks, before);
-    const int found = block == (int)rank ? (int)rank * kWarps + find(sums, kWarps, before) : -1;
+    const int found = !lost && block == (int)rank ? (int)rank * kWarps + find(sums, kWarps, before) : -1;
     if (found == gw) {
         const int y1 = min(end, (gw + 1) * per);
         int best = -1;
@@ -290,12 +317,16 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         if (lane == 0) p.next[b] = best;
     }
     if (rank == 0) {
-        if (block < 0 && tid == 0) p.next[b] = -1;   // the row holds no positive number
+        if ((block < 0 || lost) && tid == 0) p.next[b] = -1;       // the row holds no positive number
         __syncthreads();
         if (tid < n) p.path[n0 + tid] = tid < count ? path[tid] : -1;
         if (tid == 0) p.count[b] = count;
     }
-    if (blocks > 1) cluster_sync();                  // no block leaves while another may still write to it
+    __syncwarp();
+    if (blocks > 1) {                                // no block leaves while another may still write to it
+        cluster_arrive();
+        cluster_wait();
+    }
 }
 
 }  // namespace

@@ -1991,6 +1991,7 @@ kvm_status draft_verify(kvm_ctx* c, int vocab, int prob_type, const int32_t* tok
     p.count = count;
     p.next = next;
     p.err = c->err;
+    p.diag = c->diag;
     const int ps = prof_begin(c, KVM_K_DRAFT_VERIFY, s);
     launch_draft_verify(p, prob_type == KVM_PROB_BF16, c->num_sms, s);
     prof_end(c, ps, s);

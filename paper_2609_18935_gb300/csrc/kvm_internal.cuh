@@ -406,6 +406,7 @@ struct DraftVerifyParams {
     int32_t* count;                           // [n_chars]
     int32_t* next;                            // [n_chars]
     int32_t* err;
+    int32_t* diag;                            // first expired wait: block + 1, tag, parity
 };
 void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cudaStream_t s);
 
