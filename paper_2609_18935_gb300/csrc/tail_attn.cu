@@ -449,10 +449,13 @@ void launch_attn_combine(const CombineParams& p, cudaStream_t s) {
     }
     const int part_blocks = (rows * (p.D / 4) + 31) / 32;
     if (p.draft) {
-        // up to a warp for two parts, while all of them are resident at once
+        // up to a warp for two parts, while that grid is two waves (54 registers a
+        // thread: 36 warps an SM), blocks of 16 warps only in one: 43 parts of two full
+        // tiles 17.6 us a layer with 16 warps (two waves), 16.7 with eight; 16 tiles of
+        // 64 rows 18.4 with four (two waves), 19.8 with two
         const int64_t blocks = (int64_t)p.n_split_tiles * part_blocks, room = 64 * (int64_t)sms;
         int lanes = 2;
-        while (lanes < 16 && 2 * lanes < parts && 2 * lanes * blocks <= room) lanes *= 2;
+        while (lanes < 16 && 2 * lanes < parts && 2 * lanes * blocks <= (lanes < 8 ? room : 36 * (int64_t)sms)) lanes *= 2;
         if (lanes * blocks <= room) {
             const dim3 grid(p.n_split_tiles, part_blocks), block(32 * lanes);
             if (lanes == 2) launch_pdl(attn_combine_parts_kernel<2>, grid, block, 0, s, p);
