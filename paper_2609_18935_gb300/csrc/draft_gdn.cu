@@ -158,7 +158,7 @@ __device__ __forceinline__ void block_mma(float (&d)[2][4], float (&lo)[2][4], c
 // result is rounded to eight bits (from -88.7 down, where it is below 2^-121, 0).
 __device__ __forceinline__ float silu(float x) {
     float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-1.4426950408889634f * x)));
     return x * r;
 }
 // Place of channel e's taps in shared memory: lanes read octets of channels, 128
@@ -183,18 +183,21 @@ __device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim
         const float4 f = w[2 * e ^ turn], g = w[(2 * e + 1) ^ turn];
         tap[0][e] = pack2(f.x, g.x); tap[1][e] = pack2(f.y, g.y); tap[2][e] = pack2(f.z, g.z); tap[3][e] = pack2(f.w, g.w);
     }
+    const int lead = (threadIdx.x & ~31) / per;                // the warp's first node: it leaves out what is past the last one
 #pragma unroll 1
-    for (int i0 = first; i0 - first < n; i0 += AHEAD * step) {
+    for (int i0 = 0; lead + i0 < n; i0 += AHEAD * step) {
+        const bool two = lead + i0 + step < n;                 // uniform per warp
         uint4 x[AHEAD][4];
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
-            const uint32_t r = rows[min(i0 + a * step, n - 1)];
+            if (a > 0 && !two) break;
+            const uint32_t r = rows[min(first + i0 + a * step, n - 1)];
 #pragma unroll
             for (int t = 0; t < 4; ++t) x[a][t] = *reinterpret_cast<const uint4*>(raw + (r >> (8 * t) & 255) * pitch);
         }
-        float y[AHEAD][8], sq[AHEAD];
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
+            if (a > 0 && !two) break;
             f2 acc[4] = {};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -203,32 +206,24 @@ __device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim
                 for (int e = 0; e < 4; ++e)
                     acc[e] = fma2(tap[t][e], pack2(__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xffff0000u)), acc[e]);
             }
-            sq[a] = 0.f;
+            float y[8], sq = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float2 v = unpack2(acc[e]);
-                y[a][2 * e] = silu(v.x);
-                y[a][2 * e + 1] = silu(v.y);
-                sq[a] = fmaf(y[a][2 * e], y[a][2 * e], fmaf(y[a][2 * e + 1], y[a][2 * e + 1], sq[a]));
+                y[2 * e] = silu(v.x);
+                y[2 * e + 1] = silu(v.y);
+                sq = fmaf(y[2 * e], y[2 * e], fmaf(y[2 * e + 1], y[2 * e + 1], sq));
             }
-        }
-        if (norm) {                                            // whole warps run the loop
-            for (int o = per / 2; o > 0; o >>= 1)
+            if (norm) {                                        // whole warps run this
+                for (int o = per / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                const float inv = sq > 0.f ? rsqrtf(sq) : 0.f;
 #pragma unroll
-                for (int a = 0; a < AHEAD; ++a) sq[a] += __shfl_xor_sync(0xffffffffu, sq[a], o);
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const float inv = sq[a] > 0.f ? rsqrtf(sq[a]) : 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[a][e] *= inv;
+                for (int e = 0; e < 8; ++e) y[e] *= inv;
             }
+            // rounded to bf16, the operands' type, as after the convolution of a tail
+            if (act && first + i0 + a * step < n)
+                put(first + i0 + a * step, c, make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])));
         }
-        // rounded to bf16, the operands' type, as after the convolution of a tail
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-            if (act && i0 + a * step < n)
-                put(i0 + a * step, c, make_uint4(pack_bf16(y[a][0], y[a][1]), pack_bf16(y[a][2], y[a][3]), pack_bf16(y[a][4], y[a][5]),
-                                                 pack_bf16(y[a][6], y[a][7])));
     }
 }
 
