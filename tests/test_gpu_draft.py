@@ -632,6 +632,7 @@ def test_steps_of_a_population(conv):
             paths.append(got)
         pair.ctx.draft_commit(cu_of(paths), sum(paths, []))
         _advance_oracle(pair, trees, paths, x)
+        pair.ctx.check()
         _compare_states(pair)
         if step == 0:
             tails = [5, 0, 40, 1]
@@ -652,6 +653,7 @@ def test_deep_paths_of_wide_rows():
         pair.ctx.draft_begin(cu_of(trees), packed(trees))
         outs = _layers(pair, x)
         pair.ctx.draft_commit(cu_of(paths), sum(paths, []))
+        pair.ctx.check()
         _advance_oracle(pair, trees, paths, x)
         _compare_states(pair)
         del outs
@@ -739,6 +741,114 @@ def test_a_step_on_a_side_stream_and_in_a_graph():
     _advance_oracle(pair, trees, [path, []], y)
     _compare_states(pair)
     del ref
+
+
+def test_a_character_behind_a_long_slab():
+    """Cache offsets past 2^31 elements: the second character's slots lie behind 2.2M slots of the first, in the second of two
+    layers."""
+    import torch
+    from harness import rel_l2
+    from paper_2609_18935_gb300 import kvm
+    first = 2_200_000
+    assert 2 * (first + 256) * 256 > 2 ** 30 and 4 * (first + 256) * 256 > 2 ** 31
+    ctx = kvm.Context([kvm.LAYER_ATTN, kvm.LAYER_ATTN], 8, 2, 256, 64, THETA, 8, 64, 64, [first, 200], 64)
+    ctx.draft_reserve(32)
+    live, n = 70, 20
+    t = tree("comb", n)
+    path = O.draft_path(t, 18)
+    cache, x = {}, {}
+    ctx.load_prefix(1, live, live, np.arange(live, dtype=np.int32))
+    ctx.draft_begin([0, 0, n], t)
+    for l in range(2):
+        cache[l] = (W.normal_bf16((161, l, 1), (2, live, 256), unit_last=True), W.normal_bf16((161, l, 2), (2, live, 256)))
+        x[l] = (W.normal_bf16((161, l, 3), (n, 8, 256)), W.normal_bf16((161, l, 4), (n, 2, 256), unit_last=True),
+                W.normal_bf16((161, l, 5), (n, 2, 256)))
+        ctx.set_kv(l, 1, _bf(cache[l][0]), _bf(cache[l][1]))
+    ctx.draft_begin([0, 0, n], t)
+    for l in range(2):
+        q, k, v = (_bf(y) for y in x[l])
+        out = torch.empty_like(q)
+        ctx.draft_attn(l, q, k, v, out)
+        c = O.AttnCache(*(O.bf16_to_f64(y) for y in cache[l]), np.arange(live))
+        assert rel_l2(_f64(out), O.draft_attention(c, *(O.bf16_to_f64(y) for y in x[l]), t, live, 64, THETA)) <= 5e-3
+    ctx.draft_commit([0, 0, len(path)], path)
+    ctx.check()
+    for l in range(2):
+        k, v = (_f64(y) for y in ctx.get_kv(l, 1))
+        assert np.array_equal(v[:, :live], O.bf16_to_f64(cache[l][1])) and np.array_equal(k[:, :live], O.bf16_to_f64(cache[l][0]))
+        assert np.array_equal(v[:, live:], O.bf16_to_f64(x[l][2])[path].transpose(1, 0, 2))
+        rot = O.rope(O.bf16_to_f64(x[l][1])[path], live + np.arange(len(path)), 64, THETA).transpose(1, 0, 2)
+        assert np.all(np.abs(k[:, live:] - rot) <= 2.0 ** -8 * np.abs(rot) + 1e-6)
+    assert np.array_equal(ctx.get_positions(1).cpu().numpy(), np.arange(live + len(path)))
+
+
+def test_as_many_characters_as_a_context_holds():
+    """256 characters of zero to four nodes, a draft that fills every cache to its last slot."""
+    import torch
+    r = np.random.default_rng(171)
+    sizes = [int(n) for n in r.integers(0, 5, 256)]
+    trees = [tree("tree", n, b) for b, n in enumerate(sizes)]
+    a = Attn(4, 1, 64, 32, [64 - n for n in sizes], seed=172, extra=0)
+    x = a.inputs(sum(sizes), seed=173)
+    a.check(trees, x, a.run(trees, x))
+    g = Gdn(1, 64, 32, 256, seed=174, conv=True)
+    y = g.inputs(sum(sizes), seed=175)
+    g.check(trees, y, g.run(trees, y))
+    V = 40
+    v = Verdict(256)
+    target, draft = _rows(r, sum(sizes), V, torch.float32, near=0.4)
+    v.check(trees, r.integers(0, V, sum(sizes)), target, draft, 0.5 * r.random(sum(sizes)), r.random(256))
+
+
+def test_two_contexts_on_two_streams():
+    """Steps of two contexts at once, on a stream each: what each computes alone, bit for bit."""
+    import torch
+    trees = [tree("tree", 30), tree("star", 9)]
+    pairs = [_stack(True, 2, [300, 120], 181 + i) for i in range(2)]
+    xs = [_step_inputs(p, 39, 183 + i) for i, p in enumerate(pairs)]
+    alone = []
+    for p, x in zip(pairs, xs):
+        p.ctx.draft_begin(cu_of(trees), packed(trees))
+        alone.append({l: o.clone() for l, o in _layers(p, x).items()})
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pairs]
+    for _ in range(5):
+        outs = []
+        for p, st in zip(pairs, streams):
+            p.ctx.draft_begin(cu_of(trees), packed(trees), stream=st)
+        for p, x, st in zip(pairs, xs, streams):
+            with torch.cuda.stream(st):
+                outs.append(_layers(p, x))
+        torch.cuda.synchronize()
+        for o, ref in zip(outs, alone):
+            for l in ref:
+                assert torch.equal(o[l].view(torch.int16), ref[l].view(torch.int16)), l
+    for p in pairs:
+        p.ctx.check()
+
+
+DEBUG = r"""
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import test_gpu_draft as T
+T.test_steps_of_a_population(True)
+T.test_deep_paths_of_wide_rows()
+print("bands intact")
+"""
+
+
+def test_drafts_write_nothing_outside_their_buffers():
+    """The canary-checking build: steps whose every check reads the bands around the context's buffers (those of the drafts
+    among them)."""
+    import os
+    import subprocess
+    import sys
+    from paper_2609_18935_gb300 import build_lib
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, KVM_LIB=build_lib.build(debug=True))
+    r = subprocess.run([sys.executable, "-c", DEBUG.format(root=root, tests=os.path.join(root, "tests"))], capture_output=True,
+                       text=True, timeout=600, env=env)
+    assert r.returncode == 0 and "bands intact" in r.stdout, r.stdout[-2000:] + r.stderr[-3000:]
 
 
 # ---------------------------------------------------------------------------- refusals
