@@ -10,8 +10,8 @@
 //                 character's next tokens:
 //                 * attention caches: the path's key and value rows move from
 //                   live + node to live + rank.  A path's indices increase, so
-//                   rank <= node, and a block that reads all rows of its slab
-//                   before it writes the first moves them in place;
+//                   rank <= node, and a block that reads the rows of its slab in
+//                   pieces, each before it is written, moves them in place;
 //                 * states: S <- G S + sum_r w_r u_r k_r^T, with G the product
 //                   of alpha along the path and w_r that of the nodes after r.
 //                   u_r, the delta rule's update at node r, depends on the
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant
 constexpr int kThreads = 128;
 constexpr int kStateRows = 32;               // rows of S a block
 constexpr int kTile = 16;                    // path nodes staged at a time
-constexpr int kMoveVec = kDraftNodes * 256 / 8 / kThreads;   // 16-byte pieces a thread moves, longest path of the widest rows
+constexpr int kMoveVec = 4;                  // 16-byte pieces a thread moves at a time
 
 // Blocks of one character (blockIdx.y), in blockIdx.x order: states [layer][head][32-row slice], cache slabs
 // [K, V][layer][KV head], convolution states [layer][1024-channel piece], position ids.
@@ -181,18 +181,22 @@ __device__ void commit_kv(const DraftCommitParams& p, int b, int item, const int
     const int slabs = p.n_attn * p.Hkv;
     const int slab = item % slabs;
     uint4* rows = reinterpret_cast<uint4*>((item < slabs ? p.K : p.V) + ((int64_t)slab * p.slab_rows + p.slot[b]) * p.D);
+    // In pieces from the first row on: a row comes from its own place or a later one,
+    // so no piece overwrites what a later piece reads.
     const int vec = p.D / 8, n = d * vec;
-    uint4 v[kMoveVec];
+    for (int x0 = 0; x0 < n; x0 += kMoveVec * kThreads) {
+        uint4 v[kMoveVec];
 #pragma unroll
-    for (int e = 0; e < kMoveVec; ++e) {
-        const int x = threadIdx.x + e * kThreads;
-        if (x < n) v[e] = rows[path[x / vec] * vec + x % vec];
-    }
-    __syncthreads();
+        for (int e = 0; e < kMoveVec; ++e) {
+            const int x = x0 + threadIdx.x + e * kThreads;
+            if (x < n) v[e] = rows[path[x / vec] * vec + x % vec];
+        }
+        __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kMoveVec; ++e) {
-        const int x = threadIdx.x + e * kThreads;
-        if (x < n) rows[x] = v[e];
+        for (int e = 0; e < kMoveVec; ++e) {
+            const int x = x0 + threadIdx.x + e * kThreads;
+            if (x < n) rows[x] = v[e];
+        }
     }
 }
 
