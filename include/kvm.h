@@ -395,9 +395,11 @@ kvm_status kvm_update_round(kvm_ctx* ctx, const kvm_round* round, void* stream);
  * read.  Beginning another draft, or any call that changes caches, states or
  * lengths, ends an open one; the draft calls then fail with KVM_E_INVAL.
  * Tensors of nodes are packed like tails, [sum n][heads][dim] with character
- * b's nodes at rows node_cu[b] .. node_cu[b+1]-1, and must be finite.  Every
- * device pointer is checked for its 16-byte alignment, and out may not overlap
- * an input.  The context's device must be current.  All calls enqueue on
+ * b's nodes at rows node_cu[b] .. node_cu[b+1]-1, and must be finite: what is
+ * not reaches no output but those of its node and the node's descendants (where
+ * keys, values and gates count as 0 or give NaN), and kvm_check reports such a
+ * key, value or gate (KVM_E_DEVICE).  Every device pointer is checked for its
+ * 16-byte alignment, and out may not overlap an input.  The context's device must be current.  All calls enqueue on
  * `stream` and may be captured into a graph; the host's lengths and cursors move
  * when kvm_draft_commit is called, not when such a graph is launched. */
 

@@ -17,10 +17,11 @@
 //    rows of S, of [K; Q]) into TMEM, 3 T columns.
 //  * S is fp32: 64 columns at a time (side by side where that costs no block an
 //    SM, so that the second half is split while the first one's products run),
-//    loaded as whole lines into registers while the inputs are staged, then split into three bf16 parts of eight bits each
-//    (by truncation: two masks and two exact differences, where rounding took
-//    conversions at an eighth of the rate and 2.9 us a block).  u enters the states
-//    of later steps, so all of S's bits take part.
+//    loaded as whole lines into registers while the inputs are staged, then split
+//    into three bf16 parts of eight bits each (by truncation: two masks and two exact
+//    differences; with rounding, whose conversions run at an eighth of that rate, this
+//    phase of a block took 3 us against 1.8).  u enters the states of later steps, so
+//    all of S's bits take part.
 //  * C_ij = -beta_i R_ij (k_i . k_j) and E_ij = R_ij (q_i . k_j), 0 off the paths,
 //    go to shared memory over the consumed parts of S, in three and two bf16 parts.
 //  * The triangular solve and the outputs: a warp owns 16 rows of S and works
@@ -30,10 +31,17 @@
 //    mma.sync with u in registers: a round through TMEM and shared memory a block
 //    would cost more than the product.  (With u in registers a row a thread and
 //    the coefficients as broadcast loads, 16 bytes a lane, shared memory returned
-//    a coefficient a clock and warp: 9 us at 64 nodes, against 0.8.)  The inverses
+//    a coefficient a clock and warp: 9 us at 64 nodes, against 3.1.)  The inverses
 //    of the diagonal blocks are formed in fp32, a column a lane.
+// What is not finite in C, E and the right-hand sides (a node's key, value or gate was
+// not) counts as 0, as a coefficient of 0 off the paths would not hide it.
 // R_ij = G_i / G_j while no G is small, else products down the path (a decay of 0
 // is one).
+//
+// 32 characters of up to 64 nodes, 16 heads of 128 x 128, convolved: 29.3 us, 47 MB
+// (1.6 TB/s).  Neither memory nor the tensor pipe bounds it (15 % and 11 % of their
+// peaks): a block is a chain of short phases between barriers, each run once, and its
+// warps wait for instructions and for one another.  One character: 6.1 us, the chain.
 #include <type_traits>
 
 #include "kvm_internal.cuh"
@@ -98,6 +106,19 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// What is not finite among x becomes 0, and bad true.
+template <int N>
+__device__ __forceinline__ void clear_not_finite(float (&x)[N], bool& bad) {
+    f2 z = 0;                                    // two zeros, and a NaN where 0 x is one
+#pragma unroll
+    for (int e = 0; e < N; e += 2) z = fma2(pack2(x[e], x[e + 1]), 0, z);
+    const float2 t = unpack2(z);
+    if (t.x + t.y == 0.f) return;
+    bad = true;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] : 0.f;
+}
+
 // 16 TMEM lanes x 16 columns, as two such D (to be waited for).
 __device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -450,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int i = lane + 32 * x;
-            if (i < n && !(g[x] >= kSmallDecay)) *small = 1;
+            if (i < n && fabsf(g[x]) < kSmallDecay) *small = 1;
             G[i] = g[x];
             rG[i] = 1.f / g[x];
             if (i >= n) be[i] = 0.f;
@@ -459,6 +480,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     ok = ok && mbar_wait(bar + 8 * (HALVES - 1), 0, abort_flag, p.err, kErrWait, p.diag, 0x62);
     ok = __syncthreads_and(ok);
     tc_fence_after();
+    bool bad = false;                                // something was not finite
     if (ok) {
         // ---- C and E: lane l of the product holds k row l, or q row l - T; the two warps of a quarter take 16 columns in turn
         const int l = (warp & 3) * 32 + lane;
@@ -493,6 +515,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                     if (real && (anc[i] >> (16 * J + c) & 1)) R *= al[16 * J + c];
                 }
             }
+            clear_not_finite(y, bad);
             if (is_c && J == I) {
                 float* row = Cd + (I * 16 + (i & 15)) * kLdf;
 #pragma unroll
@@ -565,9 +588,11 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                     const int node = 16 * I + 8 * t + col + (e & 1), r = row + 8 * (e >> 1);
                     const float v = __bfloat162float(vs[node * kLdv + r]), gn = G[node];
                     const float sk = __uint_as_float(xa[4 * t + e]), sq = __uint_as_float(oa[4 * t + e]);
-                    x[t][e] = node < n ? be[node] * (v - gn * sk) : 0.f;                 // a padding row holds anything
+                    x[t][e] = node < n && r < dv ? be[node] * (v - gn * sk) : 0.f;       // padding holds anything
                     o[t][e] = gn * sq;
                 }
+            clear_not_finite(x[0], bad);
+            clear_not_finite(x[1], bad);
             if (I + 1 < NB) {
                 tmem_ld_16x16(lanes + 16 * (I + 1), xa);
                 tmem_ld_16x16(lanes + T + 16 * (I + 1), oa);
@@ -595,6 +620,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                     if (node < n && r < dv) p.rec_u[((int64_t)(n0 + node) * H + h) * dv + r] = y[t][e];
                 }
         }
+        if (bad) atomicOr(p.err, kErrValue);
     } else if (*abort_flag) {
         // what was issued completes before TMEM and shared memory are released
         volatile int never = 0;

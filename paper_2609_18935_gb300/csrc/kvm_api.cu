@@ -1221,7 +1221,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
     if (p.turn) {
         DraftAppendParams d{total, c->Hkv, c->D, c->R, c->T_cap, p.k_new, p.v_new, p.K, p.V, c->pos, c->draft_pos, c->draft_slot,
-                            c->draft_turn};
+                            c->draft_turn, c->err};
         launch_draft_append(d, s);
     } else {
         launch_rope_append(p, total, s);
@@ -2396,8 +2396,9 @@ extern "C" kvm_status kvm_check(kvm_ctx* c, void* stream) {
         CUDA_TRY(cudaMemset(c->err, 0, 4));
         CUDA_TRY(cudaMemset(c->diag, 0, 16 * sizeof(int32_t)));
         CUDA_TRY(cudaMemset(c->tickets, 0, sizeof(int32_t) * (size_t)c->B * (2 * c->n_attn * c->Hkv + 1)));
-        return fail(KVM_E_DEVICE, "device error word 0x%x (%s%s); first expired wait: block %d, tag 0x%x, parity %d",
-                    e, (e & kErrBounds) ? "bounds " : "", (e & kErrWait) ? "wait-timeout" : "", d[0] - 1, d[1], d[2]);
+        return fail(KVM_E_DEVICE, "device error word 0x%x (%s%s%s); first expired wait: block %d, tag 0x%x, parity %d",
+                    e, (e & kErrBounds) ? "bounds " : "", (e & kErrWait) ? "wait-timeout " : "",
+                    (e & kErrValue) ? "value-not-finite" : "", d[0] - 1, d[1], d[2]);
     }
     return KVM_OK;
 }

@@ -41,6 +41,7 @@ constexpr int kMaxRotaryHalf = 128; // rotary_dim / 2
 // Device error word bits (read by kvm_check).
 constexpr int kErrBounds = 1;       // an index fell outside the buffers a kernel was given
 constexpr int kErrWait = 2;         // a bounded wait expired
+constexpr int kErrValue = 4;        // a draft's key, value or gate is not finite
 
 // ----------------------------------------------------------------------------
 // kv_compact
@@ -361,6 +362,7 @@ struct DraftAppendParams {
     const int32_t* pos;                       // as the tree kernel left them
     const int32_t* slot;
     const float2* turn;
+    int32_t* err;
 };
 void launch_draft_append(const DraftAppendParams& p, cudaStream_t s);
 

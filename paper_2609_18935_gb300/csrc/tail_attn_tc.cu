@@ -133,7 +133,7 @@ __device__ __forceinline__ Tile decode_tile(const AttnParams& p, int t) {
 
 // Rows of a draft's Q tile into TMEM, 16 lanes x 8 columns (a k step of the MMA) at
 // a time, eight rows of 32 bytes a load: with a row a thread every load touched 32
-// lines and the block's 64 KB took 2.3 us against 1.1.  The two warps of a quarter
+// lines and the block's 64 KB took 2.3 us against 1.6.  The two warps of a quarter
 // take the steps in turn.  With p.turn the caller's q is rotated here (R is a
 // multiple of 32: a pair's elements are in the same place of steps R / 32 apart),
 // and nothing of the previous grid, which only appends the nodes' keys and values,

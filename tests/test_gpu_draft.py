@@ -377,6 +377,78 @@ def test_delta_rule_outside_the_path_changes_nothing():
             assert torch.equal(out[i], base[i]) == (j not in O.draft_path(t, i)), (i, j)
 
 
+def _reported(ctx):
+    from paper_2609_18935_gb300 import kvm
+    with pytest.raises(kvm.KvmError) as ei:
+        ctx.check()
+    assert ei.value.code == kvm.KVM_E_DEVICE and "value-not-finite" in str(ei.value)
+    ctx.check()
+
+
+NOT_FINITE = (0x7FC0, 0x7F80, 0xFF80, 0xFFFF)                                   # NaN, inf, -inf, -NaN in bf16
+
+
+@pytest.mark.parametrize("d,rot", [(64, 64), (128, 0), (256, 64)])
+def test_keys_and_values_that_are_not_finite_stay_with_their_node(d, rot):
+    """Other nodes' outputs bit for bit, and those of a later, shorter draft whose last tile holds the rows."""
+    import torch
+    n, live = 21, 70
+    a = Attn(8, 2, d, rot, [live], seed=75)
+    t = tree("tree", n, 5)
+    x = a.inputs(n, seed=76)
+    base = a.run([t], x).clone()
+    y = [z[:3] for z in x]
+    short = a.run([t[:3]], y).clone()
+    for which in (1, 2):
+        for j, bits in zip((0, 4, 13, 20), NOT_FINITE):
+            bad = [z.copy() for z in x]
+            bad[which][j, 1, 5] = bits
+            bad[which][j, 0, -1] = bits
+            q, k, v = (_bf(z) for z in bad)
+            out = torch.zeros_like(q)
+            a.ctx.draft_begin(cu_of([t]), packed([t]))
+            a.ctx.draft_attn(0, q, k, v, out)
+            _reported(a.ctx)
+            for i in range(n):
+                assert j in O.draft_path(t, i) or torch.equal(out[i], base[i]), (which, i, j)
+            assert torch.equal(a.run([t[:3]], y), short)
+
+
+@pytest.mark.parametrize("conv", [False, True])
+def test_a_delta_rule_node_that_is_not_finite_stays_alone(conv):
+    """Other nodes' outputs bit for bit, and the state after a commit of a path without it."""
+    import torch
+    n = 37
+    t = tree("tree", n, 8)
+    g = Gdn(2, 128, 64, 1, seed=77, conv=conv)
+    x = g.inputs(n, seed=78)
+    base = g.run([t], x).clone()
+    path = O.draft_path(t, 36)
+    out_of_path = [i for i in range(n) if i not in path and not set(O.draft_path(t, i)[1:]) & set(path[1:])]
+    for name in ("k", "v", "alpha", "beta"):
+        for j, bits in zip((5, out_of_path[0], out_of_path[-1]), NOT_FINITE):
+            bad = {m: z.copy() for m, z in x.items()}
+            if name in ("k", "v"):
+                bad[name][j, 0, 3] = bits
+            else:
+                bad[name][j, 0] = np.array([bits << 16], np.uint32).view(np.float32)[0]
+            dev = {m: _bf(z) if z.dtype == np.uint16 else torch.from_numpy(z).cuda() for m, z in bad.items()}
+            out = torch.zeros_like(dev["v"])
+            g.ctx.draft_begin(cu_of([t]), packed([t]))
+            g.ctx.draft_gdn(0, dev["q"], dev["k"], dev["v"], dev["alpha"], dev["beta"], out)
+            _reported(g.ctx)
+            for i in range(n):
+                assert j in O.draft_path(t, i) or torch.equal(out[i], base[i]), (name, i, j)
+    # the last draft's bad node is off this path
+    assert j not in path
+    g.ctx.draft_commit([0, len(path)], path)
+    got = g.ctx.get_state(0).cpu().numpy()[0]
+    other = Gdn(2, 128, 64, 1, seed=77, conv=conv)
+    other.run([t], x)
+    other.ctx.draft_commit([0, len(path)], path)
+    assert np.array_equal(got, other.ctx.get_state(0).cpu().numpy()[0])
+
+
 # ---------------------------------------------------------------------------- verdicts
 class Verdict:
     def __init__(self, chars):
