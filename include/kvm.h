@@ -399,15 +399,16 @@ kvm_status kvm_update_round(kvm_ctx* ctx, const kvm_round* round, void* stream);
  * not reaches no output but those of its node and the node's descendants (where
  * keys, values and gates count as 0 or give NaN), and kvm_check reports such a
  * key, value or gate (KVM_E_DEVICE).  Every device pointer is checked for its
- * 16-byte alignment, and out may not overlap an input.  The context's device must be current.  All calls enqueue on
+ * 16-byte alignment, and outputs may not overlap inputs.  The context's device must be current.  All calls enqueue on
  * `stream` and may be captured into a graph; the host's lengths and cursors move
  * when kvm_draft_commit is called, not when such a graph is launched. */
 
 /* Room for trees of max_nodes nodes (all characters together) in this context:
  * per delta-rule layer, node and head d_v fp32 and d_k bf16 values (with the
  * convolution the node's raw inputs too).  Allocates, and synchronizes the
- * device if it has to grow; the calls below allocate nothing.  Ends an open
- * draft if it grows.  Errors: KVM_E_INVAL (max_nodes outside [1,
+ * device if it has to grow; the calls below allocate nothing.  Where it grows
+ * it ends an open draft, and graphs with draft calls that were captured before
+ * must not be launched any more.  Errors: KVM_E_INVAL (max_nodes outside [1,
  * max_tail_tokens]), KVM_E_UNSUPPORTED (more than 1024 delta-rule layers),
  * KVM_E_CUDA. */
 kvm_status kvm_draft_reserve(kvm_ctx* ctx, int32_t max_nodes);

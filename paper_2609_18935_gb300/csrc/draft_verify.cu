@@ -153,12 +153,13 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         ptx::mbar_init(bar, 1);
         ptx::mbar_init(bar + 8, 1);
         ptx::fence_mbar_init();
+        if (rank == 0) p.next[b] = -1;               // unless a token is found
     }
     __syncwarp();
     if (blocks > 1) cluster_arrive();                // the neighbours' barriers stand before the first sum arrives: waited for below
     if (n <= 0) {                                    // uniform over the cluster
         if (blocks > 1) cluster_wait();
-        if (rank == 0 && tid == 0) { p.count[b] = 0; p.next[b] = -1; }
+        if (rank == 0 && tid == 0) p.count[b] = 0;
         return;
     }
     if (tid < kDraftNodes) kids[tid] = 0;
@@ -319,7 +320,6 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         if (lane == 0) p.next[b] = best;
     }
     if (rank == 0) {
-        if ((block < 0 || lost) && tid == 0) p.next[b] = -1;       // the row holds no positive number
         __syncthreads();
         if (tid < n) p.path[n0 + tid] = tid < count ? path[tid] : -1;
         if (tid == 0) p.count[b] = count;

@@ -1977,6 +1977,16 @@ kvm_status draft_verify(kvm_ctx* c, int vocab, int prob_type, const int32_t* tok
         return fail(KVM_E_INVAL, "NULL tensor");
     if (!aligned16({tokens, target, draft, u, u_next, path, count, next}))
         return fail(KVM_E_INVAL, "a tensor is not 16-byte aligned");
+    {
+        struct Range { const void* p; size_t n; };
+        const size_t nodes = (size_t)total * 4, chars = (size_t)c->B * 4;
+        const size_t rows = (size_t)total * vocab * (prob_type == KVM_PROB_F32 ? 4 : 2);
+        const Range r[] = {{path, nodes}, {count, chars}, {next, chars}, {tokens, nodes}, {target, rows}, {draft, rows},
+                           {u, nodes}, {u_next, chars}};
+        for (int i = 0; i < 3; ++i)
+            for (int j = i + 1; j < 8; ++j)
+                if (overlap(r[i].p, r[i].n, r[j].p, r[j].n)) return fail(KVM_E_INVAL, "an output overlaps another tensor");
+    }
     thread_local static DraftVerifyParams p;
     p.n_chars = c->B;
     p.vocab = vocab;
@@ -2050,7 +2060,7 @@ kvm_status guarded(F&& f) noexcept {
     try {
         return f();
     } catch (const std::exception&) {
-        g_err.clear();
+        g_err = "host memory";                       // short enough to be held in place
         return KVM_E_CAPACITY;
     }
 }

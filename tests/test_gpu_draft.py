@@ -556,6 +556,38 @@ def test_a_token_outside_the_vocabulary_is_refused_and_reported():
     v.ctx.check()
 
 
+def test_a_verdict_refuses_outputs_over_its_inputs_and_each_other():
+    import torch
+    from paper_2609_18935_gb300 import kvm
+    v = Verdict(2)
+    r = np.random.default_rng(85)
+    target, draft = (t.cuda() for t in _rows(r, 5, 40, torch.float32))
+    ints = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    tokens, path, u, u_next = ints(5), ints(5), torch.zeros(5, device="cuda"), torch.zeros(2, device="cuda")
+    count, nxt = ints(2), ints(2)
+    v.ctx.draft_begin([0, 3, 5], [-1, 0, 0, -1, 0])
+    as_int = lambda t, n: t.view(torch.int32).flatten()[:n]
+    for bad in (dict(path=tokens), dict(path=as_int(target, 5)), dict(path=as_int(draft[4], 5)), dict(path=as_int(u, 5)),
+                dict(nxt=as_int(u_next, 2)), dict(count=nxt), dict(count=as_int(path, 2)), dict(nxt=as_int(tokens, 2))):
+        a = dict(dict(path=path, count=count, nxt=nxt), **bad)
+        with pytest.raises(kvm.KvmError) as ei:
+            v.ctx.draft_verify(tokens, target, draft, u, u_next, a["path"], a["count"], a["nxt"])
+        assert ei.value.code == kvm.KVM_E_INVAL, bad
+    v.ctx.draft_verify(tokens, target, draft, u, u_next, path, count, nxt)
+    v.ctx.check()
+
+
+def test_a_verdict_always_writes_its_token():
+    """Where nothing can be drawn the token is -1: an empty row, and a uniform below its range."""
+    import torch
+    r = np.random.default_rng(86)
+    for V in (40, 5000):
+        target, draft = _rows(r, 2, V, torch.float32)
+        target[0] = 0.0
+        _, count, nxt = Verdict(2).run([[-1], [-1]], [0, 0], target, draft, [0, 0], [0.5, -0.25])
+        assert list(count) == [1, 1] and list(nxt) == [-1, -1], V
+
+
 def test_verdicts_keep_the_targets_distribution():
     """256 characters, 64 calls: tokens that follow a decided one, with three guesses from the draft, against p.  A frequency of
     16384 draws is within 5 sigma = 5 sqrt(p (1 - p) / 16384) of p but for one in 10^6."""
