@@ -213,6 +213,7 @@ __device__ __forceinline__ void stage_q_tree(const AttnParams& p, const Tile& T,
         }
     }
 }
+
 // DEAL: p.waves > 0 (a kernel of its own: the segment lookup with waves cost
 // 1 % of the time where there are none).  TREE: the tail is a draft (p.anc): a
 // row sees the live entries and, of the tail, the nodes of its ancestor word.

@@ -579,48 +579,68 @@ class Context:
         _check(_lib.kvm_draft_begin(self._h, cu, par, _stream(stream)))
         self._draft_nodes = n
 
-    def _draft_ptr(self, name, t, dtype, rest) -> int:
-        """Address of one of an open draft's tensors, [nodes][rest..]: shapes are checked because the library reads them
-        unseen (with no draft begun it refuses the call itself)."""
+    def _draft_check(self, *tensors):
+        """Raises unless every (name, tensor, dtype, shape after the nodes) fits the open draft: shapes are checked because
+        the library reads tensors unseen (with no draft begun it refuses the call itself).  The draft calls ask this only
+        where their own test of all tensors at once, half its time, fails."""
         n = self._draft_nodes
-        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (n is None or t.shape == (n, *rest)):
-            return t.data_ptr()
-        _dptr(t, dtype)
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, need {(n, *rest)}")
+        for name, t, dtype, rest in tensors:
+            _dptr(t, dtype)
+            if n is not None and t.shape != (n, *rest):
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, need {(n, *rest)}")
 
     def draft_attn(self, layer, q, k_new, v_new, out, stream=None):
         """kvm_draft_attn: one attention layer over the open draft; q, out CUDA bf16 [nodes][Hq][D], k_new, v_new
         [nodes][Hkv][D]."""
-        bf, ptr = _torch().bfloat16, self._draft_ptr
-        heads, kv = (self.Hq, self.D), (self.Hkv, self.D)
-        _check(_lib.kvm_draft_attn(self._h, layer, ptr("q", q, bf, heads), ptr("k_new", k_new, bf, kv),
-                                   ptr("v_new", v_new, bf, kv), ptr("out", out, bf, heads), _stream(stream)))
+        n, bf = self._draft_nodes, _torch().bfloat16
+        if not (q.dtype is bf and k_new.dtype is bf and v_new.dtype is bf and out.dtype is bf
+                and q.is_cuda and k_new.is_cuda and v_new.is_cuda and out.is_cuda
+                and q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous() and out.is_contiguous()
+                and q.shape == out.shape == (n, self.Hq, self.D) and k_new.shape == v_new.shape == (n, self.Hkv, self.D)):
+            heads, kv = (self.Hq, self.D), (self.Hkv, self.D)
+            self._draft_check(("q", q, bf, heads), ("k_new", k_new, bf, kv), ("v_new", v_new, bf, kv), ("out", out, bf, heads))
+        _check(_lib.kvm_draft_attn(self._h, layer, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(),
+                                   _stream(stream)))
 
     def draft_gdn(self, layer, q, k, v, alpha, beta, out, stream=None):
         """kvm_draft_gdn: one delta-rule layer over the open draft; q, k CUDA bf16 [nodes][H][dk], v, out [nodes][H][dv],
         alpha, beta fp32 [nodes][H]."""
-        torch, ptr = _torch(), self._draft_ptr
+        torch, n = _torch(), self._draft_nodes
         bf, f = torch.bfloat16, torch.float32
-        key, val, gate = (self.H, self.dk), (self.H, self.dv), (self.H,)
-        _check(_lib.kvm_draft_gdn(self._h, layer, ptr("q", q, bf, key), ptr("k", k, bf, key), ptr("v", v, bf, val),
-                                  ptr("alpha", alpha, f, gate), ptr("beta", beta, f, gate), ptr("out", out, bf, val),
-                                  _stream(stream)))
+        if not (q.dtype is bf and k.dtype is bf and v.dtype is bf and alpha.dtype is f and beta.dtype is f and out.dtype is bf
+                and q.is_cuda and k.is_cuda and v.is_cuda and alpha.is_cuda and beta.is_cuda and out.is_cuda
+                and q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and alpha.is_contiguous()
+                and beta.is_contiguous() and out.is_contiguous()
+                and q.shape == k.shape == (n, self.H, self.dk) and v.shape == out.shape == (n, self.H, self.dv)
+                and alpha.shape == beta.shape == (n, self.H)):
+            key, val, gate = (self.H, self.dk), (self.H, self.dv), (self.H,)
+            self._draft_check(("q", q, bf, key), ("k", k, bf, key), ("v", v, bf, val), ("alpha", alpha, f, gate),
+                              ("beta", beta, f, gate), ("out", out, bf, val))
+        _check(_lib.kvm_draft_gdn(self._h, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
+                                  out.data_ptr(), _stream(stream)))
 
     def draft_verify(self, tokens, target, draft, u, u_next, path, count, next_token, stream=None):
         """kvm_draft_verify: target, draft CUDA fp32 or bf16 [nodes][vocab]; tokens int32 [nodes], u fp32 [nodes], u_next
         fp32 [n_chars]; path int32 [nodes], count and next_token int32 [n_chars] are written."""
-        torch, ptr = _torch(), self._draft_ptr
+        torch, n = _torch(), self._draft_nodes
         i, f, t = torch.int32, torch.float32, target.dtype
         if target.dim() != 2 or (t is not f and t is not torch.bfloat16):
             raise ValueError("target must be [nodes][vocab] in float32 or bfloat16")
-        row, one = (target.shape[1],), (self.n_chars,)
-        for name, x in (("u_next", u_next), ("count", count), ("next_token", next_token)):
-            if x.shape != one:
-                raise ValueError(f"{name} has shape {tuple(x.shape)}, need {one}")
-        _check(_lib.kvm_draft_verify(self._h, row[0], PROB_F32 if t is f else PROB_BF16, ptr("tokens", tokens, i, ()),
-                                     ptr("target", target, t, row), ptr("draft", draft, t, row), ptr("u", u, f, ()),
-                                     _dptr(u_next, f), ptr("path", path, i, ()), _dptr(count, i), _dptr(next_token, i),
-                                     _stream(stream)))
+        vocab, one = target.shape[1], (self.n_chars,)
+        if not (draft.dtype is t and tokens.dtype is i and u.dtype is f and path.dtype is i
+                and target.is_cuda and draft.is_cuda and tokens.is_cuda and u.is_cuda and path.is_cuda
+                and target.is_contiguous() and draft.is_contiguous() and tokens.is_contiguous() and u.is_contiguous()
+                and path.is_contiguous() and target.shape == draft.shape == (n, vocab)
+                and tokens.shape == u.shape == path.shape == (n,)):
+            self._draft_check(("tokens", tokens, i, ()), ("target", target, t, (vocab,)), ("draft", draft, t, (vocab,)),
+                              ("u", u, f, ()), ("path", path, i, ()))
+        if not (u_next.shape == count.shape == next_token.shape == one):
+            for name, x in (("u_next", u_next), ("count", count), ("next_token", next_token)):
+                if x.shape != one:
+                    raise ValueError(f"{name} has shape {tuple(x.shape)}, need {one}")
+        _check(_lib.kvm_draft_verify(self._h, vocab, PROB_F32 if t is f else PROB_BF16, tokens.data_ptr(), target.data_ptr(),
+                                     draft.data_ptr(), u.data_ptr(), _dptr(u_next, f), path.data_ptr(), _dptr(count, i),
+                                     _dptr(next_token, i), _stream(stream)))
 
     def draft_commit(self, path_cu, path, stream=None):
         """kvm_draft_commit: keep one path of each tree (host int32 offsets [n_chars + 1] and packed node indices)."""
