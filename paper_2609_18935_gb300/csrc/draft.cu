@@ -5,7 +5,8 @@
 //                 cursor + depth, and the cosines and sines of its rotary angles.
 //                 Once a step, for every layer.
 //  draft_append : an attention layer's keys (rotated) and values of the nodes to
-//                 the slots behind the live entries.
+//                 the slots behind the live entries, where the attention does
+//                 not do it itself.
 //  draft_commit : one launch for every layer.  The nodes of a path are the
 //                 character's next tokens:
 //                 * attention caches: the path's key and value rows move from
@@ -24,6 +25,7 @@
 //                 128); a block holds 32 rows of it in registers.  Six
 //                 delta-rule layers of 16 characters (16 heads): 201 MB in 34 us,
 //                 5.9 TB/s.
+#include "draft_rows.cuh"
 #include "kvm_internal.cuh"
 
 namespace kvm {
@@ -61,24 +63,9 @@ __global__ void __launch_bounds__(256) draft_tree_kernel(const __grid_constant__
     }
 }
 
-// bf16 elements that are not finite become 0; true if there was one.
-__device__ __forceinline__ bool clear_not_finite(uint4& v) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const bool lo = (w[e] & 0x7f80u) == 0x7f80u, hi = (w[e] & 0x7f800000u) == 0x7f800000u;
-        w[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-        bad = bad || lo || hi;
-    }
-    return bad;
-}
-
 // A block a node, a thread eight elements of a key or value row, those of a rotary
 // pair (i, i + R / 2) together: the attention that follows rotates q itself and
-// waits for this kernel only where it reads the nodes' rows.  What is not finite goes
-// in as 0: a tile's weight of 0 for a value out of sight would turn it into a NaN of
-// every row, in later calls too while the slot lies in their last tile.
+// waits for this kernel only where it reads the nodes' rows.
 __global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant__ DraftAppendParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
@@ -92,24 +79,16 @@ __global__ void __launch_bounds__(128) draft_append_kernel(const __grid_constant
         const int d = 8 * (is_v || turned ? g : g + rot);            // past the pairs' second halves
         const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + ((int64_t)n * p.Hkv + h) * D + d;
         __nv_bfloat16* dst = (is_v ? p.V : p.K) + ((int64_t)h * p.slab_rows + slot) * D + d;
-        uint4 a = *reinterpret_cast<const uint4*>(src);
-        bool bad = clear_not_finite(a);
+        bool bad;
         if (turned) {
-            uint4 y = *reinterpret_cast<const uint4*>(src + half);
-            bad = clear_not_finite(y) || bad;
-            const float4* t = reinterpret_cast<const float4*>(p.turn + (int64_t)n * half + d);
-            __nv_bfloat162* u = reinterpret_cast<__nv_bfloat162*>(&a);
-            __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&y);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 cs = t[q];              // (cos, sin) of two dims
-                const float2 f = __bfloat1622float2(u[q]), s = __bfloat1622float2(w[q]);
-                u[q] = __floats2bfloat162_rn(f.x * cs.x - s.x * cs.y, f.y * cs.z - s.y * cs.w);
-                w[q] = __floats2bfloat162_rn(s.x * cs.x + f.x * cs.y, s.y * cs.z + f.y * cs.w);
-            }
-            *reinterpret_cast<uint4*>(dst + half) = y;
+            TurnedNode x;
+            x.load(src, half, p.turn + (int64_t)n * half + d);
+            bad = x.store(dst, half);
+        } else {
+            uint4 v = *reinterpret_cast<const uint4*>(src);
+            bad = clear_not_finite(v);
+            *reinterpret_cast<uint4*>(dst) = v;
         }
-        *reinterpret_cast<uint4*>(dst) = a;
         if (bad) atomicOr(p.err, kErrValue);
     }
     if (threadIdx.x == 0) p.cache_pos[slot] = p.pos[n];

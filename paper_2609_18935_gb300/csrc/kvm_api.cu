@@ -1195,6 +1195,9 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     // a draft's q is rotated in the attention where a rotary pair's elements lie whole
     // 32-byte steps apart; else as a tail's, before it
     p.turn = anc && c->R % 32 == 0 ? c->draft_turn : nullptr;
+    // and where each query tile holds all its character's nodes, so that each of their
+    // rows lies in one block's range, that block puts them into the caches
+    p.append = p.turn && *std::max_element(pl.n_qtiles.begin(), pl.n_qtiles.end()) == 1;
     p.part_o = c->part_o;
     p.part_ml = c->part_ml;
     p.err = c->err;
@@ -1218,17 +1221,19 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_tile.begin(), pl.cta_tile.end(), p.cta_tile);
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
-    int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
-    if (p.turn) {
-        DraftAppendParams d{total, c->Hkv, c->D, c->R, c->T_cap, p.k_new, p.v_new, p.K, p.V, c->pos, c->draft_pos, c->draft_slot,
-                            c->draft_turn, c->err};
-        launch_draft_append(d, s);
-    } else {
-        launch_rope_append(p, total, s);
+    if (!p.append) {
+        const int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
+        if (p.turn) {
+            DraftAppendParams d{total, c->Hkv, c->D, c->R, c->T_cap, p.k_new, p.v_new, p.K, p.V, c->pos, c->draft_pos, c->draft_slot,
+                                c->draft_turn, c->err};
+            launch_draft_append(d, s);
+        } else {
+            launch_rope_append(p, total, s);
+        }
+        prof_end(c, ps, s);
+        LAUNCH_CHECK(c);
     }
-    prof_end(c, ps, s);
-    LAUNCH_CHECK(c);
-    ps = prof_begin(c, KVM_K_ATTENTION, s);
+    int ps = prof_begin(c, KVM_K_ATTENTION, s);
     launch_tail_attention(p, s);
     prof_end(c, ps, s);
     LAUNCH_CHECK(c);

@@ -163,6 +163,7 @@ struct AttnParams {
     int32_t* diag;                // first expired wait: block + 1, tag, parity
     const uint64_t* anc;          // device [sum M]: a draft's ancestor bits (DraftTreeParams), or null: a causal tail
     const float2* turn;           // of a draft: (cos, sin) [sum M][R / 2], with which the attention rotates q itself; or null
+    int32_t append;               // of a draft: the attention puts the nodes' keys and values into the caches itself
     double inv_freq[kMaxRotaryHalf];
     int32_t cta_tile[kMaxAttnCtas + 1];
     int32_t cta_k[kMaxAttnCtas + 1];

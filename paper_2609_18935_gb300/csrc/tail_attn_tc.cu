@@ -61,6 +61,7 @@
 // issuing, the softmax warps run their loops to the end without waiting (so
 // that their pair barriers stay matched), and every copy and MMA already
 // issued completes before TMEM and shared memory are released.
+#include "draft_rows.cuh"
 #include "kvm_internal.cuh"
 #include "sm100_ptx.cuh"
 
@@ -75,11 +76,13 @@ constexpr int kSoftmaxThreads = 256;          // warps 2-9
 constexpr int kThreads = 64 + kSoftmaxThreads + 64;   // + warp 10 (PV issuer), warp 11 (V producer)
 constexpr int kPvWarp = 10;
 constexpr int kVWarp = 11;
+constexpr int kTail = 0, kDraft = 1, kAppends = 2;     // what a kernel's rows are (TREE below)
+constexpr int kAppendThreads = 64;            // warps 1 and 10
 
 constexpr int STAGES = 3;                     // K and V ring depth (a fourth of either: the same time or more)
 
 enum Bar { K_FULL = 0, K_EMPTY = 3, V_FULL = 6, V_EMPTY = 9, S_FULL = 12, S_EMPTY = 14, P_FULL = 16,
-           PV_DONE = 18, Q_FULL = 20, O_FINAL = 21, O_EMPTY = 22, DRAIN_S = 23, DRAIN_PV = 24, N_BARS = 25 };
+           PV_DONE = 18, Q_FULL = 20, O_FINAL = 21, O_EMPTY = 22, DRAIN_S = 23, DRAIN_PV = 24, NODES = 25, N_BARS = 26 };
 
 template <int D>
 struct Cfg {
@@ -136,12 +139,12 @@ __device__ __forceinline__ Tile decode_tile(const AttnParams& p, int t) {
 // lines and the block's 64 KB took 2.3 us against 1.6.  The two warps of a quarter
 // take the steps in turn.  With p.turn the caller's q is rotated here (R is a
 // multiple of 32: a pair's elements are in the same place of steps R / 32 apart),
-// and nothing of the previous grid, which only appends the nodes' keys and values,
-// is read: the kernel before that one has completed before this one could start.
-template <int D>
+// and nothing of the previous grid is read where that only appends the nodes' keys and
+// values (not kAppends): the kernel before it has completed before this one could start.
+template <int D, int TREE>
 __device__ __forceinline__ void stage_q_tree(const AttnParams& p, const Tile& T, int quarter, int grp, int lane, uint32_t tq) {
     constexpr int HALVES = 2;                              // of a warp's 32 rows
-    if (!p.turn) grid_dependency_wait();                   // q_rot comes from the previous grid
+    if (!p.turn || TREE == kAppends) grid_dependency_wait();   // q_rot, or q, comes from the previous grid
     const AttnChar& ch = p.ch[T.b];
     const int j = lane & 3, half = p.R / 2;
     const __nv_bfloat16* q = p.turn ? p.q : p.q_rot;
@@ -214,10 +217,64 @@ __device__ __forceinline__ void stage_q_tree(const AttnParams& p, const Tile& T,
     }
 }
 
+// A draft's keys and values into the caches: of each of this block's segments the
+// nodes with keys in its range, in the segment's KV head.  Each such row lies in one
+// block's range.  By the issuer warps, which have nothing to do before Q is staged
+// (by the softmax warps after their staging the block with the nodes came 1 us later).
+// Seven flat pieces in flight a thread: one character's 16 nodes of 256 16.7 us, 17.5
+// with ten, 17.1 with fourteen.  Against a launch before this one: five nodes of 64 9.6
+// -> 8.6 us, 4 nodes behind 8192 keys 13.2 -> 12.2, 16 there as before, 32 characters
+// of them 56.4 -> 54.2, and the host's 2.7 us of the launch.
+template <int D, typename TileOf, typename KeyBegin, typename KeyEnd>
+__device__ __forceinline__ void append_nodes(const AttnParams& p, int n_seg, int t, TileOf tile_of, KeyBegin key_begin, KeyEnd key_end) {
+    constexpr int AHEAD = 7;
+    const int half = p.R / 2, rot = half / 8, flat = D / 8 - 2 * rot + D / 8;      // eights of a node's K (turned in pairs) and V
+    bool bad = false;
+    grid_dependency_wait();
+    for (int seg = 0; seg < n_seg; ++seg) {
+        const Tile T = decode_tile(p, tile_of(seg));
+        const AttnChar& ch = p.ch[T.b];
+        const int i0 = max(key_begin(seg) * BN - ch.L_prev, 0), n = min(key_end(seg, T.nk) * BN - ch.L_prev, ch.M) - i0;
+        if (n <= 0) continue;
+        const int64_t src = ((int64_t)(ch.tail_off + i0) * p.Hkv + T.kvh) * D;
+        const int64_t dst = ((int64_t)T.kvh * p.slab_rows + ch.cap_off + ch.L_prev + i0) * D;
+        const int step = p.Hkv * D;
+        for (int et = t, ef = t; et < n * rot || ef < n * flat; et += kAppendThreads, ef += AHEAD * kAppendThreads) {
+            TurnedNode x;
+            const int it = et < n * rot ? et / rot : 0, dt = et < n * rot ? 8 * (et % rot) : 0;
+            if (et < n * rot) x.load(p.k_new + src + (int64_t)it * step + dt, half, p.turn + (int64_t)(ch.tail_off + i0 + it) * half + dt);
+            uint4 v[AHEAD];
+            int to[AHEAD];                           // element of the head's rows; V's past all of K's
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int e = ef + a * kAppendThreads, i = e / flat, c = e % flat + 2 * rot;   // past the turned ones
+                const bool is_v = c >= D / 8;
+                const int d = 8 * (is_v ? c - D / 8 : c);
+                to[a] = (is_v ? kDraftNodes * D : 0) + i * D + d;
+                if (e < n * flat) v[a] = *reinterpret_cast<const uint4*>((is_v ? p.v_new : p.k_new) + src + (int64_t)i * step + d);
+            }
+            if (et < n * rot) bad = x.store(p.K + dst + it * D + dt, half) || bad;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a)
+                if (ef + a * kAppendThreads < n * flat) {
+                    bad = clear_not_finite(v[a]) || bad;
+                    const bool is_v = to[a] >= kDraftNodes * D;
+                    *reinterpret_cast<uint4*>((is_v ? p.V : p.K) + dst + to[a] - (is_v ? kDraftNodes * D : 0)) = v[a];
+                }
+        }
+        if (T.kvh == 0 && t < n) p.pos[ch.cap_off + ch.L_prev + i0 + t] = p.tail_pos[ch.tail_off + i0 + t];
+    }
+    if (bad) atomicOr(p.err, kErrValue);
+    fence_proxy_async_global();
+}
+
 // DEAL: p.waves > 0 (a kernel of its own: the segment lookup with waves cost
 // 1 % of the time where there are none).  TREE: the tail is a draft (p.anc): a
-// row sees the live entries and, of the tail, the nodes of its ancestor word.
-template <int D, bool DEAL, bool TREE>
+// row sees the live entries and, of the tail, the nodes of its ancestor word; where
+// every query tile holds all its character's nodes (kAppends) the block with a node's
+// keys in its range puts them into the caches itself, a launch less.  A kernel of its
+// own too: with a branch the drafts without it took 1 us more of 38.
+template <int D, bool DEAL, int TREE>
 __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __grid_constant__ AttnParams p) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -274,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
         mbar_init(bar(Q_FULL), kSoftmaxThreads);
         mbar_init(bar(O_FINAL), 1);
         mbar_init(bar(O_EMPTY), kSoftmaxThreads);
+        mbar_init(bar(NODES), kAppendThreads);
         mbar_init(bar(DRAIN_S), 1);
         mbar_init(bar(DRAIN_PV), 1);
         fence_mbar_init();
@@ -291,12 +349,21 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
     // earlier (by kv_compact, complete before rope_append began).  So the
     // producers stream survivor tiles at once and wait for the previous grid
     // only before a tile that reaches the tail; the softmax warps wait before
-    // staging Q.  The issuers touch no global memory.
+    // staging Q.  The issuers touch no global memory.  A draft that appends here
+    // (kAppends) has no such kernel before it: its live rows were in place before
+    // draft_tree, after every call that changes caches.
     grid_dependents_launch();
 
     // copies issued by a producer lane (for the drain after an abort)
     int last_load[STAGES] = {-1, -1, -1};
 
+    if constexpr (TREE == kAppends) {
+        if (warp == 1 || warp == kPvWarp) {
+            append_nodes<D>(p, n_seg, lane + (warp == 1 ? 0 : 32), tile_of, key_begin, key_end);
+            mbar_arrive(bar(NODES));
+            __syncwarp();
+        }
+    }
     if (warp == 0 || warp == kVWarp) {
         // ------------------------------------------------------------ producers: warp 0 K, warp 11 V
         if (lane == 0) {
@@ -314,12 +381,13 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 const int key_row0 = (p.attn_layer * p.Hkv + T.kvh) * (int)p.slab_rows + ch.cap_off;
                 for (int kt = k; kt < k1; ++kt, ++j) {
                     if (!waited && (kt + 1) * BN > ch.L_prev) {    // the tile reaches the tail
-                        grid_dependency_wait();
+                        if (TREE == kAppends) ok = mbar_wait(bar(NODES), 0, abort_flag, p.err, kErrWait, p.diag, 0x15);
+                        else grid_dependency_wait();
                         waited = true;
                     }
                     const int st = j % STAGES;
                     // a draft's blocks have few units: their first Q and K tiles come before the rings fill up
-                    if (TREE && j == (is_k ? 1 : 0)) ok = mbar_wait(bar(Q_FULL), 0, abort_flag, p.err, kErrWait, p.diag, 0x14);
+                    if (TREE && ok && j == (is_k ? 1 : 0)) ok = mbar_wait(bar(Q_FULL), 0, abort_flag, p.err, kErrWait, p.diag, 0x14);
                     if (ok && j >= STAGES)
                         ok = mbar_wait(bar(empty + st), (j / STAGES - 1) & 1, abort_flag, p.err, kErrWait, p.diag,
                                        (is_k ? 0x12 : 0x13) + 256 * j);
@@ -439,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
         // bf16 = D / 4 columns); rows past the character's tail are zero
         auto stage_q = [&](int t) {
             if constexpr (TREE) {
-                stage_q_tree<D>(p, decode_tile(p, t), quarter, grp, lane, tmem + lane_off + C::TMEM_Q);
+                stage_q_tree<D, TREE>(p, decode_tile(p, t), quarter, grp, lane, tmem + lane_off + C::TMEM_Q);
                 tmem_st_wait();
                 tc_fence_before();
                 mbar_arrive(bar(Q_FULL));
@@ -675,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
     }
 }
 
-template <int D, bool DEAL, bool TREE>
+template <int D, bool DEAL, int TREE>
 void launch_tc(const AttnParams& p, cudaStream_t s) {
     using C = Cfg<D>;
     static unsigned long long configured = 0;   // one bit per device
@@ -693,8 +761,9 @@ void launch_tc(const AttnParams& p, cudaStream_t s) {
 namespace {
 template <int D>
 void launch_d(const AttnParams& p, cudaStream_t s) {
-    if (p.anc) p.waves > 0 ? launch_tc<D, true, true>(p, s) : launch_tc<D, false, true>(p, s);
-    else p.waves > 0 ? launch_tc<D, true, false>(p, s) : launch_tc<D, false, false>(p, s);
+    if (p.append) p.waves > 0 ? launch_tc<D, true, kAppends>(p, s) : launch_tc<D, false, kAppends>(p, s);
+    else if (p.anc) p.waves > 0 ? launch_tc<D, true, kDraft>(p, s) : launch_tc<D, false, kDraft>(p, s);
+    else p.waves > 0 ? launch_tc<D, true, kTail>(p, s) : launch_tc<D, false, kTail>(p, s);
 }
 }  // namespace
 

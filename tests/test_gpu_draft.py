@@ -164,6 +164,34 @@ def test_attention_of_a_long_cache_split_over_blocks():
         a.check([tree("tree", n)], x, a.run([tree("tree", n)], x))
 
 
+@pytest.mark.parametrize("hq,hkv,d,rot", [(16, 2, 256, 64), (8, 2, 64, 64), (16, 4, 128, 0)])
+def test_nodes_appended_by_the_attention_or_before_it(hq, hkv, d, rot):
+    """Characters of one query tile each are appended by the attention itself: one launch.  With a larger tree beside them their
+    outputs and rows are the same bits (every tile here is one block's)."""
+    import torch
+    small, big = 128 * hkv // hq, 64
+    lives = [130, 0, 63, 77]
+    trees = [tree("tree", small, b) for b in range(3)]
+    x = Attn(hq, hkv, d, rot, lives, seed=25).inputs(3 * small + big, seed=26)
+    rows = []
+    for extra in (False, True):
+        a = Attn(hq, hkv, d, rot, lives, seed=25)
+        t = trees + [tree("tree", big, 3) if extra else []]
+        n = sum(map(len, t))
+        q, k, v = (_bf(z[:n]) for z in x)
+        out = torch.empty_like(q)
+        a.ctx.draft_begin(cu_of(t), packed(t))
+        before = a.ctx.launch_count()
+        a.ctx.draft_attn(0, q, k, v, out)
+        assert a.ctx.launch_count() - before == (2 if extra else 1)
+        path = [O.draft_path(y, len(y) - 1) if y else [] for y in t]
+        a.ctx.draft_commit(cu_of(path), packed(path))
+        a.ctx.check()
+        rows.append([out[:3 * small]] + [z for b in range(3) for z in (*a.ctx.get_kv(0, b), a.ctx.get_positions(b))])
+    for y, z in zip(*rows):
+        assert torch.equal(y, z) if torch.is_tensor(y) else np.array_equal(y, z)
+
+
 def test_attention_of_many_trees_dealt_in_waves():
     lives = [700 + 37 * b for b in range(24)]
     trees = [tree("tree", 64 - b, b) for b in range(24)]
