@@ -82,7 +82,7 @@ constexpr int kAppendThreads = 64;            // warps 1 and 10
 constexpr int STAGES = 3;                     // K and V ring depth (a fourth of either: the same time or more)
 
 enum Bar { K_FULL = 0, K_EMPTY = 3, V_FULL = 6, V_EMPTY = 9, S_FULL = 12, S_EMPTY = 14, P_FULL = 16,
-           PV_DONE = 18, Q_FULL = 20, O_FINAL = 21, O_EMPTY = 22, DRAIN_S = 23, DRAIN_PV = 24, NODES = 25, N_BARS = 26 };
+           PV_DONE = 18, Q_FULL = 20, O_FINAL = 21, O_EMPTY = 22, DRAIN_S = 23, DRAIN_PV = 24, N_BARS = 25 };
 
 template <int D>
 struct Cfg {
@@ -96,7 +96,8 @@ struct Cfg {
     static constexpr int OFF_ABORT = OFF_SLOT + 4;
     static constexpr int OFF_X = (OFF_ABORT + 4 + 15) / 16 * 16;   // float [2][2][BM]: (sum, reference max) of each group at a segment's end
     static constexpr int OFF_MR = OFF_X + 2 * 2 * BM * 4;  // float [BM]: the rows' reference maxima
-    static constexpr int USED = OFF_MR + BM * 4;
+    static constexpr int OFF_NODES = OFF_MR + BM * 4;      // barrier: a draft's keys and values are in the caches
+    static constexpr int USED = OFF_NODES + 8;
     // head_dim 256 leaves no room to align the base up: a block without static
     // shared variables gets a 1024-aligned dynamic base (checked at run time)
     static constexpr int SLACK = (D == 256) ? 0 : 1024;
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
         mbar_init(bar(Q_FULL), kSoftmaxThreads);
         mbar_init(bar(O_FINAL), 1);
         mbar_init(bar(O_EMPTY), kSoftmaxThreads);
-        mbar_init(bar(NODES), kAppendThreads);
+        if (TREE == kAppends) mbar_init(sbase + C::OFF_NODES, kAppendThreads);
         mbar_init(bar(DRAIN_S), 1);
         mbar_init(bar(DRAIN_PV), 1);
         fence_mbar_init();
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
     if constexpr (TREE == kAppends) {
         if (warp == 1 || warp == kPvWarp) {
             append_nodes<D>(p, n_seg, lane + (warp == 1 ? 0 : 32), tile_of, key_begin, key_end);
-            mbar_arrive(bar(NODES));
+            mbar_arrive(sbase + C::OFF_NODES);
             __syncwarp();
         }
     }
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 const int key_row0 = (p.attn_layer * p.Hkv + T.kvh) * (int)p.slab_rows + ch.cap_off;
                 for (int kt = k; kt < k1; ++kt, ++j) {
                     if (!waited && (kt + 1) * BN > ch.L_prev) {    // the tile reaches the tail
-                        if (TREE == kAppends) ok = mbar_wait(bar(NODES), 0, abort_flag, p.err, kErrWait, p.diag, 0x15);
+                        if (TREE == kAppends) ok = mbar_wait(sbase + C::OFF_NODES, 0, abort_flag, p.err, kErrWait, p.diag, 0x15);
                         else grid_dependency_wait();
                         waited = true;
                     }
