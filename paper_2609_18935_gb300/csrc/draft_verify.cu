@@ -84,10 +84,12 @@ __device__ __forceinline__ bool less(Pair a, Pair x) { return positive(sub(x, a)
 __device__ __forceinline__ Pair shuffle_xor(Pair a, int o) {
     return {__shfl_xor_sync(0xffffffffu, a.hi, o), __shfl_xor_sync(0xffffffffu, a.lo, o)};
 }
-// Every lane gets the sum in the same bits: a sum of two does not depend on their order.
-__device__ __forceinline__ Pair warp_sum(Pair a) {
+// The sum over each N neighbouring lanes (N a power of two), in the same bits in every
+// one of them: a sum of two does not depend on their order.
+template <int N>
+__device__ __forceinline__ Pair lane_sum(Pair a) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a = add(a, shuffle_xor(a, o));
+    for (int o = N / 2; o > 0; o >>= 1) a = add(a, shuffle_xor(a, o));
     return a;
 }
 
@@ -166,12 +168,12 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     __syncthreads();
     if (tid < n) {
         const unsigned long long up = p.anc[n0 + tid] & ~(1ull << tid);
+        const int t = p.tokens[n0 + tid];
         const int pa = up ? 63 - __clzll(up) : -1;
         if (pa >= 0) atomicOr(kids + pa, 1ull << tid);
         us[tid] = p.u[n0 + tid];
         float x = 0.f, y = 0.f;
         if (pa >= 0) {
-            const int t = p.tokens[n0 + tid];
             if (t >= 0 && t < V) {
                 x = (float)target[(int64_t)(n0 + pa) * V + t];
                 y = (float)draft[(int64_t)(n0 + pa) * V + t];
@@ -212,12 +214,12 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
             add(acc, weights(pack2(a[2], a[3]), pack2(d[2], d[3]), ch2, nch2, ncl2));
         }
         const float2 hi = unpack2(acc.hi), lo = unpack2(acc.lo);
-        const Pair mine = warp_sum(add(Pair{hi.x, lo.x}, Pair{hi.y, lo.y}));
+        const Pair mine = lane_sum<32>(add(Pair{hi.x, lo.x}, Pair{hi.y, lo.y}));
         if (lane == 0) sums[warp] = mine;
         __syncthreads();
         Pair* all = parts[pass & 1];
         if (warp == 0) {
-            const Pair z = warp_sum(lane < kWarps ? sums[lane] : Pair{0.f, 0.f});
+            const Pair z = lane_sum<kWarps>(sums[lane & (kWarps - 1)]);
             if (blocks == 1) {
                 if (lane == 0) all[0] = z;
             } else {
@@ -232,7 +234,9 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         if (blocks == 1) __syncthreads();
         else lost = __syncthreads_or(!ptx::mbar_wait(bar + 8 * (pass & 1), pass >> 1 & 1, abort_flag, p.err, kErrWait, p.diag, 0x71));
         ++pass;
-        return warp_sum(lane < blocks ? all[lane] : Pair{0.f, 0.f});   // the same order in every warp
+        Pair z = all[lane & (blocks - 1)];           // blocks is a power of two; the same order in every warp
+        for (int o = blocks / 2; o > 0; o >>= 1) z = add(z, shuffle_xor(z, o));
+        return z;
     };
     for (;;) {
         const int64_t at = (int64_t)(n0 + cur) * V;
