@@ -15,7 +15,7 @@
 // failed and for the last draw.  A row's pass is spread over a cluster of blocks,
 // and its warps' sums meet in distributed shared memory.  Passes depend on one
 // another, about 2 us each, so a verdict takes as long as its longest walk: 8 us over
-// one tree of 16 nodes and 50001 tokens, 32 us over 32 trees of up to 24 and 131072.
+// one tree of 16 nodes and 50001 tokens, 30 us over 32 trees of up to 24 and 131072.
 //
 // Sums decide between neighbouring tokens, so they are carried in pairs of fp32
 // (the error-free sum and product; Dekker, "A floating-point technique for
@@ -23,6 +23,8 @@
 // relative, where a sum in 32 bits would move the draw by many tokens of a large
 // vocabulary, and the 64-bit pipe gives two results a cycle and SM: with the few
 // scalars of the walk alone in 64 bits, in every thread, a verdict took twice as long.
+#include <type_traits>
+
 #include "kvm_internal.cuh"
 #include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
@@ -45,14 +47,22 @@ __device__ __forceinline__ float probability(float x) {       // what is not a f
     return __float_as_uint(x) < 0x7f800000u ? x : 0.f;
 }
 
-// max(p - c q, 0) of two elements; c = ch + cl
+// w where t > 0, else 0
+__device__ __forceinline__ Pairs where_positive(f2 hi, f2 lo) {
+    const float2 t = unpack2(add2(hi, lo)), x = unpack2(hi), y = unpack2(lo);
+    return {pack2(t.x > 0.f ? x.x : 0.f, t.y > 0.f ? x.y : 0.f), pack2(t.x > 0.f ? y.x : 0.f, t.y > 0.f ? y.y : 0.f)};
+}
+// max(p - q, 0) of two elements: p may be anything (0 for what is no probability), q is one
+__device__ __forceinline__ Pairs weights(f2 p, f2 q) {
+    const f2 s = sub2(p, q), bv = sub2(s, p), av = sub2(s, bv);
+    return where_positive(s, sub2(sub2(p, av), add2(q, bv)));
+}
+// max(p - c q, 0), c = ch + cl
 __device__ __forceinline__ Pairs weights(f2 p, f2 q, f2 ch, f2 nch, f2 ncl) {
     const f2 m = mul2(nch, q), e = fma2(ch, q, m);             // -c q = m - e + ncl q
     const f2 s = add2(p, m);
     const f2 bv = sub2(s, p), av = sub2(s, bv);
-    const f2 lo = fma2(ncl, q, sub2(add2(sub2(p, av), sub2(m, bv)), e));
-    const float2 t = unpack2(add2(s, lo)), x = unpack2(s), y = unpack2(lo);
-    return {pack2(t.x > 0.f ? x.x : 0.f, t.y > 0.f ? x.y : 0.f), pack2(t.x > 0.f ? y.x : 0.f, t.y > 0.f ? y.y : 0.f)};
+    return where_positive(s, fma2(ncl, q, sub2(add2(sub2(p, av), sub2(m, bv)), e)));
 }
 
 __device__ __forceinline__ void add(Pairs& a, const Pairs& x) {
@@ -93,8 +103,7 @@ __device__ __forceinline__ Pair lane_sum(Pair a) {
     return a;
 }
 
-// Four neighbouring values of a row from virtual place y (a multiple of 4), as
-// probabilities: place y holds element y - m, so that places on the vector grid lie
+// Four neighbouring values of a row from virtual place y (a multiple of 4): place y holds element y - m, so that places on the vector grid lie
 // on it in memory too.
 template <typename T>
 __device__ __forceinline__ void load4(const T* row, int y, int m, int end, float (&x)[4]) {
@@ -111,6 +120,8 @@ __device__ __forceinline__ void load4(const T* row, int y, int m, int end, float
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = y + e >= m && y + e < end ? (float)row[y + e - m] : 0.f;
     }
+}
+__device__ __forceinline__ void probabilities(float (&x)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = probability(x[e]);
 }
@@ -201,18 +212,38 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         nch2 = pack2(-c.hi, -c.hi);
         ncl2 = pack2(-c.lo, -c.lo);
     };
-    auto row_sum = [&]() {
-        set_c();
+    // This thread's sum of w over the row: c is 0 (q is not read), 1 (no rounding in c q)
+    // or another number.  Its instructions bound a pass over a large vocabulary: with
+    // the last form for all three 32 trees over 131072 tokens took 31.9 us against 29.9.
+    auto thread_sum = [&](auto kind) {
+        constexpr int C = decltype(kind)::value;
         Pairs acc{0, 0};                             // four zeros
         const int y1 = min(end, (gw + 1) * per);
 #pragma unroll 4
         for (int y = gw * per + 4 * lane; y < y1; y += 128) {
             float a[4], d[4];
             load4(rp, y, m, end, a);
+            if constexpr (C == 0) {
+                probabilities(a);
+                add(acc, {pack2(a[0], a[1]), 0});
+                add(acc, {pack2(a[2], a[3]), 0});
+                continue;
+            }
             load4(rq, y, m, end, d);
-            add(acc, weights(pack2(a[0], a[1]), pack2(d[0], d[1]), ch2, nch2, ncl2));
-            add(acc, weights(pack2(a[2], a[3]), pack2(d[2], d[3]), ch2, nch2, ncl2));
+            probabilities(d);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const f2 x = pack2(a[e], a[e + 1]), z = pack2(d[e], d[e + 1]);
+                add(acc, C == 1 ? weights(x, z) : weights(x, z, ch2, nch2, ncl2));
+            }
         }
+        return acc;
+    };
+    auto row_sum = [&]() {
+        set_c();
+        const Pairs acc = !positive(c) ? thread_sum(std::integral_constant<int, 0>())
+                          : c.hi == 1.f && c.lo == 0.f ? thread_sum(std::integral_constant<int, 1>())
+                                                       : thread_sum(std::integral_constant<int, 2>());
         const float2 hi = unpack2(acc.hi), lo = unpack2(acc.lo);
         const Pair mine = lane_sum<32>(add(Pair{hi.x, lo.x}, Pair{hi.y, lo.y}));
         if (lane == 0) sums[warp] = mine;
@@ -301,6 +332,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
             if (y < y1) {
                 load4(rp, y, m, end, a);
                 load4(rq, y, m, end, d);
+                probabilities(d);
             }
             Pair w[4], x{0.f, 0.f};
 #pragma unroll
@@ -367,10 +399,12 @@ void launch(const DraftVerifyParams& p, int blocks, cudaStream_t s) {
 // Blocks of a character's cluster: a power of two up to 16 that leaves each thread at
 // least four elements, while all characters' blocks fit the SMs at once (two of 512
 // threads or four of 256 an SM).  Blocks of 512 threads where 16 of them fit for every
-// character, else of 256: 131072 tokens of one character 17 | 22 us, 32768 of 32
-// characters 16.4 | 15.0, 131072 of 32 36 | 33 with 512 | 256 (up to 8 | 16 blocks).
+// character and 256 threads would have more than eight elements each, else of 256, whose
+// sums meet sooner; with 512 | 256: 131072 tokens of one character 15.1 | 18.7 us, 50001
+// 7.9 | 9.1, 32768 of 8 (16-bit, 64 nodes) 19.4 | 17.5, of one 9.4 | 9.7; of 32 15.3 | 14.2,
+// 131072 of 32 32.4 | 30.0.
 void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cudaStream_t s) {
-    const bool large = (int64_t)kMaxCluster * p.n_chars <= 2 * num_sms;
+    const bool large = (int64_t)kMaxCluster * p.n_chars <= 2 * num_sms && p.vocab > 8 * 256 * kMaxCluster;
     const int threads = large ? 512 : 256;
     int blocks = 1;
     while (blocks < kMaxCluster && blocks * threads * 4 < p.vocab && (int64_t)2 * blocks * p.n_chars * threads <= (int64_t)1024 * num_sms)

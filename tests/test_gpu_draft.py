@@ -570,6 +570,28 @@ def test_verdicts_at_their_edges():
     v.check(t, tokens, less, draft, np.full(n, 0.999), r.random(4))
 
 
+@pytest.mark.parametrize("V", [700, 5003])
+def test_verdicts_over_rows_that_hold_no_probabilities(V):
+    """What is not a finite positive number counts as 0, in the target's rows, the draft's and both, after none, one and several
+    guesses that fail."""
+    import torch
+    r = np.random.default_rng([87, V])
+    v = Verdict(4)
+    n = 24
+    rows = _rows(r, n, V, torch.float32)
+    odd = []
+    for z in rows:
+        z = z.clone()
+        z[:, ::5], z[:, 1::7], z[:, 2::11], z[:, 3::13] = -1.0, float("nan"), float("inf"), float("-inf")
+        odd.append(z)
+    tokens = r.integers(0, V, n)
+    for kind in ("star", "chain"):
+        t = [tree(kind, 6, 0)] * 4
+        for target, draft in ((rows[0], odd[1]), (odd[0], rows[1]), odd):
+            for u in (np.zeros(n), r.random(n), np.full(n, 0.99999994)):
+                v.check(t, tokens, target, draft, u, r.random(4))
+
+
 def test_a_token_outside_the_vocabulary_is_refused_and_reported():
     import torch
     from paper_2609_18935_gb300 import kvm
