@@ -157,8 +157,6 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     const int V = p.vocab;
     const T* target = static_cast<const T*>(p.target);
     const T* draft = static_cast<const T*>(p.draft);
-    grid_dependency_wait();
-    grid_dependents_launch();
     volatile int* abort_flag = &abort_word;
     const uint32_t bar = ptx::smem_u32(arrived);
     if (tid == 0) {
@@ -166,17 +164,20 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         ptx::mbar_init(bar, 1);
         ptx::mbar_init(bar + 8, 1);
         ptx::fence_mbar_init();
-        if (rank == 0) p.next[b] = -1;               // unless a token is found
-    }
-    __syncwarp();
-    if (blocks > 1) cluster_arrive();                // the neighbours' barriers stand before the first sum arrives: waited for below
-    if (n <= 0) {                                    // uniform over the cluster
-        if (blocks > 1) cluster_wait();
-        if (rank == 0 && tid == 0) p.count[b] = 0;
-        return;
     }
     if (tid < kDraftNodes) kids[tid] = 0;
     __syncthreads();
+    if (blocks > 1) {                                // the neighbours' barriers stand before the first sum arrives
+        cluster_arrive();
+        cluster_wait();
+    }
+    grid_dependency_wait();
+    grid_dependents_launch();
+    if (n <= 0) {                                    // uniform over the cluster
+        if (rank == 0 && tid == 0) { p.count[b] = 0; p.next[b] = -1; }
+        return;
+    }
+    const float u_next = p.u_next[b];
     if (tid < n) {
         const unsigned long long up = p.anc[n0 + tid] & ~(1ull << tid);
         const int t = p.tokens[n0 + tid];
@@ -196,7 +197,6 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         qt[tid] = probability(y);
     }
     __syncthreads();
-    if (blocks > 1) cluster_wait();
 
     const int gw = rank * kWarps + warp, n_gw = blocks * kWarps;
     int cur = 0, count = 1, pass = 0;
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         c = {0.f, 0.f};
         Z = row_sum();
     }
-    const Pair T0 = mul(Z, p.u_next[b]);
+    const Pair T0 = mul(Z, u_next);
     // running sum of x over the lanes before this one
     auto before_lane = [&](Pair x) {
         Pair inc = x;
@@ -322,7 +322,12 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
     };
     Pair before{0.f, 0.f};
     const int block = find(last, blocks, before);
-    const int found = !lost && block == (int)rank ? (int)rank * kWarps + find(sums, kWarps, before) : -1;
+    int found = -1;                                  // the warp whose part holds the token
+    if (!lost && block == (int)rank) {
+        const int w = find(sums, kWarps, before);
+        if (w >= 0) found = (int)rank * kWarps + w;
+        else if (tid == 0) p.next[b] = -1;           // sums that are no numbers
+    }
     if (found == gw) {
         const int y1 = min(end, (gw + 1) * per);
         int best = -1;
@@ -356,6 +361,7 @@ __global__ void __launch_bounds__(THREADS) draft_verify_kernel(const __grid_cons
         if (lane == 0) p.next[b] = best;
     }
     if (rank == 0) {
+        if ((block < 0 || lost) && tid == 0) p.next[b] = -1;       // the row holds no positive number
         __syncthreads();
         if (tid < n) p.path[n0 + tid] = tid < count ? path[tid] : -1;
         if (tid == 0) p.count[b] = count;
