@@ -14,7 +14,7 @@
 // fetches them for the whole tree, and the walk reads a row only where a guess
 // failed and for the last draw.  A row's pass is spread over a cluster of blocks,
 // and its warps' sums meet in distributed shared memory.  Passes depend on one
-// another, about 2 us each, so a verdict takes as long as its longest walk: 8 us over
+// another, about 2 us each, so a verdict takes as long as its longest walk: 7 us over
 // one tree of 16 nodes and 50001 tokens, 30 us over 32 trees of up to 24 and 131072.
 //
 // Sums decide between neighbouring tokens, so they are carried in pairs of fp32
