@@ -200,6 +200,16 @@ def test_attention_of_many_trees_dealt_in_waves():
     a.check(trees, x, a.run(trees, x))
 
 
+@pytest.mark.parametrize("d", [64, 256])
+def test_attention_of_many_small_trees_dealt_in_waves(d):
+    """More than two waves of query tiles whose blocks append the nodes themselves."""
+    lives = [100 + 11 * b for b in range(96)]
+    trees = [tree("tree", 1 + b % 7, b) for b in range(96)]
+    a = Attn(8, 4, d, 32, lives, seed=27)
+    x = a.inputs(sum(map(len, trees)), seed=28)
+    a.check(trees, x, a.run(trees, x))
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_a_node_outside_the_path_changes_nothing(d):
     """Bit for bit: other keys and values of node j move the outputs of j and its descendants only."""
