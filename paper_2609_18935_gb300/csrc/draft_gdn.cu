@@ -119,6 +119,12 @@ __device__ __forceinline__ void clear_not_finite(float (&x)[N], bool& bad) {
     for (int e = 0; e < N; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] : 0.f;
 }
 
+// Four 8 x 8 blocks of 16-bit elements, lane l giving row l % 8 of block l / 8: each
+// lane gets two neighbours of row l / 4.
+__device__ __forceinline__ void ldmatrix(uint32_t (&f)[2][2], uint32_t row) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(f[0][0]), "=r"(f[0][1]), "=r"(f[1][0]), "=r"(f[1][1]) : "r"(row) : "memory");
+}
 // 16 TMEM lanes x 16 columns, as two such D (to be waited for).
 __device__ __forceinline__ void tmem_ld_16x16(uint32_t addr, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -158,15 +164,11 @@ __device__ __forceinline__ void block_mma(float (&d)[2][4], float (&lo)[2][4], c
                                           int pitch, int part_step) {
     constexpr int LAST = NB - 1;                 // parts i of a and j of B with i + j <= LAST
     const int lane = threadIdx.x & 31;
-    const uint32_t* b = reinterpret_cast<const uint32_t*>(B + (lane >> 2) * pitch) + (lane & 3);
+    const uint32_t b = smem_u32(B + ((lane >> 4) * 8 + (lane & 7)) * pitch + (lane & 8));
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        uint32_t f[2][2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f[t][0] = b[(j * part_step + 8 * t * pitch) / 2];
-            f[t][1] = b[(j * part_step + 8 * t * pitch) / 2 + 4];
-        }
+        uint32_t f[2][2];                        // [columns 8 t ..][k 0 - 7, 8 - 15]
+        ldmatrix(f, b + j * part_step * 2);
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
