@@ -97,7 +97,8 @@ struct Cfg {
     static constexpr int OFF_X = (OFF_ABORT + 4 + 15) / 16 * 16;   // float [2][2][BM]: (sum, reference max) of each group at a segment's end
     static constexpr int OFF_MR = OFF_X + 2 * 2 * BM * 4;  // float [BM]: the rows' reference maxima
     static constexpr int OFF_NODES = OFF_MR + BM * 4;      // barrier: a draft's keys and values are in the caches
-    static constexpr int USED = OFF_NODES + 8;
+    static constexpr int OFF_FIRST = OFF_NODES + 8;        // barrier: the block's first Q is staged
+    static constexpr int USED = OFF_FIRST + 8;
     // head_dim 256 leaves no room to align the base up: a block without static
     // shared variables gets a 1024-aligned dynamic base (checked at run time)
     static constexpr int SLACK = (D == 256) ? 0 : 1024;
@@ -333,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
         mbar_init(bar(O_FINAL), 1);
         mbar_init(bar(O_EMPTY), kSoftmaxThreads);
         if (TREE == kAppends) mbar_init(sbase + C::OFF_NODES, kAppendThreads);
+        if (TREE) mbar_init(sbase + C::OFF_FIRST, kSoftmaxThreads);
         mbar_init(bar(DRAIN_S), 1);
         mbar_init(bar(DRAIN_PV), 1);
         fence_mbar_init();
@@ -387,8 +389,10 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                         waited = true;
                     }
                     const int st = j % STAGES;
-                    // a draft's blocks have few units: their first Q and K tiles come before the rings fill up
-                    if (TREE && ok && j == (is_k ? 1 : 0)) ok = mbar_wait(bar(Q_FULL), 0, abort_flag, p.err, kErrWait, p.diag, 0x14);
+                    // a draft's blocks have few units: their first Q and K tiles come before the rings fill up.  A barrier
+                    // with one phase: Q_FULL's first may be over, and its second too, before a producer looks (a first
+                    // segment of one key tile needs nothing of what this wait holds back).
+                    if (TREE && ok && j == (is_k ? 1 : 0)) ok = mbar_wait(sbase + C::OFF_FIRST, 0, abort_flag, p.err, kErrWait, p.diag, 0x14);
                     if (ok && j >= STAGES)
                         ok = mbar_wait(bar(empty + st), (j / STAGES - 1) & 1, abort_flag, p.err, kErrWait, p.diag,
                                        (is_k ? 0x12 : 0x13) + 256 * j);
@@ -543,7 +547,10 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             tc_fence_before();
             mbar_arrive(bar(Q_FULL));
         };
-        if (n_seg > 0) stage_q(tile_of(0));
+        if (n_seg > 0) {
+            stage_q(tile_of(0));
+            if (TREE) mbar_arrive(sbase + C::OFF_FIRST);
+        }
         int j = 0;
         for (int seg = 0; seg < n_seg; ++seg) {
             const Tile T = decode_tile(p, tile_of(seg));

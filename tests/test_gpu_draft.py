@@ -211,6 +211,21 @@ def test_attention_of_many_small_trees_dealt_in_waves(d):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("most", [3, 40])
+def test_attention_of_segments_of_one_key_tile(d, most):
+    """Blocks of several query tiles of one or two key tiles each, the first one among them: a block's second Q may be staged
+    before its producers have looked for the first.  Nodes appended by the attention (up to 3 nodes) and before it."""
+    lives = [(7 * b) % 61 for b in range(100)]
+    trees = [tree("tree", 1 + b % most, b) for b in range(100)]
+    a = Attn(16, 4, d, 32, lives, seed=29)
+    x = a.inputs(sum(map(len, trees)), seed=30)
+    out = a.run(trees, x).clone()
+    a.check(trees, x, out)
+    for _ in range(10):
+        assert bool((a.run(trees, x) == out).all())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
 def test_a_node_outside_the_path_changes_nothing(d):
     """Bit for bit: other keys and values of node j move the outputs of j and its descendants only."""
     import torch
