@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         fence_mbar_init();
     }
     if (warp == 0) {
+        __syncwarp();
         tmem_alloc(smem_u32(slot), cols);
         tmem_relinquish();
     }
@@ -494,6 +495,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
         const float scale = real ? (is_c ? -be[i] : 1.f) * (exact ? 1.f : G[i]) : 0.f;
         for (int J = warp >> 2; J < NB; J += 2) {
             uint32_t g[16];
+            __syncwarp();                            // lanes part ways below, a load from TMEM is the warp's
             tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + 2 * T + 16 * J, g);
             tmem_ld_wait();
             if (l >= 2 * T || J > I) continue;
@@ -595,6 +597,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                 }
             clear_not_finite(x[0], bad);
             clear_not_finite(x[1], bad);
+            __syncwarp();                            // the loads and products below are the warp's
             if (I + 1 < NB) {
                 tmem_ld_16x16(lanes + 16 * (I + 1), xa);
                 tmem_ld_16x16(lanes + T + 16 * (I + 1), oa);
@@ -621,6 +624,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                     vs[node * kLdv + r] = __float2bfloat16_rn(o[t][e]);                 // in v's place, read by this lane alone
                     if (node < n && r < dv) p.rec_u[((int64_t)(n0 + node) * H + h) * dv + r] = y[t][e];
                 }
+            __syncwarp();
         }
         if (bad) atomicOr(p.err, kErrValue);
     } else if (*abort_flag) {
@@ -637,6 +641,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
                 *reinterpret_cast<uint4*>(p.out + ((int64_t)(n0 + i) * H + h) * dv + c) = *reinterpret_cast<const uint4*>(vs + i * kLdv + c);
     }
     if (warp == 0) {
+        __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, cols);
     }

@@ -502,6 +502,37 @@ def test_a_delta_rule_node_that_is_not_finite_stays_alone(conv):
     assert np.array_equal(got, other.ctx.get_state(0).cpu().numpy()[0])
 
 
+@pytest.mark.parametrize("h,dk,dv", [(16, 128, 128), (4, 64, 32)])
+@pytest.mark.parametrize("name", ["k", "v", "alpha"])
+def test_lanes_of_a_warp_that_part_ways(h, dk, dv, name):
+    """64 nodes, one of them not finite: rows of a warp with and without a coefficient in a block of nodes, with and without
+    something to clear, and (a small decay) with paths of their own length to multiply along.  Again and again the same bits, those of
+    the draft without it where they do not depend on it."""
+    import torch
+    for kind in ("tree", "comb", "forest"):
+        t = tree(kind, 64, 9)
+        g = Gdn(h, dk, dv, 2, seed=79)
+        x = g.inputs(128, seed=80)
+        x["alpha"][5] = 2.0 ** -60
+        base = g.run([t, t], x).clone()
+        g.check([t, t], x, base)
+        bad = {m: z.copy() for m, z in x.items()}
+        bad[name][40, 0, ...] = np.nan if name == "alpha" else 0x7FC0
+        dev = g.tensors(bad)
+        first = None
+        for _ in range(10):
+            out = torch.zeros_like(dev[2])
+            g.ctx.draft_begin(cu_of([t, t]), packed([t, t]))
+            g.ctx.draft_gdn(0, *dev, out)
+            _reported(g.ctx)
+            for i in range(64):
+                assert 40 in O.draft_path(t, i) or torch.equal(out[i], base[i]), (kind, i)
+            assert torch.equal(out[64:], base[64:])
+            bits = out.view(torch.int16)
+            first = bits.clone() if first is None else first
+            assert torch.equal(bits, first)
+
+
 # ---------------------------------------------------------------------------- verdicts
 class Verdict:
     def __init__(self, chars):
