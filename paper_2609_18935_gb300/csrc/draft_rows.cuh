@@ -21,6 +21,12 @@ __device__ __forceinline__ bool clear_not_finite(uint4& v) {
     return bad;
 }
 
+__device__ __forceinline__ bool clear_not_finite(__nv_bfloat16& v) {
+    const bool bad = (__bfloat16_as_ushort(v) & 0x7f80) == 0x7f80;
+    if (bad) v = __ushort_as_bfloat16(0);
+    return bad;
+}
+
 // Eight elements of a key and those `half` further on, rotated by the (cos, sin) of
 // their pairs.  store: true if one was not finite (and went in as 0).
 struct TurnedNode {

@@ -17,6 +17,7 @@
 //                sum); a thread per 4-column piece of a row, or per 32-column
 //                group when the round shares more tiles than one wave of
 //                pieces covers.
+#include "draft_rows.cuh"
 #include "kvm_internal.cuh"
 
 namespace kvm {
@@ -48,6 +49,9 @@ __device__ __forceinline__ void rotate8(uint4& lo, uint4& hi, const float* cs, c
     }
 }
 
+// DRAFT: the rows are a draft's nodes (their rotary dims not a multiple of 32); what
+// is not finite in a key or value goes in as 0 and is reported, as in draft_append.
+template <bool DRAFT>
 __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant__ AttnParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
@@ -71,6 +75,7 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
     __nv_bfloat16* qdst = p.q_rot + (int64_t)n * p.Hq * D;
     const __nv_bfloat16* krow = p.k_new + (int64_t)n * p.Hkv * D;
     const __nv_bfloat16* vrow = p.v_new + (int64_t)n * p.Hkv * D;
+    bool bad = false;                         // something of a draft was not finite
     if ((half & 7) == 0) {
         // 16-byte groups: group g < half/8 rotates with group g + half/8;
         // groups from R/8 on are copied.  The first kPre items of each thread
@@ -79,6 +84,7 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
         const int rot = half / 8, copy = (D - p.R) / 8, per_head = rot + copy;
         const int n_items = (p.Hq + p.Hkv) * per_head;
         constexpr int kPre = 4;
+        auto is_key = [&](int idx) { return idx >= p.Hq * per_head; };
         auto src_of = [&](int idx, int& d0, bool& rotated, __nv_bfloat16*& dst) -> const __nv_bfloat16* {
             const int h = idx / per_head, gidx = idx % per_head;
             const bool is_q = h < p.Hq;
@@ -103,8 +109,9 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
         // that the first ones form the angles meanwhile
         for (int idx = blockDim.x - 1 - threadIdx.x; idx < p.Hkv * (D / 8); idx += blockDim.x) {
             const int h = idx / (D / 8), d0 = (idx % (D / 8)) * 8;
-            *reinterpret_cast<uint4*>(p.V + ((int64_t)h * p.slab_rows + slot) * D + d0) =
-                *reinterpret_cast<const uint4*>(vrow + h * D + d0);
+            uint4 v = *reinterpret_cast<const uint4*>(vrow + h * D + d0);
+            if (DRAFT) bad = clear_not_finite(v) || bad;
+            *reinterpret_cast<uint4*>(p.V + ((int64_t)h * p.slab_rows + slot) * D + d0) = v;
         }
         for (int d = threadIdx.x; d < half; d += blockDim.x) {
             const double ang = (double)pos * p.inv_freq[d];
@@ -121,6 +128,10 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
             if (idx < n_items) {
                 int d0; bool rotated; __nv_bfloat16* dst;
                 src_of(idx, d0, rotated, dst);
+                if (DRAFT && is_key(idx)) {
+                    bad = clear_not_finite(la[u]) || bad;
+                    if (rotated) bad = clear_not_finite(lb[u]) || bad;
+                }
                 if (rotated) {
                     rotate8(la[u], lb[u], cs, sn, d0);
                     *reinterpret_cast<uint4*>(dst + d0) = la[u];
@@ -134,8 +145,10 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
             int d0; bool rotated; __nv_bfloat16* dst;
             const __nv_bfloat16* src = src_of(idx, d0, rotated, dst);
             uint4 a = *reinterpret_cast<const uint4*>(src + d0);
+            if (DRAFT && is_key(idx)) bad = clear_not_finite(a) || bad;
             if (rotated) {
                 uint4 bb = *reinterpret_cast<const uint4*>(src + d0 + half);
+                if (DRAFT && is_key(idx)) bad = clear_not_finite(bb) || bad;
                 rotate8(a, bb, cs, sn, d0);
                 *reinterpret_cast<uint4*>(dst + d0 + half) = bb;
             }
@@ -151,21 +164,26 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
             sn[d] = sv;
         }
         __syncthreads();
-        auto rotated = [&](const __nv_bfloat16* row, int d) -> float {
-            const float x = __bfloat162float(row[d]);
+        auto element = [&](__nv_bfloat16 x, bool clear) {
+            if (clear) bad = clear_not_finite(x) || bad;
+            return x;
+        };
+        auto rotated = [&](const __nv_bfloat16* row, int d, bool clear) -> float {
+            const float x = __bfloat162float(element(row[d], clear));
             if (d >= p.R) return x;
-            if (d < half) return x * cs[d] - __bfloat162float(row[d + half]) * sn[d];
-            return x * cs[d - half] + __bfloat162float(row[d - half]) * sn[d - half];
+            if (d < half) return x * cs[d] - __bfloat162float(element(row[d + half], clear)) * sn[d];
+            return x * cs[d - half] + __bfloat162float(element(row[d - half], clear)) * sn[d - half];
         };
         for (int idx = threadIdx.x; idx < p.Hq * D; idx += blockDim.x)
-            qdst[idx] = __float2bfloat16_rn(rotated(qrow + (idx / D) * D, idx % D));
+            qdst[idx] = __float2bfloat16_rn(rotated(qrow + (idx / D) * D, idx % D, false));
         for (int idx = threadIdx.x; idx < p.Hkv * D; idx += blockDim.x) {
             const int h = idx / D, d = idx % D;
             const int64_t dst = ((int64_t)h * p.slab_rows + slot) * D + d;
-            p.K[dst] = __float2bfloat16_rn(rotated(krow + h * D, d));
-            p.V[dst] = vrow[h * D + d];
+            p.K[dst] = __float2bfloat16_rn(rotated(krow + h * D, d, DRAFT));
+            p.V[dst] = element(vrow[h * D + d], DRAFT);
         }
     }
+    if (DRAFT && bad) atomicOr(p.err, kErrValue);
     if (threadIdx.x == 0) p.pos[slot] = (int32_t)pos;
 }
 
@@ -422,7 +440,7 @@ void launch_rerotate(const RerotateParams& p, cudaStream_t s) {
 
 void launch_rope_append(const AttnParams& p, int total_tokens, cudaStream_t s) {
     if (total_tokens <= 0) return;
-    launch_pdl(rope_append_kernel, dim3(total_tokens), dim3(128), 0, s, p);
+    launch_pdl(p.anc ? rope_append_kernel<true> : rope_append_kernel<false>, dim3(total_tokens), dim3(128), 0, s, p);
 }
 
 void launch_attn_combine(const CombineParams& p, cudaStream_t s) {

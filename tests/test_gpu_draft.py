@@ -467,6 +467,51 @@ def test_keys_and_values_that_are_not_finite_stay_with_their_node(d, rot):
             assert torch.equal(a.run([t[:3]], y), short)
 
 
+@pytest.mark.parametrize("d,rot,n", [(64, 6, 21), (128, 48, 21), (256, 250, 21), (64, 64, 50), (128, 0, 50), (256, 16, 50), (128, 2, 64)])
+def test_every_way_into_the_caches_keeps_what_is_not_finite_out(d, rot, n):
+    """Rotary dims of any number, and trees of several query tiles: other nodes' outputs and the rows that a commit keeps bit for
+    bit, a later tail's outputs too, and every call reports."""
+    import torch
+    live = 70
+    a, ref = Attn(8, 2, d, rot, [live], seed=75), Attn(8, 2, d, rot, [live], seed=75)
+    t = tree("tree", n, 5)
+    x = a.inputs(n, seed=76)
+    base = a.run([t], x).clone()
+    one = [_bf(z[:1]) for z in x]
+    cu = np.array([0, 1], np.int32)
+    after = torch.empty_like(one[0])
+    ref.ctx.tail_attn_prefill(0, cu, *one, after)
+    for which in (1, 2):
+        for j, bits in zip((0, 4, 13, n - 1), NOT_FINITE):
+            bad = [z.copy() for z in x]
+            bad[which][j, 1, 5 * d // 8] = bits
+            bad[which][j, 0, -1] = bits
+            bad[which][j, 1, 0] = bits
+            q, k, v = (_bf(z) for z in bad)
+            out = torch.zeros_like(q)
+            a.ctx.draft_begin(cu_of([t]), packed([t]))
+            a.ctx.draft_attn(0, q, k, v, out)
+            _reported(a.ctx)
+            for i in range(n):
+                assert j in O.draft_path(t, i) or torch.equal(out[i], base[i]), (which, i, j)
+            got = torch.zeros_like(after)
+            a.ctx.tail_attn_prefill(0, cu, *one, got)
+            a.ctx.check()
+            assert torch.equal(got, after), (which, j)
+    # a path through the last of them (the value of its first head's last dim): what was not finite went in as 0
+    a.ctx.draft_begin(cu_of([t]), packed([t]))
+    a.ctx.draft_attn(0, q, k, v, out)
+    _reported(a.ctx)
+    path = O.draft_path(t, n - 1)
+    a.ctx.draft_commit([0, len(path)], path)
+    K, V = a.ctx.get_kv(0, 0)
+    want = x[2][path].copy()
+    want[-1][0, -1] = want[-1][1, 5 * d // 8] = want[-1][1, 0] = 0
+    assert torch.equal(V[:, live:].view(torch.int16), _bf(want).transpose(0, 1).contiguous().view(torch.int16))
+    assert bool(torch.isfinite(K).all())
+    a.ctx.check()
+
+
 @pytest.mark.parametrize("conv", [False, True])
 def test_a_delta_rule_node_that_is_not_finite_stays_alone(conv):
     """Other nodes' outputs bit for bit, and the state after a commit of a path without it."""
