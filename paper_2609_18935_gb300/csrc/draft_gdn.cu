@@ -177,18 +177,12 @@ __device__ __forceinline__ void block_mma(float (&d)[2][4], float (&lo)[2][4], c
     }
 }
 
-// x / (1 + e^-x) with approximate exponential and reciprocal: within 2^-21, and the
-// result is rounded to eight bits (from -88.7 down, where it is below 2^-121, 0).
-__device__ __forceinline__ float silu(float x) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-1.4426950408889634f * x)));
-    return x * r;
-}
 // Place of channel e's taps in shared memory: lanes read octets of channels, 128
 // bytes apart.
 __device__ __forceinline__ int tap_slot(int e) { return (e & ~7) | ((e ^ e >> 3) & 7); }
 // The convolution, SiLU and (norm) the scaling to unit length of one part of the
-// staged raw rows [3 carried + nodes][pitch bytes], for put(node, channel, eight
+// staged raw rows [3 carried + nodes][pitch bytes], in gdn_conv_kernel's order of
+// operations (so bit for bit what a tail's inputs become), for put(node, channel, eight
 // outputs): eight channels a lane, their taps in registers, two nodes a thread at a
 // time.  rows: per node the staged rows of its four taps, a byte each.
 template <typename Put>
@@ -232,12 +226,13 @@ __device__ __forceinline__ void conv_part(const uint8_t* raw, int pitch, int dim
             float y[8], sq = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float2 v = unpack2(acc[e]);
-                y[2 * e] = silu(v.x);
-                y[2 * e + 1] = silu(v.y);
-                sq = fmaf(y[2 * e], y[2 * e], fmaf(y[2 * e + 1], y[2 * e + 1], sq));
+                const float2 v = silu2(acc[e]);
+                y[2 * e] = v.x;
+                y[2 * e + 1] = v.y;
             }
             if (norm) {                                        // whole warps run this
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sq = fmaf(y[e], y[e], sq);
                 for (int o = per / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
                 const float inv = sq > 0.f ? rsqrtf(sq) : 0.f;
 #pragma unroll

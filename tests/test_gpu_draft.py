@@ -430,6 +430,50 @@ def test_delta_rule_outside_the_path_changes_nothing():
             assert torch.equal(out[i], base[i]) == (j not in O.draft_path(t, i)), (i, j)
 
 
+@pytest.mark.parametrize("h,dk,dv", [(16, 128, 128), (5, 64, 96)])
+def test_convolved_inputs_are_those_of_a_tail(h, dk, dv):
+    """Bit for bit: from a state of 0, gates of 1 and one token a committed node leaves v k^T (exact products of two bf16 numbers),
+    and so does a tail."""
+    import torch
+    chars = 64
+    a, b = (Gdn(h, dk, dv, chars, seed=63, conv=True) for _ in range(2))
+    x = a.inputs(chars, seed=64)
+    for m in ("q", "k", "v"):                                   # pre-activations from small to about -40
+        x[m][::2] = W.f64_to_bf16_bits(8.0 * O.bf16_to_f64(x[m][::2])) if m != "k" else W.f64_to_bf16_bits(60.0 * O.bf16_to_f64(x[m][::2]))
+    x["alpha"][:], x["beta"][:] = 1.0, 1.0
+    for g in (a, b):
+        g.ctx.set_state(0, torch.zeros(chars, h, dv, dk, device="cuda"))
+    a.run([[-1]] * chars, x)
+    cu = np.arange(chars + 1, dtype=np.int32)
+    a.ctx.draft_commit(cu, np.zeros(chars, np.int32))
+    q, k, v, al, be = b.tensors(x)
+    b.ctx.gdn_chunk_scan_from_state(0, cu, q, k, v, al, be, torch.empty_like(v))
+    S, T = a.ctx.get_state(0), b.ctx.get_state(0)
+    assert bool((T != 0).any()) and int((S != T).sum()) == 0
+
+
+@pytest.mark.parametrize("h,dk,dv", [(16, 128, 128), (5, 64, 96)])
+@pytest.mark.parametrize("kind,n", [("chain", 30), ("tree", 64), ("comb", 40), ("forest", 50), ("star", 12)])
+def test_a_convolved_path_leaves_the_state_of_a_tail(h, dk, dv, kind, n):
+    """The state after the commit of a path, and after a tail of the path's tokens (at most 30: token by token, in 32 bits), from the
+    same inputs bit for bit (the test above): within the 1e-5 of either from the oracle without the convolution."""
+    import torch
+    from harness import rel_l2
+    t = tree(kind, n, 7)
+    path = max((O.draft_path(t, i) for i in range(n)), key=len)
+    assert len(path) <= 32
+    a, b = (Gdn(h, dk, dv, 1, seed=65, conv=True) for _ in range(2))
+    x = a.inputs(n, seed=66)
+    a.run([t], x)
+    a.ctx.draft_commit([0, len(path)], path)
+    q, k, v, al, be = b.tensors({m: np.ascontiguousarray(z[path]) for m, z in x.items()})
+    b.ctx.gdn_chunk_scan_from_state(0, [0, len(path)], q, k, v, al, be, torch.empty_like(v))
+    S, T = (c.ctx.get_state(0).cpu().numpy()[0] for c in (a, b))
+    for hh in range(h):
+        assert rel_l2(S[hh], T[hh]) <= 2e-5, hh
+    assert torch.equal(a.ctx.get_conv_state(0).view(torch.int16), b.ctx.get_conv_state(0).view(torch.int16))
+
+
 def _reported(ctx):
     from paper_2609_18935_gb300 import kvm
     with pytest.raises(kvm.KvmError) as ei:
