@@ -39,6 +39,8 @@ kvm_status fail(kvm_status code, const char* fmt, ...) {
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
     g_err = buf;
+    // reported here: the check after a later launch is not to find it again
+    if (code == KVM_E_CUDA) cudaGetLastError();
     return code;
 }
 

@@ -1241,6 +1241,18 @@ def test_refusals():
             assert np.array_equal(u, w), key
 
 
+def test_an_allocation_that_failed_is_reported_once():
+    """Room that the device does not have (8 TB a cache) is refused; the next calls of another context do not report it again."""
+    from paper_2609_18935_gb300 import kvm
+    a = Attn(4, 2, 64, 64, [70], seed=155)
+    x = a.inputs(5, seed=156)
+    for _ in range(2):
+        with pytest.raises(kvm.KvmError) as ei:
+            kvm.Context([kvm.LAYER_ATTN] * 4, 8, 2, 256, 64, THETA, 8, 64, 64, [2_000_000_000], 64)
+        assert ei.value.code == kvm.KVM_E_CUDA
+        a.check([tree("tree", 5)], x, a.run([tree("tree", 5)], x))
+
+
 def test_a_context_without_drafts_or_attention():
     """An empty draft commits nothing; a stack of delta-rule layers alone drafts too; room can grow."""
     import torch
