@@ -44,6 +44,7 @@
 // warps wait for instructions and for one another.  One character: 6.1 us, the chain.
 #include <type_traits>
 
+#include "draft_rows.cuh"
 #include "kvm_internal.cuh"
 #include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
@@ -435,8 +436,9 @@ __global__ void __launch_bounds__(kThreads, 2) draft_gdn_kernel(const __grid_con
     // ---- while the products run: the keys' record, and the decays from the root
     for (int e = tid; e < n * GK; e += kThreads) {
         const int i = e / GK, c = 8 * (e % GK);
-        *reinterpret_cast<uint4*>(p.rec_k + ((int64_t)(n0 + i) * H + h) * DK + c) =
-            *reinterpret_cast<const uint4*>(smem + at.kq + sw128_off16(i, c, 2 * T));
+        uint4 key = *reinterpret_cast<const uint4*>(smem + at.kq + sw128_off16(i, c, 2 * T));
+        kvm::clear_not_finite(key);                  // its u is 0, and 0 times it is to stay 0 in a commit (reported with E_ii)
+        *reinterpret_cast<uint4*>(p.rec_k + ((int64_t)(n0 + i) * H + h) * DK + c) = key;
     }
     if (warp == 1) {
         // products up the tree by doubling: g holds the nodes from i up to before `up`

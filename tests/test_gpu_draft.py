@@ -591,6 +591,37 @@ def test_a_delta_rule_node_that_is_not_finite_stays_alone(conv):
     assert np.array_equal(got, other.ctx.get_state(0).cpu().numpy()[0])
 
 
+@pytest.mark.parametrize("conv", [False, True])
+@pytest.mark.parametrize("bits", NOT_FINITE)
+def test_a_committed_key_that_is_not_finite_counts_as_0(conv, bits):
+    """Without the convolution the state is, bit for bit, what a key of 0 leaves in the head (in 32-bit sums a coefficient of 0 and an
+    update of 0 both add nothing); with it the state is finite."""
+    import torch
+    n = 37
+    t = tree("tree", n, 8)
+    path = O.draft_path(t, 36)
+    assert len(path) > 4
+    got = []
+    for put in (bits, 0):
+        g = Gdn(2, 128, 64, 1, seed=77, conv=conv)
+        x = g.inputs(n, seed=78)
+        x["k"][path[2], 0, :] = 0
+        x["k"][path[2], 0, 3] = put
+        q, k, v, al, be = g.tensors(x)
+        out = torch.zeros_like(v)
+        g.ctx.draft_begin(cu_of([t]), packed([t]))
+        g.ctx.draft_gdn(0, q, k, v, al, be, out)
+        if put:
+            _reported(g.ctx)
+        g.ctx.draft_commit([0, len(path)], path)
+        g.ctx.check()
+        got.append(g.ctx.get_state(0))
+    assert bool(torch.isfinite(got[0]).all()) and bool(torch.isfinite(got[1]).all())
+    if not conv:
+        assert torch.equal(got[0], got[1])
+    assert torch.equal(got[0][0, 1], got[1][0, 1])              # the other head
+
+
 @pytest.mark.parametrize("h,dk,dv", [(16, 128, 128), (4, 64, 32)])
 @pytest.mark.parametrize("name", ["k", "v", "alpha"])
 def test_lanes_of_a_warp_that_part_ways(h, dk, dv, name):
