@@ -270,6 +270,41 @@ def test_a_chain_equals_a_tail():
             assert torch.equal(s.view(torch.int16) if s.dtype == torch.bfloat16 else s, t.view(torch.int16) if t.dtype == torch.bfloat16 else t)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(16, 2, 256), (8, 2, 64), (16, 4, 128)])
+@pytest.mark.parametrize("spread", [3.0, 10.0])
+def test_attention_of_scores_far_apart(hq, hkv, d, spread):
+    """Scores with a standard deviation of 3 and 10: a few keys hold a row's weight, its maximum moves from tile to tile and from
+    block to block, tiles and parts weigh nothing, and a tile that the tree masks throughout stands beside the one with the maximum.
+    Without rotary dims queries and keys are exact, so a score is off by its sum in 32 bits alone, e = 2 D 2^-24 max sum_d |q_d k_d| /
+    sqrt(D) (and 2^-21 for the exponential), and an output by 2^-8 |o| + (2^-8 + expm1(2 e) + 1e-5) sum_j p_j |v_j|."""
+    for live, n, kind in ((0, 64, "roots"), (60, 64, "star"), (63, 2, "chain"), (200, 33, "comb"), (8192, 16, "tree"), (20000, 24, "tree")):
+        a = Attn(hq, hkv, d, 0, [live], seed=35)
+        V = W.normal_bf16((36, live, 1), (hkv, live, d))
+        K = W.normal_bf16((36, live, 2), (hkv, live, d), scale=spread)
+        if live:
+            a.ctx.set_kv(0, 0, _bf(K), _bf(V))
+        a.caches[0] = O.AttnCache(O.bf16_to_f64(K), O.bf16_to_f64(V), np.arange(live))
+        x = list(a.inputs(n, seed=37))
+        x[1] = W.normal_bf16((38, n), (n, hkv, d), scale=spread)
+        t = tree(kind, n, 3)
+        got = _f64(a.run([t], x))
+        q, k, v = (O.bf16_to_f64(z) for z in x)
+        c, far = a.caches[0], 0.0
+        for i in range(n):
+            p = O.draft_path(t, i)
+            for h in range(hq):
+                kk = np.concatenate([c.K[h // (hq // hkv)], k[p][:, h // (hq // hkv)]])
+                vv = np.concatenate([c.V[h // (hq // hkv)], v[p][:, h // (hq // hkv)]])
+                sc = kk @ q[i, h] / math.sqrt(d)
+                w = np.exp(sc - sc.max())
+                w /= w.sum()
+                far = max(far, sc.max() - sc.min())
+                e = 2 * d * 2.0 ** -24 * (np.abs(kk) @ np.abs(q[i, h])).max() / math.sqrt(d) + 2.0 ** -21
+                off = 2.0 ** -8 * np.abs(w @ vv) + (2.0 ** -8 + math.expm1(2 * e) + 1e-5) * (w @ np.abs(vv))
+                assert np.all(np.abs(got[i, h] - w @ vv) <= off), (live, i, h, np.abs(got[i, h] - w @ vv).max())
+        assert live < 200 or far > 4 * spread
+
+
 # ---------------------------------------------------------------------------- delta rule
 class Gdn:
     def __init__(self, h, dk, dv, chars, seed, conv=False, layers=1):
