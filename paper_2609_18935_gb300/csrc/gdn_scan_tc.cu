@@ -227,11 +227,6 @@ __device__ __forceinline__ uint32_t ld_acquire_u32(const uint32_t* p) {
 __device__ __forceinline__ void st_release_u32(uint32_t* p, uint32_t v) {
     asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
-// Orders this thread's async-proxy (bulk copy) accesses of global memory
-// with its generic-proxy ones.
-__device__ __forceinline__ void fence_proxy_async_global() {
-    asm volatile("fence.proxy.async.global;" ::: "memory");
-}
 
 // Record `rec` (chunk * H + head) of a fused launch: wait (one thread,
 // bounded in wall time) until the prep has published it, then order the

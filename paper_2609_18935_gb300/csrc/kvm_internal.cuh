@@ -418,7 +418,6 @@ void launch_draft_verify(const DraftVerifyParams& p, bool bf16, int num_sms, cud
 struct DraftCommitParams {
     int32_t n_chars, n_attn, Hkv, D;
     int32_t n_gdn, H, dk, dv, channels;       // channels: of the convolution, 0 without
-    int32_t nodes;                            // sum n
     int32_t rec_nodes;                        // nodes a layer's records have room for
     int64_t slab_rows;
     __nv_bfloat16* K;                         // [n_attn][Hkv][slab_rows][D]
