@@ -2025,6 +2025,9 @@ kvm_status draft_commit(kvm_ctx* c, const int32_t* path_cu, const int32_t* path,
     if (total > 0)
         for (int l = 0; l < c->n_layers; ++l)
             if (!c->draft_done[l]) return fail(KVM_E_INVAL, "layer %d has not run on this draft", l);
+    // room for the new positions' mirror before anything is enqueued: what throws leaves all as it was
+    for (int b = 0; b < c->B; ++b)
+        if (c->hpos[b].capacity() < c->hpos[b].size() + (path_cu[b + 1] - path_cu[b])) c->hpos[b].reserve(c->cap[b]);
     if (total > 0) {
         thread_local static DraftCommitParams p;
         std::memset(&p, 0, offsetof(DraftCommitParams, path));
