@@ -50,7 +50,7 @@ enum {
     KVM_OK = 0,
     KVM_E_INVAL = 1,        /* NULL or inconsistent argument, bad layer index */
     KVM_E_SPAN = 2,         /* deletion span unsorted, overlapping, empty or outside the live cache */
-    KVM_E_CAPACITY = 3,     /* L' + M exceeds a character's capacity, or sum M exceeds max_tail_tokens; host memory */
+    KVM_E_CAPACITY = 3,     /* L' + M exceeds a character's capacity, or sum M exceeds max_tail_tokens; on the draft calls host memory too */
     KVM_E_CUDA = 4,         /* CUDA runtime / launch failure (text in kvm_last_error) */
     KVM_E_DEVICE = 5,       /* a kernel reported a bounds violation or an expired wait */
     KVM_E_UNSUPPORTED = 6   /* shape outside what the kernels implement */
@@ -396,12 +396,16 @@ kvm_status kvm_update_round(kvm_ctx* ctx, const kvm_round* round, void* stream);
  * lengths, ends an open one; the draft calls then fail with KVM_E_INVAL.
  * Tensors of nodes are packed like tails, [sum n][heads][dim] with character
  * b's nodes at rows node_cu[b] .. node_cu[b+1]-1, and must be finite: what is
- * not reaches no output but those of its node and the node's descendants (where
- * keys, values and gates count as 0 or give NaN), and kvm_check reports such a
- * key, value or gate (KVM_E_DEVICE).  Every device pointer is checked for its
- * 16-byte alignment, and outputs may not overlap inputs.  The context's device must be current.  All calls enqueue on
- * `stream` and may be captured into a graph; the host's lengths and cursors move
- * when kvm_draft_commit is called, not when such a graph is launched. */
+ * not reaches no output but those of its node and the node's descendants, and
+ * kvm_check reports such a key, value or gate (KVM_E_DEVICE).  Such keys and
+ * values count as 0, in a commit too; a decay that is not finite gives NaN, in
+ * the state too once its node is committed, and what is not finite among a
+ * convolution's raw inputs is carried on by a commit like any other input.
+ * Every device pointer is checked for its 16-byte alignment, and outputs may
+ * not overlap inputs.  The context's device must be current.  All calls enqueue
+ * on `stream` and may be captured into a graph, which keeps the trees, lengths
+ * and slots of its capture; the host's lengths and cursors move when
+ * kvm_draft_commit is called, not when such a graph is launched. */
 
 /* Room for trees of max_nodes nodes (all characters together) in this context:
  * per delta-rule layer, node and head d_v fp32 and d_k bf16 values (with the
@@ -454,7 +458,8 @@ kvm_status kvm_draft_gdn(kvm_ctx* ctx, int32_t layer, const void* q, const void*
  * Outputs, device int32: path [sum n], character b's accepted nodes (node 0
  * first) from node_cu[b] on, then -1; count [n_chars] of them; next [n_chars],
  * -1 where the row holds nothing or the character has no nodes.  A token
- * outside [0, vocab) is not accepted and is reported by kvm_check (KVM_E_DEVICE).
+ * outside [0, vocab) is not accepted and is reported by kvm_check
+ * (KVM_E_DEVICE); node 0's token is not read.
  * Errors: KVM_E_INVAL (several roots), KVM_E_UNSUPPORTED (vocab > 2^24). */
 enum { KVM_PROB_F32 = 0, KVM_PROB_BF16 = 1 };
 kvm_status kvm_draft_verify(kvm_ctx* ctx, int32_t vocab, int32_t prob_type, const int32_t* tokens,

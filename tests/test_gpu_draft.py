@@ -1192,6 +1192,54 @@ def test_two_contexts_on_two_streams():
         p.ctx.check()
 
 
+@pytest.mark.parametrize("nodes", [(12, 5), (64, 40)])
+def test_inputs_written_just_before_the_calls_that_read_them(nodes):
+    """Steps enqueued one after another without a wait of the host, their trees and the same buffers' contents alternating (the
+    copies right before each layer's call, which starts while they may still run): every output is that of the step alone, bit for
+    bit.  Trees of one query tile and of several."""
+    import torch
+    pair = _stack(True, 2, [300, 77], 191)
+    trees = [[tree("tree", nodes[0], i), tree("comb", nodes[1], i)] for i in range(2)]
+    trees[1][0] = tree("star", nodes[0])
+    xs = [_step_inputs(pair, sum(nodes), 192 + i) for i in range(2)]
+    dev = [{l: {m: _bf(z) if z.dtype == np.uint16 else torch.from_numpy(z).cuda() for m, z in y.items()} for l, y in x.items()} for x in xs]
+    V, r = 2000, np.random.default_rng(194)
+    rows = [[z.cuda() for z in _rows(r, sum(nodes), V, torch.float32, near=0.4)] for _ in range(2)]
+    n = sum(nodes)
+    tok = [torch.as_tensor(r.integers(0, V, n), dtype=torch.int32).cuda() for _ in range(2)]
+    u, un = torch.as_tensor(0.4 * r.random(n), dtype=torch.float32).cuda(), torch.as_tensor(r.random(2), dtype=torch.float32).cuda()
+    buf = {l: {m: torch.empty_like(z) for m, z in y.items()} for l, y in dev[0].items()}
+    target, draft = (torch.empty_like(z) for z in rows[0])
+
+    def step(i):
+        outs = []
+        pair.ctx.draft_begin(cu_of(trees[i]), packed(trees[i]))
+        for l, t in buf.items():
+            for m, z in t.items():
+                z.copy_(dev[i][l][m])
+            if pair.shape.layer_kind[l] == W.ATTN:
+                outs.append(torch.empty_like(t["q"]))
+                pair.ctx.draft_attn(l, t["q"], t["k"], t["v"], outs[-1])
+            else:
+                outs.append(torch.empty_like(t["v"]))
+                pair.ctx.draft_gdn(l, t["q"], t["k"], t["v"], t["alpha"], t["beta"], outs[-1])
+        target.copy_(rows[i][0])
+        draft.copy_(rows[i][1])
+        path, count, nxt = (torch.empty(m, dtype=torch.int32, device="cuda") for m in (n, 2, 2))
+        pair.ctx.draft_verify(tok[i], target, draft, u, un, path, count, nxt)
+        return outs + [path, count, nxt]
+
+    alone = []
+    for i in range(2):
+        alone.append(step(i))
+        torch.cuda.synchronize()
+    got = [step(k % 2) for k in range(60)]
+    pair.ctx.check()
+    for k, outs in enumerate(got):
+        for a, b in zip(outs, alone[k % 2]):
+            assert torch.equal(a, b), k
+
+
 DEBUG = r"""
 import sys
 sys.path[:0] = [{root!r}, {tests!r}]
