@@ -38,10 +38,11 @@
 // R_ij = G_i / G_j while no G is small, else products down the path (a decay of 0
 // is one).
 //
-// 32 characters of up to 64 nodes, 16 heads of 128 x 128, convolved: 29.0 us, 47 MB
-// (1.6 TB/s).  Neither memory nor the tensor pipe bounds it (15 % and 11 % of their
+// 32 characters of up to 64 nodes, 16 heads of 128 x 128, convolved: 30.7 us, 47 MB
+// (1.5 TB/s).  Neither memory nor the tensor pipe bounds it (14 % and 11 % of their
 // peaks): a block is a chain of short phases between barriers, each run once, and its
-// warps wait for instructions and for one another.  One character: 6.1 us, the chain.
+// warps wait for instructions and for one another.  One character, the chain alone: 6.1
+// us of 16 nodes and 10.0 of 64, convolved 9.0 and 16.9.
 #include <type_traits>
 
 #include "draft_rows.cuh"

@@ -402,8 +402,8 @@ constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 // A draft has few query tiles with long key lists: what a segment costs beside its
 // units (its parts' stores and their merge) weighs more, and where the cache bounds
 // the time even cuts matter less.  32 characters of up to 16K live entries and 24
-// nodes, us a layer with 8 | 12 | 24 | 40: 113 | 107 | 106 | 102 (8K, 64 nodes: 102 | 100 | 98
-// | 100).  Three units at least: one character's 4 nodes over 8K 14.0 with four, 13.7
+// nodes, us a layer with 8 | 12 | 24 | 32 | 40: 112 | 108 | 106 | 105 | 103 (8K, 64 nodes: 101.5
+// | 101.5 | 98.9 | 97.9 | 100.6; one character the same with all).  Three units at least: one character's 4 nodes over 8K 14.0 with four, 13.7
 // with three, 14.4 with two.
 constexpr PlanCost kDraftCost{3, 32.0};
 
