@@ -146,6 +146,22 @@ kvm_status kvm_set_conv_weights(kvm_ctx* ctx, int32_t layer, const float* w, voi
 kvm_status kvm_get_conv_state(kvm_ctx* ctx, int32_t layer, void* state_out, void* stream);
 kvm_status kvm_set_conv_state(kvm_ctx* ctx, int32_t layer, const void* state, void* stream);
 
+/* A sliding window for attention layer `layer` (model index), for every call from
+ * here on: a token at live index x attends to the live entries j <= x with
+ * j > x - window (its `window` newest, itself among them) or j < n_sink (the
+ * first n_sink live entries, the sinks).  Indices count live entries, whatever
+ * their position ids: what a removal leaves behind moves closer.  window 0: the
+ * whole cache, as every layer begins (n_sink is 0 then).  The tail attention
+ * (kvm_tail_attn_prefill, rounds, one-token rounds), drafts and the probe follow
+ * it.  The cache keeps every entry until a round removes it.  Keys and values
+ * must be finite, those out of sight too: one that is not may reach the rows
+ * that attend to any of the 64 entries around it.
+ * In a draft a node of depth e counts as live index L + e and sees all its
+ * ancestors; kvm_draft_begin takes windows of 64 entries or more
+ * (KVM_E_UNSUPPORTED).  Ends an open draft.  kvm_fork copies windows along.
+ * Errors: KVM_E_INVAL (negative, sinks without a window, wrong layer). */
+kvm_status kvm_set_window(kvm_ctx* ctx, int32_t layer, int32_t window, int32_t n_sink);
+
 /* Host view of character b's live length and cursor (no synchronization). */
 kvm_status kvm_get_live(kvm_ctx* ctx, int32_t b, int32_t* live, int64_t* cursor);
 
@@ -218,6 +234,16 @@ kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* live, const
                                      int32_t* block_tile, int32_t* block_key, int32_t* n_split,
                                      int32_t* split_first_block);
 
+/* kvm_plan_attention_launch for a layer with a window (kvm_set_window): a query
+ * tile whose first token is at live index x attends to fewer 64-key tiles.  Its
+ * units are, in this order, the key tiles below min(ceil(n_sink / 64), f) with
+ * f = floor(max(0, x + 1 - window) / 64), and those from f on. */
+kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
+                                     int32_t n_q_heads, int32_t n_kv_heads, int32_t window, int32_t n_sink,
+                                     int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks, int32_t* n_tiles,
+                                     int32_t* block_tile, int32_t* block_key, int32_t* n_split,
+                                     int32_t* split_first_block);
+
 /* Partition of a character population over ranks (one GPU per rank):
  * characters are independent, so each rank maintains its own share with no
  * exchange on the data path.  cost host [n_chars] >= 0, e.g. a round's
@@ -264,7 +290,8 @@ kvm_status kvm_kv_compact(kvm_ctx* ctx, const int32_t* span_cu,
  * append rotated keys and values at live slots L'_b + i (L'_b = the current
  * live length, i.e. after kv_compact) and write positions p_b + i, then
  * o_i = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j over every surviving entry
- * and the tail's keys j <= i.
+ * and the tail's keys j <= i (in a windowed layer over those in sight, see
+ * kvm_set_window).
  * tail_cu host [n_chars+1]; q device [sum M][n_q_heads][D] bf16;
  * k_new, v_new device [sum M][n_kv_heads][D] bf16; out device
  * [sum M][n_q_heads][D] bf16.  Does not move live lengths or cursors (see
@@ -420,15 +447,16 @@ kvm_status kvm_draft_reserve(kvm_ctx* ctx, int32_t max_nodes);
 /* Announce a step's trees: node_cu host [n_chars+1], parent host [sum n]
  * (indices within the character's nodes, -1: a root).  A character without
  * nodes takes no part.  Errors: KVM_E_INVAL (offsets, a parent that is no
- * smaller index), KVM_E_UNSUPPORTED (a tree of more than 64 nodes),
+ * smaller index), KVM_E_UNSUPPORTED (a tree of more than 64 nodes, a layer with a
+ * window below 64),
  * KVM_E_CAPACITY (more nodes than reserved, live + n beyond a character's
  * capacity, position ids past int32). */
 kvm_status kvm_draft_begin(kvm_ctx* ctx, const int32_t* node_cu, const int32_t* parent, void* stream);
 
 /* One attention layer over the draft: rotate node i's query and key at
  * position p_b + depth(i), put keys and values behind the live entries, then
- * o_i = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j over every live entry, node
- * i's ancestors and itself.  Tensors as kvm_tail_attn_prefill's, of which a
+ * o_i = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j over every live entry (in a
+ * windowed layer those in sight), node i's ancestors and itself.  Tensors as kvm_tail_attn_prefill's, of which a
  * draft that is one chain is the equal.  Errors: KVM_E_INVAL. */
 kvm_status kvm_draft_attn(kvm_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
                           void* out, void* stream);
@@ -527,7 +555,8 @@ kvm_status kvm_kv_compact_noalloc_check(void* stream);
  * 0 .. L - n_q + i (causal in processing order).  Removed records leave no
  * entries, so the denominator runs over live tokens only (holes excluded).
  * probs_out: device fp32 [L] (L = live length), the probability of each live
- * entry averaged over the n_q queries and all query heads (sums to 1).
+ * entry averaged over the n_q queries and all query heads (sums to 1; 0 for
+ * entries that no query's window shows).
  * group_of: optional device int32 [L], a group id in [0, n_groups) per live
  * entry (-1: in no group), e.g. the memory record it belongs to;
  * group_mass_out: device fp32 [n_groups], the summed probability per group.

@@ -133,16 +133,17 @@ __global__ void __launch_bounds__(kScoreThreads) probe_scores_kernel(const __gri
                 for (int b = 0; b < 4; ++b) acc[a][b] = fma2(qq[a], kk[b], acc[a][b]);
         }
     }
-    // rows past the end, keys past the row's causal limit: -inf
+    // rows past the end, keys past the row's causal limit or out of its window: -inf
     const int j = j0 + 4 * tx, first_q = p.L - p.n_q;
 #pragma unroll
     for (int a = 0; a < 8; ++a) {
         const int r = 8 * ty + a, rg = r0 + r, lim = rg < rows_kv ? first_q + rg / p.g : -1;
+        const int low = p.window ? lim + 1 - p.window : 0;       // older keys are out of a window's sight
         float s[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const float2 x = unpack2(acc[a >> 1][b]);
-            s[b] = j + b <= lim ? (a & 1 ? x.y : x.x) * p.scale : -INFINITY;
+            s[b] = j + b <= lim && (j + b >= low || j + b < p.n_sink) ? (a & 1 ? x.y : x.x) * p.scale : -INFINITY;
         }
         if (j < p.pitch)
             *reinterpret_cast<float4*>(p.scores + ((int64_t)blockIdx.y * kProbeRows + r) * p.pitch + j) =

@@ -98,6 +98,7 @@ struct kvm_ctx {
     int n_attn = 0, n_gdn = 0;
     int Hq = 0, Hkv = 0, D = 0, R = 0, g = 0;
     double theta = 0;
+    std::vector<int> window, n_sink;      // per layer (kvm_set_window); window 0: the whole cache
     int H = 0, dk = 0, dv = 0;
     int conv = 0;                         // short-convolution width of the delta-rule layers (0 or 4)
     int conv_ch = 0;                      // its channels, H (2 d_k + d_v)
@@ -181,14 +182,15 @@ struct kvm_ctx {
     std::vector<DevAlloc> allocs;
     // drafts (kvm_draft_*): room for draft_cap nodes; the open draft's tree on the
     // host (packed parents) and as ancestor words and positions on the device; the
-    // attention's partition for it, one for all layers; which layers have run; and per
+    // attention's partitions for it, one for all layers of a window; which layers have run; and per
     // delta-rule layer what a commit needs of each node
     int draft_cap = 0;
     bool draft_open = false;
     std::vector<int32_t> draft_cu, draft_parent;
     std::vector<char> draft_done;
     std::vector<int16_t> draft_order;     // characters by decreasing number of nodes
-    AttnPlan draft_plan;
+    std::vector<AttnPlan> draft_plans;    // one for each window that the attention layers have
+    std::vector<int> draft_plan_of;       // per layer: which of them
     uint64_t* draft_anc = nullptr;
     int32_t* draft_pos = nullptr;
     int32_t* draft_slot = nullptr;
@@ -255,6 +257,22 @@ void free_all(kvm_ctx* c) {
     if (c->compact_stream) cudaStreamDestroy(c->compact_stream);
     for (cudaEvent_t e : c->ev) cudaEventDestroy(e);
     c->ev.clear();
+}
+
+// No exception of the host's allocator leaves a C entry point.
+template <typename F>
+kvm_status guarded(F&& f) noexcept {
+    try {
+        return f();
+    } catch (const std::exception&) {
+        g_err = "host memory";                       // short enough to be held in place
+        return KVM_E_CAPACITY;
+    }
+}
+kvm_status check_window(int window, int n_sink) {
+    if (window < 0 || n_sink < 0) return fail(KVM_E_INVAL, "window %d and n_sink %d must not be negative", window, n_sink);
+    if (window == 0 && n_sink > 0) return fail(KVM_E_INVAL, "sinks belong to a window: n_sink %d, window 0 (the whole cache)", n_sink);
+    return KVM_OK;
 }
 
 kvm_status check_tail_cu(const kvm_ctx* c, const int32_t* tail_cu, int* total) {
@@ -407,8 +425,15 @@ constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 // with three, 14.4 with two.
 constexpr PlanCost kDraftCost{3, 32.0};
 
+// What a layer's rows see: of a windowed layer (kvm_set_window) fewer key tiles, the
+// same for all query tiles of a draft, whose first rows all follow the last live entry.
+struct Sight {
+    int window = 0, n_sink = 0;
+    bool draft = false;
+};
+
 void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, int grid_cap, bool deal, const PlanCost& cost_of,
-                    AttnPlan& pl) {
+                    const Sight& sight, AttnPlan& pl) {
     pl.n_qtiles.assign(B, 0);
     pl.tile_off.assign(B, 0);
     std::vector<int> nk_of;
@@ -423,7 +448,8 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
     for (int b = 0; b < B; ++b)
         for (int h = 0; h < Hkv; ++h)
             for (int qt = 0; qt < pl.n_qtiles[b]; ++qt) {
-                nk_of.push_back((L_prev[b] + std::min(M[b], (qt + 1) * tpt) + 63) / 64);
+                const int gap = sight.window ? window_tiles(L_prev[b] + (sight.draft ? 0 : qt * tpt), sight.window, sight.n_sink).gap : 0;
+                nk_of.push_back((L_prev[b] + std::min(M[b], (qt + 1) * tpt) + 63) / 64 - gap);
                 units += nk_of.back();
             }
     pl.n_tiles = tiles;
@@ -548,6 +574,8 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
         delete c;
         return fail(KVM_E_UNSUPPORTED, "conv_kernel must be 0 or 4");
     }
+    c->window.assign(c->n_layers, 0);
+    c->n_sink.assign(c->n_layers, 0);
     c->B = n_chars;
     c->max_tail = max_tail_tokens;
     for (int b = 0; b < n_chars; ++b) {
@@ -919,7 +947,7 @@ namespace {
 kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_t* tail_cu, int32_t n_q_heads,
                               int32_t n_kv_heads, int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks,
                               int32_t* n_tiles, int32_t* block_tile, int32_t* block_key, int32_t* n_split,
-                              int32_t* split_first_block) {
+                              int32_t* split_first_block, const Sight& sight = {}) {
     if (n_chars <= 0 || n_chars > kMaxChars) return fail(KVM_E_INVAL, "n_chars must be in [1,%d]", kMaxChars);
     if (!live || !tail_cu || !n_blocks || !n_tiles || !block_tile || !block_key || !n_split || !split_first_block)
         return fail(KVM_E_INVAL, "NULL argument");
@@ -937,7 +965,7 @@ kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_
         if (L[b] < 0) return fail(KVM_E_INVAL, "negative live length at character %d", b);
     }
     AttnPlan pl;
-    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, kTailCost, pl);
+    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, kTailCost, sight, pl);
     if (n_waves) *n_waves = pl.waves;
     *n_blocks = pl.n_ctas;
     *n_tiles = pl.n_tiles;
@@ -965,6 +993,20 @@ extern "C" kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* 
     if (!n_waves) return fail(KVM_E_INVAL, "NULL argument");
     return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
                               block_tile, block_key, n_split, split_first_block);
+}
+
+extern "C" kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
+                                                int32_t n_q_heads, int32_t n_kv_heads, int32_t window, int32_t n_sink,
+                                                int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks, int32_t* n_tiles,
+                                                int32_t* block_tile, int32_t* block_key, int32_t* n_split,
+                                                int32_t* split_first_block) {
+    return guarded([&]() -> kvm_status {
+        if (!n_waves) return fail(KVM_E_INVAL, "NULL argument");
+        const kvm_status st = check_window(window, n_sink);
+        if (st) return st;
+        return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
+                                  block_tile, block_key, n_split, split_first_block, {window, n_sink});
+    });
 }
 
 extern "C" kvm_status kvm_plan_partition(int32_t n_chars, const int64_t* cost, int32_t n_ranks, int32_t* rank_of,
@@ -1194,6 +1236,8 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     p.out = static_cast<__nv_bfloat16*>(out);
     p.tail_pos = tail_pos_dev;
     p.anc = anc;
+    p.window = c->window[layer];
+    p.n_sink = c->n_sink[layer];
     // a draft's q is rotated in the attention where a rotary pair's elements lie whole
     // 32-byte steps apart; else as a tail's, before it
     p.turn = anc && c->R % 32 == 0 ? c->draft_turn : nullptr;
@@ -1296,7 +1340,8 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
     AttnPlan pl;
-    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, kTailCost, pl);
+    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, kTailCost,
+                   {c->window[layer], c->n_sink[layer]}, pl);
     drop_draft(c);
     return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
 }
@@ -1641,6 +1686,8 @@ extern "C" kvm_status kvm_attn_probe(kvm_ctx* c, int32_t layer, int32_t b, int32
     p.n_q = n_q;
     p.Hq = c->Hq; p.Hkv = c->Hkv; p.D = c->D; p.R = c->R; p.g = c->g;
     p.n_groups = group_of ? n_groups : 0;
+    p.window = c->window[layer];
+    p.n_sink = c->n_sink[layer];
     p.scale = (float)(1.0 / std::sqrt((double)c->D));
     p.slab_rows = c->T_cap;
     p.slot0 = c->cap_off[b];
@@ -1853,6 +1900,10 @@ kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent
             return fail(KVM_E_CAPACITY, "character %d: live %d + %d nodes exceed capacity %d", b, c->live[b], n, c->cap[b]);
         if (c->cursor[b] + n > INT32_MAX) return fail(KVM_E_CAPACITY, "character %d: position ids overflow", b);
     }
+    // a node's ancestors are in sight by its ancestor word alone
+    for (int l = 0; l < c->n_layers && total > 0; ++l)
+        if (c->window[l] && c->window[l] < kDraftNodes)
+            return fail(KVM_E_UNSUPPORTED, "layer %d has a window of %d: drafts take windows of %d entries and more", l, c->window[l], kDraftNodes);
     int dev = -1;
     CUDA_TRY(cudaGetDevice(&dev));
     if (dev != c->device) return fail(KVM_E_INVAL, "the context lives on device %d, device %d is current", c->device, dev);
@@ -1868,8 +1919,22 @@ kvm_status draft_begin(kvm_ctx* c, const int32_t* node_cu, const int32_t* parent
         if (c->n_attn > 0) {
             std::vector<int> M(c->B);
             for (int b = 0; b < c->B; ++b) M[b] = node_cu[b + 1] - node_cu[b];
-            plan_attention(c->B, c->live.data(), M.data(), c->Hkv, kAttnRows / c->g,
-                           attention_grid_cap(c->num_sms, c->D), true, kDraftCost, c->draft_plan);
+            // a partition for each window that a layer has
+            c->draft_plan_of.assign(c->n_layers, -1);
+            int plans = 0;
+            for (int l = 0; l < c->n_layers; ++l) {
+                if (c->kind[l] != KVM_LAYER_ATTN) continue;
+                int same = 0;
+                while (same < l && (c->kind[same] != KVM_LAYER_ATTN || c->window[same] != c->window[l] || c->n_sink[same] != c->n_sink[l])) ++same;
+                if (same < l) {
+                    c->draft_plan_of[l] = c->draft_plan_of[same];
+                    continue;
+                }
+                if ((int)c->draft_plans.size() == plans) c->draft_plans.emplace_back();
+                plan_attention(c->B, c->live.data(), M.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true,
+                               kDraftCost, {c->window[l], c->n_sink[l], true}, c->draft_plans[plans]);
+                c->draft_plan_of[l] = plans++;
+            }
         }
         thread_local static DraftTreeParams p;
         p.n_chars = c->B;
@@ -1905,7 +1970,7 @@ kvm_status draft_attn(kvm_ctx* c, int layer, const void* q, const void* k_new, c
         const size_t nq = (size_t)total * c->Hq * c->D * 2, nk = (size_t)total * c->Hkv * c->D * 2;
         if (overlap(out, nq, q, nq) || overlap(out, nq, k_new, nk) || overlap(out, nq, v_new, nk))
             return fail(KVM_E_INVAL, "out overlaps an input");
-        st = launch_attention(c, layer, c->draft_cu.data(), total, c->draft_plan, q, k_new, v_new, out, s, c->draft_pos,
+        st = launch_attention(c, layer, c->draft_cu.data(), total, c->draft_plans[c->draft_plan_of[layer]], q, k_new, v_new, out, s, c->draft_pos,
                               c->draft_anc);
         if (st) return st;
     }
@@ -2064,16 +2129,6 @@ kvm_status draft_commit(kvm_ctx* c, const int32_t* path_cu, const int32_t* path,
     return KVM_OK;
 }
 
-// No exception of the host's allocator leaves a C entry point.
-template <typename F>
-kvm_status guarded(F&& f) noexcept {
-    try {
-        return f();
-    } catch (const std::exception&) {
-        g_err = "host memory";                       // short enough to be held in place
-        return KVM_E_CAPACITY;
-    }
-}
 }  // namespace
 
 extern "C" kvm_status kvm_plan_draft(int32_t n_chars, const int32_t* node_cu, const int32_t* parent, int32_t* depth,
@@ -2433,6 +2488,18 @@ extern "C" kvm_status kvm_set_plan(kvm_ctx* c, int32_t what, int32_t enable) {
     return KVM_OK;
 }
 
+extern "C" kvm_status kvm_set_window(kvm_ctx* c, int32_t layer, int32_t window, int32_t n_sink) {
+    if (!c) return fail(KVM_E_INVAL, "NULL context");
+    kvm_status st = check_layer(c, layer, KVM_LAYER_ATTN);
+    if (st) return st;
+    st = check_window(window, n_sink);
+    if (st) return st;
+    drop_draft(c);
+    c->window[layer] = window;
+    c->n_sink[layer] = n_sink;
+    return KVM_OK;
+}
+
 extern "C" kvm_status kvm_debug_compact_wait(kvm_ctx* c, int32_t polls, int32_t stall) {
     if (!c) return fail(KVM_E_INVAL, "NULL context");
     if (polls < 0) return fail(KVM_E_INVAL, "polls must be >= 0");
@@ -2465,6 +2532,8 @@ extern "C" kvm_status kvm_fork(kvm_ctx* dst, const kvm_ctx* src, void* stream) {
         dst->conv_par = src->conv_par;
     }
     drop_draft(dst);
+    dst->window = src->window;
+    dst->n_sink = src->n_sink;
     dst->live = src->live;
     dst->cursor = src->cursor;
     dst->hpos = src->hpos;

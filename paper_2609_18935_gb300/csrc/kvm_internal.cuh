@@ -135,6 +135,17 @@ struct AttnChar {
 // [start_c, start_{c+1}), given as (query tile, key tile).
 constexpr int kMaxAttnCtas = 320;
 
+// The key tiles of a query tile whose first row is at live index x0, under a window:
+// `sink` tiles from the first on, then, `gap` tiles further, all up to its last key.
+// A row at x sees keys j <= x with j > x - window or j < n_sink.
+struct WindowTiles { int sink, gap; };
+__host__ __device__ inline WindowTiles window_tiles(int x0, int window, int n_sink) {
+    const int oldest = x0 + 1 - window, first = oldest > 0 ? oldest / 64 : 0;
+    const int sinks = n_sink / 64 + (n_sink % 64 > 0);
+    const int sink = sinks < first ? sinks : first;
+    return {sink, first - sink};
+}
+
 struct AttnParams {
     // TMA maps: every layer's K / V slabs as rows of D (box 64 x 64), 128-byte swizzle
     CUtensorMap tmap_k;
@@ -163,6 +174,8 @@ struct AttnParams {
     int32_t* diag;                // first expired wait: block + 1, tag, parity
     const uint64_t* anc;          // device [sum M]: a draft's ancestor bits (DraftTreeParams), or null: a causal tail
     const float2* turn;           // of a draft: (cos, sin) [sum M][R / 2], with which the attention rotates q itself; or null
+    int32_t window, n_sink;       // a row sees its `window` newest keys and the first n_sink; window 0: all
+    int32_t widened;              // the kernel before wrote all keys and values, not the tail's alone
     int32_t append;               // of a draft: the attention puts the nodes' keys and values into the caches itself
     double inv_freq[kMaxRotaryHalf];
     int32_t cta_tile[kMaxAttnCtas + 1];
@@ -206,6 +219,7 @@ struct RerotateParams {
 };
 void launch_rerotate(const RerotateParams& p, cudaStream_t s);
 void launch_tail_attention(const AttnParams& p, cudaStream_t s);
+void launch_window_attention(const AttnParams& p, cudaStream_t s);      // of which p.window > 0 is this
 void launch_attn_combine(const CombineParams& p, cudaStream_t s);
 int attention_ctas_per_sm(int head_dim);
 constexpr int kAttnRows = 128;   // query rows per attention tile
@@ -222,6 +236,7 @@ struct ProbeParams {
     int32_t n_q;          // probe queries: the last n_q live entries
     int32_t Hq, Hkv, D, R, g;
     int32_t n_groups;
+    int32_t window, n_sink;   // of the layer (window 0: none)
     float scale;          // 1 / sqrt(D)
     int64_t slab_rows;
     int64_t slot0;        // the character's first slot

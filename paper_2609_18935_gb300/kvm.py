@@ -108,6 +108,11 @@ _SIGS = {
                                             C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                             C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                             C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
+    "kvm_plan_attention_window": (C.c_int, [C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_int32,
+                                            C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                            C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                            C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
+    "kvm_set_window": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]),
     "kvm_plan_partition": (C.c_int, [C.c_int32, C.POINTER(C.c_int64), C.c_int32, C.POINTER(C.c_int32),
                                      C.POINTER(C.c_int64)]),
     "kvm_kv_compact_noalloc": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32,
@@ -315,15 +320,24 @@ def plan_attention_launch(live, tail_cu, n_q_heads, n_kv_heads, max_blocks):
     return _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, True)
 
 
-def _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, launch):
+def plan_attention_window(live, tail_cu, n_q_heads, n_kv_heads, window, n_sink, max_blocks):
+    """kvm_plan_attention_window: plan_attention_launch for a layer with a window and sinks."""
+    return _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, True, (int(window), int(n_sink)))
+
+
+def _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, launch, window=None):
     load_library()
     L, cu = _i32(live), _i32(tail_cu)
     tile, key = np.zeros(max_blocks + 1, np.int32), np.zeros(max_blocks + 1, np.int32)
     split = np.zeros(max_blocks, np.int32)
     nw, nb, nt, ns = C.c_int32(), C.c_int32(), C.c_int32(), C.c_int32()
-    head = (len(L), _p32(L), _p32(cu), int(n_q_heads), int(n_kv_heads), int(max_blocks))
+    head = (len(L), _p32(L), _p32(cu), int(n_q_heads), int(n_kv_heads))
+    call = _lib.kvm_plan_attention_launch if launch else _lib.kvm_plan_attention
+    if window is not None:
+        call, head = _lib.kvm_plan_attention_window, (*head, *window)
+    head = (*head, int(max_blocks), *((C.byref(nw),) if launch else ()))
     rest = (C.byref(nb), C.byref(nt), _p32(tile), _p32(key), C.byref(ns), _p32(split))
-    _check(_lib.kvm_plan_attention_launch(*head, C.byref(nw), *rest) if launch else _lib.kvm_plan_attention(*head, *rest))
+    _check(call(*head, *rest))
     n = nb.value
     plan = {"n_blocks": n, "n_tiles": nt.value, "block_tile": tile[:n + 1].copy(), "block_key": key[:n + 1].copy(),
             "split_first_block": split[:ns.value].copy()}
@@ -485,6 +499,10 @@ class Context:
     def set_conv_state(self, layer, state, stream=None):
         import torch
         _check(_lib.kvm_set_conv_state(self._h, layer, _dptr(state, torch.bfloat16), _stream(stream)))
+
+    def set_window(self, layer, window, n_sink=0):
+        """kvm_set_window: attention layer `layer` attends to the `window` newest entries and the first n_sink; 0: to all."""
+        _check(_lib.kvm_set_window(self._h, int(layer), int(window), int(n_sink)))
 
     def get_live(self, b):
         live, cur = C.c_int32(), C.c_int64()
