@@ -4,7 +4,7 @@
  * The library keeps, for a population of characters, the inference state
  * (A_t, R_t, p_t) of a hybrid gated-delta-rule / GQA-attention model (§4.1):
  *   A_t  live attention KV per attention layer (rotated keys and values,
- *        bf16, plus one int32 position id per live entry, shared by all
+ *        bf16 (or 8 bits, kvm_create_kv8), plus one int32 position id per live entry, shared by all
  *        attention layers of a character),
  *   R_t  the recurrent state S [H][d_v][d_k] (fp32) of every delta-rule layer,
  *   p_t  the next position id (cursor), which only moves forward (§4.2).
@@ -102,6 +102,30 @@ typedef struct kvm_model_desc {
 kvm_status kvm_create(const kvm_model_desc* model, int32_t n_chars,
                       const int32_t* capacity, int32_t max_tail_tokens,
                       kvm_ctx** out);
+
+/* kvm_create with the attention caches in 8 bits: half the memory and half of what
+ * a decode step reads.  Keys and values are e4m3 numbers times a power of two for
+ * each block of 64 live slots of a KV head, K and V apart: 2^e with e the smallest
+ * integer, -117 <= e <= 119, for which the block's largest magnitude is at most
+ * 448 * 2^e; each number is rounded to the nearest, ties to even (to 2^-4 of its value
+ * from 2^-6 of the scale on, to 2^-10 of the scale below).  A power of two, so that what
+ * moves into another block keeps its value, but for the part that falls below 2^-6 of a
+ * larger scale there.  All the other entry points take such a context as any other, with
+ * these differences:
+ *  - kvm_set_kv and tails round what they store (a tail's keys once, after their
+ *    rotation), the attention and the probe read what the cache then holds, kvm_get_kv
+ *    returns it in bf16, exactly.  A tail's first entries share a block with older ones,
+ *    which take over its scale, whether the tail becomes live or not.  A removal forms the
+ *    blocks from its first entry's on anew;
+ *  - numbers that are not finite are stored as 0 and reported by kvm_check
+ *    (in a tail's key before its rotation);
+ *  - drafts and kvm_rerotate_keys return KVM_E_UNSUPPORTED; kvm_fork takes two contexts
+ *    of this kind; the context's device must be current (KVM_E_INVAL).
+ * One layer's caches in bf16 are part of the workspace: tails of more than 16 rows
+ * (tokens times group size) of a character and removals go by way of them. */
+kvm_status kvm_create_kv8(const kvm_model_desc* model, int32_t n_chars,
+                          const int32_t* capacity, int32_t max_tail_tokens,
+                          kvm_ctx** out);
 
 /* Free everything the context owns.  Synchronizes the device first. */
 kvm_status kvm_destroy(kvm_ctx* ctx);

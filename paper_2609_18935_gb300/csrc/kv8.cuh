@@ -1,0 +1,51 @@
+// Numbers of a cache in 8 bits.
+//
+// A block is 64 slots of one KV head, of K or of V.  Its numbers are e4m3 times 2^e, e
+// the smallest integer (and at least -117, so that 2^(e-9) is a normal float) with
+// max |x| <= 448 * 2^e (and at most 119: what is beyond 448 * 2^119, a bf16 number,
+// becomes that); x becomes the nearest multiple of the grid, ties to even.  The
+// scale is a power of two so that numbers of one block carry over into another (a
+// removal, a token appended to a half-filled block) as they are: with a larger scale
+// only what falls below 2^-6 of it is rounded again, by at most 2^-10 of the scale
+// where the block's largest number is over 224 of it.  A scale of max / 448 would use the
+// last bit of range better (at most a factor 2 of 2^17) and round every survivor of a
+// removal again, to 2^-4 of its value.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include <cstdint>
+
+namespace kvm {
+
+// The exponent e of a block whose largest magnitude is amax (finite).
+__device__ __forceinline__ int kv8_exponent(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    // amax = m 2^E with m in [1/2, 1): 448 = 7/8 2^9
+    const int E = (int)(b >> 23) - 126;
+    return min(max(E - 9 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -117), 119);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// Four floats as e4m3, in order from the lowest byte (to the nearest, ties to even).
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)lo | (uint32_t)hi << 16;
+}
+
+// Two e4m3 numbers in bytes 1 and 3 of x (whatever the others hold) as bf16, exactly:
+// sign, exponent and mantissa moved to their places give the number times 2^-120 (a
+// subnormal one stays one), the product undoes that.
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t x) {
+    const uint32_t y = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
+    const uint32_t k = 0x7b807b80u;                          // 2^120
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), *reinterpret_cast<const __nv_bfloat162*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// The low and the high two numbers of a word.
+__device__ __forceinline__ uint32_t e4m3_low(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x1000)); }
+__device__ __forceinline__ uint32_t e4m3_high(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x3020)); }
+
+}  // namespace kvm

@@ -1,0 +1,377 @@
+// Attention of a few query rows a KV head (a decode step: one token, a group of heads)
+// straight from a cache in 8 bits.
+//
+// S^T = K Q^T and O^T = V^T P^T with mma.sync (m16n8k16, bf16): the 16 keys of a step are
+// the rows of the first product and the depth of the second, 8 query rows its columns.
+// The work is bound by the cache's bytes: 8 rows are a sixteenth of a tcgen05 tile, whose
+// bf16 operands would have to pass through shared memory; here a warp turns its bytes
+// into bf16 in registers and feeds them to the products there.
+//
+// The partition is the tensor-core attention's: 64-key units in contiguous ranges, a
+// block an SM, partials of shared tiles for attn_combine.  A warp takes every kWarps-th
+// 16 keys of a segment through a ring of its own in shared memory (cp.async, no barrier
+// but the warp's), keeps its own softmax reference, sum and output in registers, and the
+// block's warps meet at the segment's end.
+//
+// Layout.  The sum over d takes any order, the same for K and Q: lane (g, j) = (lane / 4,
+// lane mod 4) reads 16 bytes of key g (and g + 8) at a time and each word of them is its
+// part of one product step.  For V it reads 16 bytes of its four keys 2j, 2j + 1, 2j + 8,
+// 2j + 9, whose bytes meet in pairs of keys; a product's 16 rows are then two numbers of
+// each lane g.  The rings' 16-byte pieces are turned by their row, so that each quarter
+// of a warp reads all banks.
+#include "attn_tiles.cuh"
+#include "kv8.cuh"
+#include "kvm_internal.cuh"
+#include "sm100_ptx.cuh"
+
+namespace kvm {
+namespace {
+
+using ptx::ex2;
+using ptx::smem_u32;
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStep = 16;                      // keys of a warp's step
+constexpr int BM = kAttnRows;
+
+template <int D, int NT>
+struct Cfg {
+    static constexpr int SIDE = kStep * D;                     // bytes of a step's K, or V
+    static constexpr int STAGE = 2 * SIDE + 16;                // and its two scales
+    static constexpr int STAGES = D == 256 ? 3 : 6;
+    static constexpr int RING = STAGES * STAGE;
+    static constexpr int ROWS = 8 * NT;
+    static constexpr int PITCH = D + 4;                        // floats of a merged row
+    static constexpr int MERGE = kWarps * ROWS * PITCH * 4;
+    static constexpr int SMEM = (kWarps * RING > MERGE ? kWarps * RING : MERGE) + 2 * kWarps * ROWS * 4;
+};
+static_assert(Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448, "shared memory");
+
+// Byte offset of 16-byte piece `col` of row `row` of a step's K or V.
+template <int D>
+__device__ __forceinline__ int piece(int row, int col) {
+    if (D == 64) return (row >> 1) * 128 + (((((row & 1) << 2) | col) ^ ((row & 6))) << 4);
+    return row * D + (((col & ~7) | ((col ^ row) & 7)) << 4);
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t f2_bf2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
+    using C = Cfg<D, NT>;
+    constexpr int KS = D / 16;                                 // steps of the sum over d, and 16-row pieces of O^T
+    extern __shared__ __align__(128) uint8_t smem[];
+    const AttnParams& p = pp.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+    uint8_t* ring = smem + warp * C::RING;
+    const uint32_t ring_at = smem_u32(ring);
+    float* meet = reinterpret_cast<float*>(smem);              // [warp][row][PITCH], once the rings are done
+    float* wm = reinterpret_cast<float*>(smem + C::SMEM - 2 * kWarps * C::ROWS * 4);   // [warp][row]: reference, then sum
+    float* wl = wm + kWarps * C::ROWS;
+
+    // the block's segments, as the tensor-core attention walks them
+    const int cta = blockIdx.x, waves = p.waves;
+    const int t_begin = p.cta_tile[cta], k_begin = p.cta_k[cta];
+    const int t_end = p.cta_tile[cta + 1], k_end = p.cta_k[cta + 1];
+    const int n_seg = waves + ((t_begin == t_end && k_begin == k_end) ? 0 : t_end - t_begin + (k_end > 0 ? 1 : 0));
+
+    // the blocks behind the live entries were formed by the grid before; it also wrote q_rot
+    grid_dependency_wait();
+    grid_dependents_launch();
+
+    for (int seg = 0; seg < n_seg; ++seg) {
+        const int t = seg < waves ? seg * p.n_ctas + ((seg & 1) ? p.n_ctas - 1 - cta : cta) : t_begin + (seg - waves);
+        const Tile T = p.window ? decode_tile<true, false>(p, t) : decode_tile<false, false>(p, t);
+        const AttnChar& ch = p.ch[T.b];
+        const int k0 = seg == waves ? k_begin : 0, k1 = (seg >= waves && t == t_end) ? k_end : T.nk;
+        const bool full = k0 == 0 && k1 == T.nk;
+        const int steps = (k1 - k0) * (kAttnKeys / kStep);
+        const int64_t slab = (int64_t)T.kvh * p.slab_rows + ch.cap_off;
+        const int rows = (T.tok_end - T.tok0) * p.g;           // of them real
+
+        // step s of the segment into ring place `at`
+        auto fetch = [&](int s, int at) {
+            if (s < steps) {
+                const int64_t row = slab + (int64_t)key_tile<true>(T, k0 + s / 4) * kAttnKeys + s % 4 * kStep;
+                const uint8_t* k = pp.from.K + row * D;
+                const uint8_t* v = pp.from.V + row * D;
+                const uint32_t to = ring_at + at * C::STAGE;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    const int id = c * 32 + lane, r = id / (D / 16), col = id % (D / 16);
+                    const uint32_t o = to + piece<D>(r, col);
+                    cp16(o, k + id * 16);
+                    cp16(o + C::SIDE, v + id * 16);
+                }
+                if (lane < 2) cp4(to + 2 * C::SIDE + 4 * lane, (lane ? pp.from.Vs : pp.from.Ks) + row / kKv8Rows);
+            }
+            cp_commit();
+        };
+#pragma unroll
+        for (int s = 0; s < C::STAGES - 1; ++s) fetch(warp + s * kWarps, s);
+
+        // Q: a lane's words of each step of the sum, rows g (and g + 8)
+        uint32_t q[NT][KS][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = 8 * n + g;
+            const bool real = r < rows;
+            const __nv_bfloat16* src = p.q_rot + ((int64_t)(ch.tail_off + T.tok0 + (real ? r / p.g : 0)) * p.Hq + T.kvh * p.g + (real ? r % p.g : 0)) * D;
+#pragma unroll
+            for (int c = 0; c < KS / 4; ++c) {
+                const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
+                uint4 a = make_uint4(0, 0, 0, 0), b = a;
+                if (real) {
+                    a = *reinterpret_cast<const uint4*>(src + 16 * col);
+                    b = *reinterpret_cast<const uint4*>(src + 16 * col + 8);
+                }
+                q[n][4 * c][0] = a.x; q[n][4 * c][1] = a.y;
+                q[n][4 * c + 1][0] = a.z; q[n][4 * c + 1][1] = a.w;
+                q[n][4 * c + 2][0] = b.x; q[n][4 * c + 2][1] = b.y;
+                q[n][4 * c + 3][0] = b.z; q[n][4 * c + 3][1] = b.w;
+            }
+        }
+        // rows 8 n + 2 j and the next: their live indices, references, and this lane's share of the sums
+        int at[NT][2];
+        float m[NT][2], l[NT][2], o[NT][KS][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                at[n][e] = ch.L_prev + min(T.tok0 + (8 * n + 2 * j + e) / p.g, ch.M - 1);
+                m[n][e] = -INFINITY;
+                l[n][e] = 0.f;
+            }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < KS; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][c][e] = 0.f;
+        const int first_at = ch.L_prev + T.tok0, last_at = ch.L_prev + T.tok_end - 1;
+
+        for (int s = warp, i = 0; s < steps; s += kWarps, ++i) {
+            cp_wait<C::STAGES - 2>();
+            __syncwarp();
+            const uint8_t* kt = ring + (i % C::STAGES) * C::STAGE;
+            const uint8_t* vt = kt + C::SIDE;
+            const float ks = *reinterpret_cast<const float*>(kt + 2 * C::SIDE) * p.scale_log2;
+            const float vs = *reinterpret_cast<const float*>(kt + 2 * C::SIDE + 4);
+            fetch(s + (C::STAGES - 1) * kWarps, (i + C::STAGES - 1) % C::STAGES);
+            float sc[NT][2][4];                                // two chains of products
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sc[n][e >> 2][e & 3] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KS / 4; ++c) {
+                const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
+                const uint4 x = *reinterpret_cast<const uint4*>(kt + piece<D>(g, col));
+                const uint4 y = *reinterpret_cast<const uint4*>(kt + piece<D>(g + 8, col));
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t a0 = e4m3_low(xs[w]), a1 = e4m3_low(ys[w]), a2 = e4m3_high(xs[w]), a3 = e4m3_high(ys[w]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma16816(sc[n][w & 1], a0, a1, a2, a3, q[n][4 * c + w][0], q[n][4 * c + w][1]);
+                }
+            }
+            // keys g and g + 8 of the step for rows 2 j, 2 j + 1
+            const int key0 = key_tile<true>(T, k0 + s / 4) * kAttnKeys + s % 4 * kStep;
+            bool above = false;
+            float x[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[n][e] = (sc[n][0][e] + sc[n][1][e]) * ks;
+            if (key0 + kStep - 1 > first_at || (p.window && key0 <= last_at - p.window)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + g + 8 * (e >> 1), me = at[n][e & 1];
+                        if (key > me || (p.window && key <= me - p.window && key >= p.n_sink)) x[n][e] = -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) above = above || x[n][e] > m[n][e & 1] + 8.f;
+            // the reference moves only when a score is 2^8 above it
+            if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(x[n][e], x[n][e + 2]);
+#pragma unroll
+                        for (int b = 4; b < 32; b <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
+                        top = fmaxf(top, m[n][e]);
+                        const float f = m[n][e] == top ? 1.f : ex2(m[n][e] - top);
+                        m[n][e] = top;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int c = 0; c < KS; ++c) {
+                            o[n][c][e] *= f;
+                            o[n][c][e + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t b[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = ex2(x[n][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
+                    l[n][e & 1] += w[e];
+                }
+                b[n][0] = transposed(f2_bf2(w[0] * vs, w[1] * vs));
+                b[n][1] = transposed(f2_bf2(w[2] * vs, w[3] * vs));
+            }
+            if constexpr (D == 64) {
+                uint2 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint2*>(vt + piece<D>(2 * j + (k & 1) + 8 * (k >> 1), g >> 1) + 8 * (g & 1));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t w0 = u < 2 ? v[0].x : v[0].y, w1 = u < 2 ? v[1].x : v[1].y, w2 = u < 2 ? v[2].x : v[2].y, w3 = u < 2 ? v[3].x : v[3].y;
+                    const uint32_t s0 = u & 1 ? 0x6020 : 0x4000, s1 = u & 1 ? 0x7030 : 0x5010;
+                    const uint32_t a0 = e4m3_pair(__byte_perm(w0, w1, s0)), a1 = e4m3_pair(__byte_perm(w0, w1, s1));
+                    const uint32_t a2 = e4m3_pair(__byte_perm(w2, w3, s0)), a3 = e4m3_pair(__byte_perm(w2, w3, s1));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma16816(o[n][u], a0, a1, a2, a3, b[n][0], b[n][1]);
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < D / 128; ++h) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(vt + piece<D>(2 * j + (k & 1) + 8 * (k >> 1), 8 * h + g));
+                    const uint32_t* w[4] = {&v[0].x, &v[1].x, &v[2].x, &v[3].x};
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const uint32_t s0 = u & 1 ? 0x6020 : 0x4000, s1 = u & 1 ? 0x7030 : 0x5010;
+                        const uint32_t a0 = e4m3_pair(__byte_perm(w[0][u >> 1], w[1][u >> 1], s0));
+                        const uint32_t a1 = e4m3_pair(__byte_perm(w[0][u >> 1], w[1][u >> 1], s1));
+                        const uint32_t a2 = e4m3_pair(__byte_perm(w[2][u >> 1], w[3][u >> 1], s0));
+                        const uint32_t a3 = e4m3_pair(__byte_perm(w[2][u >> 1], w[3][u >> 1], s1));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816(o[n][8 * h + u], a0, a1, a2, a3, b[n][0], b[n][1]);
+                    }
+                }
+            }
+            __syncwarp();                                      // the ring's place is read before it is filled again
+        }
+        cp_wait<0>();
+        // ------------------------------------------------------------ the warps meet
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int b = 4; b < 32; b <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], b);
+                if (g == 0) {
+                    wm[warp * C::ROWS + 8 * n + 2 * j + e] = m[n][e];
+                    wl[warp * C::ROWS + 8 * n + 2 * j + e] = l[n][e];
+                }
+            }
+        __syncthreads();                                       // every ring is done
+        // a lane's numbers of a row are neighbours, 16 (D 64: 8) of them a piece; every
+        // other lane's 16-byte words change places, so that a quarter warp meets all banks
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float* row = meet + (warp * C::ROWS + 8 * n + 2 * j + e) * C::PITCH;
+#pragma unroll
+                for (int c = 0; c < KS; c += 2) {
+                    const int d4 = D == 64 ? 2 * g + c / 2 : 32 * (c >> 3) + 4 * g + (c & 7) / 2;
+                    *reinterpret_cast<float4*>(row + 4 * (d4 ^ (g & 1))) =
+                        make_float4(o[n][c][e], o[n][c][e + 2], o[n][c + 1][e], o[n][c + 1][e + 2]);
+                }
+            }
+        __syncthreads();
+        const int64_t slot = 2 * cta + (seg == waves ? 0 : 1);
+        for (int it = tid; it < rows * (D / 4); it += kThreads) {
+            const int r = it % rows, d4 = it / rows;           // rows fastest, as in the partials
+            float top = -INFINITY, lt = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wm[w * C::ROWS + r]);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int gw = D == 64 ? d4 >> 1 : d4 >> 2;        // the lane that wrote it
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = wm[w * C::ROWS + r];
+                const float f = mw == -INFINITY ? 0.f : ex2(mw - top);
+                const float4 v = *reinterpret_cast<const float4*>(meet + (w * C::ROWS + r) * C::PITCH + 4 * (d4 ^ (gw & 1)));
+                lt += f * wl[w * C::ROWS + r];
+                acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+            }
+            if (full) {
+                const float inv = 1.f / lt;                    // a row sees itself
+                __nv_bfloat16* dst = p.out + ((int64_t)(ch.tail_off + T.tok0 + r / p.g) * p.Hq + T.kvh * p.g + r % p.g) * D + 4 * d4;
+                *reinterpret_cast<uint2*>(dst) = make_uint2(f2_bf2(acc.x * inv, acc.y * inv), f2_bf2(acc.z * inv, acc.w * inv));
+            } else {
+                reinterpret_cast<float4*>(p.part_o + (slot * (D / 32) + d4 / 8) * 8 * BM * 4)[d4 % 8 * BM + r] = acc;
+                if (d4 == 0) {
+                    p.part_ml[(slot * BM + r) * 2] = top;
+                    p.part_ml[(slot * BM + r) * 2 + 1] = lt;
+                }
+            }
+        }
+        __syncthreads();                                       // before the next segment fills the rings
+    }
+}
+
+template <int D, int NT>
+void launch(const Kv8AttnParams& p, cudaStream_t s) {
+    static unsigned long long configured = 0;   // one bit per device
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!(configured >> (dev & 63) & 1ull)) {
+        cudaFuncSetAttribute(kv8_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, NT>::SMEM);
+        configured |= 1ull << (dev & 63);
+    }
+    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(kThreads), Cfg<D, NT>::SMEM, s, p);
+}
+
+template <int D>
+void launch_d(const Kv8AttnParams& p, cudaStream_t s) {
+    p.rows <= 8 ? launch<D, 1>(p, s) : launch<D, 2>(p, s);
+}
+
+}  // namespace
+
+void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s) {
+    if (p.a.n_ctas <= 0) return;
+    if (p.a.D == 64) launch_d<64>(p, s);
+    else if (p.a.D == 128) launch_d<128>(p, s);
+    else launch_d<256>(p, s);
+}
+
+}  // namespace kvm

@@ -113,6 +113,14 @@ struct kvm_ctx {
     // device state
     __nv_bfloat16* K = nullptr;
     __nv_bfloat16* V = nullptr;
+    // a context of kvm_create_kv8 keeps its keys and values here, [n_attn][Hkv][T_cap][D] with a
+    // scale for each 64 slots; K and V are then room for one layer in bf16 (see kv8.cu)
+    bool kv8 = false;
+    uint8_t* K8 = nullptr;
+    uint8_t* V8 = nullptr;
+    float* K8s = nullptr;
+    float* V8s = nullptr;
+    uint64_t turn[kMaxRotaryHalf] = {};   // inv_freq in 2^-64 of a whole turn
     int32_t* pos = nullptr;
     float* S = nullptr;
     // workspace
@@ -534,8 +542,9 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
 // ============================================================================
 // lifetime
 // ============================================================================
-extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity,
-                                 int32_t max_tail_tokens, kvm_ctx** out) {
+namespace {
+kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity, int32_t max_tail_tokens, bool kv8,
+                  kvm_ctx** out) {
     if (!m || !capacity || !out) return fail(KVM_E_INVAL, "NULL argument");
     *out = nullptr;
     if (m->n_layers <= 0 || !m->layer_kind) return fail(KVM_E_INVAL, "model has no layers");
@@ -561,6 +570,9 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
         if (c->R < 0 || c->R > c->D || (c->R & 1)) { delete c; return fail(KVM_E_UNSUPPORTED, "rotary_dim must be even and <= head_dim"); }
         if (!(c->theta > 0)) { delete c; return fail(KVM_E_INVAL, "rope_theta must be positive"); }
         for (int d = 0; d < c->R / 2; ++d) c->inv_freq[d] = std::pow(c->theta, -2.0 * d / c->R);
+        c->kv8 = kv8;
+        for (int d = 0; d < c->R / 2; ++d)
+            c->turn[d] = (uint64_t)std::ldexp(std::fmod((long double)c->inv_freq[d] / 6.283185307179586476925286766559L, 1.0L), 64);
     }
     if (c->n_gdn > 0) {
         c->H = m->n_gdn_heads; c->dk = m->d_k; c->dv = m->d_v;
@@ -594,7 +606,8 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, c->device);
     if (e != cudaSuccess) { delete c; return fail(KVM_E_CUDA, "no CUDA device: %s", cudaGetErrorString(e)); }
 
-    const size_t kv_elems = (size_t)c->n_attn * c->Hkv * c->T_cap * c->D;
+    const int kv_layers = c->kv8 ? 1 : c->n_attn;          // of the bf16 slabs
+    const size_t layer_elems = (size_t)c->Hkv * c->T_cap * c->D, kv_elems = (size_t)kv_layers * layer_elems;
     const int vec_per_row = c->D * 2 / 16;
     c->rows_kv = c->n_attn ? kCompactVecPerChunk / std::max(vec_per_row, 1) : 1;
     c->rows_pos = kCompactVecPerChunk;
@@ -608,6 +621,13 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
     e = cudaSuccess;
     if (e == cudaSuccess) e = alloc_zero(&c->K, kv_elems);
     if (e == cudaSuccess) e = alloc_zero(&c->V, kv_elems);
+    if (c->kv8) {
+        const size_t n = (size_t)c->n_attn * layer_elems, blocks = n / ((size_t)kKv8Rows * c->D);
+        if (e == cudaSuccess) e = alloc_zero(&c->K8, n);
+        if (e == cudaSuccess) e = alloc_zero(&c->V8, n);
+        if (e == cudaSuccess) e = alloc_zero(&c->K8s, blocks);
+        if (e == cudaSuccess) e = alloc_zero(&c->V8s, blocks);
+    }
     if (e == cudaSuccess) e = alloc_zero(&c->pos, c->n_attn ? (size_t)c->T_cap : 0);
     if (e == cudaSuccess) e = alloc_zero(&c->S, (size_t)c->n_gdn * n_chars * c->H * c->dv * c->dk);
     if (e == cudaSuccess) e = alloc_zero(&c->q_rot, c->n_attn ? (size_t)max_tail_tokens * c->Hq * c->D : 0);
@@ -693,7 +713,7 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
         // TMA maps: rotated q as [max_tail][Hq][D] with a (64, g, 128/g) box;
         // every layer's K and V as rows of D with a (64, 64) box
         const uint64_t row_bytes = (uint64_t)c->D * 2;
-        const uint64_t kd[2] = {(uint64_t)c->D, (uint64_t)c->n_attn * c->Hkv * c->T_cap};
+        const uint64_t kd[2] = {(uint64_t)c->D, (uint64_t)kv_layers * c->Hkv * c->T_cap};
         const uint64_t ks[1] = {row_bytes};
         const uint32_t kb[2] = {64, 64};
         if (kd[1] > (uint64_t)INT32_MAX ||
@@ -706,6 +726,17 @@ extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const
     }
     *out = c;
     return KVM_OK;
+}
+}  // namespace
+
+extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity,
+                                 int32_t max_tail_tokens, kvm_ctx** out) {
+    return create(m, n_chars, capacity, max_tail_tokens, false, out);
+}
+
+extern "C" kvm_status kvm_create_kv8(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity,
+                                     int32_t max_tail_tokens, kvm_ctx** out) {
+    return create(m, n_chars, capacity, max_tail_tokens, true, out);
 }
 
 extern "C" kvm_status kvm_destroy(kvm_ctx* c) {
@@ -796,11 +827,105 @@ kvm_status copy_state(kvm_ctx* c, void* const* dst, const void* const* src, int 
     return KVM_OK;
 }
 
+// The calls over 8-bit caches launch kernels only, so the context's device must be current.
+kvm_status check_device(const kvm_ctx* c) {
+    int dev = -1;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev != c->device) return fail(KVM_E_INVAL, "the context lives on device %d, device %d is current", c->device, dev);
+    return KVM_OK;
+}
+
+Kv8Layer kv8_layer(const kvm_ctx* c, int a) {
+    const size_t n = (size_t)c->Hkv * c->T_cap * c->D, blocks = n / ((size_t)kKv8Rows * c->D);
+    return {c->K8 + a * n, c->V8 + a * n, c->K8s + a * blocks, c->V8s + a * blocks};
+}
+
+// Blocks [block0, ...) of character b up to row `rows`, as items of a kv8 kernel: `sides`
+// (K, V or both) of every head.
+Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int row0, int sides, int& items) {
+    const int n = std::max(0, (rows + kKv8Rows - 1) / kKv8Rows - block0);
+    const Kv8Char ch{row0, c->cap_off[b], block0, n, rows, items};
+    items += n * sides * c->Hkv;
+    return ch;
+}
+
+// Keys and values (v null: keys alone) of attention layer a's character b as bf16 rows at row0 of k's and v's
+// slabs of dst_rows; block_rows: whole blocks, what lies behind the live entries too.
+kvm_status widen_char(kvm_ctx* c, int a, int b, void* k, void* v, int row0, int64_t dst_rows, bool block_rows, cudaStream_t s) {
+    thread_local static Kv8WidenParams p;
+    p.from = kv8_layer(c, a);
+    p.n_chars = 1;
+    p.Hkv = c->Hkv;
+    p.D = c->D;
+    p.n_items = 0;
+    p.slab_rows = c->T_cap;
+    p.dst_rows = dst_rows;
+    p.K = static_cast<__nv_bfloat16*>(k);
+    p.V = static_cast<__nv_bfloat16*>(v);
+    const int L = c->live[b], rows = block_rows ? (L + kKv8Rows - 1) / kKv8Rows * kKv8Rows : L;
+    p.ch[0] = kv8_char(c, b, 0, rows, row0, v ? 2 : 1, p.n_items);
+    p.sink[0] = p.gap[0] = 0;
+    ++c->launches;
+    launch_kv8_widen(p, s);
+    LAUNCH_CHECK(c);
+    return KVM_OK;
+}
+
+// bf16 rows of every character with a block0 >= 0, up to rows[b], into blocks of layer a.
+kvm_status pack_chars(kvm_ctx* c, int a, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t src_rows, const Kv8Char* ch, int n_chars,
+                      int items, cudaStream_t s) {
+    if (!items) return KVM_OK;
+    thread_local static Kv8PackParams p;
+    p.to = kv8_layer(c, a);
+    p.n_chars = n_chars;
+    p.Hkv = c->Hkv;
+    p.D = c->D;
+    p.n_items = items;
+    p.slab_rows = c->T_cap;
+    p.src_rows = src_rows;
+    p.K = k;
+    p.V = v;
+    p.err = c->err;
+    std::copy(ch, ch + n_chars, p.ch);
+    ++c->launches;
+    launch_kv8_pack(p, s);
+    LAUNCH_CHECK(c);
+    return KVM_OK;
+}
+
+kvm_status copy_slabs(kvm_ctx* c, int a, int b, void* k, void* v, bool in, cudaStream_t s);
+
+// KV of character b of an 8-bit layer: straight between the blocks and the caller's buffers
+// where a kernel can reach those, else by way of the bf16 slabs.
+kvm_status copy_kv8(kvm_ctx* c, int a, int b, void* k, void* v, bool in, cudaStream_t s) {
+    kvm_status st = check_device(c);
+    if (st) return st;
+    const int L = c->live[b];
+    const bool own = !((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15) && own_memory(c, k) && own_memory(c, v);
+    const int row0 = own ? 0 : c->cap_off[b];
+    const int64_t rows = own ? L : c->T_cap;
+    if (!in) {
+        st = widen_char(c, a, b, own ? k : c->K, own ? v : c->V, row0, rows, !own, s);
+        return st || own ? st : copy_slabs(c, 0, b, k, v, false, s);
+    }
+    if (!own) st = copy_slabs(c, 0, b, k, v, true, s);
+    if (st) return st;
+    int items = 0;
+    const Kv8Char ch = kv8_char(c, b, 0, L, row0, 2, items);
+    return pack_chars(c, a, own ? static_cast<const __nv_bfloat16*>(k) : c->K, own ? static_cast<const __nv_bfloat16*>(v) : c->V, rows, &ch, 1,
+                      items, s);
+}
+
 // KV of character b in attention layer `layer`: slab rows of every KV head.
 kvm_status copy_kv(kvm_ctx* c, int layer, int b, void* k, void* v, bool in, cudaStream_t s) {
+    const int a = c->attn_idx[layer];
+    return c->kv8 ? copy_kv8(c, a, b, k, v, in, s) : copy_slabs(c, a, b, k, v, in, s);
+}
+
+kvm_status copy_slabs(kvm_ctx* c, int a, int b, void* k, void* v, bool in, cudaStream_t s) {
     const int L = c->live[b];
     const size_t row = (size_t)c->D * 2, slab = (size_t)c->T_cap * row;
-    const size_t at = ((size_t)c->attn_idx[layer] * c->Hkv) * slab + (size_t)c->cap_off[b] * row;
+    const size_t at = ((size_t)a * c->Hkv) * slab + (size_t)c->cap_off[b] * row;
     void* own[2] = {reinterpret_cast<char*>(c->K) + at, reinterpret_cast<char*>(c->V) + at};
     void* user[2] = {k, v};
     return in ? copy_state(c, own, user, 2, slab, L * row, L * row, c->Hkv, s)
@@ -1097,21 +1222,59 @@ extern "C" kvm_status kvm_plan_spans_from_positions(int32_t live, const int32_t*
 // ============================================================================
 namespace {
 
+// A removal in 8-bit layers [a_lo, a_hi): the survivors, widened, to their new places in
+// the bf16 slabs, and back into blocks from the first removed entry's on.
+kvm_status compact_kv8(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int a_lo, int a_hi) {
+    thread_local static Kv8GatherParams p;
+    p.n_chars = c->B;
+    p.Hkv = c->Hkv;
+    p.D = c->D;
+    p.slab_rows = c->T_cap;
+    p.K = c->K;
+    p.V = c->V;
+    p.n_items = 0;
+    for (int b = 0; b < c->B; ++b) {
+        const bool any = pl.n_seg[b] > 0;
+        p.ch[b] = kv8_char(c, b, any ? pl.first[b] / kKv8Rows : 0, any ? pl.L_new[b] : 0, c->cap_off[b], 2, p.n_items);
+        p.first[b] = pl.first[b];
+        p.seg_off[b] = pl.seg_off[b];
+        p.n_seg[b] = pl.n_seg[b];
+    }
+    if (!p.n_items) return KVM_OK;
+    std::copy(pl.seg_start.begin(), pl.seg_start.end(), p.seg_start);
+    std::copy(pl.seg_shift.begin(), pl.seg_shift.end(), p.seg_shift);
+    for (int a = a_lo; a < a_hi; ++a) {
+        p.from = kv8_layer(c, a);
+        const int ps = prof_begin(c, KVM_K_COMPACT, s);
+        launch_kv8_gather(p, s);
+        LAUNCH_CHECK(c);
+        const kvm_status st = pack_chars(c, a, c->K, c->V, c->T_cap, p.ch, c->B, p.n_items, s);
+        prof_end(c, ps, s);
+        if (st) return st;
+    }
+    return KVM_OK;
+}
+
 // Compaction of the attention layers [a_lo, a_hi) (K and V slabs of those
 // layers, and the position slab when with_pos) under a validated plan.
 kvm_status launch_compaction(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int a_lo, int a_hi, bool with_pos) {
+    if (c->kv8 && a_hi > a_lo) {
+        const kvm_status st = compact_kv8(c, pl, s, a_lo, a_hi);
+        if (st) return st;
+    }
     if (c->n_attn > 0 && a_hi > a_lo) {
         thread_local static CompactParams p;   // large parameter block, copied into the launch
         std::memset(&p, 0, sizeof p);
         p.n_chars = c->B;
-        p.n_kv_slabs = 2 * (a_hi - a_lo) * c->Hkv;
+        p.n_kv_slabs = c->kv8 ? 0 : 2 * (a_hi - a_lo) * c->Hkv;    // else the positions alone
         p.vec_per_row = c->D * 2 / 16;
         p.rows_kv = c->rows_kv;
         p.rows_pos = c->rows_pos;
         p.epoch = ++c->epoch;
         p.slab_rows = c->T_cap;
-        p.K = reinterpret_cast<uint4*>(c->K + (size_t)a_lo * c->Hkv * c->T_cap * c->D);
-        p.V = reinterpret_cast<uint4*>(c->V + (size_t)a_lo * c->Hkv * c->T_cap * c->D);
+        const size_t kv_lo = c->kv8 ? 0 : (size_t)a_lo * c->Hkv * c->T_cap * c->D;
+        p.K = reinterpret_cast<uint4*>(c->K + kv_lo);
+        p.V = reinterpret_cast<uint4*>(c->V + kv_lo);
         p.pos = c->pos;
         p.tickets = c->tickets;
         p.flags = c->flags;
@@ -1130,7 +1293,7 @@ kvm_status launch_compaction(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int
             ch.seg_off = pl.seg_off[b];
             ch.n_seg = pl.n_seg[b];
             ch.cap_off = c->cap_off[b];
-            ch.chunks_kv = (moved + p.rows_kv - 1) / p.rows_kv;
+            ch.chunks_kv = c->kv8 ? 0 : (moved + p.rows_kv - 1) / p.rows_kv;
             ch.chunks_pos = with_pos ? (moved + p.rows_pos - 1) / p.rows_pos : 0;
             ch.blk_off = blk;
             ch.flag_off = c->flag_off[b];
@@ -1201,12 +1364,70 @@ kvm_status do_compact(kvm_ctx* c, const int32_t* span_cu, const int32_t* sbeg, c
     SpanPlan pl;
     kvm_status st = plan_spans(c, span_cu, sbeg, send, pl);
     if (st) return st;
+    if (c->kv8 && (st = check_device(c))) return st;
     drop_draft(c);
     st = launch_compaction(c, pl, s, 0, c->n_attn, true);
     if (st) return st;
     st = launch_gather(c, pl, gather_out, s);
     if (st) return st;
     apply_plan(c, pl, span_cu, sbeg, send);
+    return KVM_OK;
+}
+
+// The rows that attention layer `layer` of a context in 8 bits reads: the tail's into the
+// blocks, and, unless the attention reads 8 bits itself, the blocks in sight as bf16.
+kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int total, bool widen, cudaStream_t s) {
+    thread_local static Kv8AppendParams ap;
+    ap.to = kv8_layer(c, c->attn_idx[layer]);
+    ap.n_chars = c->B;
+    ap.Hq = c->Hq; ap.Hkv = c->Hkv; ap.D = c->D; ap.R = c->R;
+    ap.total = total;
+    ap.slab_rows = c->T_cap;
+    ap.q = p.q;
+    ap.k_new = p.k_new;
+    ap.v_new = p.v_new;
+    ap.q_rot = p.q_rot;
+    ap.pos = p.pos;
+    ap.tail_pos = p.tail_pos;
+    ap.err = p.err;
+    std::copy(c->turn, c->turn + kMaxRotaryHalf, ap.turn);
+    ap.n_items = 0;
+    for (int b = 0; b < c->B; ++b) {
+        const AttnChar& ch = p.ch[b];
+        ap.ch[b] = kv8_char(c, b, ch.L_prev / kKv8Rows, ch.M ? ch.L_prev + ch.M : 0, c->cap_off[b], 2, ap.n_items);
+        ap.L_prev[b] = ch.L_prev;
+        ap.tail_off[b] = ch.tail_off;
+        ap.p[b] = ch.p;
+    }
+    int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
+    launch_kv8_append(ap, s);
+    LAUNCH_CHECK(c);
+    if (widen) {
+        thread_local static Kv8WidenParams wp;
+        wp.from = ap.to;
+        wp.n_chars = c->B;
+        wp.Hkv = c->Hkv;
+        wp.D = c->D;
+        wp.slab_rows = wp.dst_rows = c->T_cap;
+        wp.K = c->K;
+        wp.V = c->V;
+        wp.n_items = 0;
+        for (int b = 0; b < c->B; ++b) {
+            const AttnChar& ch = p.ch[b];
+            // what the tail's first token sees, and all from there on; whole blocks, so that no row the
+            // attention loads is left over from another layer
+            const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
+            const int blocks = ch.M ? (ch.L_prev + ch.M + kKv8Rows - 1) / kKv8Rows : 0;
+            wp.ch[b] = {c->cap_off[b], c->cap_off[b], 0, blocks ? blocks - w.gap : 0, blocks * kKv8Rows, wp.n_items};
+            wp.n_items += wp.ch[b].n_blocks * 2 * c->Hkv;
+            wp.sink[b] = w.sink;
+            wp.gap[b] = w.gap;
+        }
+        launch_kv8_widen(wp, s);
+        ++c->launches;
+        LAUNCH_CHECK(c);
+    }
+    prof_end(c, ps, s);
     return KVM_OK;
 }
 
@@ -1220,7 +1441,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     const int a = c->attn_idx[layer];
     p.tmap_k = c->tmap_k;
     p.tmap_v = c->tmap_v;
-    p.attn_layer = a;
+    p.attn_layer = c->kv8 ? 0 : a;
     p.n_chars = c->B;
     p.Hq = c->Hq; p.Hkv = c->Hkv; p.D = c->D; p.R = c->R; p.g = c->g;
     p.tok_per_tile = kAttnRows / c->g;
@@ -1230,8 +1451,8 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     p.k_new = static_cast<const __nv_bfloat16*>(k_new);
     p.v_new = static_cast<const __nv_bfloat16*>(v_new);
     p.q_rot = c->q_rot;
-    p.K = c->K + (size_t)a * c->Hkv * c->T_cap * c->D;
-    p.V = c->V + (size_t)a * c->Hkv * c->T_cap * c->D;
+    p.K = c->K + (size_t)p.attn_layer * c->Hkv * c->T_cap * c->D;
+    p.V = c->V + (size_t)p.attn_layer * c->Hkv * c->T_cap * c->D;
     p.pos = c->pos;
     p.out = static_cast<__nv_bfloat16*>(out);
     p.tail_pos = tail_pos_dev;
@@ -1267,7 +1488,14 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_tile.begin(), pl.cta_tile.end(), p.cta_tile);
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
-    if (!p.append) {
+    int rows = 0;                                    // most of a character
+    for (int b = 0; b < c->B; ++b) rows = std::max(rows, p.ch[b].M * c->g);
+    const bool direct = c->kv8 && rows <= kKv8Direct;
+    if (c->kv8) {
+        p.widened = !direct;
+        const kvm_status st = launch_kv8_before(c, layer, p, total, !direct, s);
+        if (st) return st;
+    } else if (!p.append) {
         const int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
         if (p.turn) {
             DraftAppendParams d{total, c->Hkv, c->D, c->R, c->T_cap, p.k_new, p.v_new, p.K, p.V, c->pos, c->draft_pos, c->draft_slot,
@@ -1280,7 +1508,15 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
         LAUNCH_CHECK(c);
     }
     int ps = prof_begin(c, KVM_K_ATTENTION, s);
-    launch_tail_attention(p, s);
+    if (direct) {
+        thread_local static Kv8AttnParams dp;
+        dp.a = p;
+        dp.from = kv8_layer(c, a);
+        dp.rows = rows;
+        launch_kv8_attention(dp, s);
+    } else {
+        launch_tail_attention(p, s);
+    }
     prof_end(c, ps, s);
     LAUNCH_CHECK(c);
     if (!pl.split_cb.empty()) {
@@ -1336,6 +1572,7 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     if (st) return st;
     if (total == 0) return KVM_OK;
     if (!q || !k_new || !v_new || !out) return fail(KVM_E_INVAL, "NULL tensor");
+    if (c->kv8 && (st = check_device(c))) return st;
 
     std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
@@ -1629,6 +1866,7 @@ extern "C" kvm_status kvm_rerotate_keys(kvm_ctx* c, int32_t b, int32_t live_begi
                                         const int32_t* new_pos, void* stream) {
     if (!c) return fail(KVM_E_INVAL, "NULL context");
     if (c->n_attn == 0) return fail(KVM_E_INVAL, "the model has no attention layer");
+    if (c->kv8) return fail(KVM_E_UNSUPPORTED, "keys in 8 bits are not rotated again");
     if (b < 0 || b >= c->B) return fail(KVM_E_INVAL, "character %d out of range", b);
     if (!(0 <= live_begin && live_begin <= live_end && live_end <= c->live[b]))
         return fail(KVM_E_SPAN, "range [%d,%d) outside the live entries [0,%d)", live_begin, live_end, c->live[b]);
@@ -1693,7 +1931,8 @@ extern "C" kvm_status kvm_attn_probe(kvm_ctx* c, int32_t layer, int32_t b, int32
     p.slot0 = c->cap_off[b];
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.q_rot = c->probe_q;
-    p.K = c->K + (size_t)c->attn_idx[layer] * c->Hkv * c->T_cap * c->D;
+    p.K = c->K;
+    if (!c->kv8) p.K += (size_t)c->attn_idx[layer] * c->Hkv * c->T_cap * c->D;
     p.pos = c->pos;
     p.scores = c->part_o;
     p.scores_cap = (int64_t)c->part_floats;
@@ -1703,6 +1942,11 @@ extern "C" kvm_status kvm_attn_probe(kvm_ctx* c, int32_t layer, int32_t b, int32
     p.group_mass = group_mass_out;
     p.err = c->err;
     for (int d = 0; d < c->R / 2; ++d) p.inv_freq[d] = c->inv_freq[d];
+    if (c->kv8) {
+        st = check_device(c);
+        if (!st) st = widen_char(c, c->attn_idx[layer], b, c->K, nullptr, c->cap_off[b], c->T_cap, true, s);
+        if (st) return st;
+    }
     if (group_of) CUDA_TRY(cudaMemsetAsync(group_mass_out, 0, sizeof(float) * (size_t)n_groups, s));
     c->launches += launch_attn_probe(p, s);
     LAUNCH_CHECK(c);
@@ -1860,6 +2104,7 @@ kvm_status draft_reserve(kvm_ctx* c, int max_nodes) {
     if (!c) return fail(KVM_E_INVAL, "NULL context");
     if (max_nodes <= 0 || max_nodes > c->max_tail)
         return fail(KVM_E_INVAL, "max_nodes must be in [1, max_tail_tokens = %d]", c->max_tail);
+    if (c->kv8) return fail(KVM_E_UNSUPPORTED, "drafts need caches in 16 bits");
     if (c->n_gdn > kMaxDraftLayers)
         return fail(KVM_E_UNSUPPORTED, "drafts take at most %d delta-rule layers", kMaxDraftLayers);
     int dev = -1;
@@ -2241,6 +2486,7 @@ kvm_status update_round_impl(kvm_ctx* c, const kvm_round* r, void* stream) {
         st = plan_spans_for(c->B, tail_len.data(), r->delim_cu, r->delim_begin, r->delim_end, delim_plan);
         if (st) return st;
     }
+    if (c->kv8 && (st = check_device(c))) return st;
     drop_draft(c);
     const bool host_io = r->io_on_host && total > 0;
     auto sizes = [&](int l, size_t n[6]) {
@@ -2513,13 +2759,21 @@ extern "C" kvm_status kvm_fork(kvm_ctx* dst, const kvm_ctx* src, void* stream) {
     if (dst == src) return KVM_OK;
     if (dst->kind != src->kind || dst->Hq != src->Hq || dst->Hkv != src->Hkv || dst->D != src->D ||
         dst->R != src->R || dst->theta != src->theta || dst->H != src->H || dst->dk != src->dk ||
-        dst->dv != src->dv || dst->B != src->B || dst->cap != src->cap || dst->conv != src->conv)
+        dst->dv != src->dv || dst->B != src->B || dst->cap != src->cap || dst->conv != src->conv || dst->kv8 != src->kv8)
         return fail(KVM_E_INVAL, "contexts differ in model shape, population or capacity");
     cudaStream_t s = (cudaStream_t)stream;
     const size_t kv = (size_t)src->n_attn * src->Hkv * src->T_cap * src->D * sizeof(__nv_bfloat16);
     if (kv) {
-        CUDA_TRY(cudaMemcpyAsync(dst->K, src->K, kv, cudaMemcpyDeviceToDevice, s));
-        CUDA_TRY(cudaMemcpyAsync(dst->V, src->V, kv, cudaMemcpyDeviceToDevice, s));
+        if (src->kv8) {
+            const size_t scales = kv / 2 / ((size_t)kKv8Rows * src->D) * sizeof(float);
+            CUDA_TRY(cudaMemcpyAsync(dst->K8, src->K8, kv / 2, cudaMemcpyDeviceToDevice, s));
+            CUDA_TRY(cudaMemcpyAsync(dst->V8, src->V8, kv / 2, cudaMemcpyDeviceToDevice, s));
+            CUDA_TRY(cudaMemcpyAsync(dst->K8s, src->K8s, scales, cudaMemcpyDeviceToDevice, s));
+            CUDA_TRY(cudaMemcpyAsync(dst->V8s, src->V8s, scales, cudaMemcpyDeviceToDevice, s));
+        } else {
+            CUDA_TRY(cudaMemcpyAsync(dst->K, src->K, kv, cudaMemcpyDeviceToDevice, s));
+            CUDA_TRY(cudaMemcpyAsync(dst->V, src->V, kv, cudaMemcpyDeviceToDevice, s));
+        }
         CUDA_TRY(cudaMemcpyAsync(dst->pos, src->pos, (size_t)src->T_cap * 4, cudaMemcpyDeviceToDevice, s));
     }
     const size_t sn = (size_t)src->n_gdn * src->B * src->H * src->dv * src->dk * sizeof(float);

@@ -41,7 +41,7 @@ constexpr int kMaxRotaryHalf = 128; // rotary_dim / 2
 // Device error word bits (read by kvm_check).
 constexpr int kErrBounds = 1;       // an index fell outside the buffers a kernel was given
 constexpr int kErrWait = 2;         // a bounded wait expired
-constexpr int kErrValue = 4;        // a draft's key, value or gate is not finite
+constexpr int kErrValue = 4;        // a draft's key, value or gate is not finite, or a number on its way into an 8-bit cache
 
 // ----------------------------------------------------------------------------
 // kv_compact
@@ -221,6 +221,100 @@ void launch_rerotate(const RerotateParams& p, cudaStream_t s);
 void launch_tail_attention(const AttnParams& p, cudaStream_t s);
 void launch_window_attention(const AttnParams& p, cudaStream_t s);      // of which p.window > 0 is this
 void launch_attn_combine(const CombineParams& p, cudaStream_t s);
+
+// ----------------------------------------------------------------------------
+// caches in 8 bits: e4m3 numbers times a power of two for each block of 64 slots
+// and KV head, K and V apart (see kv8.cuh)
+// ----------------------------------------------------------------------------
+constexpr int kKv8Rows = 64;     // slots of a block
+
+// One layer's slabs [Hkv][slab_rows][D] and scales [Hkv][slab_rows / 64].
+struct Kv8Layer {
+    uint8_t* K;
+    uint8_t* V;
+    float* Ks;
+    float* Vs;
+};
+
+struct Kv8Char {
+    int32_t row0;         // first row of the other side (a cache's own slots: cap_off)
+    int32_t cap_off;      // slot offset of the character in the slabs
+    int32_t block0;       // its first block that takes part
+    int32_t n_blocks;
+    int32_t rows;         // rows in use, counted from the character's first
+    int32_t blk_off;      // first (block, head, K or V) item of this character
+};
+
+// Rows of bf16 into 8-bit blocks: rows [64 block0, rows) of a character, at row0 + row
+// of src's slabs [Hkv][src_rows][D]; the rest of the last block becomes 0.
+struct Kv8PackParams {
+    Kv8Layer to;
+    int32_t n_chars, Hkv, D, n_items;
+    int64_t slab_rows, src_rows;
+    const __nv_bfloat16* K;
+    const __nv_bfloat16* V;
+    int32_t* err;
+    Kv8Char ch[kMaxChars];
+};
+void launch_kv8_pack(const Kv8PackParams& p, cudaStream_t s);
+
+// 8-bit blocks out as bf16 rows: blocks block0 .. of a character, of a window's blocks
+// those from `sink` on `gap` further; rows at or past `rows` are left alone.
+struct Kv8WidenParams {
+    Kv8Layer from;
+    int32_t n_chars, Hkv, D, n_items;
+    int64_t slab_rows, dst_rows;
+    __nv_bfloat16* K;             // [Hkv][dst_rows][D]; V null: only keys
+    __nv_bfloat16* V;
+    Kv8Char ch[kMaxChars];
+    int32_t sink[kMaxChars], gap[kMaxChars];
+};
+void launch_kv8_widen(const Kv8WidenParams& p, cudaStream_t s);
+
+// The survivors of a removal, widened, in their new places: rows [64 block0, rows) of
+// a character from the rows that segments name (see CompactParams).
+struct Kv8GatherParams {
+    Kv8Layer from;
+    int32_t n_chars, Hkv, D, n_items;
+    int64_t slab_rows;
+    __nv_bfloat16* K;             // [Hkv][slab_rows][D]
+    __nv_bfloat16* V;
+    Kv8Char ch[kMaxChars];
+    int32_t first[kMaxChars], seg_off[kMaxChars], n_seg[kMaxChars];
+    int32_t seg_start[kMaxSpans];
+    int32_t seg_shift[kMaxSpans];
+};
+void launch_kv8_gather(const Kv8GatherParams& p, cudaStream_t s);
+
+// A tail's rotated keys and its values into the blocks behind the live entries, and
+// its rotated queries into q_rot.
+struct Kv8AppendParams {
+    Kv8Layer to;
+    int32_t n_chars, Hq, Hkv, D, R, n_items, total;
+    int64_t slab_rows;
+    const __nv_bfloat16* q;       // [sum M][Hq][D]
+    const __nv_bfloat16* k_new;   // [sum M][Hkv][D]
+    const __nv_bfloat16* v_new;
+    __nv_bfloat16* q_rot;
+    int32_t* pos;                 // [slab_rows]
+    const int32_t* tail_pos;      // as in AttnParams
+    int32_t* err;
+    uint64_t turn[kMaxRotaryHalf];   // a position's turn of each pair, in 2^-64 of a whole one
+    Kv8Char ch[kMaxChars];           // rows: live and tail
+    int32_t L_prev[kMaxChars], tail_off[kMaxChars];
+    int64_t p[kMaxChars];
+};
+void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s);
+
+// Attention of a few rows a KV head straight from the 8-bit cache, under the same
+// partition and with the same partials as launch_tail_attention.
+constexpr int kKv8Direct = 16;   // most rows (tail tokens of a character x group)
+struct Kv8AttnParams {
+    AttnParams a;
+    Kv8Layer from;
+    int32_t rows;                 // most rows of a query tile
+};
+void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s);
 int attention_ctas_per_sm(int head_dim);
 constexpr int kAttnRows = 128;   // query rows per attention tile
 

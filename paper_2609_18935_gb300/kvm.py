@@ -65,6 +65,8 @@ _HOST = C.c_void_p
 _SIGS = {
     "kvm_create": (C.c_int, [C.POINTER(ModelDesc), C.c_int32, C.POINTER(C.c_int32), C.c_int32,
                              C.POINTER(C.c_void_p)]),
+    "kvm_create_kv8": (C.c_int, [C.POINTER(ModelDesc), C.c_int32, C.POINTER(C.c_int32), C.c_int32,
+                             C.POINTER(C.c_void_p)]),
     "kvm_destroy": (C.c_int, [C.c_void_p]),
     "kvm_last_error": (C.c_char_p, []),
     "kvm_load_prefix": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_int32),
@@ -418,10 +420,10 @@ def pinned_layer_inputs(inputs):
 
 
 class Context:
-    """A population of character states on the current CUDA device (kvm_create)."""
+    """A population of character states on the current CUDA device (kvm_create; kvm_create_kv8 with kv_bits=8)."""
 
     def __init__(self, layer_kind, n_q_heads, n_kv_heads, head_dim, rotary_dim, rope_theta,
-                 n_gdn_heads, d_k, d_v, capacity, max_tail_tokens, conv_kernel=0):
+                 n_gdn_heads, d_k, d_v, capacity, max_tail_tokens, conv_kernel=0, kv_bits=16):
         lib = load_library()
         self.layer_kind = [int(x) for x in layer_kind]
         self._kinds = _i32(self.layer_kind)
@@ -433,7 +435,11 @@ class Context:
         self.H, self.dk, self.dv = n_gdn_heads, d_k, d_v
         caps = _i32(capacity)
         h = C.c_void_p()
-        _check(lib.kvm_create(C.byref(self.desc), self.n_chars, _p32(caps), int(max_tail_tokens), C.byref(h)))
+        if kv_bits not in (8, 16):
+            raise ValueError(f"kv_bits must be 16 or 8, not {kv_bits}")
+        self.kv_bits = int(kv_bits)
+        create = lib.kvm_create_kv8 if self.kv_bits == 8 else lib.kvm_create
+        _check(create(C.byref(self.desc), self.n_chars, _p32(caps), int(max_tail_tokens), C.byref(h)))
         self._h = h
         self._draft_nodes = None
 
