@@ -2,14 +2,12 @@
 //
 //  kv8_append : a tail's keys, rotated in fp32, and its values into the blocks behind
 //               the live entries, each block formed whole (its older rows too, if the
-//               new ones need a larger scale); the tail's rotated queries into q_rot.
-//  kv8_widen  : blocks as bf16 rows (exact): what the tensor-core attention and the
-//               probe read, and kvm_get_kv.
-//  kv8_gather : a removal's survivors, widened, in their new places; kv8_pack then
-//               forms the blocks there (two launches over a bf16 copy: a block's scale
-//               is known only once all its rows are, and in place its rows' sources
-//               are other blocks' rows).
-//  kv8_pack   : bf16 rows into blocks; kvm_set_kv.
+//               new ones need a larger scale); the tail's rotated queries into q_rot; and
+//               all blocks that it sees as bf16 rows (exact), which the tensor-core
+//               attention reads.
+//  kv8_widen  : blocks as bf16 rows for kvm_get_kv and the probe.
+//  kv8_pack   : bf16 rows into blocks: kvm_set_kv.
+// (Removals: kv_compact.)
 //
 // All move a 64 x D block a thread block, bound by memory.  A row past the last one in
 // use is 0 in its block, so no number in a cache is ever other than finite: what is
@@ -22,6 +20,8 @@ namespace kvm {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAppendThreads = 512;
+constexpr int kPackThreads = 512;
 
 // The item's character (the last with blk_off <= item), block, head, and K or V.
 struct Item {
@@ -29,115 +29,131 @@ struct Item {
     bool is_v;
 };
 template <typename P>
-__device__ __forceinline__ Item item_of(const P& p, int item, int sides = 2) {
+__device__ __forceinline__ Item item_of(const P& p, const Kv8Char* ch, int item, int sides = 2) {
     int lo = 0, hi = p.n_chars - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (p.ch[mid].blk_off <= item) lo = mid; else hi = mid - 1;
+        if (ch[mid].blk_off <= item) lo = mid; else hi = mid - 1;
     }
-    const int local = item - p.ch[lo].blk_off, per = sides * p.Hkv;
-    return {lo, p.ch[lo].block0 + local / per, local % per / sides, sides == 2 && (local & 1)};
+    const int local = item - ch[lo].blk_off, per = sides * p.Hkv;
+    return {lo, ch[lo].block0 + local / per, local % per / sides, sides == 2 && (local & 1)};
 }
 
+template <int THREADS>
 __device__ __forceinline__ float block_max(float m, float* red) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, red[w]);
+    for (int w = 0; w < THREADS / 32; ++w) m = fmaxf(m, red[w]);
     return m;
 }
 
-__device__ __forceinline__ float2 bf2_f2(uint32_t w) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w)); }
-__device__ __forceinline__ uint32_t f2_bf2(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// (cos, sin) of a position's turn of a pair: pos * turn modulo a whole turn is the low
-// 64 bits of a product of integers, exact but for the 2^-64 that `turn` is rounded to
-// (2^-33 of a turn at position 2^31), where 64-bit floats take a hundred times as long.
-__device__ __forceinline__ void turn_of(int64_t pos, uint64_t turn, float& c, float& s) {
-    const int64_t frac = (int64_t)((uint64_t)pos * turn);              // in [-1/2, 1/2) turns
-    sincospif(__ll2float_rn(frac) * 0x1p-63f, &s, &c);
-}
-
-// A block of 64 rows of fp32 in shared memory, formed and stored.
-template <int D>
-__device__ __forceinline__ void store_block(const float* tile, float amax, uint8_t* dst, float* scale) {
-    const int e = kv8_exponent(amax);
-    const float inv = pow2(-e);
-    uint32_t* d = reinterpret_cast<uint32_t*>(dst);
-#pragma unroll 4
-    for (int i = threadIdx.x; i < kKv8Rows * D / 4; i += kThreads) {
-        const float4 x = reinterpret_cast<const float4*>(tile)[i];
-        d[i] = to_e4m3(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+// A block's 64 x D numbers as bf16 rows, those below `rows`.
+template <int D, int THREADS>
+__device__ __forceinline__ void widen_block(const uint8_t* from, float scale, __nv_bfloat16* to, int rows) {
+    constexpr int kAll = kKv8Rows * D / 16, kEach = (kAll + THREADS - 1) / THREADS;
+    const uint4* src = reinterpret_cast<const uint4*>(from);
+    uint4* dst = reinterpret_cast<uint4*>(to);
+    const int n = min(rows, kKv8Rows) * (D / 16);
+    uint4 w[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        if (i < n) w[k] = src[i];
     }
-    if (threadIdx.x == 0) *scale = pow2(e);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        uint4 a, b;
+        if (i < n) {
+            widen16(w[k], scale, a, b);
+            dst[2 * i] = a;
+            dst[2 * i + 1] = b;
+        }
+    }
 }
 
-// Blocks first, then a block of threads for each token's queries.
+// A packed tail token's queries, rotated.
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_append_kernel(const __grid_constant__ Kv8AppendParams p) {
+__device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, float* cs, float* sn) {
+    const int t = threadIdx.x, half = p.R / 2;
+    int lo = 0, hi = p.n_chars - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.tail_off[mid] <= n) lo = mid; else hi = mid - 1;
+    }
+    const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : p.p[lo] + n - p.tail_off[lo];
+    const __nv_bfloat16* q = p.q + (int64_t)n * p.Hq * D;
+    __nv_bfloat16* o = p.q_rot + (int64_t)n * p.Hq * D;
+    if (half % 8 == 0) {
+        const int per = half / 8 + (D - p.R) / 8;              // 16-byte pieces of a head: those turned in pairs first
+        uint4 a, b;
+        auto place = [&](int i) { return i / per * D + (i % per < half / 8 ? 8 * (i % per) : p.R + 8 * (i % per - half / 8)); };
+        auto load = [&](int i) {
+            if (i >= p.Hq * per) return;
+            a = *reinterpret_cast<const uint4*>(q + place(i));
+            if (i % per < half / 8) b = *reinterpret_cast<const uint4*>(q + place(i) + half);
+        };
+        load(t);                                               // under way during the angles
+        for (int d = t; d < half; d += kAppendThreads) turn_of(pos, p.turn[d], cs[d], sn[d]);
+        __syncthreads();
+        for (int i = t; i < p.Hq * per; i += kAppendThreads) {
+            if (i > t) load(i);
+            const int c = i % per;
+            if (c < half / 8) {
+                uint32_t* x = reinterpret_cast<uint32_t*>(&a);
+                uint32_t* y = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 u = bf2_f2(x[k]), v = bf2_f2(y[k]);
+                    const int d = 8 * c + 2 * k;
+                    x[k] = f2_bf2(u.x * cs[d] - v.x * sn[d], u.y * cs[d + 1] - v.y * sn[d + 1]);
+                    y[k] = f2_bf2(v.x * cs[d] + u.x * sn[d], v.y * cs[d + 1] + u.y * sn[d + 1]);
+                }
+                *reinterpret_cast<uint4*>(o + place(i) + half) = b;
+            }
+            *reinterpret_cast<uint4*>(o + place(i)) = a;
+        }
+        return;
+    }
+    for (int d = t; d < half; d += kAppendThreads) turn_of(pos, p.turn[d], cs[d], sn[d]);
+    __syncthreads();
+    for (int i = t; i < p.Hq * D; i += kAppendThreads) {
+        const int d = i % D;
+        const float x = __bfloat162float(q[i]);
+        o[i] = d >= p.R     ? q[i]
+               : d < half   ? __float2bfloat16_rn(x * cs[d] - __bfloat162float(q[i + half]) * sn[d])
+                            : __float2bfloat16_rn(x * cs[d - half] + __bfloat162float(q[i - half]) * sn[d - half]);
+    }
+}
+
+// Blocks first (the longest way), then the blocks in sight that only need widening, then
+// a thread block for each token's queries.  One launch for the three: 8192 entries and
+// 256 tokens of 16 heads of 256 took 11.1 us for blocks and queries and 8.5 behind them
+// for the widening.
+template <int D>
+__global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const __grid_constant__ Kv8AppendParams p) {
     extern __shared__ __align__(16) float tile[];              // [64][D]
-    __shared__ float red[kThreads / 32];
+    __shared__ float red[kAppendThreads / 32];
     __shared__ float cs[kMaxRotaryHalf], sn[kMaxRotaryHalf];
     grid_dependency_wait();
     grid_dependents_launch();
     const int t = threadIdx.x, half = p.R / 2;
-    if ((int)blockIdx.x >= p.n_items) {
-        const int n = blockIdx.x - p.n_items;                  // packed tail token
-        int lo = 0, hi = p.n_chars - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (p.tail_off[mid] <= n) lo = mid; else hi = mid - 1;
-        }
-        const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : p.p[lo] + n - p.tail_off[lo];
-        for (int d = t; d < half; d += kThreads) turn_of(pos, p.turn[d], cs[d], sn[d]);
-        const __nv_bfloat16* q = p.q + (int64_t)n * p.Hq * D;
-        __nv_bfloat16* o = p.q_rot + (int64_t)n * p.Hq * D;
-        if (half % 8 == 0) {
-            const int per = half / 8 + (D - p.R) / 8;          // 16-byte pieces of a head: those turned in pairs first
-            uint4 a, b;
-            auto place = [&](int i) { return i / per * D + (i % per < half / 8 ? 8 * (i % per) : p.R + 8 * (i % per - half / 8)); };
-            auto load = [&](int i) {
-                if (i >= p.Hq * per) return;
-                a = *reinterpret_cast<const uint4*>(q + place(i));
-                if (i % per < half / 8) b = *reinterpret_cast<const uint4*>(q + place(i) + half);
-            };
-            load(t);
-            __syncthreads();                                   // the angles are there
-            for (int i = t; i < p.Hq * per; i += kThreads) {
-                if (i > t) load(i);
-                const int c = i % per;
-                if (c < half / 8) {
-                    uint32_t* x = reinterpret_cast<uint32_t*>(&a);
-                    uint32_t* y = reinterpret_cast<uint32_t*>(&b);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 u = bf2_f2(x[k]), v = bf2_f2(y[k]);
-                        const int d = 8 * c + 2 * k;
-                        x[k] = f2_bf2(u.x * cs[d] - v.x * sn[d], u.y * cs[d + 1] - v.y * sn[d + 1]);
-                        y[k] = f2_bf2(v.x * cs[d] + u.x * sn[d], v.y * cs[d + 1] + u.y * sn[d + 1]);
-                    }
-                    *reinterpret_cast<uint4*>(o + place(i) + half) = b;
-                }
-                *reinterpret_cast<uint4*>(o + place(i)) = a;
-            }
-        } else {
-            __syncthreads();
-            for (int i = t; i < p.Hq * D; i += kThreads) {
-                const int d = i % D;
-                const float x = __bfloat162float(q[i]);
-                o[i] = d >= p.R     ? q[i]
-                       : d < half   ? __float2bfloat16_rn(x * cs[d] - __bfloat162float(q[i + half]) * sn[d])
-                                    : __float2bfloat16_rn(x * cs[d - half] + __bfloat162float(q[i - half]) * sn[d - half]);
-            }
-        }
+    if ((int)blockIdx.x >= p.n_items + p.n_widen) {
+        turn_queries<D>(p, blockIdx.x - p.n_items - p.n_widen, cs, sn);
         return;
     }
-    const Item it = item_of(p, blockIdx.x);
+    if ((int)blockIdx.x >= p.n_items) {
+        const Item it = item_of(p, p.old, blockIdx.x - p.n_items);
+        const int block = it.block + (it.block >= p.sink[it.b] ? p.gap[it.b] : 0);
+        const int64_t slot = (int64_t)it.head * p.slab_rows + p.old[it.b].cap_off + block * kKv8Rows;
+        widen_block<D, kAppendThreads>((it.is_v ? p.to.V : p.to.K) + slot * D, (it.is_v ? p.to.Vs : p.to.Ks)[slot / kKv8Rows],
+                                       (it.is_v ? p.V : p.K) + slot * D, kKv8Rows);
+        return;
+    }
+    const Item it = item_of(p, p.ch, blockIdx.x);
     const Kv8Char& c = p.ch[it.b];
     const int row0 = it.block * kKv8Rows, L = p.L_prev[it.b];
     const int old = min(max(L - row0, 0), kKv8Rows), end = min(c.rows - row0, kKv8Rows);   // rows [old, end) are new
@@ -146,30 +162,56 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(const __grid_const
     float* scale = (it.is_v ? p.to.Vs : p.to.Ks) + slot / kKv8Rows;
     const int n0 = p.tail_off[it.b] + row0 - L;                // packed token of the block's first row
     bool bad = false;
+    float m = 0.f;
     {
+        constexpr int kOld = (kKv8Rows * D / 16 + kAppendThreads - 1) / kAppendThreads, kNew = kKv8Rows * D / 8 / kAppendThreads;
         const float s = old ? *scale : 0.f;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(dst);
-#pragma unroll 4
-        for (int i = t; i < old * (D / 4); i += kThreads) {
-            const uint32_t w = src[i];
-            const float2 a = bf2_f2(e4m3_low(w)), b = bf2_f2(e4m3_high(w));
-            reinterpret_cast<float4*>(tile)[i] = make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
-        }
+        const uint4* src = reinterpret_cast<const uint4*>(dst);
         const __nv_bfloat16* x = it.is_v ? p.v_new : p.k_new;
-#pragma unroll 2
-        for (int i = old * (D / 8) + t; i < kKv8Rows * (D / 8); i += kThreads) {
-            const int r = i / (D / 8), d = i % (D / 8) * 8;
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (r < end) w = *reinterpret_cast<const uint4*>(x + ((int64_t)(n0 + r) * p.Hkv + it.head) * D + d);
-            bad = clear_not_finite(w) || bad;
-            const float2 a = bf2_f2(w.x), b = bf2_f2(w.y), e = bf2_f2(w.z), f = bf2_f2(w.w);
-            reinterpret_cast<float4*>(tile)[2 * i] = make_float4(a.x, a.y, b.x, b.y);
-            reinterpret_cast<float4*>(tile)[2 * i + 1] = make_float4(e.x, e.y, f.x, f.y);
+        uint4 was[kOld], is[kNew];
+#pragma unroll
+        for (int k = 0; k < kOld; ++k) {
+            const int i = t + k * kAppendThreads;
+            if (i < old * (D / 16)) was[k] = src[i];
+        }
+#pragma unroll
+        for (int k = 0; k < kNew; ++k) {
+            const int i = t + k * kAppendThreads, r = i / (D / 8);
+            is[k] = make_uint4(0, 0, 0, 0);
+            if (r >= old && r < end) is[k] = *reinterpret_cast<const uint4*>(x + ((int64_t)(n0 + r) * p.Hkv + it.head) * D + i % (D / 8) * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < kOld; ++k) {
+            const int i = t + k * kAppendThreads;
+            if (i < old * (D / 16)) {
+                m = fmaxf(m, e4m3_max(was[k]) * s);
+                const uint32_t w[4] = {was[k].x, was[k].y, was[k].z, was[k].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float2 a = bf2_f2(e4m3_low(w[q])), b = bf2_f2(e4m3_high(w[q]));
+                    reinterpret_cast<float4*>(tile)[4 * i + q] = make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
+                }
+            }
+        }
+        // the numbers that are not turned take part in the maximum here
+        const int flat = it.is_v ? 0 : p.R;
+#pragma unroll
+        for (int k = 0; k < kNew; ++k) {
+            const int i = t + k * kAppendThreads, d = i % (D / 8) * 8;
+            if (i / (D / 8) < old) continue;
+            bad = clear_not_finite(is[k]) || bad;
+            const float2 f[4] = {bf2_f2(is[k].x), bf2_f2(is[k].y), bf2_f2(is[k].z), bf2_f2(is[k].w)};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (d + 2 * q >= flat) m = fmaxf(m, fmaxf(fabsf(f[q].x), fabsf(f[q].y)));
+            }
+            reinterpret_cast<float4*>(tile)[2 * i] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+            reinterpret_cast<float4*>(tile)[2 * i + 1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
         }
     }
-    __syncthreads();
-    if (!it.is_v) {
-        for (int i = t; i < (end - old) * half; i += kThreads) {
+    if (!it.is_v && half) {
+        __syncthreads();
+        for (int i = t; i < (end - old) * half; i += kAppendThreads) {
             const int r = old + i / half, d = i % half;
             const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n0 + r] : p.p[it.b] + row0 + r - L;
             float co, si;
@@ -178,130 +220,64 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(const __grid_const
             float a = x[0] * co - x[half] * si, b = x[half] * co + x[0] * si;
             if (!isfinite(a)) { a = 0.f; bad = true; }         // two of the largest numbers together
             if (!isfinite(b)) { b = 0.f; bad = true; }
+            m = fmaxf(m, fmaxf(fabsf(a), fabsf(b)));
             x[0] = a;
             x[half] = b;
         }
-        if (it.head == 0)
-            for (int r = old + t; r < end; r += kThreads)
-                p.pos[c.cap_off + row0 + r] = p.tail_pos ? p.tail_pos[n0 + r] : (int32_t)(p.p[it.b] + row0 + r - L);
-        __syncthreads();
     }
-    float m = 0.f;
-#pragma unroll 4
-    for (int i = t; i < end * (D / 4); i += kThreads) {
-        const float4 x = reinterpret_cast<const float4*>(tile)[i];
-        m = fmaxf(m, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w))));
-    }
-    m = block_max(m, red);
-    store_block<D>(tile, m, dst, scale);
-    if (bad) atomicOr(p.err, kErrValue);
-}
-
-// Sixteen numbers as bf16, times a block's scale.
-__device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& a, uint4& b) {
-    const __nv_bfloat162 s = __float2bfloat162_rn(scale);
-    auto pair = [&](uint32_t x) {
-        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), s);
+    if (!it.is_v && it.head == 0)
+        for (int r = old + t; r < end; r += kAppendThreads)
+            p.pos[c.cap_off + row0 + r] = p.tail_pos ? p.tail_pos[n0 + r] : (int32_t)(p.p[it.b] + row0 + r - L);
+    m = block_max<kAppendThreads>(m, red);
+    const int e = kv8_exponent(m);
+    const float to = pow2(e), inv = pow2(-e);
+    uint32_t* d8 = reinterpret_cast<uint32_t*>(dst);
+    uint2* d16 = reinterpret_cast<uint2*>((it.is_v ? p.V : p.K) + slot * D);
+    const __nv_bfloat162 to2 = __float2bfloat162_rn(to);
+    auto wide = [&](uint32_t x) {
+        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), to2);
         return *reinterpret_cast<const uint32_t*>(&r);
     };
-    a = make_uint4(pair(e4m3_low(w.x)), pair(e4m3_high(w.x)), pair(e4m3_low(w.y)), pair(e4m3_high(w.y)));
-    b = make_uint4(pair(e4m3_low(w.z)), pair(e4m3_high(w.z)), pair(e4m3_low(w.w)), pair(e4m3_high(w.w)));
+#pragma unroll 4
+    for (int i = t; i < kKv8Rows * D / 4; i += kAppendThreads) {
+        const float4 x = reinterpret_cast<const float4*>(tile)[i];
+        const uint32_t w = to_e4m3(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+        d8[i] = w;
+        d16[i] = make_uint2(wide(e4m3_low(w)), wide(e4m3_high(w)));
+    }
+    if (t == 0) *scale = to;
+    if (bad) atomicOr(p.err, kErrValue);
 }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) kv8_widen_kernel(const __grid_constant__ Kv8WidenParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
-    Item it = item_of(p, blockIdx.x, p.V ? 2 : 1);
+    const Item it = item_of(p, p.ch, blockIdx.x, p.V ? 2 : 1);
     const Kv8Char& c = p.ch[it.b];
-    if (it.block - c.block0 >= p.sink[it.b]) it.block += p.gap[it.b];
     const int row0 = it.block * kKv8Rows;
     const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
-    const uint4* src = reinterpret_cast<const uint4*>((it.is_v ? p.from.V : p.from.K) + slot * D);
-    const float s = (it.is_v ? p.from.Vs : p.from.Ks)[slot / kKv8Rows];
-    uint4* dst = reinterpret_cast<uint4*>((it.is_v ? p.V : p.K) + ((int64_t)it.head * p.dst_rows + c.row0 + row0) * D);
-    const int n = min(c.rows - row0, kKv8Rows) * (D / 16);
-    constexpr int kEach = kKv8Rows * D / 16 / kThreads;        // 1, 2 or 4 vectors a thread
-    uint4 w[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        if (i < n) w[k] = src[i];
-    }
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        uint4 a, b;
-        if (i < n) {
-            widen16(w[k], s, a, b);
-            dst[2 * i] = a;
-            dst[2 * i + 1] = b;
-        }
-    }
+    widen_block<D, kThreads>((it.is_v ? p.from.V : p.from.K) + slot * D, (it.is_v ? p.from.Vs : p.from.Ks)[slot / kKv8Rows],
+                             (it.is_v ? p.V : p.K) + ((int64_t)it.head * p.dst_rows + c.row0 + row0) * D, c.rows - row0);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_gather_kernel(const __grid_constant__ Kv8GatherParams p) {
+__global__ void __launch_bounds__(kPackThreads) kv8_pack_kernel(const __grid_constant__ Kv8PackParams p) {
+    __shared__ float red[kPackThreads / 32];
     grid_dependency_wait();
     grid_dependents_launch();
-    const Item it = item_of(p, blockIdx.x);
-    const Kv8Char& c = p.ch[it.b];
-    const int32_t* seg_start = p.seg_start + p.seg_off[it.b];
-    const int32_t* seg_shift = p.seg_shift + p.seg_off[it.b];
-    const int n_seg = p.n_seg[it.b];
-    const uint8_t* from = it.is_v ? p.from.V : p.from.K;
-    const float* scales = it.is_v ? p.from.Vs : p.from.Ks;
-    __nv_bfloat16* to = it.is_v ? p.V : p.K;
-    const int row0 = it.block * kKv8Rows, n = min(c.rows - row0, kKv8Rows) * (D / 16);
-    const int64_t base = (int64_t)it.head * p.slab_rows + c.cap_off;
-    constexpr int kEach = kKv8Rows * D / 16 / kThreads;
-    uint4 w[kEach];
-    float s[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        if (i >= n) continue;
-        int row = row0 + i / (D / 16);
-        if (row >= p.first[it.b]) {                            // the last segment that starts at or before it
-            int lo = 0, hi = n_seg - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (seg_start[mid] <= row) lo = mid; else hi = mid - 1;
-            }
-            row += seg_shift[lo];
-        }
-        w[k] = *reinterpret_cast<const uint4*>(from + (base + row) * D + i % (D / 16) * 16);
-        s[k] = scales[(base + row) / kKv8Rows];
-    }
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kThreads;
-        if (i >= n) continue;
-        uint4* dst = reinterpret_cast<uint4*>(to + (base + row0) * D) + 2 * i;
-        uint4 a, b;
-        widen16(w[k], s[k], a, b);
-        dst[0] = a;
-        dst[1] = b;
-    }
-}
-
-template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_pack_kernel(const __grid_constant__ Kv8PackParams p) {
-    __shared__ float red[kThreads / 32];
-    grid_dependency_wait();
-    grid_dependents_launch();
-    const Item it = item_of(p, blockIdx.x);
+    const Item it = item_of(p, p.ch, blockIdx.x);
     const Kv8Char& c = p.ch[it.b];
     const int row0 = it.block * kKv8Rows, n = min(c.rows - row0, kKv8Rows) * (D / 8);
     const uint4* src = reinterpret_cast<const uint4*>((it.is_v ? p.V : p.K) + ((int64_t)it.head * p.src_rows + c.row0 + row0) * D);
     const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
-    constexpr int kEach = kKv8Rows * D / 8 / kThreads;         // 2, 4 or 8 vectors a thread
+    constexpr int kEach = kKv8Rows * D / 8 / kPackThreads;     // 1, 2 or 4 vectors a thread
     uint4 w[kEach];
     float m = 0.f;
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kThreads;
+        const int i = threadIdx.x + k * kPackThreads;
         w[k] = i < n ? src[i] : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
@@ -314,14 +290,14 @@ __global__ void __launch_bounds__(kThreads) kv8_pack_kernel(const __grid_constan
             m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
         }
     }
-    m = block_max(m, red);
+    m = block_max<kPackThreads>(m, red);
     const int e = kv8_exponent(m);
     const float inv = pow2(-e);
     uint2* dst = reinterpret_cast<uint2*>((it.is_v ? p.to.V : p.to.K) + slot * D);
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const float2 a = bf2_f2(w[k].x), b = bf2_f2(w[k].y), f = bf2_f2(w[k].z), g = bf2_f2(w[k].w);
-        dst[threadIdx.x + k * kThreads] = make_uint2(to_e4m3(a.x * inv, a.y * inv, b.x * inv, b.y * inv),
+        dst[threadIdx.x + k * kPackThreads] = make_uint2(to_e4m3(a.x * inv, a.y * inv, b.x * inv, b.y * inv),
                                                      to_e4m3(f.x * inv, f.y * inv, g.x * inv, g.y * inv));
     }
     if (threadIdx.x == 0) (it.is_v ? p.to.Vs : p.to.Ks)[slot / kKv8Rows] = pow2(e);
@@ -338,7 +314,7 @@ void launch_append(const Kv8AppendParams& p, cudaStream_t s) {
         cudaFuncSetAttribute(kv8_append_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(kv8_append_kernel<D>, dim3(p.n_items + p.total), dim3(kThreads), smem, s, p);
+    launch_pdl(kv8_append_kernel<D>, dim3(p.n_items + p.n_widen + p.total), dim3(kAppendThreads), smem, s, p);
 }
 
 }  // namespace
@@ -356,16 +332,10 @@ void launch_kv8_widen(const Kv8WidenParams& p, cudaStream_t s) {
                dim3(kThreads), 0, s, p);
 }
 
-void launch_kv8_gather(const Kv8GatherParams& p, cudaStream_t s) {
-    if (p.n_items <= 0) return;
-    launch_pdl(p.D == 64 ? kv8_gather_kernel<64> : p.D == 128 ? kv8_gather_kernel<128> : kv8_gather_kernel<256>, dim3(p.n_items),
-               dim3(kThreads), 0, s, p);
-}
-
 void launch_kv8_pack(const Kv8PackParams& p, cudaStream_t s) {
     if (p.n_items <= 0) return;
     launch_pdl(p.D == 64 ? kv8_pack_kernel<64> : p.D == 128 ? kv8_pack_kernel<128> : kv8_pack_kernel<256>, dim3(p.n_items),
-               dim3(kThreads), 0, s, p);
+               dim3(kPackThreads), 0, s, p);
 }
 
 }  // namespace kvm

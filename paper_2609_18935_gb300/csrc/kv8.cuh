@@ -48,4 +48,48 @@ __device__ __forceinline__ uint32_t e4m3_pair(uint32_t x) {
 __device__ __forceinline__ uint32_t e4m3_low(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x1000)); }
 __device__ __forceinline__ uint32_t e4m3_high(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x3020)); }
 
+
+__device__ __forceinline__ float2 bf2_f2(uint32_t w) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w)); }
+__device__ __forceinline__ uint32_t f2_bf2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// (cos, sin) of a position's turn of a pair: pos * turn modulo a whole turn is the low
+// 64 bits of a product of integers, exact but for the 2^-64 that `turn` is rounded to
+// (2^-33 of a turn at position 2^31), where 64-bit floats take a hundred times as long.
+__device__ __forceinline__ void turn_of(int64_t pos, uint64_t turn, float& c, float& s) {
+    const int64_t frac = (int64_t)((uint64_t)pos * turn);              // in [-1/2, 1/2) turns
+    sincospif(__ll2float_rn(frac) * 0x1p-63f, &s, &c);
+}
+
+// Sixteen numbers as bf16, times a block's scale (exactly: see the least exponent above).
+__device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& a, uint4& b) {
+    const __nv_bfloat162 s = __float2bfloat162_rn(scale);
+    auto pair = [&](uint32_t x) {
+        const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), s);
+        return *reinterpret_cast<const uint32_t*>(&r);
+    };
+    a = make_uint4(pair(e4m3_low(w.x)), pair(e4m3_high(w.x)), pair(e4m3_low(w.y)), pair(e4m3_high(w.y)));
+    b = make_uint4(pair(e4m3_low(w.z)), pair(e4m3_high(w.z)), pair(e4m3_low(w.w)), pair(e4m3_high(w.w)));
+}
+
+// Largest magnitude of sixteen numbers, as their bytes' order has it.
+__device__ __forceinline__ float e4m3_max(const uint4& w) {
+    const uint32_t k = 0x7f7f7f7fu;
+    const uint32_t m = __vmaxu4(__vmaxu4(w.x & k, w.y & k), __vmaxu4(w.z & k, w.w & k));
+    const uint32_t h = __vmaxu4(m, m >> 16), b = max(h & 0xffu, h >> 8 & 0xffu);
+    return __uint_as_float(e4m3_pair(b << 8) << 16);
+}
+
+// Sixteen numbers of scale `from` under the scale whose reciprocal is `inv`.
+__device__ __forceinline__ uint4 requantised(const uint4& w, float from, float inv) {
+    auto word = [&](uint32_t x) {
+        const uint32_t lo = e4m3_low(x), hi = e4m3_high(x);
+        auto f = [&](uint32_t bits) { return __uint_as_float(bits) * from * inv; };
+        return to_e4m3(f(lo << 16), f(lo & 0xffff0000u), f(hi << 16), f(hi & 0xffff0000u));
+    };
+    return make_uint4(word(w.x), word(w.y), word(w.z), word(w.w));
+}
+
 }  // namespace kvm

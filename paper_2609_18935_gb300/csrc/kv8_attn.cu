@@ -7,6 +7,11 @@
 // bf16 operands would have to pass through shared memory; here a warp turns its bytes
 // into bf16 in registers and feeds them to the products there.
 //
+// One launch takes in the tail: a block turns its rows' queries itself, and the block
+// whose range holds the end of a character's cache puts the new keys and values there
+// (a character has one query tile a KV head, so no other block reads that end).  As a
+// launch before this one that took 4 - 8 us of a step.
+//
 // The partition is the tensor-core attention's: 64-key units in contiguous ranges, a
 // block an SM, partials of shared tiles for attn_combine.  A warp takes every kWarps-th
 // 16 keys of a segment through a ring of its own in shared memory (cp.async, no barrier
@@ -20,6 +25,7 @@
 // each lane g.  The rings' 16-byte pieces are turned by their row, so that each quarter
 // of a warp reads all banks.
 #include "attn_tiles.cuh"
+#include "draft_rows.cuh"
 #include "kv8.cuh"
 #include "kvm_internal.cuh"
 #include "sm100_ptx.cuh"
@@ -44,7 +50,13 @@ struct Cfg {
     static constexpr int ROWS = 8 * NT;
     static constexpr int PITCH = D + 4;                        // floats of a merged row
     static constexpr int MERGE = kWarps * ROWS * PITCH * 4;
-    static constexpr int SMEM = (kWarps * RING > MERGE ? kWarps * RING : MERGE) + 2 * kWarps * ROWS * 4;
+    // behind the rings: the warps' references and sums, a maximum of K and of V a warp,
+    // the rows' turns, and their queries (bf16) or new keys (fp32)
+    static constexpr int OFF_WM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
+    static constexpr int OFF_RED = OFF_WM + 2 * kWarps * ROWS * 4;
+    static constexpr int OFF_TURN = OFF_RED + 2 * kWarps * 4;
+    static constexpr int OFF_X = OFF_TURN + ROWS * D * 4;
+    static constexpr int SMEM = OFF_X + ROWS * D * 4;
 };
 static_assert(Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448, "shared memory");
 
@@ -75,9 +87,127 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t f2_bf2(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+
+// The new keys and values of one head that lie in key tile kt: into the cache's block, and
+// the whole block under a larger (or smaller) scale where they need it.  By all threads,
+// between two barriers of the block.
+template <int D, int NT>
+__device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt, float* red, const float2* turn,
+                                           float* keys) {
+    constexpr int kOld = kKv8Rows * D / 16 / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
+    const AttnParams& p = pp.a;
+    const int tid = threadIdx.x, half = p.R / 2, row0 = kt * kAttnKeys;
+    const int old = min(max(ch.L_prev - row0, 0), kKv8Rows), n = min(ch.L_prev + ch.M - row0, kKv8Rows) - old;
+    const int tok0 = row0 + old - ch.L_prev;                   // of the new rows
+    const int64_t slot = (int64_t)kvh * p.slab_rows + ch.cap_off + row0, src = ((int64_t)(ch.tail_off + tok0) * p.Hkv + kvh) * D;
+    const int64_t row = (int64_t)p.Hkv * D;
+    uint4* bk = reinterpret_cast<uint4*>(pp.from.K + slot * D);
+    uint4* bv = reinterpret_cast<uint4*>(pp.from.V + slot * D);
+    float* pk = pp.from.Ks + slot / kKv8Rows;
+    float* pv = pp.from.Vs + slot / kKv8Rows;
+    const float sk = old ? *pk : 0.f, sv = old ? *pv : 0.f;
+    uint4 wk[kOld], wv[kOld], nv[kNew];
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) {
+        const int i = tid + k * kThreads;
+        wk[k] = wv[k] = make_uint4(0, 0, 0, 0);
+        if (i < old * (D / 16)) {
+            wk[k] = bk[i];
+            wv[k] = bv[i];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kNew; ++k) {
+        const int i = tid + k * kThreads;
+        nv[k] = make_uint4(0, 0, 0, 0);
+        if (i < n * (D / 8)) nv[k] = *reinterpret_cast<const uint4*>(p.v_new + src + i / (D / 8) * row + i % (D / 8) * 8);
+    }
+    float mk = 0.f, mv = 0.f;
+    bool bad = false;
+    auto key = [&](int r, int d) {
+        __nv_bfloat16 x = p.k_new[src + r * row + d];
+        bad = clear_not_finite(x) || bad;
+        return __bfloat162float(x);
+    };
+    for (int i = tid; i < n * half; i += kThreads) {
+        const int r = i / half, d = i % half;
+        const float2 t = turn[(tok0 + r) * half + d];
+        const float x = key(r, d), y = key(r, d + half);
+        float a = x * t.x - y * t.y, b = y * t.x + x * t.y;
+        if (!isfinite(a)) { a = 0.f; bad = true; }             // two of the largest numbers together
+        if (!isfinite(b)) { b = 0.f; bad = true; }
+        keys[r * D + d] = a;
+        keys[r * D + d + half] = b;
+        mk = fmaxf(mk, fmaxf(fabsf(a), fabsf(b)));
+    }
+    for (int i = tid; i < n * (D - p.R); i += kThreads) {
+        const int r = i / (D - p.R), d = p.R + i % (D - p.R);
+        const float x = key(r, d);
+        keys[r * D + d] = x;
+        mk = fmaxf(mk, fabsf(x));
+    }
+#pragma unroll
+    for (int k = 0; k < kNew; ++k) {
+        bad = clear_not_finite(nv[k]) || bad;
+        const uint32_t w[4] = {nv[k].x, nv[k].y, nv[k].z, nv[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = bf2_f2(w[e]);
+            mv = fmaxf(mv, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) {
+        mk = fmaxf(mk, e4m3_max(wk[k]) * sk);
+        mv = fmaxf(mv, e4m3_max(wv[k]) * sv);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        mk = fmaxf(mk, __shfl_xor_sync(0xffffffffu, mk, o));
+        mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, o));
+    }
+    if ((tid & 31) == 0) {
+        red[tid >> 5] = mk;
+        red[kWarps + (tid >> 5)] = mv;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        mk = fmaxf(mk, red[w]);
+        mv = fmaxf(mv, red[kWarps + w]);
+    }
+    const int ek = kv8_exponent(mk), ev = kv8_exponent(mv);
+    const float tk = pow2(ek), tv = pow2(ev), ik = pow2(-ek), iv = pow2(-ev);
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) {
+        const int i = tid + k * kThreads;
+        if (i < old * (D / 16)) {
+            if (tk != sk) bk[i] = requantised(wk[k], sk, ik);
+            if (tv != sv) bv[i] = requantised(wv[k], sv, iv);
+        }
+    }
+    for (int i = tid; i < n * (D / 4); i += kThreads) {
+        const float4 x = reinterpret_cast<const float4*>(keys)[i];
+        reinterpret_cast<uint32_t*>(bk)[old * (D / 4) + i] = to_e4m3(x.x * ik, x.y * ik, x.z * ik, x.w * ik);
+    }
+#pragma unroll
+    for (int k = 0; k < kNew; ++k) {
+        const int i = tid + k * kThreads;
+        const float2 a = bf2_f2(nv[k].x), b = bf2_f2(nv[k].y), c = bf2_f2(nv[k].z), d = bf2_f2(nv[k].w);
+        if (i < n * (D / 8))
+            reinterpret_cast<uint2*>(bv)[old * (D / 8) + i] =
+                make_uint2(to_e4m3(a.x * iv, a.y * iv, b.x * iv, b.y * iv), to_e4m3(c.x * iv, c.y * iv, d.x * iv, d.y * iv));
+    }
+    if (tid == 0) {
+        *pk = tk;
+        *pv = tv;
+    }
+    if (kvh == 0 && tid < n) {
+        const int t = tok0 + tid;
+        p.pos[ch.cap_off + row0 + old + tid] = p.tail_pos ? p.tail_pos[ch.tail_off + t] : (int32_t)(ch.p + t);
+    }
+    if (bad) atomicOr(p.err, kErrValue);
+    __syncthreads();
 }
 
 template <int D, int NT>
@@ -90,8 +220,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
     uint8_t* ring = smem + warp * C::RING;
     const uint32_t ring_at = smem_u32(ring);
     float* meet = reinterpret_cast<float*>(smem);              // [warp][row][PITCH], once the rings are done
-    float* wm = reinterpret_cast<float*>(smem + C::SMEM - 2 * kWarps * C::ROWS * 4);   // [warp][row]: reference, then sum
+    float* wm = reinterpret_cast<float*>(smem + C::OFF_WM);    // [warp][row]: reference, then sum
     float* wl = wm + kWarps * C::ROWS;
+    float2* turn = reinterpret_cast<float2*>(smem + C::OFF_TURN);                      // [token][R / 2]
+    __nv_bfloat16* q_s = reinterpret_cast<__nv_bfloat16*>(smem + C::OFF_X);            // [row][D]
 
     // the block's segments, as the tensor-core attention walks them
     const int cta = blockIdx.x, waves = p.waves;
@@ -99,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
     const int t_end = p.cta_tile[cta + 1], k_end = p.cta_k[cta + 1];
     const int n_seg = waves + ((t_begin == t_end && k_begin == k_end) ? 0 : t_end - t_begin + (k_end > 0 ? 1 : 0));
 
-    // the blocks behind the live entries were formed by the grid before; it also wrote q_rot
+    // a removal, or the layer's last step, wrote the cache
     grid_dependency_wait();
     grid_dependents_launch();
 
@@ -114,38 +246,92 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
         const int rows = (T.tok_end - T.tok0) * p.g;           // of them real
 
         // step s of the segment into ring place `at`
-        auto fetch = [&](int s, int at) {
-            if (s < steps) {
-                const int64_t row = slab + (int64_t)key_tile<true>(T, k0 + s / 4) * kAttnKeys + s % 4 * kStep;
-                const uint8_t* k = pp.from.K + row * D;
-                const uint8_t* v = pp.from.V + row * D;
-                const uint32_t to = ring_at + at * C::STAGE;
+        auto load = [&](int s, int at) {
+            if (s >= steps) return;
+            const int64_t row = slab + (int64_t)key_tile<true>(T, k0 + s / 4) * kAttnKeys + s % 4 * kStep;
+            const uint8_t* k = pp.from.K + row * D;
+            const uint8_t* v = pp.from.V + row * D;
+            const uint32_t to = ring_at + at * C::STAGE;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    const int id = c * 32 + lane, r = id / (D / 16), col = id % (D / 16);
-                    const uint32_t o = to + piece<D>(r, col);
-                    cp16(o, k + id * 16);
-                    cp16(o + C::SIDE, v + id * 16);
-                }
-                if (lane < 2) cp4(to + 2 * C::SIDE + 4 * lane, (lane ? pp.from.Vs : pp.from.Ks) + row / kKv8Rows);
+            for (int c = 0; c < D / 32; ++c) {
+                const int id = c * 32 + lane, r = id / (D / 16), col = id % (D / 16);
+                const uint32_t o = to + piece<D>(r, col);
+                cp16(o, k + id * 16);
+                cp16(o + C::SIDE, v + id * 16);
             }
-            cp_commit();
+            if (lane < 2) cp4(to + 2 * C::SIDE + 4 * lane, (lane ? pp.from.Vs : pp.from.Ks) + row / kKv8Rows);
         };
+        // units from `fresh` on have new rows (a query tile holds all of its character's): this block
+        // forms those of its range before anyone loads them, the others are under way meanwhile
+        const int fresh = ch.L_prev / kAttnKeys - T.gap;
+        const bool forms = fresh < k1;
 #pragma unroll
-        for (int s = 0; s < C::STAGES - 1; ++s) fetch(warp + s * kWarps, s);
-
+        for (int s = 0; s < C::STAGES - 1; ++s) {
+            const int step = warp + s * kWarps;
+            if (!forms || k0 + step / 4 < fresh) load(step, s);
+            if (!forms) cp_commit();
+        }
+        {
+            const int half = p.R / 2;
+            for (int i = tid; i < ch.M * half; i += kThreads) {
+                const int t = i / half;
+                const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[ch.tail_off + t] : ch.p + t;
+                turn_of(pos, pp.turn[i % half], turn[i].x, turn[i].y);
+            }
+            auto row_of = [&](int r) { return p.q + ((int64_t)(ch.tail_off + r / p.g) * p.Hq + T.kvh * p.g + r % p.g) * D; };
+            if (half % 8 == 0) {
+                const int per = half / 8 + (D - p.R) / 8;      // 16-byte pieces of a row: those turned in pairs first
+                uint4 a, b;
+                auto place = [&](int i) { return i % per < half / 8 ? 8 * (i % per) : p.R + 8 * (i % per - half / 8); };
+                auto get = [&](int i) {
+                    if (i >= rows * per) return;
+                    const __nv_bfloat16* x = row_of(i / per) + place(i);
+                    a = *reinterpret_cast<const uint4*>(x);
+                    if (i % per < half / 8) b = *reinterpret_cast<const uint4*>(x + half);
+                };
+                get(tid);
+                __syncthreads();                               // the turns are there
+                for (int i = tid; i < rows * per; i += kThreads) {
+                    if (i > tid) get(i);
+                    __nv_bfloat16* o = q_s + i / per * D + place(i);
+                    if (i % per < half / 8) {
+                        const float2* t = turn + i / per / p.g * half + place(i);
+                        uint32_t* x = reinterpret_cast<uint32_t*>(&a);
+                        uint32_t* y = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 u = bf2_f2(x[k]), v = bf2_f2(y[k]), t0 = t[2 * k], t1 = t[2 * k + 1];
+                            x[k] = f2_bf2(u.x * t0.x - v.x * t0.y, u.y * t1.x - v.y * t1.y);
+                            y[k] = f2_bf2(v.x * t0.x + u.x * t0.y, v.y * t1.x + u.y * t1.y);
+                        }
+                        *reinterpret_cast<uint4*>(o + half) = b;
+                    }
+                    *reinterpret_cast<uint4*>(o) = a;
+                }
+            } else {
+                __syncthreads();
+                for (int i = tid; i < rows * D; i += kThreads) {
+                    const int r = i / D, d = i % D;
+                    const __nv_bfloat16* x = row_of(r) + d;
+                    const float2* t = turn + r / p.g * half;
+                    q_s[i] = d >= p.R   ? *x
+                             : d < half ? __float2bfloat16_rn(__bfloat162float(x[0]) * t[d].x - __bfloat162float(x[half]) * t[d].y)
+                                        : __float2bfloat16_rn(__bfloat162float(x[0]) * t[d - half].x + __bfloat162float(x[-half]) * t[d - half].y);
+                }
+            }
+            __syncthreads();
+        }
         // Q: a lane's words of each step of the sum, rows g (and g + 8)
         uint32_t q[NT][KS][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = 8 * n + g;
-            const bool real = r < rows;
-            const __nv_bfloat16* src = p.q_rot + ((int64_t)(ch.tail_off + T.tok0 + (real ? r / p.g : 0)) * p.Hq + T.kvh * p.g + (real ? r % p.g : 0)) * D;
+            const __nv_bfloat16* src = q_s + r * D;
 #pragma unroll
             for (int c = 0; c < KS / 4; ++c) {
                 const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
                 uint4 a = make_uint4(0, 0, 0, 0), b = a;
-                if (real) {
+                if (r < rows) {
                     a = *reinterpret_cast<const uint4*>(src + 16 * col);
                     b = *reinterpret_cast<const uint4*>(src + 16 * col + 8);
                 }
@@ -153,6 +339,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 q[n][4 * c + 1][0] = a.z; q[n][4 * c + 1][1] = a.w;
                 q[n][4 * c + 2][0] = b.x; q[n][4 * c + 2][1] = b.y;
                 q[n][4 * c + 3][0] = b.z; q[n][4 * c + 3][1] = b.w;
+            }
+        }
+        if (forms) {
+            __syncthreads();                                   // the queries' place takes the new keys
+            for (int u = max(k0, fresh); u < k1; ++u)
+                form_block<D, NT>(pp, ch, T.kvh, key_tile<true>(T, u), reinterpret_cast<float*>(smem + C::OFF_RED), turn,
+                                  reinterpret_cast<float*>(smem + C::OFF_X));
+#pragma unroll
+            for (int s = 0; s < C::STAGES - 1; ++s) {
+                const int step = warp + s * kWarps;
+                if (k0 + step / 4 >= fresh) load(step, s);
+                cp_commit();
             }
         }
         // rows 8 n + 2 j and the next: their live indices, references, and this lane's share of the sums
@@ -181,7 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             const uint8_t* vt = kt + C::SIDE;
             const float ks = *reinterpret_cast<const float*>(kt + 2 * C::SIDE) * p.scale_log2;
             const float vs = *reinterpret_cast<const float*>(kt + 2 * C::SIDE + 4);
-            fetch(s + (C::STAGES - 1) * kWarps, (i + C::STAGES - 1) % C::STAGES);
+            load(s + (C::STAGES - 1) * kWarps, (i + C::STAGES - 1) % C::STAGES);
+            cp_commit();
             float sc[NT][2][4];                                // two chains of products
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -339,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             } else {
                 reinterpret_cast<float4*>(p.part_o + (slot * (D / 32) + d4 / 8) * 8 * BM * 4)[d4 % 8 * BM + r] = acc;
                 if (d4 == 0) {
-                    p.part_ml[(slot * BM + r) * 2] = top;
+                    p.part_ml[(slot * BM + r) * 2] = lt == lt ? top : 0.f;   // a query that is not finite: NaN, not nothing
                     p.part_ml[(slot * BM + r) * 2 + 1] = lt;
                 }
             }

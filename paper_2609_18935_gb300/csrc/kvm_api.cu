@@ -423,6 +423,7 @@ kvm_status plan_spans(const kvm_ctx* c, const int32_t* span_cu, const int32_t* s
 struct PlanCost {
     int min_units;                                   // smallest share of a block
     double segment;                                  // extra cost of a segment, in units
+    int whole = kWholeTile;                          // tiles of up to this many units get a block each
 };
 constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 // A draft has few query tiles with long key lists: what a segment costs beside its
@@ -432,6 +433,10 @@ constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 // | 101.5 | 98.9 | 97.9 | 100.6; one character the same with all).  Three units at least: one character's 4 nodes over 8K 14.0 with four, 13.7
 // with three, 14.4 with two.
 constexpr PlanCost kDraftCost{3, 32.0};
+
+// Few rows over 8-bit caches (kv8_attn.cu): a unit is 128 D bytes to load, a segment the
+// rows' queries, the warps' meeting and the partials, whatever D is.
+PlanCost kv8_cost(int D) { return {1024 / D, 2048.0 / D, 4096 / D}; }
 
 // What a layer's rows see: of a windowed layer (kvm_set_window) fewer key tiles, the
 // same for all query tiles of a draft, whose first rows all follow the last live entry.
@@ -461,7 +466,7 @@ void plan_attention(int B, const int* L_prev, const int* M, int Hkv, int tpt, in
                 units += nk_of.back();
             }
     pl.n_tiles = tiles;
-    if (deal && tiles > 0 && tiles <= grid_cap && *std::max_element(nk_of.begin(), nk_of.end()) <= kWholeTile) {
+    if (deal && tiles > 0 && tiles <= grid_cap && *std::max_element(nk_of.begin(), nk_of.end()) <= cost_of.whole) {
         // short key lists: a block a tile, nothing to merge
         pl.n_ctas = tiles;
         pl.waves = 0;
@@ -609,7 +614,7 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     const int kv_layers = c->kv8 ? 1 : c->n_attn;          // of the bf16 slabs
     const size_t layer_elems = (size_t)c->Hkv * c->T_cap * c->D, kv_elems = (size_t)kv_layers * layer_elems;
     const int vec_per_row = c->D * 2 / 16;
-    c->rows_kv = c->n_attn ? kCompactVecPerChunk / std::max(vec_per_row, 1) : 1;
+    c->rows_kv = c->kv8 ? kKv8Rows : c->n_attn ? kCompactVecPerChunk / std::max(vec_per_row, 1) : 1;
     c->rows_pos = kCompactVecPerChunk;
     const int n_kv_slabs = 2 * c->n_attn * c->Hkv;
     size_t n_flags = 0;
@@ -864,29 +869,26 @@ kvm_status widen_char(kvm_ctx* c, int a, int b, void* k, void* v, int row0, int6
     p.V = static_cast<__nv_bfloat16*>(v);
     const int L = c->live[b], rows = block_rows ? (L + kKv8Rows - 1) / kKv8Rows * kKv8Rows : L;
     p.ch[0] = kv8_char(c, b, 0, rows, row0, v ? 2 : 1, p.n_items);
-    p.sink[0] = p.gap[0] = 0;
     ++c->launches;
     launch_kv8_widen(p, s);
     LAUNCH_CHECK(c);
     return KVM_OK;
 }
 
-// bf16 rows of every character with a block0 >= 0, up to rows[b], into blocks of layer a.
-kvm_status pack_chars(kvm_ctx* c, int a, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t src_rows, const Kv8Char* ch, int n_chars,
-                      int items, cudaStream_t s) {
-    if (!items) return KVM_OK;
+// bf16 rows of character b into blocks of layer a.
+kvm_status pack_char(kvm_ctx* c, int a, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t src_rows, int b, int row0, cudaStream_t s) {
     thread_local static Kv8PackParams p;
     p.to = kv8_layer(c, a);
-    p.n_chars = n_chars;
+    p.n_chars = 1;
     p.Hkv = c->Hkv;
     p.D = c->D;
-    p.n_items = items;
+    p.n_items = 0;
     p.slab_rows = c->T_cap;
     p.src_rows = src_rows;
     p.K = k;
     p.V = v;
     p.err = c->err;
-    std::copy(ch, ch + n_chars, p.ch);
+    p.ch[0] = kv8_char(c, b, 0, c->live[b], row0, 2, p.n_items);
     ++c->launches;
     launch_kv8_pack(p, s);
     LAUNCH_CHECK(c);
@@ -910,10 +912,7 @@ kvm_status copy_kv8(kvm_ctx* c, int a, int b, void* k, void* v, bool in, cudaStr
     }
     if (!own) st = copy_slabs(c, 0, b, k, v, true, s);
     if (st) return st;
-    int items = 0;
-    const Kv8Char ch = kv8_char(c, b, 0, L, row0, 2, items);
-    return pack_chars(c, a, own ? static_cast<const __nv_bfloat16*>(k) : c->K, own ? static_cast<const __nv_bfloat16*>(v) : c->V, rows, &ch, 1,
-                      items, s);
+    return pack_char(c, a, own ? static_cast<const __nv_bfloat16*>(k) : c->K, own ? static_cast<const __nv_bfloat16*>(v) : c->V, rows, b, row0, s);
 }
 
 // KV of character b in attention layer `layer`: slab rows of every KV head.
@@ -1222,59 +1221,29 @@ extern "C" kvm_status kvm_plan_spans_from_positions(int32_t live, const int32_t*
 // ============================================================================
 namespace {
 
-// A removal in 8-bit layers [a_lo, a_hi): the survivors, widened, to their new places in
-// the bf16 slabs, and back into blocks from the first removed entry's on.
-kvm_status compact_kv8(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int a_lo, int a_hi) {
-    thread_local static Kv8GatherParams p;
-    p.n_chars = c->B;
-    p.Hkv = c->Hkv;
-    p.D = c->D;
-    p.slab_rows = c->T_cap;
-    p.K = c->K;
-    p.V = c->V;
-    p.n_items = 0;
-    for (int b = 0; b < c->B; ++b) {
-        const bool any = pl.n_seg[b] > 0;
-        p.ch[b] = kv8_char(c, b, any ? pl.first[b] / kKv8Rows : 0, any ? pl.L_new[b] : 0, c->cap_off[b], 2, p.n_items);
-        p.first[b] = pl.first[b];
-        p.seg_off[b] = pl.seg_off[b];
-        p.n_seg[b] = pl.n_seg[b];
-    }
-    if (!p.n_items) return KVM_OK;
-    std::copy(pl.seg_start.begin(), pl.seg_start.end(), p.seg_start);
-    std::copy(pl.seg_shift.begin(), pl.seg_shift.end(), p.seg_shift);
-    for (int a = a_lo; a < a_hi; ++a) {
-        p.from = kv8_layer(c, a);
-        const int ps = prof_begin(c, KVM_K_COMPACT, s);
-        launch_kv8_gather(p, s);
-        LAUNCH_CHECK(c);
-        const kvm_status st = pack_chars(c, a, c->K, c->V, c->T_cap, p.ch, c->B, p.n_items, s);
-        prof_end(c, ps, s);
-        if (st) return st;
-    }
-    return KVM_OK;
-}
-
 // Compaction of the attention layers [a_lo, a_hi) (K and V slabs of those
 // layers, and the position slab when with_pos) under a validated plan.
 kvm_status launch_compaction(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int a_lo, int a_hi, bool with_pos) {
-    if (c->kv8 && a_hi > a_lo) {
-        const kvm_status st = compact_kv8(c, pl, s, a_lo, a_hi);
-        if (st) return st;
-    }
     if (c->n_attn > 0 && a_hi > a_lo) {
         thread_local static CompactParams p;   // large parameter block, copied into the launch
         std::memset(&p, 0, sizeof p);
         p.n_chars = c->B;
-        p.n_kv_slabs = c->kv8 ? 0 : 2 * (a_hi - a_lo) * c->Hkv;    // else the positions alone
-        p.vec_per_row = c->D * 2 / 16;
+        p.n_kv_slabs = 2 * (a_hi - a_lo) * c->Hkv;
+        p.vec_per_row = c->D * (c->kv8 ? 1 : 2) / 16;
         p.rows_kv = c->rows_kv;
         p.rows_pos = c->rows_pos;
         p.epoch = ++c->epoch;
         p.slab_rows = c->T_cap;
-        const size_t kv_lo = c->kv8 ? 0 : (size_t)a_lo * c->Hkv * c->T_cap * c->D;
-        p.K = reinterpret_cast<uint4*>(c->K + kv_lo);
-        p.V = reinterpret_cast<uint4*>(c->V + kv_lo);
+        if (c->kv8) {
+            const Kv8Layer l = kv8_layer(c, a_lo);
+            p.K = reinterpret_cast<uint4*>(l.K);
+            p.V = reinterpret_cast<uint4*>(l.V);
+            p.K_scale = l.Ks;
+            p.V_scale = l.Vs;
+        } else {
+            p.K = reinterpret_cast<uint4*>(c->K + (size_t)a_lo * c->Hkv * c->T_cap * c->D);
+            p.V = reinterpret_cast<uint4*>(c->V + (size_t)a_lo * c->Hkv * c->T_cap * c->D);
+        }
         p.pos = c->pos;
         p.tickets = c->tickets;
         p.flags = c->flags;
@@ -1293,7 +1262,9 @@ kvm_status launch_compaction(kvm_ctx* c, const SpanPlan& pl, cudaStream_t s, int
             ch.seg_off = pl.seg_off[b];
             ch.n_seg = pl.n_seg[b];
             ch.cap_off = c->cap_off[b];
-            ch.chunks_kv = c->kv8 ? 0 : (moved + p.rows_kv - 1) / p.rows_kv;
+            // (blocks of 8 bits: from the first removed entry's on, whether anything moves or not)
+            const int kv_rows = !c->kv8 ? moved : pl.n_seg[b] > 0 ? pl.L_new[b] - pl.first[b] / kKv8Rows * kKv8Rows : 0;
+            ch.chunks_kv = (kv_rows + p.rows_kv - 1) / p.rows_kv;
             ch.chunks_pos = with_pos ? (moved + p.rows_pos - 1) / p.rows_pos : 0;
             ch.blk_off = blk;
             ch.flag_off = c->flag_off[b];
@@ -1374,11 +1345,12 @@ kvm_status do_compact(kvm_ctx* c, const int32_t* span_cu, const int32_t* sbeg, c
     return KVM_OK;
 }
 
-// The rows that attention layer `layer` of a context in 8 bits reads: the tail's into the
-// blocks, and, unless the attention reads 8 bits itself, the blocks in sight as bf16.
-kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int total, bool widen, cudaStream_t s) {
+// What comes before the tensor-core attention of a layer in 8 bits (kv8_append).
+kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int total, cudaStream_t s) {
     thread_local static Kv8AppendParams ap;
     ap.to = kv8_layer(c, c->attn_idx[layer]);
+    ap.K = c->K;
+    ap.V = c->V;
     ap.n_chars = c->B;
     ap.Hq = c->Hq; ap.Hkv = c->Hkv; ap.D = c->D; ap.R = c->R;
     ap.total = total;
@@ -1391,44 +1363,32 @@ kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int tot
     ap.tail_pos = p.tail_pos;
     ap.err = p.err;
     std::copy(c->turn, c->turn + kMaxRotaryHalf, ap.turn);
-    ap.n_items = 0;
+    ap.n_items = ap.n_widen = 0;
     for (int b = 0; b < c->B; ++b) {
         const AttnChar& ch = p.ch[b];
-        ap.ch[b] = kv8_char(c, b, ch.L_prev / kKv8Rows, ch.M ? ch.L_prev + ch.M : 0, c->cap_off[b], 2, ap.n_items);
+        const int whole = ch.L_prev / kKv8Rows;      // blocks that the tail leaves as they are
+        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, c->cap_off[b], 2, ap.n_items);
         ap.L_prev[b] = ch.L_prev;
         ap.tail_off[b] = ch.tail_off;
         ap.p[b] = ch.p;
+        // of them what the tail's first token sees; later ones begin later
+        const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
+        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, c->cap_off[b], 2, ap.n_widen);
+        ap.sink[b] = w.sink;
+        ap.gap[b] = w.gap;
     }
-    int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
+    const int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
     launch_kv8_append(ap, s);
-    LAUNCH_CHECK(c);
-    if (widen) {
-        thread_local static Kv8WidenParams wp;
-        wp.from = ap.to;
-        wp.n_chars = c->B;
-        wp.Hkv = c->Hkv;
-        wp.D = c->D;
-        wp.slab_rows = wp.dst_rows = c->T_cap;
-        wp.K = c->K;
-        wp.V = c->V;
-        wp.n_items = 0;
-        for (int b = 0; b < c->B; ++b) {
-            const AttnChar& ch = p.ch[b];
-            // what the tail's first token sees, and all from there on; whole blocks, so that no row the
-            // attention loads is left over from another layer
-            const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
-            const int blocks = ch.M ? (ch.L_prev + ch.M + kKv8Rows - 1) / kKv8Rows : 0;
-            wp.ch[b] = {c->cap_off[b], c->cap_off[b], 0, blocks ? blocks - w.gap : 0, blocks * kKv8Rows, wp.n_items};
-            wp.n_items += wp.ch[b].n_blocks * 2 * c->Hkv;
-            wp.sink[b] = w.sink;
-            wp.gap[b] = w.gap;
-        }
-        launch_kv8_widen(wp, s);
-        ++c->launches;
-        LAUNCH_CHECK(c);
-    }
     prof_end(c, ps, s);
+    LAUNCH_CHECK(c);
     return KVM_OK;
+}
+
+// Most rows (tokens x group) of a character.
+int most_rows(const kvm_ctx* c, const int32_t* tail_cu) {
+    int m = 0;
+    for (int b = 0; b < c->B; ++b) m = std::max(m, tail_cu[b + 1] - tail_cu[b]);
+    return (int)std::min<int64_t>((int64_t)m * c->g, INT32_MAX);
 }
 
 // One attention layer's launches under its partition pl: a tail of `total` tokens
@@ -1488,12 +1448,13 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_tile.begin(), pl.cta_tile.end(), p.cta_tile);
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
-    int rows = 0;                                    // most of a character
-    for (int b = 0; b < c->B; ++b) rows = std::max(rows, p.ch[b].M * c->g);
+    const int rows = most_rows(c, tail_cu);
     const bool direct = c->kv8 && rows <= kKv8Direct;
-    if (c->kv8) {
-        p.widened = !direct;
-        const kvm_status st = launch_kv8_before(c, layer, p, total, !direct, s);
+    if (direct) {
+        // the attention appends
+    } else if (c->kv8) {
+        p.widened = 1;
+        const kvm_status st = launch_kv8_before(c, layer, p, total, s);
         if (st) return st;
     } else if (!p.append) {
         const int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
@@ -1513,6 +1474,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
         dp.a = p;
         dp.from = kv8_layer(c, a);
         dp.rows = rows;
+        std::copy(c->turn, c->turn + kMaxRotaryHalf, dp.turn);
         launch_kv8_attention(dp, s);
     } else {
         launch_tail_attention(p, s);
@@ -1577,8 +1539,8 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
     AttnPlan pl;
-    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true, kTailCost,
-                   {c->window[layer], c->n_sink[layer]}, pl);
+    plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true,
+                   c->kv8 && most_rows(c, tail_cu) <= kKv8Direct ? kv8_cost(c->D) : kTailCost, {c->window[layer], c->n_sink[layer]}, pl);
     drop_draft(c);
     return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
 }

@@ -37,6 +37,7 @@ inline cudaError_t launch_pdl(void (*kernel)(Params), dim3 grid, dim3 block, siz
 constexpr int kMaxChars = 256;      // characters per context (per-round descriptors travel as kernel parameters)
 constexpr int kMaxSpans = 1024;     // deletion spans per round, all characters together
 constexpr int kMaxRotaryHalf = 128; // rotary_dim / 2
+constexpr int kKv8Rows = 64;        // slots of a block of a cache in 8 bits
 
 // Device error word bits (read by kvm_check).
 constexpr int kErrBounds = 1;       // an index fell outside the buffers a kernel was given
@@ -74,6 +75,8 @@ struct CompactParams {
     int64_t slab_rows;    // rows per (layer, head) slab = total capacity
     uint4* K;
     uint4* V;
+    float* K_scale;       // of caches in 8 bits: per 64 rows; else null
+    float* V_scale;
     int32_t* pos;
     int32_t* tickets;     // [n_chars][n_kv_slabs + 1]
     uint32_t* flags;      // read flag of chunk i at flags[i * flag_stride]
@@ -226,8 +229,6 @@ void launch_attn_combine(const CombineParams& p, cudaStream_t s);
 // caches in 8 bits: e4m3 numbers times a power of two for each block of 64 slots
 // and KV head, K and V apart (see kv8.cuh)
 // ----------------------------------------------------------------------------
-constexpr int kKv8Rows = 64;     // slots of a block
-
 // One layer's slabs [Hkv][slab_rows][D] and scales [Hkv][slab_rows / 64].
 struct Kv8Layer {
     uint8_t* K;
@@ -258,8 +259,8 @@ struct Kv8PackParams {
 };
 void launch_kv8_pack(const Kv8PackParams& p, cudaStream_t s);
 
-// 8-bit blocks out as bf16 rows: blocks block0 .. of a character, of a window's blocks
-// those from `sink` on `gap` further; rows at or past `rows` are left alone.
+// 8-bit blocks out as bf16 rows: blocks block0 .. of a character; rows at or past `rows`
+// are left alone.
 struct Kv8WidenParams {
     Kv8Layer from;
     int32_t n_chars, Hkv, D, n_items;
@@ -267,30 +268,17 @@ struct Kv8WidenParams {
     __nv_bfloat16* K;             // [Hkv][dst_rows][D]; V null: only keys
     __nv_bfloat16* V;
     Kv8Char ch[kMaxChars];
-    int32_t sink[kMaxChars], gap[kMaxChars];
 };
 void launch_kv8_widen(const Kv8WidenParams& p, cudaStream_t s);
 
-// The survivors of a removal, widened, in their new places: rows [64 block0, rows) of
-// a character from the rows that segments name (see CompactParams).
-struct Kv8GatherParams {
-    Kv8Layer from;
-    int32_t n_chars, Hkv, D, n_items;
-    int64_t slab_rows;
-    __nv_bfloat16* K;             // [Hkv][slab_rows][D]
-    __nv_bfloat16* V;
-    Kv8Char ch[kMaxChars];
-    int32_t first[kMaxChars], seg_off[kMaxChars], n_seg[kMaxChars];
-    int32_t seg_start[kMaxSpans];
-    int32_t seg_shift[kMaxSpans];
-};
-void launch_kv8_gather(const Kv8GatherParams& p, cudaStream_t s);
-
 // A tail's rotated keys and its values into the blocks behind the live entries, and
-// its rotated queries into q_rot.
+// its rotated queries into q_rot; those blocks and the older ones in sight as bf16 rows
+// of K and V.
 struct Kv8AppendParams {
     Kv8Layer to;
-    int32_t n_chars, Hq, Hkv, D, R, n_items, total;
+    __nv_bfloat16* K;             // [Hkv][slab_rows][D]
+    __nv_bfloat16* V;
+    int32_t n_chars, Hq, Hkv, D, R, n_items, n_widen, total;
     int64_t slab_rows;
     const __nv_bfloat16* q;       // [sum M][Hq][D]
     const __nv_bfloat16* k_new;   // [sum M][Hkv][D]
@@ -303,16 +291,21 @@ struct Kv8AppendParams {
     Kv8Char ch[kMaxChars];           // rows: live and tail
     int32_t L_prev[kMaxChars], tail_off[kMaxChars];
     int64_t p[kMaxChars];
+    // the older blocks in sight: of those from `sink` on, `gap` further
+    Kv8Char old[kMaxChars];
+    int32_t sink[kMaxChars], gap[kMaxChars];
 };
 void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s);
 
 // Attention of a few rows a KV head straight from the 8-bit cache, under the same
-// partition and with the same partials as launch_tail_attention.
+// partition and with the same partials as launch_tail_attention.  It rotates the tail's
+// queries and puts its keys and values into the cache itself.
 constexpr int kKv8Direct = 16;   // most rows (tail tokens of a character x group)
 struct Kv8AttnParams {
     AttnParams a;
     Kv8Layer from;
     int32_t rows;                 // most rows of a query tile
+    uint64_t turn[kMaxRotaryHalf];   // as in Kv8AppendParams
 };
 void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s);
 int attention_ctas_per_sm(int head_dim);

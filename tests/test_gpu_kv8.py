@@ -304,6 +304,15 @@ def test_rows_around_the_direct_kernels_limit(shape):
         _tail(p, [n, max(n - 1, 0)], what=n)
 
 
+@pytest.mark.parametrize("shape,n", [((8, 8, 64, 64), 16), ((4, 4, 256, 256), 13), ((8, 4, 128, 6), 8), (HYBRID, 2), ((16, 1, 256, 0), 1)])
+def test_few_rows_over_two_blocks(shape, n):
+    """A step whose new entries end one block and begin the next, at every place, with blocks split over ranges or not."""
+    lives = [64 - n, 63, 64, 127, 5000 // 64 * 64 + 64 - (n + 1) // 2, 0]
+    p = Pop(shape, lives, 31, [(0, 0), (1, 0), (70, 3)], extra=4 * n, most=6 * n)
+    for size in (1.0, 8.0, 0.5):
+        _tail(p, [n] * 6, [p.tail(6 * n, size=size) for _ in range(3)])
+
+
 def test_values_of_many_sizes():
     """Blocks whose scales differ, and tails that raise the scale of the block they begin in."""
     p = Pop(MID, [200, 90], 14, extra=256, most=256)
