@@ -23,20 +23,19 @@ constexpr int kThreads = 256;
 constexpr int kAppendThreads = 512;
 constexpr int kPackThreads = 512;
 
-// The item's character (the last with blk_off <= item), block, head, and K or V.
+// An item's character (the last with blk_off <= item), block, head, and K or V.
 struct Item {
     int b, block, head;
     bool is_v;
 };
-template <typename P>
-__device__ __forceinline__ Item item_of(const P& p, const Kv8Char* ch, int item, int sides = 2) {
+__device__ __forceinline__ Item item_of(const Kv8AppendParams& p, const Kv8Char* ch, int item) {
     int lo = 0, hi = p.n_chars - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (ch[mid].blk_off <= item) lo = mid; else hi = mid - 1;
     }
-    const int local = item - ch[lo].blk_off, per = sides * p.Hkv;
-    return {lo, ch[lo].block0 + local / per, local % per / sides, sides == 2 && (local & 1)};
+    const int local = item - ch[lo].blk_off, per = 2 * p.Hkv;
+    return {lo, ch[lo].block0 + local / per, local % per / 2, (bool)(local & 1)};
 }
 
 template <int THREADS>
@@ -249,28 +248,27 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const __grid
     if (bad) atomicOr(p.err, kErrValue);
 }
 
+// grid (blocks, heads, K and V)
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_widen_kernel(const __grid_constant__ Kv8WidenParams p) {
+__global__ void __launch_bounds__(kThreads) kv8_widen_kernel(const __grid_constant__ Kv8CopyParams p) {
     grid_dependency_wait();
     grid_dependents_launch();
-    const Item it = item_of(p, p.ch, blockIdx.x, p.V ? 2 : 1);
-    const Kv8Char& c = p.ch[it.b];
-    const int row0 = it.block * kKv8Rows;
-    const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
-    widen_block<D, kThreads>((it.is_v ? p.from.V : p.from.K) + slot * D, (it.is_v ? p.from.Vs : p.from.Ks)[slot / kKv8Rows],
-                             (it.is_v ? p.V : p.K) + ((int64_t)it.head * p.dst_rows + c.row0 + row0) * D, c.rows - row0);
+    const bool is_v = blockIdx.z;
+    const int row0 = blockIdx.x * kKv8Rows, head = blockIdx.y;
+    const int64_t slot = head * p.slab_rows + p.cap_off + row0;
+    widen_block<D, kThreads>((is_v ? p.cache.V : p.cache.K) + slot * D, (is_v ? p.cache.Vs : p.cache.Ks)[slot / kKv8Rows],
+                             (is_v ? p.V : p.K) + (head * p.other_rows + p.row0 + row0) * D, p.rows - row0);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kPackThreads) kv8_pack_kernel(const __grid_constant__ Kv8PackParams p) {
+__global__ void __launch_bounds__(kPackThreads) kv8_pack_kernel(const __grid_constant__ Kv8CopyParams p) {
     __shared__ float red[kPackThreads / 32];
     grid_dependency_wait();
     grid_dependents_launch();
-    const Item it = item_of(p, p.ch, blockIdx.x);
-    const Kv8Char& c = p.ch[it.b];
-    const int row0 = it.block * kKv8Rows, n = min(c.rows - row0, kKv8Rows) * (D / 8);
-    const uint4* src = reinterpret_cast<const uint4*>((it.is_v ? p.V : p.K) + ((int64_t)it.head * p.src_rows + c.row0 + row0) * D);
-    const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
+    const bool is_v = blockIdx.z;
+    const int row0 = blockIdx.x * kKv8Rows, head = blockIdx.y, n = min(p.rows - row0, kKv8Rows) * (D / 8);
+    const uint4* src = reinterpret_cast<const uint4*>((is_v ? p.V : p.K) + (head * p.other_rows + p.row0 + row0) * D);
+    const int64_t slot = head * p.slab_rows + p.cap_off + row0;
     constexpr int kEach = kKv8Rows * D / 8 / kPackThreads;     // 1, 2 or 4 vectors a thread
     uint4 w[kEach];
     float m = 0.f;
@@ -293,14 +291,14 @@ __global__ void __launch_bounds__(kPackThreads) kv8_pack_kernel(const __grid_con
     m = block_max<kPackThreads>(m, red);
     const int e = kv8_exponent(m);
     const float inv = pow2(-e);
-    uint2* dst = reinterpret_cast<uint2*>((it.is_v ? p.to.V : p.to.K) + slot * D);
+    uint2* dst = reinterpret_cast<uint2*>((is_v ? p.cache.V : p.cache.K) + slot * D);
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const float2 a = bf2_f2(w[k].x), b = bf2_f2(w[k].y), f = bf2_f2(w[k].z), g = bf2_f2(w[k].w);
         dst[threadIdx.x + k * kPackThreads] = make_uint2(to_e4m3(a.x * inv, a.y * inv, b.x * inv, b.y * inv),
                                                      to_e4m3(f.x * inv, f.y * inv, g.x * inv, g.y * inv));
     }
-    if (threadIdx.x == 0) (it.is_v ? p.to.Vs : p.to.Ks)[slot / kKv8Rows] = pow2(e);
+    if (threadIdx.x == 0) (is_v ? p.cache.Vs : p.cache.Ks)[slot / kKv8Rows] = pow2(e);
     if (bad) atomicOr(p.err, kErrValue);
 }
 
@@ -326,16 +324,16 @@ void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s) {
     else launch_append<256>(p, s);
 }
 
-void launch_kv8_widen(const Kv8WidenParams& p, cudaStream_t s) {
-    if (p.n_items <= 0) return;
-    launch_pdl(p.D == 64 ? kv8_widen_kernel<64> : p.D == 128 ? kv8_widen_kernel<128> : kv8_widen_kernel<256>, dim3(p.n_items),
-               dim3(kThreads), 0, s, p);
+void launch_kv8_widen(const Kv8CopyParams& p, cudaStream_t s) {
+    if (p.rows <= 0) return;
+    launch_pdl(p.D == 64 ? kv8_widen_kernel<64> : p.D == 128 ? kv8_widen_kernel<128> : kv8_widen_kernel<256>,
+               dim3((p.rows + kKv8Rows - 1) / kKv8Rows, p.Hkv, p.sides), dim3(kThreads), 0, s, p);
 }
 
-void launch_kv8_pack(const Kv8PackParams& p, cudaStream_t s) {
-    if (p.n_items <= 0) return;
-    launch_pdl(p.D == 64 ? kv8_pack_kernel<64> : p.D == 128 ? kv8_pack_kernel<128> : kv8_pack_kernel<256>, dim3(p.n_items),
-               dim3(kPackThreads), 0, s, p);
+void launch_kv8_pack(const Kv8CopyParams& p, cudaStream_t s) {
+    if (p.rows <= 0) return;
+    launch_pdl(p.D == 64 ? kv8_pack_kernel<64> : p.D == 128 ? kv8_pack_kernel<128> : kv8_pack_kernel<256>,
+               dim3((p.rows + kKv8Rows - 1) / kKv8Rows, p.Hkv, p.sides), dim3(kPackThreads), 0, s, p);
 }
 
 }  // namespace kvm

@@ -845,52 +845,22 @@ Kv8Layer kv8_layer(const kvm_ctx* c, int a) {
     return {c->K8 + a * n, c->V8 + a * n, c->K8s + a * blocks, c->V8s + a * blocks};
 }
 
-// Blocks [block0, ...) of character b up to row `rows`, as items of a kv8 kernel: `sides`
-// (K, V or both) of every head.
-Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int row0, int sides, int& items) {
+// Blocks [block0, ...) of character b up to row `rows`, as items of kv8_append.
+Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int& items) {
     const int n = std::max(0, (rows + kKv8Rows - 1) / kKv8Rows - block0);
-    const Kv8Char ch{row0, c->cap_off[b], block0, n, rows, items};
-    items += n * sides * c->Hkv;
+    const Kv8Char ch{c->cap_off[b], block0, n, rows, items};
+    items += n * 2 * c->Hkv;
     return ch;
 }
 
-// Keys and values (v null: keys alone) of attention layer a's character b as bf16 rows at row0 of k's and v's
-// slabs of dst_rows; block_rows: whole blocks, what lies behind the live entries too.
-kvm_status widen_char(kvm_ctx* c, int a, int b, void* k, void* v, int row0, int64_t dst_rows, bool block_rows, cudaStream_t s) {
-    thread_local static Kv8WidenParams p;
-    p.from = kv8_layer(c, a);
-    p.n_chars = 1;
-    p.Hkv = c->Hkv;
-    p.D = c->D;
-    p.n_items = 0;
-    p.slab_rows = c->T_cap;
-    p.dst_rows = dst_rows;
-    p.K = static_cast<__nv_bfloat16*>(k);
-    p.V = static_cast<__nv_bfloat16*>(v);
-    const int L = c->live[b], rows = block_rows ? (L + kKv8Rows - 1) / kKv8Rows * kKv8Rows : L;
-    p.ch[0] = kv8_char(c, b, 0, rows, row0, v ? 2 : 1, p.n_items);
+// Attention layer a's first `rows` rows of character b between its blocks and bf16 rows at
+// row0 of k's and v's slabs (v null: keys alone): into the blocks or out of them.
+kvm_status launch_kv8_copy(kvm_ctx* c, int a, int b, int rows, void* k, void* v, int64_t row0, int64_t other_rows, bool in, cudaStream_t s) {
+    const Kv8CopyParams p{kv8_layer(c, a), c->Hkv, c->D, rows, v ? 2 : 1, c->T_cap, other_rows, c->cap_off[b], row0,
+                          static_cast<__nv_bfloat16*>(k), static_cast<__nv_bfloat16*>(v), c->err};
     ++c->launches;
-    launch_kv8_widen(p, s);
-    LAUNCH_CHECK(c);
-    return KVM_OK;
-}
-
-// bf16 rows of character b into blocks of layer a.
-kvm_status pack_char(kvm_ctx* c, int a, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t src_rows, int b, int row0, cudaStream_t s) {
-    thread_local static Kv8PackParams p;
-    p.to = kv8_layer(c, a);
-    p.n_chars = 1;
-    p.Hkv = c->Hkv;
-    p.D = c->D;
-    p.n_items = 0;
-    p.slab_rows = c->T_cap;
-    p.src_rows = src_rows;
-    p.K = k;
-    p.V = v;
-    p.err = c->err;
-    p.ch[0] = kv8_char(c, b, 0, c->live[b], row0, 2, p.n_items);
-    ++c->launches;
-    launch_kv8_pack(p, s);
+    if (in) launch_kv8_pack(p, s);
+    else launch_kv8_widen(p, s);
     LAUNCH_CHECK(c);
     return KVM_OK;
 }
@@ -904,15 +874,10 @@ kvm_status copy_kv8(kvm_ctx* c, int a, int b, void* k, void* v, bool in, cudaStr
     if (st) return st;
     const int L = c->live[b];
     const bool own = !((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15) && own_memory(c, k) && own_memory(c, v);
-    const int row0 = own ? 0 : c->cap_off[b];
-    const int64_t rows = own ? L : c->T_cap;
-    if (!in) {
-        st = widen_char(c, a, b, own ? k : c->K, own ? v : c->V, row0, rows, !own, s);
-        return st || own ? st : copy_slabs(c, 0, b, k, v, false, s);
-    }
-    if (!own) st = copy_slabs(c, 0, b, k, v, true, s);
-    if (st) return st;
-    return pack_char(c, a, own ? static_cast<const __nv_bfloat16*>(k) : c->K, own ? static_cast<const __nv_bfloat16*>(v) : c->V, rows, b, row0, s);
+    if (own) return launch_kv8_copy(c, a, b, L, k, v, 0, L, in, s);
+    if (in) st = copy_slabs(c, 0, b, k, v, true, s);
+    if (!st) st = launch_kv8_copy(c, a, b, L, c->K, c->V, c->cap_off[b], c->T_cap, in, s);
+    return st || in ? st : copy_slabs(c, 0, b, k, v, false, s);
 }
 
 // KV of character b in attention layer `layer`: slab rows of every KV head.
@@ -1367,13 +1332,13 @@ kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int tot
     for (int b = 0; b < c->B; ++b) {
         const AttnChar& ch = p.ch[b];
         const int whole = ch.L_prev / kKv8Rows;      // blocks that the tail leaves as they are
-        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, c->cap_off[b], 2, ap.n_items);
+        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, ap.n_items);
         ap.L_prev[b] = ch.L_prev;
         ap.tail_off[b] = ch.tail_off;
         ap.p[b] = ch.p;
         // of them what the tail's first token sees; later ones begin later
         const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
-        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, c->cap_off[b], 2, ap.n_widen);
+        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, ap.n_widen);
         ap.sink[b] = w.sink;
         ap.gap[b] = w.gap;
     }
@@ -1906,7 +1871,7 @@ extern "C" kvm_status kvm_attn_probe(kvm_ctx* c, int32_t layer, int32_t b, int32
     for (int d = 0; d < c->R / 2; ++d) p.inv_freq[d] = c->inv_freq[d];
     if (c->kv8) {
         st = check_device(c);
-        if (!st) st = widen_char(c, c->attn_idx[layer], b, c->K, nullptr, c->cap_off[b], c->T_cap, true, s);
+        if (!st) st = launch_kv8_copy(c, c->attn_idx[layer], b, L, c->K, nullptr, c->cap_off[b], c->T_cap, false, s);
         if (st) return st;
     }
     if (group_of) CUDA_TRY(cudaMemsetAsync(group_mass_out, 0, sizeof(float) * (size_t)n_groups, s));

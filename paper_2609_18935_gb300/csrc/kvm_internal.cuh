@@ -238,7 +238,6 @@ struct Kv8Layer {
 };
 
 struct Kv8Char {
-    int32_t row0;         // first row of the other side (a cache's own slots: cap_off)
     int32_t cap_off;      // slot offset of the character in the slabs
     int32_t block0;       // its first block that takes part
     int32_t n_blocks;
@@ -246,30 +245,21 @@ struct Kv8Char {
     int32_t blk_off;      // first (block, head, K or V) item of this character
 };
 
-// Rows of bf16 into 8-bit blocks: rows [64 block0, rows) of a character, at row0 + row
-// of src's slabs [Hkv][src_rows][D]; the rest of the last block becomes 0.
-struct Kv8PackParams {
-    Kv8Layer to;
-    int32_t n_chars, Hkv, D, n_items;
-    int64_t slab_rows, src_rows;
-    const __nv_bfloat16* K;
-    const __nv_bfloat16* V;
-    int32_t* err;
-    Kv8Char ch[kMaxChars];
-};
-void launch_kv8_pack(const Kv8PackParams& p, cudaStream_t s);
-
-// 8-bit blocks out as bf16 rows: blocks block0 .. of a character; rows at or past `rows`
-// are left alone.
-struct Kv8WidenParams {
-    Kv8Layer from;
-    int32_t n_chars, Hkv, D, n_items;
-    int64_t slab_rows, dst_rows;
-    __nv_bfloat16* K;             // [Hkv][dst_rows][D]; V null: only keys
+// A character's `rows` rows between its 8-bit blocks and bf16 rows, at row0 on of
+// slabs [Hkv][other_rows][D].  pack: into the blocks, the rest of the last becomes 0.
+// widen: out of them, rows at or past `rows` are left alone.
+struct Kv8CopyParams {
+    Kv8Layer cache;
+    int32_t Hkv, D, rows;
+    int32_t sides;                // 2: keys and values, 1: keys
+    int64_t slab_rows, other_rows;
+    int64_t cap_off, row0;
+    __nv_bfloat16* K;
     __nv_bfloat16* V;
-    Kv8Char ch[kMaxChars];
+    int32_t* err;
 };
-void launch_kv8_widen(const Kv8WidenParams& p, cudaStream_t s);
+void launch_kv8_pack(const Kv8CopyParams& p, cudaStream_t s);
+void launch_kv8_widen(const Kv8CopyParams& p, cudaStream_t s);
 
 // A tail's rotated keys and its values into the blocks behind the live entries, and
 // its rotated queries into q_rot; those blocks and the older ones in sight as bf16 rows
