@@ -74,6 +74,45 @@ __device__ __forceinline__ void widen_block(const uint8_t* from, float scale, __
     }
 }
 
+// Some older blocks in sight of one head's K or V, all loads under way at once.
+template <int D>
+__device__ __forceinline__ void widen_old(const Kv8AppendParams& p, int item) {
+    constexpr int kEach = 8, kVecs = kKv8Rows * D / 16;        // vectors a thread, of a block
+    static_assert(kEach * kAppendThreads == kv8_widen_blocks(D) * kVecs, "an item");
+    const Item it = item_of(p, p.old, item);                   // (`block` counts items)
+    const Kv8Char& c = p.old[it.b];
+    const int first = it.block * kv8_widen_blocks(D), sink = p.sink[it.b], gap = p.gap[it.b];
+    const int64_t slot0 = (int64_t)it.head * p.slab_rows + c.cap_off;
+    const uint4* src = reinterpret_cast<const uint4*>((it.is_v ? p.to.V : p.to.K) + slot0 * D);
+    uint4* dst = reinterpret_cast<uint4*>((it.is_v ? p.V : p.K) + slot0 * D);
+    const float* scales = (it.is_v ? p.to.Vs : p.to.Ks) + slot0 / kKv8Rows;
+    uint4 w[kEach];
+    float s[kEach];
+    auto at = [&](int k, int& block) {                         // vector of the character's slab
+        const int v = threadIdx.x + k * kAppendThreads, n = first + v / kVecs;
+        block = n + (n >= sink ? gap : 0);
+        return n < c.n_blocks ? (int64_t)block * kVecs + v % kVecs : (int64_t)-1;
+    };
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        int block;
+        const int64_t v = at(k, block);
+        if (v < 0) continue;
+        w[k] = src[v];
+        s[k] = scales[block];
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        int block;
+        const int64_t v = at(k, block);
+        if (v < 0) continue;
+        uint4 a, b;
+        widen16(w[k], s[k], a, b);
+        dst[2 * v] = a;
+        dst[2 * v + 1] = b;
+    }
+}
+
 // A packed tail token's queries, rotated.
 template <int D>
 __device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, float* cs, float* sn) {
@@ -133,7 +172,7 @@ __device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, fl
 // 256 tokens of 16 heads of 256 took 11.1 us for blocks and queries and 8.5 behind them
 // for the widening.
 template <int D>
-__global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const __grid_constant__ Kv8AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __grid_constant__ Kv8AppendParams p) {
     extern __shared__ __align__(16) float tile[];              // [64][D]
     __shared__ float red[kAppendThreads / 32];
     __shared__ float cs[kMaxRotaryHalf], sn[kMaxRotaryHalf];
@@ -145,11 +184,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(const __grid
         return;
     }
     if ((int)blockIdx.x >= p.n_items) {
-        const Item it = item_of(p, p.old, blockIdx.x - p.n_items);
-        const int block = it.block + (it.block >= p.sink[it.b] ? p.gap[it.b] : 0);
-        const int64_t slot = (int64_t)it.head * p.slab_rows + p.old[it.b].cap_off + block * kKv8Rows;
-        widen_block<D, kAppendThreads>((it.is_v ? p.to.V : p.to.K) + slot * D, (it.is_v ? p.to.Vs : p.to.Ks)[slot / kKv8Rows],
-                                       (it.is_v ? p.V : p.K) + slot * D, kKv8Rows);
+        widen_old<D>(p, blockIdx.x - p.n_items);
         return;
     }
     const Item it = item_of(p, p.ch, blockIdx.x);

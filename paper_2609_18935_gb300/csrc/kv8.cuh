@@ -35,19 +35,22 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
     return (uint32_t)lo | (uint32_t)hi << 16;
 }
 
-// Two e4m3 numbers in bytes 1 and 3 of x (whatever the others hold) as bf16, exactly:
-// sign, exponent and mantissa moved to their places give the number times 2^-120 (a
-// subnormal one stays one), the product undoes that.
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t x) {
-    const uint32_t y = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
+// Two e4m3 numbers as bf16, exactly: bytes n and m of the eight of (lo, hi), each beside
+// eight copies of its sign (a selector's bit 3), move up four bits into sign, exponent
+// and mantissa: the number times 2^-120, a subnormal one as a subnormal.  The product
+// undoes that.
+__device__ __forceinline__ constexpr uint32_t e4m3_pick(int n, int m) { return n | (8 + n) << 4 | m << 8 | (8 + m) << 12; }
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t lo, uint32_t hi, uint32_t pick) {
+    uint32_t x;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x) : "r"(lo), "r"(hi), "r"(pick));
+    x = x << 4 & 0x87f087f0u;
     const uint32_t k = 0x7b807b80u;                          // 2^120
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), *reinterpret_cast<const __nv_bfloat162*>(&k));
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&k));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 // The low and the high two numbers of a word.
-__device__ __forceinline__ uint32_t e4m3_low(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x1000)); }
-__device__ __forceinline__ uint32_t e4m3_high(uint32_t w) { return e4m3_pair(__byte_perm(w, w, 0x3020)); }
-
+__device__ __forceinline__ uint32_t e4m3_low(uint32_t w) { return e4m3_pair(w, w, e4m3_pick(0, 1)); }
+__device__ __forceinline__ uint32_t e4m3_high(uint32_t w) { return e4m3_pair(w, w, e4m3_pick(2, 3)); }
 
 __device__ __forceinline__ float2 bf2_f2(uint32_t w) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w)); }
 __device__ __forceinline__ uint32_t f2_bf2(float a, float b) {
@@ -76,10 +79,10 @@ __device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& a, u
 
 // Largest magnitude of sixteen numbers, as their bytes' order has it.
 __device__ __forceinline__ float e4m3_max(const uint4& w) {
-    const uint32_t k = 0x7f7f7f7fu;
-    const uint32_t m = __vmaxu4(__vmaxu4(w.x & k, w.y & k), __vmaxu4(w.z & k, w.w & k));
-    const uint32_t h = __vmaxu4(m, m >> 16), b = max(h & 0xffu, h >> 8 & 0xffu);
-    return __uint_as_float(e4m3_pair(b << 8) << 16);
+    const uint32_t k = 0x007f007fu;
+    const uint32_t m = __vmaxu2(__vmaxu2(__vmaxu2(w.x & k, w.y & k), __vmaxu2(w.z & k, w.w & k)),
+                                __vmaxu2(__vmaxu2(w.x >> 8 & k, w.y >> 8 & k), __vmaxu2(w.z >> 8 & k, w.w >> 8 & k)));
+    return __uint_as_float(e4m3_low(max(m & 0xffffu, m >> 16)) << 16);
 }
 
 // Sixteen numbers of scale `from` under the scale whose reciprocal is `inv`.

@@ -1,11 +1,18 @@
 // Attention of a few query rows a KV head (a decode step: one token, a group of heads)
 // straight from a cache in 8 bits.
 //
-// S^T = K Q^T and O^T = V^T P^T with mma.sync (m16n8k16, bf16): the 16 keys of a step are
-// the rows of the first product and the depth of the second, 8 query rows its columns.
-// The work is bound by the cache's bytes: 8 rows are a sixteenth of a tcgen05 tile, whose
-// bf16 operands would have to pass through shared memory; here a warp turns its bytes
-// into bf16 in registers and feeds them to the products there.
+// S^T = K Q^T and O^T = V^T P^T with mma.sync: the 16 keys of a step are the rows of the
+// first product and the depth of the second, 8 query rows its columns.  The work is
+// bound by the cache's bytes: 8 rows are a sixteenth of a tcgen05 tile, whose operands
+// would have to pass through shared memory.
+// Cache numbers become f16 (one instruction a pair), exactly; their blocks' scales stay
+// outside, of K in the scores, of V as the sums are added up.  A query, rounded to bf16,
+// is f16 times a power of two of its row (down to 2^-39 of the row's largest).  A weight is
+// rounded to f16: 2^-12 of it, or 2^-33 of the reference's where it is small, 2^-9 of a
+// row's sum after 2^24 keys.
+// As bf16 (a pair in five instructions, K and V), with 8 warps and 903 instructions a
+// step, 32 characters' step over 16K took 64.4 us; m16n8k32 on e4m3 itself, the queries
+// as two such numbers each, is made of the same conversions.
 //
 // One launch takes in the tail: a block turns its rows' queries itself, and the block
 // whose range holds the end of a character's cache puts the new keys and values there
@@ -19,11 +26,13 @@
 // block's warps meet at the segment's end.
 //
 // Layout.  The sum over d takes any order, the same for K and Q: lane (g, j) = (lane / 4,
-// lane mod 4) reads 16 bytes of key g (and g + 8) at a time and each word of them is its
+// lane mod 4) reads 16 bytes of key g (and g + 8) at a time, and two words of them are its
 // part of one product step.  For V it reads 16 bytes of its four keys 2j, 2j + 1, 2j + 8,
 // 2j + 9, whose bytes meet in pairs of keys; a product's 16 rows are then two numbers of
 // each lane g.  The rings' 16-byte pieces are turned by their row, so that each quarter
 // of a warp reads all banks.
+#include <cuda_fp16.h>
+
 #include "attn_tiles.cuh"
 #include "draft_rows.cuh"
 #include "kv8.cuh"
@@ -36,16 +45,19 @@ namespace {
 using ptx::ex2;
 using ptx::smem_u32;
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
 constexpr int kStep = 16;                      // keys of a warp's step
 constexpr int BM = kAttnRows;
+constexpr float kUp = 7.f;                     // weights are taken 2^7 higher: up to 2^15, where f16 has room
 
 template <int D, int NT>
 struct Cfg {
+    // as many warps as their registers allow (O and Q: 96 D NT / 256 of a thread's): a step is
+    // bound by its instructions' latency, with two warps a scheduler twice as much as by memory
+    static constexpr int kWarps = D * NT > 256 ? 8 : D * NT > 128 ? 12 : 16;
+    static constexpr int kThreads = 32 * kWarps;
     static constexpr int SIDE = kStep * D;                     // bytes of a step's K, or V
     static constexpr int STAGE = 2 * SIDE + 16;                // and its two scales
-    static constexpr int STAGES = D == 256 ? 3 : 6;
+    static constexpr int STAGES = D == 256 ? (NT == 2 ? 3 : 2) : D == 128 ? (NT == 2 ? 4 : 3) : 6;
     static constexpr int RING = STAGES * STAGE;
     static constexpr int ROWS = 8 * NT;
     static constexpr int PITCH = D + 4;                        // floats of a merged row
@@ -58,7 +70,8 @@ struct Cfg {
     static constexpr int OFF_X = OFF_TURN + ROWS * D * 4;
     static constexpr int SMEM = OFF_X + ROWS * D * 4;
 };
-static_assert(Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448, "shared memory");
+static_assert(Cfg<256, 1>::SMEM <= 232448 && Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 1>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448 &&
+              Cfg<64, 2>::SMEM <= 232448, "shared memory");
 
 // Byte offset of 16-byte piece `col` of row `row` of a step's K or V.
 template <int D>
@@ -78,9 +91,24 @@ template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// c += scale * (A B)
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float scale) {
+    float d[4] = {0.f, 0.f, 0.f, 0.f};
+    mma16816(d, a0, a1, a2, a3, b0, b1);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = fmaf(scale, d[e], c[e]);
+}
+// The low and the high two e4m3 numbers of a word as f16 (exactly).
+__device__ __forceinline__ void e4m3_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t f2_h2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
@@ -94,7 +122,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 template <int D, int NT>
 __device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt, float* red, const float2* turn,
                                            float* keys) {
-    constexpr int kOld = kKv8Rows * D / 16 / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
+    constexpr int kWarps = Cfg<D, NT>::kWarps, kThreads = Cfg<D, NT>::kThreads;
+    constexpr int kOld = (kKv8Rows * D / 16 + kThreads - 1) / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
     const AttnParams& p = pp.a;
     const int tid = threadIdx.x, half = p.R / 2, row0 = kt * kAttnKeys;
     const int old = min(max(ch.L_prev - row0, 0), kKv8Rows), n = min(ch.L_prev + ch.M - row0, kKv8Rows) - old;
@@ -211,9 +240,10 @@ __device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnCh
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
+__global__ void __launch_bounds__(Cfg<D, NT>::kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
     using C = Cfg<D, NT>;
-    constexpr int KS = D / 16;                                 // steps of the sum over d, and 16-row pieces of O^T
+    constexpr int kWarps = C::kWarps, kThreads = C::kThreads;
+    constexpr int KS = D / 16;                                 // 16-row pieces of O^T
     extern __shared__ __align__(128) uint8_t smem[];
     const AttnParams& p = pp.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
@@ -321,25 +351,44 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             }
             __syncthreads();
         }
-        // Q: a lane's words of each step of the sum, rows g (and g + 8)
+        // Q: a lane's words of each step of the sum, rows g (and g + 8), as f16 times a power of two of the row
         uint32_t q[NT][KS][2];
+        float row_scale[NT][2];                                // of rows 8 n + 2 j and the next
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = 8 * n + g;
             const __nv_bfloat16* src = q_s + r * D;
+            uint4 x[KS / 4][2];
+            float top = 0.f;
 #pragma unroll
             for (int c = 0; c < KS / 4; ++c) {
                 const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
-                uint4 a = make_uint4(0, 0, 0, 0), b = a;
-                if (r < rows) {
-                    a = *reinterpret_cast<const uint4*>(src + 16 * col);
-                    b = *reinterpret_cast<const uint4*>(src + 16 * col + 8);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    x[c][h] = r < rows ? *reinterpret_cast<const uint4*>(src + 16 * col + 8 * h) : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(bf2_f2(w[k]).x), fabsf(bf2_f2(w[k]).y)));
                 }
-                q[n][4 * c][0] = a.x; q[n][4 * c][1] = a.y;
-                q[n][4 * c + 1][0] = a.z; q[n][4 * c + 1][1] = a.w;
-                q[n][4 * c + 2][0] = b.x; q[n][4 * c + 2][1] = b.y;
-                q[n][4 * c + 3][0] = b.z; q[n][4 * c + 3][1] = b.w;
             }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // top < 2^E: its row's numbers below 2^15
+            const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -110), 128);
+            const float up = pow2(15 - E), scale = pow2(E - 15) * p.scale_log2;
+#pragma unroll
+            for (int c = 0; c < KS / 4; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 a = bf2_f2(w[k]);
+                        q[n][4 * c + 2 * h + (k >> 1)][k & 1] = f2_h2(a.x * up, a.y * up);
+                    }
+                }
+            row_scale[n][0] = __shfl_sync(0xffffffffu, scale, 8 * j);
+            row_scale[n][1] = __shfl_sync(0xffffffffu, scale, 8 * j + 4);
         }
         if (forms) {
             __syncthreads();                                   // the queries' place takes the new keys
@@ -377,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             __syncwarp();
             const uint8_t* kt = ring + (i % C::STAGES) * C::STAGE;
             const uint8_t* vt = kt + C::SIDE;
-            const float ks = *reinterpret_cast<const float*>(kt + 2 * C::SIDE) * p.scale_log2;
+            const float ks = *reinterpret_cast<const float*>(kt + 2 * C::SIDE);
             const float vs = *reinterpret_cast<const float*>(kt + 2 * C::SIDE + 4);
             load(s + (C::STAGES - 1) * kWarps, (i + C::STAGES - 1) % C::STAGES);
             cp_commit();
@@ -394,7 +443,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const uint32_t a0 = e4m3_low(xs[w]), a1 = e4m3_low(ys[w]), a2 = e4m3_high(xs[w]), a3 = e4m3_high(ys[w]);
+                    uint32_t a0, a1, a2, a3;
+                    e4m3_f16(xs[w], a0, a2);
+                    e4m3_f16(ys[w], a1, a3);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma16816(sc[n][w & 1], a0, a1, a2, a3, q[n][4 * c + w][0], q[n][4 * c + w][1]);
                 }
@@ -406,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][e] = (sc[n][0][e] + sc[n][1][e]) * ks;
+                for (int e = 0; e < 4; ++e) x[n][e] = (sc[n][0][e] + sc[n][1][e]) * (ks * row_scale[n][e & 1]);
             if (key0 + kStep - 1 > first_at || (p.window && key0 <= last_at - p.window)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -446,11 +497,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 float w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    w[e] = ex2(x[n][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1]));
+                    w[e] = ex2(x[n][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1] - kUp));
                     l[n][e & 1] += w[e];
                 }
-                b[n][0] = transposed(f2_bf2(w[0] * vs, w[1] * vs));
-                b[n][1] = transposed(f2_bf2(w[2] * vs, w[3] * vs));
+                b[n][0] = transposed(f2_h2(w[0], w[1]));
+                b[n][1] = transposed(f2_h2(w[2], w[3]));
             }
             if constexpr (D == 64) {
                 uint2 v[4];
@@ -459,11 +510,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const uint32_t w0 = u < 2 ? v[0].x : v[0].y, w1 = u < 2 ? v[1].x : v[1].y, w2 = u < 2 ? v[2].x : v[2].y, w3 = u < 2 ? v[3].x : v[3].y;
-                    const uint32_t s0 = u & 1 ? 0x6020 : 0x4000, s1 = u & 1 ? 0x7030 : 0x5010;
-                    const uint32_t a0 = e4m3_pair(__byte_perm(w0, w1, s0)), a1 = e4m3_pair(__byte_perm(w0, w1, s1));
-                    const uint32_t a2 = e4m3_pair(__byte_perm(w2, w3, s0)), a3 = e4m3_pair(__byte_perm(w2, w3, s1));
+                    const int pick = u & 1 ? 0x7362 : 0x5140;
+                    uint32_t a0, a1, a2, a3;
+                    e4m3_f16(__byte_perm(w0, w1, pick), a0, a1);
+                    e4m3_f16(__byte_perm(w2, w3, pick), a2, a3);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma16816(o[n][u], a0, a1, a2, a3, b[n][0], b[n][1]);
+                    for (int n = 0; n < NT; ++n) mma16816(o[n][u], a0, a1, a2, a3, b[n][0], b[n][1], vs);
                 }
             } else {
 #pragma unroll
@@ -474,13 +526,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                     const uint32_t* w[4] = {&v[0].x, &v[1].x, &v[2].x, &v[3].x};
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
-                        const uint32_t s0 = u & 1 ? 0x6020 : 0x4000, s1 = u & 1 ? 0x7030 : 0x5010;
-                        const uint32_t a0 = e4m3_pair(__byte_perm(w[0][u >> 1], w[1][u >> 1], s0));
-                        const uint32_t a1 = e4m3_pair(__byte_perm(w[0][u >> 1], w[1][u >> 1], s1));
-                        const uint32_t a2 = e4m3_pair(__byte_perm(w[2][u >> 1], w[3][u >> 1], s0));
-                        const uint32_t a3 = e4m3_pair(__byte_perm(w[2][u >> 1], w[3][u >> 1], s1));
+                        const int pick = u & 1 ? 0x7362 : 0x5140;
+                        uint32_t a0, a1, a2, a3;
+                        e4m3_f16(__byte_perm(w[0][u >> 1], w[1][u >> 1], pick), a0, a1);
+                        e4m3_f16(__byte_perm(w[2][u >> 1], w[3][u >> 1], pick), a2, a3);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma16816(o[n][8 * h + u], a0, a1, a2, a3, b[n][0], b[n][1]);
+                        for (int n = 0; n < NT; ++n) mma16816(o[n][8 * h + u], a0, a1, a2, a3, b[n][0], b[n][1], vs);
                     }
                 }
             }
@@ -495,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
 #pragma unroll
                 for (int b = 4; b < 32; b <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], b);
                 if (g == 0) {
-                    wm[warp * C::ROWS + 8 * n + 2 * j + e] = m[n][e];
+                    wm[warp * C::ROWS + 8 * n + 2 * j + e] = m[n][e] - kUp;
                     wl[warp * C::ROWS + 8 * n + 2 * j + e] = l[n][e];
                 }
             }
@@ -556,7 +607,7 @@ void launch(const Kv8AttnParams& p, cudaStream_t s) {
         cudaFuncSetAttribute(kv8_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, NT>::SMEM);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(kThreads), Cfg<D, NT>::SMEM, s, p);
+    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(Cfg<D, NT>::kThreads), Cfg<D, NT>::SMEM, s, p);
 }
 
 template <int D>

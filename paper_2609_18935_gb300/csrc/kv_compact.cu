@@ -17,9 +17,9 @@
 // holds).  Blocks wait only on chunks with earlier tickets, which are
 // resident or finished, so the waits always end; each wait is still bounded
 // and reports kErrWait instead of spinning forever.
-// Caches in 8 bits (kv8.cuh) move the same way, a block a chunk: 16 KB in, the largest
-// magnitude, 16 KB out.  By way of a bf16 copy (gathered there, formed from there) the
-// same bytes were moved three times.
+// Caches in 8 bits (kv8.cuh) move the same way, 32 KB of whole blocks a chunk: the rows
+// in, each block's largest magnitude, the rows out.  By way of a bf16 copy (gathered
+// there, formed from there) the same bytes were moved three times.
 #include <cstdio>
 #include <cstring>
 
@@ -55,56 +55,69 @@ __device__ __forceinline__ int src_index(const int32_t* seg_start, const int32_t
     return j + seg_shift[seg_of(seg_start, n_seg, j)];
 }
 
-// A chunk's block of an 8-bit cache (KV8): the rows' numbers and their blocks' scales, read;
-// then the new block's scale from the largest of them, and the numbers that it changes
-// rounded again.
+// A chunk of an 8-bit cache (KV8), several blocks: the rows' numbers and their blocks'
+// scales, read; then each new block's scale from the largest of them, and the numbers that
+// it changes rounded again.
+template <int D>
 struct Kv8Chunk {
-    static constexpr int kVecs = kKv8Rows * 256 / 16 / kCompactThreads;     // of 16 numbers, a thread, at head_dim 256
+    static constexpr int kVecs = kCompactVecPerThread, kPer = D / 64;   // vectors of 16 numbers a thread, of them in a block
+    static constexpr int kBlocks = kVecs / kPer, kRow = D / 16;
+    static constexpr int kRows = kBlocks * kKv8Rows;
     uint4 w[kVecs];
     float s[kVecs];
     __device__ __forceinline__ void load(const uint4* base, const float* scales, const CompactChar& c, const int32_t* seg_start,
-                                         const int32_t* seg_shift, int vec_per_row, int d0, int d1) {
-        const int lg = __ffs(vec_per_row) - 1, n_vec = (d1 - d0) << lg;
+                                         const int32_t* seg_shift, int d0, int d1) {
+        // the usual chunk is a piece of one segment
+        const int seg0 = d0 >= c.first ? seg_of(seg_start, c.n_seg, d0) : 0;
+        const bool one = d0 >= c.first && (seg0 + 1 == c.n_seg || seg_start[seg0 + 1] >= d1);
+        const int shift = seg_shift[seg0];
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
             const int v = threadIdx.x + k * kCompactThreads;
             w[k] = make_uint4(0, 0, 0, 0);
             s[k] = 0.f;
-            if (v < n_vec) {
-                int row = d0 + (v >> lg);
-                if (row >= c.first) row = src_index(seg_start, seg_shift, c.n_seg, row);
-                w[k] = __ldcg(base + (int64_t)row * vec_per_row + (v & (vec_per_row - 1)));
+            int row = d0 + v / kRow;
+            if (row < d1) {
+                if (one) row += shift;
+                else if (row >= c.first) row = src_index(seg_start, seg_shift, c.n_seg, row);
+                w[k] = __ldcg(base + (int64_t)row * kRow + v % kRow);
                 s[k] = __ldcg(scales + row / kKv8Rows);
             }
         }
     }
-    // part [kCompactThreads / 32] in shared memory, between two barriers of the block
-    __device__ __forceinline__ float warp_max() const {
-        float m = 0.f;
+    // part [kBlocks][warps], in shared memory
+    __device__ __forceinline__ void maxima(float* part) const {
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) m = fmaxf(m, e4m3_max(w[k]) * s[k]);
+        for (int b = 0; b < kBlocks; ++b) {
+            float m = 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        return m;
-    }
-    __device__ __forceinline__ void store(uint4* block, float* scale, int vec_per_row, const float* part) const {
-        float m = 0.f;
+            for (int k = b * kPer; k < (b + 1) * kPer; ++k) m = fmaxf(m, e4m3_max(w[k]) * s[k]);
 #pragma unroll
-        for (int k = 0; k < kCompactThreads / 32; ++k) m = fmaxf(m, part[k]);
-        const int e = kv8_exponent(m);
-        const float to = pow2(e), inv = pow2(-e);
-#pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
-            const int v = threadIdx.x + k * kCompactThreads;
-            if (v < kKv8Rows * vec_per_row) __stcg(block + v, s[k] == to ? w[k] : requantised(w[k], s[k], inv));
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if ((threadIdx.x & 31) == 0) part[b * (kCompactThreads / 32) + (threadIdx.x >> 5)] = m;
         }
-        if (threadIdx.x == 0) __stcg(scale, to);
+    }
+    __device__ __forceinline__ void store(uint4* chunk, float* scales, int rows, const float* part) const {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            if (b * kKv8Rows >= rows) break;
+            float m = 0.f;
+#pragma unroll
+            for (int k = 0; k < kCompactThreads / 32; ++k) m = fmaxf(m, part[b * (kCompactThreads / 32) + k]);
+            const int e = kv8_exponent(m);
+            const float to = pow2(e), inv = pow2(-e);
+#pragma unroll
+            for (int k = b * kPer; k < (b + 1) * kPer; ++k)
+                __stcg(chunk + threadIdx.x + k * kCompactThreads, s[k] == to ? w[k] : requantised(w[k], s[k], inv));
+            if (threadIdx.x == 0) __stcg(scales + b, to);
+        }
     }
 };
-
-template <bool KV8>
+// D8: head_dim of caches in 8 bits, 0 for bf16.
+template <int D8>
 __global__ void __launch_bounds__(kCompactThreads)
 kv_compact_kernel(const __grid_constant__ CompactParams p) {
+    constexpr bool KV8 = D8 != 0;
     grid_dependency_wait();
     grid_dependents_launch();
     const int tid = threadIdx.x;
@@ -140,7 +153,7 @@ kv_compact_kernel(const __grid_constant__ CompactParams p) {
     __syncthreads();
     if (s_abort) return;
     const int chunk = s_chunk;
-    // an 8-bit layer's chunks are blocks: the first one's rows before the first removed one are formed anew with it
+    // an 8-bit layer's chunks are whole blocks: the first one's rows before the first removed one are formed anew with it
     const int first = KV8 && !is_pos ? c.first / kKv8Rows * kKv8Rows : c.first;
     const int d0 = first + chunk * rows;
     const int d1 = min(d0 + rows, c.L_new);
@@ -149,15 +162,15 @@ kv_compact_kernel(const __grid_constant__ CompactParams p) {
     uint4 vbuf[kCompactVecPerThread];
     int32_t ibuf[kCompactVecPerThread];
     uint4* base = nullptr;
-    [[maybe_unused]] Kv8Chunk chunk8;
+    [[maybe_unused]] Kv8Chunk<KV8 ? D8 : 64> chunk8;
     [[maybe_unused]] float* scales = nullptr;
-    [[maybe_unused]] __shared__ float part[kCompactThreads / 32];
+    [[maybe_unused]] __shared__ float part[kCompactVecPerThread * kCompactThreads / 32];
     if (KV8 && !is_pos) {
         const int half = p.n_kv_slabs / 2;
         const int s_in = slab < half ? slab : slab - half;
         base = (slab < half ? p.K : p.V) + ((int64_t)s_in * p.slab_rows + c.cap_off) * p.vec_per_row;
         scales = (slab < half ? p.K_scale : p.V_scale) + ((int64_t)s_in * p.slab_rows + c.cap_off) / kKv8Rows;
-        chunk8.load(base, scales, c, seg_start, seg_shift, p.vec_per_row, d0, d1);
+        chunk8.load(base, scales, c, seg_start, seg_shift, d0, d1);
     } else if (!is_pos) {
         const int half = p.n_kv_slabs / 2;
         uint4* arr = slab < half ? p.K : p.V;
@@ -207,10 +220,7 @@ kv_compact_kernel(const __grid_constant__ CompactParams p) {
             if (m != 0xffffffffu) break;
         }
     }
-    if (KV8 && !is_pos) {
-        const float m = chunk8.warp_max();
-        if ((tid & 31) == 0) part[tid >> 5] = m;
-    }
+    if (KV8 && !is_pos) chunk8.maxima(part);
     __threadfence();
     __syncthreads();
     if (tid == 0) st_release(p.flags + (int64_t)(flag_base + chunk) * p.flag_stride, p.epoch);
@@ -241,7 +251,7 @@ kv_compact_kernel(const __grid_constant__ CompactParams p) {
     if (s_abort) return;
 
     if (KV8 && !is_pos) {
-        chunk8.store(base + (int64_t)d0 * p.vec_per_row, scales + d0 / kKv8Rows, p.vec_per_row, part);
+        chunk8.store(base + (int64_t)d0 * p.vec_per_row, scales + d0 / kKv8Rows, d1 - d0, part);
     } else if (!is_pos) {
         const int n_vec = (d1 - d0) * p.vec_per_row;
 #pragma unroll
@@ -309,7 +319,11 @@ void launch_copy(const CopyParams& p, cudaStream_t s) {
 
 void launch_kv_compact(const CompactParams& p, cudaStream_t s) {
     if (p.total_blocks <= 0) return;
-    launch_pdl(p.K_scale ? kv_compact_kernel<true> : kv_compact_kernel<false>, dim3(p.total_blocks), dim3(kCompactThreads), 0, s, p);
+    launch_pdl(!p.K_scale           ? kv_compact_kernel<0>
+               : p.vec_per_row == 4 ? kv_compact_kernel<64>
+               : p.vec_per_row == 8 ? kv_compact_kernel<128>
+                                    : kv_compact_kernel<256>,
+               dim3(p.total_blocks), dim3(kCompactThreads), 0, s, p);
 }
 
 void launch_gather_map(const GatherParams& p, cudaStream_t s) {

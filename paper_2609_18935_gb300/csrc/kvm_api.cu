@@ -614,7 +614,7 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     const int kv_layers = c->kv8 ? 1 : c->n_attn;          // of the bf16 slabs
     const size_t layer_elems = (size_t)c->Hkv * c->T_cap * c->D, kv_elems = (size_t)kv_layers * layer_elems;
     const int vec_per_row = c->D * 2 / 16;
-    c->rows_kv = c->kv8 ? kKv8Rows : c->n_attn ? kCompactVecPerChunk / std::max(vec_per_row, 1) : 1;
+    c->rows_kv = c->n_attn ? kCompactVecPerChunk / std::max(vec_per_row / (c->kv8 ? 2 : 1), 1) : 1;
     c->rows_pos = kCompactVecPerChunk;
     const int n_kv_slabs = 2 * c->n_attn * c->Hkv;
     size_t n_flags = 0;
@@ -845,11 +845,12 @@ Kv8Layer kv8_layer(const kvm_ctx* c, int a) {
     return {c->K8 + a * n, c->V8 + a * n, c->K8s + a * blocks, c->V8s + a * blocks};
 }
 
-// Blocks [block0, ...) of character b up to row `rows`, as items of kv8_append.
-Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int& items) {
+// Blocks [block0, ...) of character b up to row `rows`, as items of kv8_append, `each` blocks
+// of a head's K or V an item.
+Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int each, int& items) {
     const int n = std::max(0, (rows + kKv8Rows - 1) / kKv8Rows - block0);
     const Kv8Char ch{c->cap_off[b], block0, n, rows, items};
-    items += n * 2 * c->Hkv;
+    items += (n + each - 1) / each * 2 * c->Hkv;
     return ch;
 }
 
@@ -1332,13 +1333,13 @@ kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int tot
     for (int b = 0; b < c->B; ++b) {
         const AttnChar& ch = p.ch[b];
         const int whole = ch.L_prev / kKv8Rows;      // blocks that the tail leaves as they are
-        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, ap.n_items);
+        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, 1, ap.n_items);
         ap.L_prev[b] = ch.L_prev;
         ap.tail_off[b] = ch.tail_off;
         ap.p[b] = ch.p;
         // of them what the tail's first token sees; later ones begin later
         const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
-        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, ap.n_widen);
+        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, kv8_widen_blocks(c->D), ap.n_widen);
         ap.sink[b] = w.sink;
         ap.gap[b] = w.gap;
     }

@@ -286,6 +286,7 @@ struct Kv8AppendParams {
     int32_t sink[kMaxChars], gap[kMaxChars];
 };
 void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s);
+constexpr int kv8_widen_blocks(int D) { return 1024 / D; }   // of an item of `old`: 64 KB
 
 // Attention of a few rows a KV head straight from the 8-bit cache, under the same
 // partition and with the same partials as launch_tail_attention.  It rotates the tail's
