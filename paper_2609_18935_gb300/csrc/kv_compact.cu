@@ -115,7 +115,7 @@ struct Kv8Chunk {
 };
 // D8: head_dim of caches in 8 bits, 0 for bf16.
 template <int D8>
-__global__ void __launch_bounds__(kCompactThreads)
+__global__ void __launch_bounds__(kCompactThreads, D8 ? 4 : 0)
 kv_compact_kernel(const __grid_constant__ CompactParams p) {
     constexpr bool KV8 = D8 != 0;
     grid_dependency_wait();

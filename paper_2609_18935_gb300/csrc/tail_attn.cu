@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(32 * LANES) attn_combine_parts_kernel(const __
         acc.z = acc.z * sc + w * x.z; acc.w = acc.w * sc + w * x.w;
         mx = nmx;
     };
-    if (p.draft) {
+    if (p.many_parts) {
         // four parts in flight a thread
         for (int q0 = part; q0 < st.n_parts; q0 += 4 * LANES) {
             float2 ml[4];
@@ -472,7 +472,7 @@ void launch_attn_combine(const CombineParams& p, cudaStream_t s) {
         parts = max(parts, (int)p.tile[x].n_parts);
     }
     const int part_blocks = (rows * (p.D / 4) + 31) / 32;
-    if (p.draft) {
+    if (p.many_parts) {
         // up to a warp for two parts, while that grid is two waves (54 registers a
         // thread: 36 warps an SM), blocks of 16 warps only in one: 43 parts of two full
         // tiles 17.6 us a layer with 16 warps (two waves), 16.7 with eight; 16 tiles of
