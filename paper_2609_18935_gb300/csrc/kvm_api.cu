@@ -1451,7 +1451,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
         thread_local static CombineParams cp;
         cp.Hq = c->Hq; cp.D = c->D; cp.g = c->g;
         cp.n_split_tiles = (int)pl.split_cb.size();
-        cp.many_parts = anc || c->kv8 || p.window;
+        cp.many_parts = anc || c->kv8;
         cp.part_o = c->part_o;
         cp.part_ml = c->part_ml;
         cp.out = p.out;

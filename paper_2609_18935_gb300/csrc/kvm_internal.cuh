@@ -198,7 +198,7 @@ struct SplitTile {
 struct CombineParams {
     int32_t Hq, D, g;
     int32_t n_split_tiles;
-    int32_t many_parts;           // of a draft, a windowed layer or 8-bit caches: parts side by side while there is room
+    int32_t many_parts;           // of a draft or over 8-bit caches: parts side by side while there is room
     const float* part_o;          // as in AttnParams
     const float* part_ml;
     __nv_bfloat16* out;           // [sum M][Hq][D]

@@ -66,7 +66,12 @@
 // A query tile's units are then its sink tiles and the tiles from the one with its
 // first row's oldest key on; the tiles between them (Tile::gap) are no units at all,
 // so the cut, the rings and the merge are those of a shorter cache.  Only tiles at the
-// window's lower edge (one or two a query tile) compare keys with it.
+// window's lower edge (one or two a query tile) compare keys with it.  What a segment
+// costs besides its units (6 us of 14 at 17 units of head_dim 128) weighs more here: the
+// next Q is staged while the last PV runs, not before its P, and a quad of lanes stores
+// rows in turn.  4864 tokens, window 1000, us a layer with neither, the first, both:
+// head_dim 128 71.8, 68.6, 66.4; head_dim 256 105.8, 100.8, 95.8.  (Q loaded by quads too:
+// 70.5 and 97.9, the shuffles' registers are the loop's.)
 #pragma once
 
 #include "attn_tiles.cuh"
@@ -120,6 +125,26 @@ struct Cfg {
 };
 static_assert(Cfg<256>::SMEM <= 232448, "shared memory of the head_dim 256 attention");
 static_assert(Cfg<256>::TMEM_Q + 128 <= 512, "TMEM of the head_dim 256 attention");
+
+// Four lanes hold four 16-byte pieces each: afterwards lane q's a[i] is what lane i held as
+// a[q].  So 64 bytes of a row, which a thread reads from TMEM, are stored as four
+// neighbours' pieces, eight lines a store in place of 32.
+__device__ __forceinline__ void swap_quad(uint4 (&a)[4], int lane) {
+#pragma unroll
+    for (int k = 1; k <= 2; k <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i & k) continue;
+            const bool up = lane & k;
+            uint4& lo = a[i];
+            uint4& hi = a[i | k];
+            auto swap = [&](uint32_t& x, uint32_t& y) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x : y, k);
+                if (up) x = got; else y = got;
+            };
+            swap(lo.x, hi.x); swap(lo.y, hi.y); swap(lo.z, hi.z); swap(lo.w, hi.w);
+        }
+}
 
 // Rows of a draft's Q tile into TMEM, 16 lanes x 8 columns (a k step of the MMA) at
 // a time, eight rows of 32 bytes a load: with a row a thread every load touched 32
@@ -510,10 +535,10 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             }
             grid_dependency_wait();                        // q_rot comes from the previous grid
             const Tile T = decode_tile<WIN, TREE != kTail>(p, t);
-            const AttnChar& ch = p.ch[T.b];
-            const int tok = T.tok0 + r / g;
             constexpr int W = D / 4;                       // 32-bit words of this half
             uint4 v[W / 4];
+            const AttnChar& ch = p.ch[T.b];
+            const int tok = T.tok0 + r / g;
             const uint4* src = reinterpret_cast<const uint4*>(
                 p.q_rot + ((int64_t)(ch.tail_off + tok) * p.Hq + T.kvh * g + (r % g)) * D + grp * (D / 2));
 #pragma unroll
@@ -571,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 tc_fence_before();
                 mbar_arrive(bar(S_EMPTY + grp));
                 // the segment's last S has landed, so no MMA reads Q any more
-                if (!TREE && i + 1 == n && has_next) stage_q(tile_of(seg + 1));
+                if (!TREE && !WIN && i + 1 == n && has_next) stage_q(tile_of(seg + 1));
                 const int key0 = key_tile<WIN>(T, k + i) * BN;
                 if (WIN && key0 < low && key0 + BN > p.n_sink) {
                     const int from = max(p.n_sink - key0, 0), to = min(low - key0, BN);      // of the tile's keys
@@ -664,9 +689,10 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             }
             // the group without the segment's last tile stages its half of the
             // next Q too (the tile's S buffer is not filled again before that); a
-            // draft's Q, which takes more registers to stage, both groups here
+            // draft's Q, which takes more registers to stage, both groups here, and a
+            // window's, whose segments are short: the last P goes first
             const bool other = ((j + n - 1) & 1) != grp;
-            if (has_next && (TREE || other)) {
+            if (has_next && (TREE || WIN || other)) {
                 if (other) wait_all(S_FULL + (grp ^ 1), ((j + n - 1) >> 1) & 1, 0x35 + 256 * j);
                 tc_fence_after();
                 stage_q(tile_of(seg + 1));
@@ -684,28 +710,56 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             const float mfin = fmaxf(mr, mo);
             const float lt = l * scale_to(mr, mfin) + lo * scale_to(mo, mfin);
             const bool store = *abort_flag == 0;
-            const int hq = T.kvh * g + (r % g);
             if (full) {
                 // tcgen05.ld is warp-collective: every lane loads, real rows store
                 const float inv = row_valid ? 1.f / lt : 0.f;
-                __nv_bfloat16* o = p.out + ((int64_t)(ch.tail_off + (row_valid ? tok : 0)) * p.Hq + hq) * D;
+                if constexpr (WIN) {
+                    // the quad's rows are neighbours: heads of a token, then the next one's
+                    const int quad0 = quarter * 32 + (lane & ~3), n_rows = store ? (T.tok_end - T.tok0) * g : 0;
+                    const int step1 = g >= 2 ? D : p.Hq * D, step2 = g >= 4 ? 2 * D : (g == 2 ? 1 : 2) * p.Hq * D;
+                    __nv_bfloat16* o = p.out + ((int64_t)(ch.tail_off + T.tok0 + quad0 / g) * p.Hq + T.kvh * g + quad0 % g) * D + 8 * (lane & 3);
 #pragma unroll 1
-                for (int c0 = grp * C::HALF; c0 < (grp + 1) * C::HALF; c0 += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(tmem + lane_off + C::TMEM_O + c0, v);
-                    tmem_ld_wait();
-                    if (row_valid && store) {
-                        uint32_t w[16];
+                    for (int c0 = grp * C::HALF; c0 < (grp + 1) * C::HALF; c0 += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(tmem + lane_off + C::TMEM_O + c0, v);
+                        tmem_ld_wait();
+                        uint4 a[4];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * inv,
-                                                                      __uint_as_float(v[2 * e + 1]) * inv);
-                            w[e] = *reinterpret_cast<uint32_t*>(&h2);
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int x = 8 * i + 2 * e;
+                                __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(v[x]) * inv, __uint_as_float(v[x + 1]) * inv);
+                                w[e] = *reinterpret_cast<uint32_t*>(&h2);
+                            }
+                            a[i] = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        uint4* dst = reinterpret_cast<uint4*>(o + c0);
+                        swap_quad(a, lane);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            dst[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                        for (int i = 0; i < 4; ++i)
+                            if (quad0 + i < n_rows) *reinterpret_cast<uint4*>(o + (i & 1 ? step1 : 0) + (i & 2 ? step2 : 0) + c0) = a[i];
+                    }
+                } else {
+                    __nv_bfloat16* o = p.out + ((int64_t)(ch.tail_off + (row_valid ? tok : 0)) * p.Hq + T.kvh * g + r % g) * D;
+#pragma unroll 1
+                    for (int c0 = grp * C::HALF; c0 < (grp + 1) * C::HALF; c0 += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(tmem + lane_off + C::TMEM_O + c0, v);
+                        tmem_ld_wait();
+                        if (row_valid && store) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(v[2 * e]) * inv,
+                                                                          __uint_as_float(v[2 * e + 1]) * inv);
+                                w[e] = *reinterpret_cast<uint32_t*>(&h2);
+                            }
+                            uint4* dst = reinterpret_cast<uint4*>(o + c0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                dst[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                        }
                     }
                 }
             } else {
