@@ -49,15 +49,16 @@ constexpr int kStep = 16;                      // keys of a warp's step
 constexpr int BM = kAttnRows;
 constexpr float kUp = 7.f;                     // weights are taken 2^7 higher: up to 2^15, where f16 has room
 
+// Twelve and sixteen warps (of fewer stages) took longer: 62.1 against 60.9 us for 32
+// characters over 16K, 8.1 against 7.3 for one over 512, more of them meet at the end.
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+
 template <int D, int NT>
 struct Cfg {
-    // as many warps as their registers allow (O and Q: 96 D NT / 256 of a thread's): a step is
-    // bound by its instructions' latency, with two warps a scheduler twice as much as by memory
-    static constexpr int kWarps = D * NT > 256 ? 8 : D * NT > 128 ? 12 : 16;
-    static constexpr int kThreads = 32 * kWarps;
     static constexpr int SIDE = kStep * D;                     // bytes of a step's K, or V
     static constexpr int STAGE = 2 * SIDE + 16;                // and its two scales
-    static constexpr int STAGES = D == 256 ? (NT == 2 ? 3 : 2) : D == 128 ? (NT == 2 ? 4 : 3) : 6;
+    static constexpr int STAGES = D == 256 ? 3 : 6;
     static constexpr int RING = STAGES * STAGE;
     static constexpr int ROWS = 8 * NT;
     static constexpr int PITCH = D + 4;                        // floats of a merged row
@@ -70,8 +71,7 @@ struct Cfg {
     static constexpr int OFF_X = OFF_TURN + ROWS * D * 4;
     static constexpr int SMEM = OFF_X + ROWS * D * 4;
 };
-static_assert(Cfg<256, 1>::SMEM <= 232448 && Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 1>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448 &&
-              Cfg<64, 2>::SMEM <= 232448, "shared memory");
+static_assert(Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448 && Cfg<64, 2>::SMEM <= 232448, "shared memory");
 
 // Byte offset of 16-byte piece `col` of row `row` of a step's K or V.
 template <int D>
@@ -122,7 +122,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 template <int D, int NT>
 __device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt, float* red, const float2* turn,
                                            float* keys) {
-    constexpr int kWarps = Cfg<D, NT>::kWarps, kThreads = Cfg<D, NT>::kThreads;
     constexpr int kOld = (kKv8Rows * D / 16 + kThreads - 1) / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
     const AttnParams& p = pp.a;
     const int tid = threadIdx.x, half = p.R / 2, row0 = kt * kAttnKeys;
@@ -240,9 +239,8 @@ __device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnCh
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(Cfg<D, NT>::kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
+__global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
     using C = Cfg<D, NT>;
-    constexpr int kWarps = C::kWarps, kThreads = C::kThreads;
     constexpr int KS = D / 16;                                 // 16-row pieces of O^T
     extern __shared__ __align__(128) uint8_t smem[];
     const AttnParams& p = pp.a;
@@ -607,7 +605,7 @@ void launch(const Kv8AttnParams& p, cudaStream_t s) {
         cudaFuncSetAttribute(kv8_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, NT>::SMEM);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(Cfg<D, NT>::kThreads), Cfg<D, NT>::SMEM, s, p);
+    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(kThreads), Cfg<D, NT>::SMEM, s, p);
 }
 
 template <int D>

@@ -435,8 +435,12 @@ constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 constexpr PlanCost kDraftCost{3, 32.0};
 
 // Few rows over 8-bit caches (kv8_attn.cu): a unit is 128 D bytes to load, a segment the
-// rows' queries, the warps' meeting and the partials, whatever D is.
-PlanCost kv8_cost(int D) { return {1024 / D, 2048.0 / D, 4096 / D}; }
+// rows' queries, the warps' meeting, the partials and their merge, whatever D is.  With
+// 8 | 16 | 24 | 32 units a segment at D 256, us a step: 32 characters over 16K 60.9 | 56.8 |
+// 58.1 | 58.0, four over 32K 18.5 | 16.8 | 16.7 | 16.7.  Tiles of up to five units there stay
+// whole (600 entries 11.2, with up to 8 of them 13.4), two units are worth a block (4096
+// entries 11.5, with four 13.4).
+PlanCost kv8_cost(int D) { return {512 / D, 4096.0 / D, 1280 / D}; }
 
 // What a layer's rows see: of a windowed layer (kvm_set_window) fewer key tiles, the
 // same for all query tiles of a draft, whose first rows all follow the last live entry.

@@ -43,9 +43,9 @@
 //               through shared memory and a barrier between the two warps of
 //               the quarter, and each group sums its own tiles.  P_j goes back
 //               to TMEM as bf16, into one of two buffers beside S.  Both groups
-//               stage the segment's Q tile in TMEM (the next segment's as soon
-//               as the last S of the current one has landed) and store half of
-//               the O columns each at its end.
+//               stage the segment's Q tile in TMEM (the next segment's behind
+//               the current one's last P) and store half of the O columns each
+//               at its end.
 // P in TMEM spares shared memory, which the MMAs and the TMA keep busy, 32 KB
 // of traffic a unit (P written, and read again by the MMA); S then has one
 // buffer, which a thread with a whole row empties at once.  With each row split
@@ -66,12 +66,14 @@
 // A query tile's units are then its sink tiles and the tiles from the one with its
 // first row's oldest key on; the tiles between them (Tile::gap) are no units at all,
 // so the cut, the rings and the merge are those of a shorter cache.  Only tiles at the
-// window's lower edge (one or two a query tile) compare keys with it.  What a segment
-// costs besides its units (6 us of 14 at 17 units of head_dim 128) weighs more here: the
-// next Q is staged while the last PV runs, not before its P, and a quad of lanes stores
-// rows in turn.  4864 tokens, window 1000, us a layer with neither, the first, both:
-// head_dim 128 71.8, 68.6, 66.4; head_dim 256 105.8, 100.8, 95.8.  (Q loaded by quads too:
-// 70.5 and 97.9, the shuffles' registers are the loop's.)
+// window's lower edge (one or two a query tile) compare keys with it.
+//
+// What a segment costs besides its units (6 us of 14 at 17 units of head_dim 128) weighs
+// most under a window: the next Q is staged while the last PV runs, not before its P,
+// and a quad of lanes stores its rows in turn.  4864 tokens, window 1000, us a layer with
+// neither, the first, both: head_dim 128 71.8, 68.6, 66.4; head_dim 256 105.8, 100.8, 95.8;
+// without a window 1024 tokens at 32K 356 : 342 with both, 16384 from nothing 1513 : 1463.
+// (Q loaded by quads too: 70.5 and 97.9, the shuffles' registers are the loop's.)
 #pragma once
 
 #include "attn_tiles.cuh"
@@ -595,8 +597,6 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 tmem_ld_wait();
                 tc_fence_before();
                 mbar_arrive(bar(S_EMPTY + grp));
-                // the segment's last S has landed, so no MMA reads Q any more
-                if (!TREE && !WIN && i + 1 == n && has_next) stage_q(tile_of(seg + 1));
                 const int key0 = key_tile<WIN>(T, k + i) * BN;
                 if (WIN && key0 < low && key0 + BN > p.n_sink) {
                     const int from = max(p.n_sink - key0, 0), to = min(low - key0, BN);      // of the tile's keys
@@ -687,12 +687,10 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 l = l * scale_to(mr, mn) + ((sum4[0] + sum4[1]) + (sum4[2] + sum4[3]));
                 mr = mn;
             }
-            // the group without the segment's last tile stages its half of the
-            // next Q too (the tile's S buffer is not filled again before that); a
-            // draft's Q, which takes more registers to stage, both groups here, and a
-            // window's, whose segments are short: the last P goes first
+            // both groups stage the next Q, behind the last P: no MMA reads this one once the
+            // segment's last S has landed (which the group without that tile waits for here)
             const bool other = ((j + n - 1) & 1) != grp;
-            if (has_next && (TREE || WIN || other)) {
+            if (has_next) {
                 if (other) wait_all(S_FULL + (grp ^ 1), ((j + n - 1) >> 1) & 1, 0x35 + 256 * j);
                 tc_fence_after();
                 stage_q(tile_of(seg + 1));
@@ -713,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
             if (full) {
                 // tcgen05.ld is warp-collective: every lane loads, real rows store
                 const float inv = row_valid ? 1.f / lt : 0.f;
-                if constexpr (WIN) {
+                if constexpr (!TREE) {
                     // the quad's rows are neighbours: heads of a token, then the next one's
                     const int quad0 = quarter * 32 + (lane & ~3), n_rows = store ? (T.tok_end - T.tok0) * g : 0;
                     const int step1 = g >= 2 ? D : p.Hq * D, step2 = g >= 4 ? 2 * D : (g == 2 ? 1 : 2) * p.Hq * D;
