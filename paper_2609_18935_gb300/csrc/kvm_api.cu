@@ -1366,8 +1366,9 @@ int most_rows(const kvm_ctx* c, const int32_t* tail_cu) {
 kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int total, const AttnPlan& pl, const void* q,
                             const void* k_new, const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev,
                             const uint64_t* anc) {
-    thread_local static AttnParams p;
-    std::memset(&p, 0, sizeof p);
+    thread_local static Kv8AttnParams p8;         // large parameter blocks, copied into the launch
+    AttnParams& p = p8.a;
+    std::memset(&p, 0, offsetof(AttnParams, ch));  // (of its tables only what is written here is read)
     const int a = c->attn_idx[layer];
     p.tmap_k = c->tmap_k;
     p.tmap_v = c->tmap_v;
@@ -1440,12 +1441,10 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     }
     int ps = prof_begin(c, KVM_K_ATTENTION, s);
     if (direct) {
-        thread_local static Kv8AttnParams dp;
-        dp.a = p;
-        dp.from = kv8_layer(c, a);
-        dp.rows = rows;
-        std::copy(c->turn, c->turn + kMaxRotaryHalf, dp.turn);
-        launch_kv8_attention(dp, s);
+        p8.from = kv8_layer(c, a);
+        p8.rows = rows;
+        std::copy(c->turn, c->turn + kMaxRotaryHalf, p8.turn);
+        launch_kv8_attention(p8, s);
     } else {
         launch_tail_attention(p, s);
     }

@@ -442,6 +442,8 @@ class Context:
         _check(create(C.byref(self.desc), self.n_chars, _p32(caps), int(max_tail_tokens), C.byref(h)))
         self._h = h
         self._draft_nodes = None
+        self._live, self._cursor = C.c_int32(), C.c_int64()      # get_live's answers
+        self._live_refs = C.byref(self._live), C.byref(self._cursor)
 
     def destroy(self):
         if self._h:
@@ -469,14 +471,14 @@ class Context:
         live, _ = self.get_live(b)
         k = torch.empty((self.Hkv, live, self.D), dtype=torch.bfloat16, device="cuda")
         v = torch.empty_like(k)
-        _check(_lib.kvm_get_kv(self._h, layer, b, _dptr(k), _dptr(v), _stream(stream)))
+        _check(_lib.kvm_get_kv(self._h, layer, b, k.data_ptr(), v.data_ptr(), _stream(stream)))
         return k, v
 
     def get_positions(self, b, stream=None):
         torch = _torch()
         live, _ = self.get_live(b)
         out = torch.empty(live, dtype=torch.int32, device="cuda")
-        _check(_lib.kvm_get_positions(self._h, b, _dptr(out), _stream(stream)))
+        _check(_lib.kvm_get_positions(self._h, b, out.data_ptr(), _stream(stream)))
         return out
 
     def set_state(self, layer, S, stream=None):
@@ -511,9 +513,8 @@ class Context:
         _check(_lib.kvm_set_window(self._h, int(layer), int(window), int(n_sink)))
 
     def get_live(self, b):
-        live, cur = C.c_int32(), C.c_int64()
-        _check(_lib.kvm_get_live(self._h, b, C.byref(live), C.byref(cur)))
-        return live.value, cur.value
+        _check(_lib.kvm_get_live(self._h, b, *self._live_refs))
+        return self._live.value, self._cursor.value
 
     def spans_from_positions(self, b, pos_begin, pos_end):
         pb = np.ascontiguousarray(pos_begin, dtype=np.int64)
@@ -535,14 +536,18 @@ class Context:
         (host int32 [sum M], one position id per tail token) is given."""
         cu = _b32(tail_cu)
         bf = _torch().bfloat16
-        if tail_pos is None:
-            _check(_lib.kvm_tail_attn_prefill(self._h, layer, cu, _dptr(q, bf), _dptr(k_new, bf),
-                                              _dptr(v_new, bf), _dptr(out, bf), _stream(stream)))
+        # all four at once: a microsecond less than one by one, which names the one that fails
+        if (q is not None and k_new is not None and v_new is not None and out is not None
+                and q.dtype is bf and k_new.dtype is bf and v_new.dtype is bf and out.dtype is bf
+                and q.is_cuda and k_new.is_cuda and v_new.is_cuda and out.is_cuda
+                and q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous() and out.is_contiguous()):
+            ptrs = (q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr())
         else:
-            tp = _b32(tail_pos)
-            _check(_lib.kvm_tail_attn_prefill_at(self._h, layer, cu, tp, _dptr(q, bf),
-                                                 _dptr(k_new, bf), _dptr(v_new, bf), _dptr(out, bf),
-                                                 _stream(stream)))
+            ptrs = (_dptr(q, bf), _dptr(k_new, bf), _dptr(v_new, bf), _dptr(out, bf))
+        if tail_pos is None:
+            _check(_lib.kvm_tail_attn_prefill(self._h, layer, cu, *ptrs, _stream(stream)))
+        else:
+            _check(_lib.kvm_tail_attn_prefill_at(self._h, layer, cu, _b32(tail_pos), *ptrs, _stream(stream)))
 
     def rerotate_keys(self, b, live_begin, live_end, new_pos, stream=None):
         """kvm_rerotate_keys: turn the stored keys of live entries
