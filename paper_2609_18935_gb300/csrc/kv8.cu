@@ -23,19 +23,21 @@ constexpr int kThreads = 256;
 constexpr int kAppendThreads = 512;
 constexpr int kPackThreads = 512;
 
-// An item's character (the last with blk_off <= item), block, head, and K or V.
+// An item's character (the last whose first item is at or before it), head, K or V, and
+// which of its items it is.
 struct Item {
-    int b, block, head;
+    int b, index, head;
     bool is_v;
 };
-__device__ __forceinline__ Item item_of(const Kv8AppendParams& p, const Kv8Char* ch, int item) {
+template <int32_t Kv8AppendChar::*FIRST>
+__device__ __forceinline__ Item item_of(const Kv8AppendParams& p, int item) {
     int lo = 0, hi = p.n_chars - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (ch[mid].blk_off <= item) lo = mid; else hi = mid - 1;
+        if (p.ch[mid].*FIRST <= item) lo = mid; else hi = mid - 1;
     }
-    const int local = item - ch[lo].blk_off, per = 2 * p.Hkv;
-    return {lo, ch[lo].block0 + local / per, local % per / 2, (bool)(local & 1)};
+    const int local = item - p.ch[lo].*FIRST, per = 2 * p.Hkv;
+    return {lo, local / per, local % per / 2, (bool)(local & 1)};
 }
 
 template <int THREADS>
@@ -52,11 +54,12 @@ __device__ __forceinline__ float block_max(float m, float* red) {
 // A block's 64 x D numbers as bf16 rows, those below `rows`.
 template <int D, int THREADS>
 __device__ __forceinline__ void widen_block(const uint8_t* from, float scale, __nv_bfloat16* to, int rows) {
-    constexpr int kAll = kKv8Rows * D / 16, kEach = (kAll + THREADS - 1) / THREADS;
-    const uint4* src = reinterpret_cast<const uint4*>(from);
+    constexpr int kEach = kKv8Rows * D / 8 / THREADS;
+    const uint2* src = reinterpret_cast<const uint2*>(from);
     uint4* dst = reinterpret_cast<uint4*>(to);
-    const int n = min(rows, kKv8Rows) * (D / 16);
-    uint4 w[kEach];
+    const __nv_bfloat162 s = __float2bfloat162_rn(scale);
+    const int n = min(rows, kKv8Rows) * (D / 8);
+    uint2 w[kEach];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const int i = threadIdx.x + k * THREADS;
@@ -65,33 +68,28 @@ __device__ __forceinline__ void widen_block(const uint8_t* from, float scale, __
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const int i = threadIdx.x + k * THREADS;
-        uint4 a, b;
-        if (i < n) {
-            widen16(w[k], scale, a, b);
-            dst[2 * i] = a;
-            dst[2 * i + 1] = b;
-        }
+        if (i < n) dst[i] = widen8(w[k], s);
     }
 }
 
 // Some older blocks in sight of one head's K or V, all loads under way at once.
 template <int D>
 __device__ __forceinline__ void widen_old(const Kv8AppendParams& p, int item) {
-    constexpr int kEach = 8, kVecs = kKv8Rows * D / 16;        // vectors a thread, of a block
+    constexpr int kEach = 16, kVecs = kKv8Rows * D / 8;        // eights a thread, of a block
     static_assert(kEach * kAppendThreads == kv8_widen_blocks(D) * kVecs, "an item");
-    const Item it = item_of(p, p.old, item);                   // (`block` counts items)
-    const Kv8Char& c = p.old[it.b];
-    const int first = it.block * kv8_widen_blocks(D), sink = p.sink[it.b], gap = p.gap[it.b];
+    const Item it = item_of<&Kv8AppendChar::old_off>(p, item);
+    const Kv8AppendChar& c = p.ch[it.b];
+    const int first = it.index * kv8_widen_blocks(D);
     const int64_t slot0 = (int64_t)it.head * p.slab_rows + c.cap_off;
-    const uint4* src = reinterpret_cast<const uint4*>((it.is_v ? p.to.V : p.to.K) + slot0 * D);
+    const uint2* src = reinterpret_cast<const uint2*>((it.is_v ? p.to.V : p.to.K) + slot0 * D);
     uint4* dst = reinterpret_cast<uint4*>((it.is_v ? p.V : p.K) + slot0 * D);
     const float* scales = (it.is_v ? p.to.Vs : p.to.Ks) + slot0 / kKv8Rows;
-    uint4 w[kEach];
-    float s[kEach];
-    auto at = [&](int k, int& block) {                         // vector of the character's slab
+    uint2 w[kEach];
+    __nv_bfloat162 s[kEach];
+    auto at = [&](int k, int& block) {                         // eight of the character's slab
         const int v = threadIdx.x + k * kAppendThreads, n = first + v / kVecs;
-        block = n + (n >= sink ? gap : 0);
-        return n < c.n_blocks ? (int64_t)block * kVecs + v % kVecs : (int64_t)-1;
+        block = n + (n >= c.sink ? c.gap : 0);
+        return n < c.n_old ? (int64_t)block * kVecs + v % kVecs : (int64_t)-1;
     };
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
@@ -99,17 +97,14 @@ __device__ __forceinline__ void widen_old(const Kv8AppendParams& p, int item) {
         const int64_t v = at(k, block);
         if (v < 0) continue;
         w[k] = src[v];
-        s[k] = scales[block];
+        s[k] = __float2bfloat162_rn(scales[block]);
     }
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         int block;
         const int64_t v = at(k, block);
         if (v < 0) continue;
-        uint4 a, b;
-        widen16(w[k], s[k], a, b);
-        dst[2 * v] = a;
-        dst[2 * v + 1] = b;
+        dst[v] = widen8(w[k], s[k]);
     }
 }
 
@@ -120,9 +115,9 @@ __device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, fl
     int lo = 0, hi = p.n_chars - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (p.tail_off[mid] <= n) lo = mid; else hi = mid - 1;
+        if (p.ch[mid].tail_off <= n) lo = mid; else hi = mid - 1;
     }
-    const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : p.p[lo] + n - p.tail_off[lo];
+    const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : p.ch[lo].p + n - p.ch[lo].tail_off;
     const __nv_bfloat16* q = p.q + (int64_t)n * p.Hq * D;
     __nv_bfloat16* o = p.q_rot + (int64_t)n * p.Hq * D;
     if (half % 8 == 0) {
@@ -167,11 +162,129 @@ __device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, fl
     }
 }
 
+// Eight numbers under a scale (its reciprocal inv, itself as bf16 in `to`): into the block and as bf16.
+__device__ __forceinline__ void put8(const float (&x)[8], float inv, __nv_bfloat162 to, uint8_t* d8, __nv_bfloat16* d16) {
+    const uint32_t a = to_e4m3(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), b = to_e4m3(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+    *reinterpret_cast<uint2*>(d8) = make_uint2(a, b);
+    *reinterpret_cast<uint4*>(d16) = widen8(make_uint2(a, b), to);
+}
+__device__ __forceinline__ void get8(const uint4& w, float (&x)[8]) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = bf2_f2(v[e]);
+        x[2 * e] = f.x;
+        x[2 * e + 1] = f.y;
+    }
+}
+
+// A block behind the live entries, in registers from its loads to its stores: a thread has
+// eight pairs that are turned (R up to 128, a multiple of 16), up to D / 64 eights that are
+// not, and as many of older rows.  The angles are formed while the loads are under way.
+template <int D>
+__device__ __forceinline__ void form_block(const Kv8AppendParams& p, float* red) {
+    constexpr int kOld = kKv8Rows * D / 8 / kAppendThreads, kFlat = kOld;
+    const Item it = item_of<&Kv8AppendChar::blk_off>(p, blockIdx.x);
+    const Kv8AppendChar& c = p.ch[it.b];
+    const int t = threadIdx.x, L = c.L, row0 = (L / kKv8Rows + it.index) * kKv8Rows;
+    const int old = min(max(L - row0, 0), kKv8Rows), end = min(L + c.M - row0, kKv8Rows);   // rows [old, end) are new, behind them 0
+    const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
+    uint8_t* dst = (it.is_v ? p.to.V : p.to.K) + slot * D;
+    __nv_bfloat16* wide = (it.is_v ? p.V : p.K) + slot * D;
+    float* scale = (it.is_v ? p.to.Vs : p.to.Ks) + slot / kKv8Rows;
+    const int n0 = c.tail_off + row0 - L;                // packed token of the block's first row
+    const int R = it.is_v ? 0 : p.R, half = R / 2, turned = half / 8, flat = (D - R) / 8;      // of a row: eights in pairs, and alone
+    const __nv_bfloat16* x = (it.is_v ? p.v_new : p.k_new) + ((int64_t)n0 * p.Hkv + it.head) * D;
+    const int64_t row = (int64_t)p.Hkv * D;
+    const int tr = turned ? t / turned : kKv8Rows, td = turned ? t % turned * 8 : 0;           // the row and first dim of the pairs
+    const bool has = tr >= old && tr < kKv8Rows;
+    const float s = old ? *scale : 0.f;
+    uint2 was[kOld];
+    uint4 is[kFlat], a = make_uint4(0, 0, 0, 0), b = a;
+    if (has && tr < end) {
+        a = *reinterpret_cast<const uint4*>(x + tr * row + td);
+        b = *reinterpret_cast<const uint4*>(x + tr * row + td + half);
+    }
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        const int i = t + k * kAppendThreads, r = flat ? i / flat : kKv8Rows;
+        is[k] = make_uint4(0, 0, 0, 0);
+        if (r >= old && r < end) is[k] = *reinterpret_cast<const uint4*>(x + r * row + R + i % flat * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) {
+        const int i = t + k * kAppendThreads;
+        was[k] = make_uint2(0, 0);
+        if (i < old * (D / 8)) was[k] = reinterpret_cast<const uint2*>(dst)[i];
+    }
+    float u[8], v[8], m = 0.f;
+    bool bad = false;
+    if (has) {
+        float co[8], si[8];
+        const int64_t pos = tr >= end ? 0 : p.tail_pos ? (int64_t)p.tail_pos[n0 + tr] : c.p + row0 + tr - L;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turn_of(pos, p.turn[td + e], co[e], si[e]);
+        bad = clear_not_finite(a) || bad;
+        bad = clear_not_finite(b) || bad;
+        get8(a, u);
+        get8(b, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = u[e];
+            u[e] = y * co[e] - v[e] * si[e];
+            v[e] = v[e] * co[e] + y * si[e];
+            if (!isfinite(u[e])) { u[e] = 0.f; bad = true; }   // two of the largest numbers together
+            if (!isfinite(v[e])) { v[e] = 0.f; bad = true; }
+            m = fmaxf(m, fmaxf(fabsf(u[e]), fabsf(v[e])));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        bad = clear_not_finite(is[k]) || bad;
+        float y[8];
+        get8(is[k], y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
+    }
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) m = fmaxf(m, e4m3_max(make_uint4(was[k].x, was[k].y, 0, 0)) * s);
+    if (!it.is_v && it.head == 0)
+        for (int r = old + t; r < end; r += kAppendThreads)
+            p.pos[c.cap_off + row0 + r] = p.tail_pos ? p.tail_pos[n0 + r] : (int32_t)(c.p + row0 + r - L);
+    m = block_max<kAppendThreads>(m, red);
+    const int e = kv8_exponent(m);
+    const float to = pow2(e), inv = pow2(-e);
+    const __nv_bfloat162 to2 = __float2bfloat162_rn(to);
+    if (has) {
+        put8(u, inv, to2, dst + tr * D + td, wide + tr * D + td);
+        put8(v, inv, to2, dst + tr * D + td + half, wide + tr * D + td + half);
+    }
+#pragma unroll
+    for (int k = 0; k < kFlat; ++k) {
+        const int i = t + k * kAppendThreads, r = flat ? i / flat : kKv8Rows;
+        if (r < old || r >= kKv8Rows) continue;
+        float y[8];
+        get8(is[k], y);
+        put8(y, inv, to2, dst + r * D + R + i % flat * 8, wide + r * D + R + i % flat * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < kOld; ++k) {
+        const int i = t + k * kAppendThreads;
+        if (i >= old * (D / 8)) continue;
+        const uint2 w = s == to ? was[k] : requantised(was[k], s, inv);
+        if (s != to) reinterpret_cast<uint2*>(dst)[i] = w;
+        reinterpret_cast<uint4*>(wide)[i] = widen8(w, to2);
+    }
+    if (t == 0) *scale = to;
+    if (bad) atomicOr(p.err, kErrValue);
+}
+
 // Blocks first (the longest way), then the blocks in sight that only need widening, then
 // a thread block for each token's queries.  One launch for the three: 8192 entries and
 // 256 tokens of 16 heads of 256 took 11.1 us for blocks and queries and 8.5 behind them
 // for the widening.
-template <int D>
+// IN_REGS: form_block; else, for the rotary dims that it does not take, by way of shared memory.
+template <int D, bool IN_REGS>
 __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __grid_constant__ Kv8AppendParams p) {
     extern __shared__ __align__(16) float tile[];              // [64][D]
     __shared__ float red[kAppendThreads / 32];
@@ -187,14 +300,18 @@ __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __g
         widen_old<D>(p, blockIdx.x - p.n_items);
         return;
     }
-    const Item it = item_of(p, p.ch, blockIdx.x);
-    const Kv8Char& c = p.ch[it.b];
-    const int row0 = it.block * kKv8Rows, L = p.L_prev[it.b];
-    const int old = min(max(L - row0, 0), kKv8Rows), end = min(c.rows - row0, kKv8Rows);   // rows [old, end) are new
+    if constexpr (IN_REGS) {
+        form_block<D>(p, red);
+        return;
+    }
+    const Item it = item_of<&Kv8AppendChar::blk_off>(p, blockIdx.x);
+    const Kv8AppendChar& c = p.ch[it.b];
+    const int L = c.L, row0 = (L / kKv8Rows + it.index) * kKv8Rows;
+    const int old = min(max(L - row0, 0), kKv8Rows), end = min(L + c.M - row0, kKv8Rows);   // rows [old, end) are new
     const int64_t slot = (int64_t)it.head * p.slab_rows + c.cap_off + row0;
     uint8_t* dst = (it.is_v ? p.to.V : p.to.K) + slot * D;
     float* scale = (it.is_v ? p.to.Vs : p.to.Ks) + slot / kKv8Rows;
-    const int n0 = p.tail_off[it.b] + row0 - L;                // packed token of the block's first row
+    const int n0 = c.tail_off + row0 - L;                // packed token of the block's first row
     bool bad = false;
     float m = 0.f;
     {
@@ -247,7 +364,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __g
         __syncthreads();
         for (int i = t; i < (end - old) * half; i += kAppendThreads) {
             const int r = old + i / half, d = i % half;
-            const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n0 + r] : p.p[it.b] + row0 + r - L;
+            const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n0 + r] : c.p + row0 + r - L;
             float co, si;
             turn_of(pos, p.turn[d], co, si);
             float* x = tile + r * D + d;
@@ -261,7 +378,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __g
     }
     if (!it.is_v && it.head == 0)
         for (int r = old + t; r < end; r += kAppendThreads)
-            p.pos[c.cap_off + row0 + r] = p.tail_pos ? p.tail_pos[n0 + r] : (int32_t)(p.p[it.b] + row0 + r - L);
+            p.pos[c.cap_off + row0 + r] = p.tail_pos ? p.tail_pos[n0 + r] : (int32_t)(c.p + row0 + r - L);
     m = block_max<kAppendThreads>(m, red);
     const int e = kv8_exponent(m);
     const float to = pow2(e), inv = pow2(-e);
@@ -339,15 +456,20 @@ __global__ void __launch_bounds__(kPackThreads) kv8_pack_kernel(const __grid_con
 
 template <int D>
 void launch_append(const Kv8AppendParams& p, cudaStream_t s) {
+    const dim3 grid(p.n_items + p.n_widen + p.total);
+    if (p.R % 16 == 0 && p.R <= 128) {
+        launch_pdl(kv8_append_kernel<D, true>, grid, dim3(kAppendThreads), 0, s, p);
+        return;
+    }
     constexpr int smem = kKv8Rows * D * (int)sizeof(float);
     static unsigned long long configured = 0;   // one bit per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(configured >> (dev & 63) & 1ull)) {
-        cudaFuncSetAttribute(kv8_append_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        cudaFuncSetAttribute(kv8_append_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(kv8_append_kernel<D>, dim3(p.n_items + p.n_widen + p.total), dim3(kAppendThreads), smem, s, p);
+    launch_pdl(kv8_append_kernel<D, false>, grid, dim3(kAppendThreads), smem, s, p);
 }
 
 }  // namespace

@@ -120,7 +120,7 @@ struct kvm_ctx {
     uint8_t* V8 = nullptr;
     float* K8s = nullptr;
     float* V8s = nullptr;
-    uint64_t turn[kMaxRotaryHalf] = {};   // inv_freq in 2^-64 of a whole turn
+    uint64_t* turn = nullptr;             // device [R / 2]: inv_freq in 2^-64 of a whole turn
     int32_t* pos = nullptr;
     float* S = nullptr;
     // workspace
@@ -580,8 +580,6 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
         if (!(c->theta > 0)) { delete c; return fail(KVM_E_INVAL, "rope_theta must be positive"); }
         for (int d = 0; d < c->R / 2; ++d) c->inv_freq[d] = std::pow(c->theta, -2.0 * d / c->R);
         c->kv8 = kv8;
-        for (int d = 0; d < c->R / 2; ++d)
-            c->turn[d] = (uint64_t)std::ldexp(std::fmod((long double)c->inv_freq[d] / 6.283185307179586476925286766559L, 1.0L), 64);
     }
     if (c->n_gdn > 0) {
         c->H = m->n_gdn_heads; c->dk = m->d_k; c->dv = m->d_v;
@@ -636,6 +634,11 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
         if (e == cudaSuccess) e = alloc_zero(&c->V8, n);
         if (e == cudaSuccess) e = alloc_zero(&c->K8s, blocks);
         if (e == cudaSuccess) e = alloc_zero(&c->V8s, blocks);
+        uint64_t turn[kMaxRotaryHalf];
+        for (int d = 0; d < c->R / 2; ++d)
+            turn[d] = (uint64_t)std::ldexp(std::fmod((long double)c->inv_freq[d] / 6.283185307179586476925286766559L, 1.0L), 64);
+        if (e == cudaSuccess) e = alloc_zero(&c->turn, c->R / 2);
+        if (e == cudaSuccess && c->R) e = cudaMemcpy(c->turn, turn, sizeof(uint64_t) * (c->R / 2), cudaMemcpyHostToDevice);
     }
     if (e == cudaSuccess) e = alloc_zero(&c->pos, c->n_attn ? (size_t)c->T_cap : 0);
     if (e == cudaSuccess) e = alloc_zero(&c->S, (size_t)c->n_gdn * n_chars * c->H * c->dv * c->dk);
@@ -847,15 +850,6 @@ kvm_status check_device(const kvm_ctx* c) {
 Kv8Layer kv8_layer(const kvm_ctx* c, int a) {
     const size_t n = (size_t)c->Hkv * c->T_cap * c->D, blocks = n / ((size_t)kKv8Rows * c->D);
     return {c->K8 + a * n, c->V8 + a * n, c->K8s + a * blocks, c->V8s + a * blocks};
-}
-
-// Blocks [block0, ...) of character b up to row `rows`, as items of kv8_append, `each` blocks
-// of a head's K or V an item.
-Kv8Char kv8_char(const kvm_ctx* c, int b, int block0, int rows, int each, int& items) {
-    const int n = std::max(0, (rows + kKv8Rows - 1) / kKv8Rows - block0);
-    const Kv8Char ch{c->cap_off[b], block0, n, rows, items};
-    items += (n + each - 1) / each * 2 * c->Hkv;
-    return ch;
 }
 
 // Attention layer a's first `rows` rows of character b between its blocks and bf16 rows at
@@ -1332,20 +1326,17 @@ kvm_status launch_kv8_before(kvm_ctx* c, int layer, const AttnParams& p, int tot
     ap.pos = p.pos;
     ap.tail_pos = p.tail_pos;
     ap.err = p.err;
-    std::copy(c->turn, c->turn + kMaxRotaryHalf, ap.turn);
+    ap.turn = c->turn;
     ap.n_items = ap.n_widen = 0;
     for (int b = 0; b < c->B; ++b) {
         const AttnChar& ch = p.ch[b];
         const int whole = ch.L_prev / kKv8Rows;      // blocks that the tail leaves as they are
-        ap.ch[b] = kv8_char(c, b, whole, ch.M ? ch.L_prev + ch.M : 0, 1, ap.n_items);
-        ap.L_prev[b] = ch.L_prev;
-        ap.tail_off[b] = ch.tail_off;
-        ap.p[b] = ch.p;
         // of them what the tail's first token sees; later ones begin later
         const WindowTiles w = p.window ? window_tiles(ch.L_prev, p.window, p.n_sink) : WindowTiles{0, 0};
-        ap.old[b] = kv8_char(c, b, 0, ch.M ? (whole - w.gap) * kKv8Rows : 0, kv8_widen_blocks(c->D), ap.n_widen);
-        ap.sink[b] = w.sink;
-        ap.gap[b] = w.gap;
+        const int fresh = ch.M ? (ch.L_prev + ch.M - 1) / kKv8Rows - whole + 1 : 0, old = ch.M ? whole - w.gap : 0;
+        ap.ch[b] = {ch.cap_off, ch.L_prev, ch.M, ch.tail_off, ap.n_items, ap.n_widen, old, w.sink, w.gap, ch.p};
+        ap.n_items += fresh * 2 * c->Hkv;
+        ap.n_widen += (old + kv8_widen_blocks(c->D) - 1) / kv8_widen_blocks(c->D) * 2 * c->Hkv;
     }
     const int ps = prof_begin(c, KVM_K_ROPE_APPEND, s);
     launch_kv8_append(ap, s);
@@ -1443,7 +1434,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     if (direct) {
         p8.from = kv8_layer(c, a);
         p8.rows = rows;
-        std::copy(c->turn, c->turn + kMaxRotaryHalf, p8.turn);
+        p8.turn = c->turn;
         launch_kv8_attention(p8, s);
     } else {
         launch_tail_attention(p, s);

@@ -237,14 +237,6 @@ struct Kv8Layer {
     float* Vs;
 };
 
-struct Kv8Char {
-    int32_t cap_off;      // slot offset of the character in the slabs
-    int32_t block0;       // its first block that takes part
-    int32_t n_blocks;
-    int32_t rows;         // rows in use, counted from the character's first
-    int32_t blk_off;      // first (block, head, K or V) item of this character
-};
-
 // A character's `rows` rows between its 8-bit blocks and bf16 rows, at row0 on of
 // slabs [Hkv][other_rows][D].  pack: into the blocks, the rest of the last becomes 0.
 // widen: out of them, rows at or past `rows` are left alone.
@@ -263,27 +255,33 @@ void launch_kv8_widen(const Kv8CopyParams& p, cudaStream_t s);
 
 // A tail's rotated keys and its values into the blocks behind the live entries, and
 // its rotated queries into q_rot; those blocks and the older ones in sight as bf16 rows
-// of K and V.
+// of K and V.  All of a character in one line of the constant cache: a block's first
+// misses there, one after another, took 4 of the launch's 11 us.
+struct Kv8AppendChar {
+    int32_t cap_off;      // slot offset of the character in the slabs
+    int32_t L, M;         // live entries, tail tokens
+    int32_t tail_off;     // first packed tail token
+    int32_t blk_off;      // first item (block, head, K or V) of its new blocks, those from L / 64 on
+    int32_t old_off;      // first item (kv8_widen_blocks blocks, head, K or V) of its older ones in sight
+    int32_t n_old;        // those blocks; of them the ones from `sink` on lie `gap` further
+    int32_t sink, gap;
+    int64_t p;            // cursor
+};
 struct Kv8AppendParams {
     Kv8Layer to;
     __nv_bfloat16* K;             // [Hkv][slab_rows][D]
     __nv_bfloat16* V;
-    int32_t n_chars, Hq, Hkv, D, R, n_items, n_widen, total;
-    int64_t slab_rows;
     const __nv_bfloat16* q;       // [sum M][Hq][D]
     const __nv_bfloat16* k_new;   // [sum M][Hkv][D]
     const __nv_bfloat16* v_new;
     __nv_bfloat16* q_rot;
     int32_t* pos;                 // [slab_rows]
     const int32_t* tail_pos;      // as in AttnParams
+    const uint64_t* turn;         // device [R / 2]: a position's turn of each pair, in 2^-64 of a whole one
     int32_t* err;
-    uint64_t turn[kMaxRotaryHalf];   // a position's turn of each pair, in 2^-64 of a whole one
-    Kv8Char ch[kMaxChars];           // rows: live and tail
-    int32_t L_prev[kMaxChars], tail_off[kMaxChars];
-    int64_t p[kMaxChars];
-    // the older blocks in sight: of those from `sink` on, `gap` further
-    Kv8Char old[kMaxChars];
-    int32_t sink[kMaxChars], gap[kMaxChars];
+    int64_t slab_rows;
+    int32_t n_chars, Hq, Hkv, D, R, n_items, n_widen, total;
+    Kv8AppendChar ch[kMaxChars];
 };
 void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s);
 constexpr int kv8_widen_blocks(int D) { return 1024 / D; }   // of an item of `old`: 64 KB
@@ -296,7 +294,7 @@ struct Kv8AttnParams {
     AttnParams a;
     Kv8Layer from;
     int32_t rows;                 // most rows of a query tile
-    uint64_t turn[kMaxRotaryHalf];   // as in Kv8AppendParams
+    const uint64_t* turn;         // as in Kv8AppendParams
 };
 void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s);
 int attention_ctas_per_sm(int head_dim);

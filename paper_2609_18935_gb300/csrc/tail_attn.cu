@@ -496,7 +496,7 @@ void launch_attn_combine(const CombineParams& p, cudaStream_t s) {
         return;
     }
     const int piece_blocks = (kRows * (p.D / 4) + 255) / 256;
-    if ((int64_t)p.n_split_tiles * piece_blocks <= 7 * (int64_t)sms)
+    if ((int64_t)p.n_split_tiles * piece_blocks <= (p.many_parts ? 14 : 7) * (int64_t)sms)
         launch_pdl(attn_combine_piece_kernel, dim3(p.n_split_tiles, piece_blocks), dim3(256), 0, s, p);
     else
         launch_pdl(attn_combine_group_kernel, dim3(p.n_split_tiles, (kRows * (p.D / 32) + kCombineThreads - 1) / kCombineThreads),
