@@ -117,39 +117,55 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 }
 
 // The new keys and values of one head that lie in key tile kt: into the cache's block, and
-// the whole block under a larger (or smaller) scale where they need it.  By all threads,
-// between two barriers of the block.
+// the whole block under a larger (or smaller) scale where they need it.  By all threads;
+// `load` may come long before `finish`, which lies between two barriers of the block.
 template <int D, int NT>
-__device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt, float* red, const float2* turn,
-                                           float* keys) {
-    constexpr int kOld = (kKv8Rows * D / 16 + kThreads - 1) / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
+struct FormedBlock {
+    static constexpr int kOld = (kKv8Rows * D / 16 + kThreads - 1) / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
+    uint4 wk[kOld], wv[kOld], nv[kNew];
+    float sk, sv;
+    int64_t slot, src;
+    int old, n, tok0;                                          // rows there, new rows, of them the first token
+
+    __device__ __forceinline__ void load(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt) {
+        const AttnParams& p = pp.a;
+        const int tid = threadIdx.x, row0 = kt * kAttnKeys;
+        old = min(max(ch.L_prev - row0, 0), kKv8Rows);
+        n = min(ch.L_prev + ch.M - row0, kKv8Rows) - old;
+        tok0 = row0 + old - ch.L_prev;
+        slot = (int64_t)kvh * p.slab_rows + ch.cap_off + row0;
+        src = ((int64_t)(ch.tail_off + tok0) * p.Hkv + kvh) * D;
+        const uint4* bk = reinterpret_cast<const uint4*>(pp.from.K + slot * D);
+        const uint4* bv = reinterpret_cast<const uint4*>(pp.from.V + slot * D);
+        sk = old ? pp.from.Ks[slot / kKv8Rows] : 0.f;
+        sv = old ? pp.from.Vs[slot / kKv8Rows] : 0.f;
+#pragma unroll
+        for (int k = 0; k < kOld; ++k) {
+            const int i = tid + k * kThreads;
+            wk[k] = wv[k] = make_uint4(0, 0, 0, 0);
+            if (i < old * (D / 16)) {
+                wk[k] = bk[i];
+                wv[k] = bv[i];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kNew; ++k) {
+            const int i = tid + k * kThreads;
+            nv[k] = make_uint4(0, 0, 0, 0);
+            if (i < n * (D / 8)) nv[k] = *reinterpret_cast<const uint4*>(p.v_new + src + (int64_t)(i / (D / 8)) * p.Hkv * D + i % (D / 8) * 8);
+        }
+    }
+    __device__ __forceinline__ void finish(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn, float* keys);
+};
+
+template <int D, int NT>
+__device__ __forceinline__ void FormedBlock<D, NT>::finish(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn,
+                                                           float* keys) {
     const AttnParams& p = pp.a;
-    const int tid = threadIdx.x, half = p.R / 2, row0 = kt * kAttnKeys;
-    const int old = min(max(ch.L_prev - row0, 0), kKv8Rows), n = min(ch.L_prev + ch.M - row0, kKv8Rows) - old;
-    const int tok0 = row0 + old - ch.L_prev;                   // of the new rows
-    const int64_t slot = (int64_t)kvh * p.slab_rows + ch.cap_off + row0, src = ((int64_t)(ch.tail_off + tok0) * p.Hkv + kvh) * D;
+    const int tid = threadIdx.x, half = p.R / 2;
     const int64_t row = (int64_t)p.Hkv * D;
     uint4* bk = reinterpret_cast<uint4*>(pp.from.K + slot * D);
     uint4* bv = reinterpret_cast<uint4*>(pp.from.V + slot * D);
-    float* pk = pp.from.Ks + slot / kKv8Rows;
-    float* pv = pp.from.Vs + slot / kKv8Rows;
-    const float sk = old ? *pk : 0.f, sv = old ? *pv : 0.f;
-    uint4 wk[kOld], wv[kOld], nv[kNew];
-#pragma unroll
-    for (int k = 0; k < kOld; ++k) {
-        const int i = tid + k * kThreads;
-        wk[k] = wv[k] = make_uint4(0, 0, 0, 0);
-        if (i < old * (D / 16)) {
-            wk[k] = bk[i];
-            wv[k] = bv[i];
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kNew; ++k) {
-        const int i = tid + k * kThreads;
-        nv[k] = make_uint4(0, 0, 0, 0);
-        if (i < n * (D / 8)) nv[k] = *reinterpret_cast<const uint4*>(p.v_new + src + i / (D / 8) * row + i % (D / 8) * 8);
-    }
     float mk = 0.f, mv = 0.f;
     bool bad = false;
     auto key = [&](int r, int d) {
@@ -227,12 +243,12 @@ __device__ __forceinline__ void form_block(const Kv8AttnParams& pp, const AttnCh
                 make_uint2(to_e4m3(a.x * iv, a.y * iv, b.x * iv, b.y * iv), to_e4m3(c.x * iv, c.y * iv, d.x * iv, d.y * iv));
     }
     if (tid == 0) {
-        *pk = tk;
-        *pv = tv;
+        pp.from.Ks[slot / kKv8Rows] = tk;
+        pp.from.Vs[slot / kKv8Rows] = tv;
     }
     if (kvh == 0 && tid < n) {
         const int t = tok0 + tid;
-        p.pos[ch.cap_off + row0 + old + tid] = p.tail_pos ? p.tail_pos[ch.tail_off + t] : (int32_t)(ch.p + t);
+        p.pos[ch.cap_off + ch.L_prev + t] = p.tail_pos ? p.tail_pos[ch.tail_off + t] : (int32_t)(ch.p + t);
     }
     if (bad) atomicOr(p.err, kErrValue);
     __syncthreads();
@@ -293,6 +309,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
         // forms those of its range before anyone loads them, the others are under way meanwhile
         const int fresh = ch.L_prev / kAttnKeys - T.gap;
         const bool forms = fresh < k1;
+        // what the queries and the block to form need goes first: behind the rings' 128 KB a load takes 2.5 us
+        const int half = p.R / 2;
+        const uint64_t word = tid < ch.M * half ? pp.turn[tid % half] : 0;
+        auto row_of = [&](int r) { return p.q + ((int64_t)(ch.tail_off + r / p.g) * p.Hq + T.kvh * p.g + r % p.g) * D; };
+        const bool eights = half % 8 == 0;
+        const int per = half / 8 + (D - p.R) / 8;              // 16-byte pieces of a row: those turned in pairs first
+        uint4 a, b;
+        auto place = [&](int i) { return i % per < half / 8 ? 8 * (i % per) : p.R + 8 * (i % per - half / 8); };
+        auto get = [&](int i) {
+            if (i >= rows * per) return;
+            const __nv_bfloat16* x = row_of(i / per) + place(i);
+            a = *reinterpret_cast<const uint4*>(x);
+            if (i % per < half / 8) b = *reinterpret_cast<const uint4*>(x + half);
+        };
+        if (eights) get(tid);
+        FormedBlock<D, NT> block;
+        if (NT == 1 && forms) block.load(pp, ch, T.kvh, key_tile<true>(T, max(k0, fresh)));
 #pragma unroll
         for (int s = 0; s < C::STAGES - 1; ++s) {
             const int step = warp + s * kWarps;
@@ -300,24 +333,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             if (!forms) cp_commit();
         }
         {
-            const int half = p.R / 2;
             for (int i = tid; i < ch.M * half; i += kThreads) {
                 const int t = i / half;
                 const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[ch.tail_off + t] : ch.p + t;
-                turn_of(pos, pp.turn[i % half], turn[i].x, turn[i].y);
+                turn_of(pos, i == tid ? word : pp.turn[i % half], turn[i].x, turn[i].y);
             }
-            auto row_of = [&](int r) { return p.q + ((int64_t)(ch.tail_off + r / p.g) * p.Hq + T.kvh * p.g + r % p.g) * D; };
-            if (half % 8 == 0) {
-                const int per = half / 8 + (D - p.R) / 8;      // 16-byte pieces of a row: those turned in pairs first
-                uint4 a, b;
-                auto place = [&](int i) { return i % per < half / 8 ? 8 * (i % per) : p.R + 8 * (i % per - half / 8); };
-                auto get = [&](int i) {
-                    if (i >= rows * per) return;
-                    const __nv_bfloat16* x = row_of(i / per) + place(i);
-                    a = *reinterpret_cast<const uint4*>(x);
-                    if (i % per < half / 8) b = *reinterpret_cast<const uint4*>(x + half);
-                };
-                get(tid);
+            if (eights) {
                 __syncthreads();                               // the turns are there
                 for (int i = tid; i < rows * per; i += kThreads) {
                     if (i > tid) get(i);
@@ -390,9 +411,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
         }
         if (forms) {
             __syncthreads();                                   // the queries' place takes the new keys
-            for (int u = max(k0, fresh); u < k1; ++u)
-                form_block<D, NT>(pp, ch, T.kvh, key_tile<true>(T, u), reinterpret_cast<float*>(smem + C::OFF_RED), turn,
-                                  reinterpret_cast<float*>(smem + C::OFF_X));
+            for (int u = max(k0, fresh); u < k1; ++u) {
+                if (NT > 1 || u > max(k0, fresh)) block.load(pp, ch, T.kvh, key_tile<true>(T, u));
+                block.finish(pp, ch, T.kvh, reinterpret_cast<float*>(smem + C::OFF_RED), turn, reinterpret_cast<float*>(smem + C::OFF_X));
+            }
 #pragma unroll
             for (int s = 0; s < C::STAGES - 1; ++s) {
                 const int step = warp + s * kWarps;
