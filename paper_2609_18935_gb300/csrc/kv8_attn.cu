@@ -275,13 +275,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
     const int t_end = p.cta_tile[cta + 1], k_end = p.cta_k[cta + 1];
     const int n_seg = waves + ((t_begin == t_end && k_begin == k_end) ? 0 : t_end - t_begin + (k_end > 0 ? 1 : 0));
 
+    auto tile_of = [&](int seg) { return seg < waves ? seg * p.n_ctas + ((seg & 1) ? p.n_ctas - 1 - cta : cta) : t_begin + (seg - waves); };
+    auto decode = [&](int t) { return p.window ? decode_tile<true, false>(p, t) : decode_tile<false, false>(p, t); };
+    // the first segment's place, whose lines of the constant cache take 0.8 us, before the wait
+    Tile T = {};
+    if (n_seg > 0) T = decode(tile_of(0));
+
     // a removal, or the layer's last step, wrote the cache
     grid_dependency_wait();
     grid_dependents_launch();
 
     for (int seg = 0; seg < n_seg; ++seg) {
-        const int t = seg < waves ? seg * p.n_ctas + ((seg & 1) ? p.n_ctas - 1 - cta : cta) : t_begin + (seg - waves);
-        const Tile T = p.window ? decode_tile<true, false>(p, t) : decode_tile<false, false>(p, t);
+        const int t = tile_of(seg);
+        if (seg > 0) T = decode(t);
         const AttnChar& ch = p.ch[T.b];
         const int k0 = seg == waves ? k_begin : 0, k1 = (seg >= waves && t == t_end) ? k_end : T.nk;
         const bool full = k0 == 0 && k1 == T.nk;
