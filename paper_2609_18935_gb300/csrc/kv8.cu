@@ -40,6 +40,12 @@ __device__ __forceinline__ Item item_of(const Kv8AppendParams& p, int item) {
     return {lo, local / per, local % per / 2, (bool)(local & 1)};
 }
 
+// Every block finds its place first: the constant cache's misses pass beside the grid before.
+__device__ __forceinline__ void begin() {
+    grid_dependency_wait();
+    grid_dependents_launch();
+}
+
 template <int THREADS>
 __device__ __forceinline__ float block_max(float m, float* red) {
 #pragma unroll
@@ -80,6 +86,7 @@ __device__ __forceinline__ void widen_old(const Kv8AppendParams& p, int item) {
     const Item it = item_of<&Kv8AppendChar::old_off>(p, item);
     const Kv8AppendChar& c = p.ch[it.b];
     const int first = it.index * kv8_widen_blocks(D);
+    begin();
     const int64_t slot0 = (int64_t)it.head * p.slab_rows + c.cap_off;
     const uint2* src = reinterpret_cast<const uint2*>((it.is_v ? p.to.V : p.to.K) + slot0 * D);
     uint4* dst = reinterpret_cast<uint4*>((it.is_v ? p.V : p.K) + slot0 * D);
@@ -117,7 +124,9 @@ __device__ __forceinline__ void turn_queries(const Kv8AppendParams& p, int n, fl
         const int mid = (lo + hi + 1) >> 1;
         if (p.ch[mid].tail_off <= n) lo = mid; else hi = mid - 1;
     }
-    const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : p.ch[lo].p + n - p.ch[lo].tail_off;
+    const int64_t tail0 = p.ch[lo].p - p.ch[lo].tail_off;
+    begin();
+    const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : tail0 + n;
     const __nv_bfloat16* q = p.q + (int64_t)n * p.Hq * D;
     __nv_bfloat16* o = p.q_rot + (int64_t)n * p.Hq * D;
     if (half % 8 == 0) {
@@ -198,6 +207,7 @@ __device__ __forceinline__ void form_block(const Kv8AppendParams& p, float* red)
     const int64_t row = (int64_t)p.Hkv * D;
     const int tr = turned ? t / turned : kKv8Rows, td = turned ? t % turned * 8 : 0;           // the row and first dim of the pairs
     const bool has = tr >= old && tr < kKv8Rows;
+    begin();
     const float s = old ? *scale : 0.f;
     uint2 was[kOld];
     uint4 is[kFlat], a = make_uint4(0, 0, 0, 0), b = a;
@@ -289,8 +299,6 @@ __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __g
     extern __shared__ __align__(16) float tile[];              // [64][D]
     __shared__ float red[kAppendThreads / 32];
     __shared__ float cs[kMaxRotaryHalf], sn[kMaxRotaryHalf];
-    grid_dependency_wait();
-    grid_dependents_launch();
     const int t = threadIdx.x, half = p.R / 2;
     if ((int)blockIdx.x >= p.n_items + p.n_widen) {
         turn_queries<D>(p, blockIdx.x - p.n_items - p.n_widen, cs, sn);
@@ -314,6 +322,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) kv8_append_kernel(const __g
     const int n0 = c.tail_off + row0 - L;                // packed token of the block's first row
     bool bad = false;
     float m = 0.f;
+    begin();
     {
         constexpr int kOld = (kKv8Rows * D / 16 + kAppendThreads - 1) / kAppendThreads, kNew = kKv8Rows * D / 8 / kAppendThreads;
         const float s = old ? *scale : 0.f;

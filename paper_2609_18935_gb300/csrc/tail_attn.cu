@@ -53,8 +53,6 @@ __device__ __forceinline__ void rotate8(uint4& lo, uint4& hi, const float* cs, c
 // is not finite in a key or value goes in as 0 and is reported, as in draft_append.
 template <bool DRAFT>
 __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant__ AttnParams p) {
-    grid_dependency_wait();
-    grid_dependents_launch();
     const int n = blockIdx.x;                 // packed tail token
     int lo = 0, hi = p.n_chars - 1;           // last b with tail_off <= n owns token n
     while (lo < hi) {
@@ -64,6 +62,8 @@ __global__ void __launch_bounds__(128) rope_append_kernel(const __grid_constant_
     const int b = lo;
     const AttnChar& c = p.ch[b];
     const int i = n - c.tail_off;
+    grid_dependency_wait();
+    grid_dependents_launch();
     if (i < 0 || i >= c.M) { if (threadIdx.x == 0) atomicOr(p.err, kErrBounds); return; }
     const int64_t pos = p.tail_pos ? (int64_t)p.tail_pos[n] : c.p + i;
     const int64_t slot = c.cap_off + c.L_prev + i;
@@ -205,9 +205,9 @@ __device__ __forceinline__ int part_slot(const SplitTile& s, int q) { return q =
 // grid of a round with up to 33 shared tiles (x 32 blocks at head_dim 256)
 // runs in one wave.
 __global__ void __launch_bounds__(256, 7) attn_combine_piece_kernel(const __grid_constant__ CombineParams p) {
+    const SplitTile st = p.tile[blockIdx.x];                   // the constant cache's misses beside the grid before
     grid_dependency_wait();
     grid_dependents_launch();
-    const SplitTile st = p.tile[blockIdx.x];
     const int n_parts = st.n_parts;
     const int D = p.D;
     const int item = blockIdx.y * blockDim.x + threadIdx.x;        // (4-column piece, row): rows fastest
@@ -264,9 +264,9 @@ __global__ void __launch_bounds__(256, 7) attn_combine_piece_kernel(const __grid
 // pieces.
 constexpr int kCombineThreads = 128;
 __global__ void __launch_bounds__(kCombineThreads) attn_combine_group_kernel(const __grid_constant__ CombineParams p) {
+    const SplitTile st = p.tile[blockIdx.x];                   // the constant cache's misses beside the grid before
     grid_dependency_wait();
     grid_dependents_launch();
-    const SplitTile st = p.tile[blockIdx.x];
     const int n_parts = st.n_parts;
     const int D = p.D;
     const int item = blockIdx.y * blockDim.x + threadIdx.x;        // (column group, row): rows fastest
@@ -334,11 +334,11 @@ __global__ void __launch_bounds__(kCombineThreads) attn_combine_group_kernel(con
 // ceil(largest tile's rows * D / 4 / 32)).
 template <int LANES>
 __global__ void __launch_bounds__(32 * LANES) attn_combine_parts_kernel(const __grid_constant__ CombineParams p) {
-    grid_dependency_wait();
-    grid_dependents_launch();
     __shared__ float4 acc_s[LANES][32];
     __shared__ float2 md_s[LANES][32];
-    const SplitTile st = p.tile[blockIdx.x];
+    const SplitTile st = p.tile[blockIdx.x];                   // the constant cache's misses beside the grid before
+    grid_dependency_wait();
+    grid_dependents_launch();
     const int D = p.D, rows = st.rows;
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
     const int item = blockIdx.y * 32 + lane;

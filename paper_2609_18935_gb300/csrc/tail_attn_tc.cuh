@@ -535,8 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1) tail_attention_tc_kernel(const __
                 mbar_arrive(bar(Q_FULL));
                 return;
             }
-            grid_dependency_wait();                        // q_rot comes from the previous grid
             const Tile T = decode_tile<WIN, TREE != kTail>(p, t);
+            grid_dependency_wait();                        // q_rot comes from the previous grid
             constexpr int W = D / 4;                       // 32-bit words of this half
             uint4 v[W / 4];
             const AttnChar& ch = p.ch[T.b];
