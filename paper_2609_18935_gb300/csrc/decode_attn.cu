@@ -1,18 +1,21 @@
 // Attention of a few query rows a KV head (a decode step: one token, a group of heads)
-// straight from a cache in 8 bits.
+// over a cache in 8 bits, or a windowed layer's in bf16.
 //
 // S^T = K Q^T and O^T = V^T P^T with mma.sync: the 16 keys of a step are the rows of the
 // first product and the depth of the second, 8 query rows its columns.  The work is
 // bound by the cache's bytes: 8 rows are a sixteenth of a tcgen05 tile, whose operands
 // would have to pass through shared memory.
-// Cache numbers become f16 (one instruction a pair), exactly; their blocks' scales stay
+// 8-bit numbers become f16 (one instruction a pair), exactly; their blocks' scales stay
 // outside, of K in the scores, of V as the sums are added up.  A query, rounded to bf16,
 // is f16 times a power of two of its row (down to 2^-39 of the row's largest).  A weight is
 // rounded to f16: 2^-12 of it, or 2^-33 of the reference's where it is small, 2^-9 of a
-// row's sum after 2^24 keys.
-// As bf16 (a pair in five instructions, K and V), with 8 warps and 903 instructions a
-// step, 32 characters' step over 16K took 64.4 us; m16n8k32 on e4m3 itself, the queries
-// as two such numbers each, is made of the same conversions.
+// row's sum after 2^24 keys.  As bf16 (a pair in five instructions, K and V), 903
+// instructions a step, 32 characters' step over 16K (284 MB) took 64.4 us, so 60.0, and 54.4
+// (5.2 TB/s) with longer ranges and what follows; m16n8k32 on e4m3 itself, with a query as
+// two such numbers, ran as many instructions as the bf16 form.
+// bf16 caches: the words are the products' operands as they are.  Under a window of 4096
+// the same characters take 46.5 us (259 MB, 5.6 TB/s), one over 512 entries 6.4; by way of
+// rope_append and the tensor-core attention 49.5 and 9.4.
 //
 // One launch takes in the tail: a block turns its rows' queries itself, and the block
 // whose range holds the end of a character's cache puts the new keys and values there
@@ -20,10 +23,12 @@
 // launch before this one that took 4 - 8 us of a step.
 //
 // The partition is the tensor-core attention's: 64-key units in contiguous ranges, a
-// block an SM, partials of shared tiles for attn_combine.  A warp takes every kWarps-th
+// block an SM, partials of shared tiles for attn_combine.  A warp takes every WARPS-th
 // 16 keys of a segment through a ring of its own in shared memory (cp.async, no barrier
 // but the warp's), keeps its own softmax reference, sum and output in registers, and the
-// block's warps meet at the segment's end.
+// block's warps meet at the segment's end.  The loop runs at the memory's speed (54 GB/s an
+// SM); of 9 us for one character over 32K (7 units a block) 3.3 are the queries, 3.5 the
+// loop, 1 the meeting.
 //
 // Layout.  The sum over d takes any order, the same for K and Q: lane (g, j) = (lane / 4,
 // lane mod 4) reads 16 bytes of key g (and g + 8) at a time, and two words of them are its
@@ -49,35 +54,37 @@ constexpr int kStep = 16;                      // keys of a warp's step
 constexpr int BM = kAttnRows;
 constexpr float kUp = 7.f;                     // weights are taken 2^7 higher: up to 2^15, where f16 has room
 
-// Twelve and sixteen warps (of fewer stages) took longer: 62.1 against 60.9 us for 32
-// characters over 16K, 8.1 against 7.3 for one over 512, more of them meet at the end.
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-
-template <int D, int NT>
+// E: bytes of a cache's number, 1 (e4m3) or 2 (bf16).  Eight warps: twelve and sixteen (of
+// fewer stages) took longer over 8 bits, 62.1 against 60.9 us for 32 characters over 16K,
+// 8.1 against 7.3 for one over 512, more of them meet at the end.
+template <int D, int NT, int E>
 struct Cfg {
-    static constexpr int SIDE = kStep * D;                     // bytes of a step's K, or V
-    static constexpr int STAGE = 2 * SIDE + 16;                // and its two scales
-    static constexpr int STAGES = D == 256 ? 3 : 6;
+    static constexpr int WARPS = D * E == 512 ? 6 : 8;
+    static constexpr int THREADS = 32 * WARPS;
+    static constexpr int ROW = D * E;                          // bytes of a key, or value
+    static constexpr int SIDE = kStep * ROW;                   // of a step's
+    static constexpr int STAGE = 2 * SIDE + (E == 1 ? 16 : 0); // and its two scales
+    static constexpr int STAGES = ROW == 512 ? 2 : ROW == 256 ? 3 : 6;
     static constexpr int RING = STAGES * STAGE;
     static constexpr int ROWS = 8 * NT;
     static constexpr int PITCH = D + 4;                        // floats of a merged row
-    static constexpr int MERGE = kWarps * ROWS * PITCH * 4;
+    static constexpr int MERGE = WARPS * ROWS * PITCH * 4;
     // behind the rings: the warps' references and sums, a maximum of K and of V a warp,
     // the rows' turns, and their queries (bf16) or new keys (fp32)
-    static constexpr int OFF_WM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
-    static constexpr int OFF_RED = OFF_WM + 2 * kWarps * ROWS * 4;
-    static constexpr int OFF_TURN = OFF_RED + 2 * kWarps * 4;
+    static constexpr int OFF_WM = WARPS * RING > MERGE ? WARPS * RING : MERGE;
+    static constexpr int OFF_RED = OFF_WM + 2 * WARPS * ROWS * 4;
+    static constexpr int OFF_TURN = OFF_RED + 2 * WARPS * 4;
     static constexpr int OFF_X = OFF_TURN + ROWS * D * 4;
     static constexpr int SMEM = OFF_X + ROWS * D * 4;
 };
-static_assert(Cfg<256, 2>::SMEM <= 232448 && Cfg<128, 2>::SMEM <= 232448 && Cfg<64, 2>::SMEM <= 232448, "shared memory");
+static_assert(Cfg<256, 2, 1>::SMEM <= 232448 && Cfg<128, 2, 1>::SMEM <= 232448 && Cfg<64, 2, 1>::SMEM <= 232448 &&
+              Cfg<256, 2, 2>::SMEM <= 232448 && Cfg<128, 2, 2>::SMEM <= 232448 && Cfg<64, 2, 2>::SMEM <= 232448, "shared memory");
 
-// Byte offset of 16-byte piece `col` of row `row` of a step's K or V.
-template <int D>
+// Byte offset of 16-byte piece `col` of row `row` of a step's K or V, rows of ROW bytes.
+template <int ROW>
 __device__ __forceinline__ int piece(int row, int col) {
-    if (D == 64) return (row >> 1) * 128 + (((((row & 1) << 2) | col) ^ ((row & 6))) << 4);
-    return row * D + (((col & ~7) | ((col ^ row) & 7)) << 4);
+    if (ROW == 64) return (row >> 1) * 128 + (((((row & 1) << 2) | col) ^ ((row & 6))) << 4);
+    return row * ROW + (((col & ~7) | ((col ^ row) & 7)) << 4);
 }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
@@ -92,6 +99,11 @@ __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -121,13 +133,14 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // `load` may come long before `finish`, which lies between two barriers of the block.
 template <int D, int NT>
 struct FormedBlock {
+    static constexpr int kWarps = Cfg<D, NT, 1>::WARPS, kThreads = Cfg<D, NT, 1>::THREADS;
     static constexpr int kOld = (kKv8Rows * D / 16 + kThreads - 1) / kThreads, kNew = (8 * NT * D / 8 + kThreads - 1) / kThreads;
     uint4 wk[kOld], wv[kOld], nv[kNew];
     float sk, sv;
     int64_t slot, src;
     int old, n, tok0;                                          // rows there, new rows, of them the first token
 
-    __device__ __forceinline__ void load(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, int kt) {
+    __device__ __forceinline__ void load(const DecodeParams& pp, const AttnChar& ch, int kvh, int kt) {
         const AttnParams& p = pp.a;
         const int tid = threadIdx.x, row0 = kt * kAttnKeys;
         old = min(max(ch.L_prev - row0, 0), kKv8Rows);
@@ -155,11 +168,11 @@ struct FormedBlock {
             if (i < n * (D / 8)) nv[k] = *reinterpret_cast<const uint4*>(p.v_new + src + (int64_t)(i / (D / 8)) * p.Hkv * D + i % (D / 8) * 8);
         }
     }
-    __device__ __forceinline__ void finish(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn, float* keys);
+    __device__ __forceinline__ void finish(const DecodeParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn, float* keys);
 };
 
 template <int D, int NT>
-__device__ __forceinline__ void FormedBlock<D, NT>::finish(const Kv8AttnParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn,
+__device__ __forceinline__ void FormedBlock<D, NT>::finish(const DecodeParams& pp, const AttnChar& ch, int kvh, float* red, const float2* turn,
                                                            float* keys) {
     const AttnParams& p = pp.a;
     const int tid = threadIdx.x, half = p.R / 2;
@@ -254,10 +267,36 @@ __device__ __forceinline__ void FormedBlock<D, NT>::finish(const Kv8AttnParams& 
     __syncthreads();
 }
 
+// The same for a cache in bf16: tokens [t0, t1).
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid_constant__ Kv8AttnParams pp) {
-    using C = Cfg<D, NT>;
+__device__ __forceinline__ void append_rows(const AttnParams& p, const AttnChar& ch, int kvh, int t0, int t1, const float2* turn) {
+    constexpr int kThreads = Cfg<D, NT, 2>::THREADS;
+    const int tid = threadIdx.x, half = p.R / 2, n = t1 - t0;
+    const int64_t src = ((int64_t)(ch.tail_off + t0) * p.Hkv + kvh) * D, row = (int64_t)p.Hkv * D;
+    const int64_t dst = ((int64_t)kvh * p.slab_rows + ch.cap_off + ch.L_prev + t0) * D;
+    for (int i = tid; i < n * (D / 8); i += kThreads)
+        *reinterpret_cast<uint4*>(p.V + dst + 8 * i) = *reinterpret_cast<const uint4*>(p.v_new + src + i / (D / 8) * row + i % (D / 8) * 8);
+    for (int i = tid; i < n * half; i += kThreads) {
+        const int r = i / half, d = i % half;
+        const float2 t = turn[(t0 + r) * half + d];
+        const float x = __bfloat162float(p.k_new[src + r * row + d]), y = __bfloat162float(p.k_new[src + r * row + d + half]);
+        p.K[dst + r * D + d] = __float2bfloat16_rn(x * t.x - y * t.y);
+        p.K[dst + r * D + d + half] = __float2bfloat16_rn(y * t.x + x * t.y);
+    }
+    for (int i = tid; i < n * (D - p.R); i += kThreads) {
+        const int r = i / (D - p.R), d = p.R + i % (D - p.R);
+        p.K[dst + r * D + d] = p.k_new[src + r * row + d];
+    }
+    if (kvh == 0 && tid < n) p.pos[ch.cap_off + ch.L_prev + t0 + tid] = p.tail_pos ? p.tail_pos[ch.tail_off + t0 + tid] : (int32_t)(ch.p + t0 + tid);
+    __syncthreads();
+}
+
+template <int D, int NT, int E>
+__global__ void __launch_bounds__(Cfg<D, NT, E>::THREADS, 1) decode_attention_kernel(const __grid_constant__ DecodeParams pp) {
+    using C = Cfg<D, NT, E>;
+    constexpr int kWarps = C::WARPS, kThreads = C::THREADS;
     constexpr int KS = D / 16;                                 // 16-row pieces of O^T
+    constexpr bool SIXTEEN = E == 1 && D > 64;                 // a lane's dims that are neighbours
     extern __shared__ __align__(128) uint8_t smem[];
     const AttnParams& p = pp.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
@@ -299,17 +338,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
         auto load = [&](int s, int at) {
             if (s >= steps) return;
             const int64_t row = slab + (int64_t)key_tile<true>(T, k0 + s / 4) * kAttnKeys + s % 4 * kStep;
-            const uint8_t* k = pp.from.K + row * D;
-            const uint8_t* v = pp.from.V + row * D;
+            const uint8_t* k = (E == 1 ? pp.from.K : reinterpret_cast<const uint8_t*>(p.K)) + row * C::ROW;
+            const uint8_t* v = (E == 1 ? pp.from.V : reinterpret_cast<const uint8_t*>(p.V)) + row * C::ROW;
             const uint32_t to = ring_at + at * C::STAGE;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                const int id = c * 32 + lane, r = id / (D / 16), col = id % (D / 16);
-                const uint32_t o = to + piece<D>(r, col);
+            for (int c = 0; c < C::ROW / 32; ++c) {
+                const int id = c * 32 + lane, r = id / (C::ROW / 16), col = id % (C::ROW / 16);
+                const uint32_t o = to + piece<C::ROW>(r, col);
                 cp16(o, k + id * 16);
                 cp16(o + C::SIDE, v + id * 16);
             }
-            if (lane < 2) cp4(to + 2 * C::SIDE + 4 * lane, (lane ? pp.from.Vs : pp.from.Ks) + row / kKv8Rows);
+            if (E == 1 && lane < 2) cp4(to + 2 * C::SIDE + 4 * lane, (lane ? pp.from.Vs : pp.from.Ks) + row / kKv8Rows);
         };
         // units from `fresh` on have new rows (a query tile holds all of its character's): this block
         // forms those of its range before anyone loads them, the others are under way meanwhile
@@ -331,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
         };
         if (eights) get(tid);
         FormedBlock<D, NT> block;
-        if (NT == 1 && forms) block.load(pp, ch, T.kvh, key_tile<true>(T, max(k0, fresh)));
+        if (E == 1 && NT == 1 && forms) block.load(pp, ch, T.kvh, key_tile<true>(T, max(k0, fresh)));
 #pragma unroll
         for (int s = 0; s < C::STAGES - 1; ++s) {
             const int step = warp + s * kWarps;
@@ -376,50 +415,66 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             }
             __syncthreads();
         }
-        // Q: a lane's words of each step of the sum, rows g (and g + 8), as f16 times a power of two of the row
+        // Q: a lane's words of each step of the sum, rows g (and g + 8); over 8 bits as f16 times a power of two of the row
         uint32_t q[NT][KS][2];
         float row_scale[NT][2];                                // of rows 8 n + 2 j and the next
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = 8 * n + g;
             const __nv_bfloat16* src = q_s + r * D;
-            uint4 x[KS / 4][2];
-            float top = 0.f;
+            if constexpr (E == 2) {
 #pragma unroll
-            for (int c = 0; c < KS / 4; ++c) {
-                const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    x[c][h] = r < rows ? *reinterpret_cast<const uint4*>(src + 16 * col + 8 * h) : make_uint4(0, 0, 0, 0);
-                    const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(bf2_f2(w[k]).x), fabsf(bf2_f2(w[k]).y)));
+                for (int c = 0; c < KS / 2; ++c) {
+                    const int col = 8 * (c >> 1) + 2 * j + (c & 1);
+                    const uint4 x = r < rows ? *reinterpret_cast<const uint4*>(src + 8 * col) : make_uint4(0, 0, 0, 0);
+                    q[n][2 * c][0] = x.x; q[n][2 * c][1] = x.y;
+                    q[n][2 * c + 1][0] = x.z; q[n][2 * c + 1][1] = x.w;
                 }
-            }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // top < 2^E: its row's numbers below 2^15
-            const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -110), 128);
-            const float up = pow2(15 - E), scale = pow2(E - 15) * p.scale_log2;
+                row_scale[n][0] = row_scale[n][1] = p.scale_log2;
+            } else {
+                uint4 x[KS / 4][2];
+                float top = 0.f;
 #pragma unroll
-            for (int c = 0; c < KS / 4; ++c)
+                for (int c = 0; c < KS / 4; ++c) {
+                    const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
+                    for (int h = 0; h < 2; ++h) {
+                        x[c][h] = r < rows ? *reinterpret_cast<const uint4*>(src + 16 * col + 8 * h) : make_uint4(0, 0, 0, 0);
+                        const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 a = bf2_f2(w[k]);
-                        q[n][4 * c + 2 * h + (k >> 1)][k & 1] = f2_h2(a.x * up, a.y * up);
+                        for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(bf2_f2(w[k]).x), fabsf(bf2_f2(w[k]).y)));
                     }
                 }
-            row_scale[n][0] = __shfl_sync(0xffffffffu, scale, 8 * j);
-            row_scale[n][1] = __shfl_sync(0xffffffffu, scale, 8 * j + 4);
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // top < 2^ex: its row's numbers below 2^15
+                const int ex = min(max((int)(__float_as_uint(top) >> 23) - 126, -110), 128);
+                const float up = pow2(15 - ex), scale = pow2(ex - 15) * p.scale_log2;
+#pragma unroll
+                for (int c = 0; c < KS / 4; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t w[4] = {x[c][h].x, x[c][h].y, x[c][h].z, x[c][h].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 a = bf2_f2(w[k]);
+                            q[n][4 * c + 2 * h + (k >> 1)][k & 1] = f2_h2(a.x * up, a.y * up);
+                        }
+                    }
+                row_scale[n][0] = __shfl_sync(0xffffffffu, scale, 8 * j);
+                row_scale[n][1] = __shfl_sync(0xffffffffu, scale, 8 * j + 4);
+            }
         }
         if (forms) {
             __syncthreads();                                   // the queries' place takes the new keys
-            for (int u = max(k0, fresh); u < k1; ++u) {
-                if (NT > 1 || u > max(k0, fresh)) block.load(pp, ch, T.kvh, key_tile<true>(T, u));
-                block.finish(pp, ch, T.kvh, reinterpret_cast<float*>(smem + C::OFF_RED), turn, reinterpret_cast<float*>(smem + C::OFF_X));
+            if constexpr (E == 2) {
+                const int t0 = max(key_tile<true>(T, max(k0, fresh)) * kAttnKeys - ch.L_prev, 0);
+                append_rows<D, NT>(p, ch, T.kvh, t0, min((key_tile<true>(T, k1 - 1) + 1) * kAttnKeys - ch.L_prev, ch.M), turn);
+            } else {
+                for (int u = max(k0, fresh); u < k1; ++u) {
+                    if (NT > 1 || u > max(k0, fresh)) block.load(pp, ch, T.kvh, key_tile<true>(T, u));
+                    block.finish(pp, ch, T.kvh, reinterpret_cast<float*>(smem + C::OFF_RED), turn, reinterpret_cast<float*>(smem + C::OFF_X));
+                }
             }
 #pragma unroll
             for (int s = 0; s < C::STAGES - 1; ++s) {
@@ -452,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             __syncwarp();
             const uint8_t* kt = ring + (i % C::STAGES) * C::STAGE;
             const uint8_t* vt = kt + C::SIDE;
-            const float ks = *reinterpret_cast<const float*>(kt + 2 * C::SIDE);
-            const float vs = *reinterpret_cast<const float*>(kt + 2 * C::SIDE + 4);
+            const float ks = E == 1 ? *reinterpret_cast<const float*>(kt + 2 * C::SIDE) : 1.f;
+            [[maybe_unused]] const float vs = E == 1 ? *reinterpret_cast<const float*>(kt + 2 * C::SIDE + 4) : 1.f;
             load(s + (C::STAGES - 1) * kWarps, (i + C::STAGES - 1) % C::STAGES);
             cp_commit();
             float sc[NT][2][4];                                // two chains of products
@@ -461,19 +516,33 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sc[n][e >> 2][e & 3] = 0.f;
+            if constexpr (E == 2) {
 #pragma unroll
-            for (int c = 0; c < KS / 4; ++c) {
-                const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
-                const uint4 x = *reinterpret_cast<const uint4*>(kt + piece<D>(g, col));
-                const uint4 y = *reinterpret_cast<const uint4*>(kt + piece<D>(g + 8, col));
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+                for (int c = 0; c < KS / 2; ++c) {
+                    const int col = 8 * (c >> 1) + 2 * j + (c & 1);
+                    const uint4 x = *reinterpret_cast<const uint4*>(kt + piece<C::ROW>(g, col));
+                    const uint4 y = *reinterpret_cast<const uint4*>(kt + piece<C::ROW>(g + 8, col));
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t a0, a1, a2, a3;
-                    e4m3_f16(xs[w], a0, a2);
-                    e4m3_f16(ys[w], a1, a3);
+                    for (int n = 0; n < NT; ++n) {
+                        mma16816_bf16(sc[n][0], x.x, y.x, x.y, y.y, q[n][2 * c][0], q[n][2 * c][1]);
+                        mma16816_bf16(sc[n][1], x.z, y.z, x.w, y.w, q[n][2 * c + 1][0], q[n][2 * c + 1][1]);
+                    }
+                }
+            } else {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma16816(sc[n][w & 1], a0, a1, a2, a3, q[n][4 * c + w][0], q[n][4 * c + w][1]);
+                for (int c = 0; c < KS / 4; ++c) {
+                    const int col = D == 64 ? j : 8 * (c >> 1) + 2 * j + (c & 1);
+                    const uint4 x = *reinterpret_cast<const uint4*>(kt + piece<C::ROW>(g, col));
+                    const uint4 y = *reinterpret_cast<const uint4*>(kt + piece<C::ROW>(g + 8, col));
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t a0, a1, a2, a3;
+                        e4m3_f16(xs[w], a0, a2);
+                        e4m3_f16(ys[w], a1, a3);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816(sc[n][w & 1], a0, a1, a2, a3, q[n][4 * c + w][0], q[n][4 * c + w][1]);
+                    }
                 }
             }
             // keys g and g + 8 of the step for rows 2 j, 2 j + 1
@@ -526,13 +595,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                     w[e] = ex2(x[n][e] - (m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1] - kUp));
                     l[n][e & 1] += w[e];
                 }
-                b[n][0] = transposed(f2_h2(w[0], w[1]));
-                b[n][1] = transposed(f2_h2(w[2], w[3]));
+                b[n][0] = transposed(E == 1 ? f2_h2(w[0], w[1]) : f2_bf2(w[0], w[1]));
+                b[n][1] = transposed(E == 1 ? f2_h2(w[2], w[3]) : f2_bf2(w[2], w[3]));
             }
-            if constexpr (D == 64) {
+            if constexpr (E == 2) {
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(vt + piece<C::ROW>(2 * j + (k & 1) + 8 * (k >> 1), 8 * h + g));
+                    const uint32_t* w[4] = {&v[0].x, &v[1].x, &v[2].x, &v[3].x};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t a0 = __byte_perm(w[0][u], w[1][u], 0x5410), a1 = __byte_perm(w[0][u], w[1][u], 0x7632);
+                        const uint32_t a2 = __byte_perm(w[2][u], w[3][u], 0x5410), a3 = __byte_perm(w[2][u], w[3][u], 0x7632);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816_bf16(o[n][4 * h + u], a0, a1, a2, a3, b[n][0], b[n][1]);
+                    }
+                }
+            } else if constexpr (D == 64) {
                 uint2 v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint2*>(vt + piece<D>(2 * j + (k & 1) + 8 * (k >> 1), g >> 1) + 8 * (g & 1));
+                for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint2*>(vt + piece<C::ROW>(2 * j + (k & 1) + 8 * (k >> 1), g >> 1) + 8 * (g & 1));
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const uint32_t w0 = u < 2 ? v[0].x : v[0].y, w1 = u < 2 ? v[1].x : v[1].y, w2 = u < 2 ? v[2].x : v[2].y, w3 = u < 2 ? v[3].x : v[3].y;
@@ -548,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 for (int h = 0; h < D / 128; ++h) {
                     uint4 v[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(vt + piece<D>(2 * j + (k & 1) + 8 * (k >> 1), 8 * h + g));
+                    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const uint4*>(vt + piece<C::ROW>(2 * j + (k & 1) + 8 * (k >> 1), 8 * h + g));
                     const uint32_t* w[4] = {&v[0].x, &v[1].x, &v[2].x, &v[3].x};
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
@@ -577,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 }
             }
         __syncthreads();                                       // every ring is done
-        // a lane's numbers of a row are neighbours, 16 (D 64: 8) of them a piece; every
+        // a lane's numbers of a row are neighbours, 8 of them a piece (16 over 8 bits, but for D 64); every
         // other lane's 16-byte words change places, so that a quarter warp meets all banks
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -586,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
                 float* row = meet + (warp * C::ROWS + 8 * n + 2 * j + e) * C::PITCH;
 #pragma unroll
                 for (int c = 0; c < KS; c += 2) {
-                    const int d4 = D == 64 ? 2 * g + c / 2 : 32 * (c >> 3) + 4 * g + (c & 7) / 2;
+                    const int d4 = SIXTEEN ? 32 * (c >> 3) + 4 * g + (c & 7) / 2 : 16 * (c >> 2) + 2 * g + (c & 3) / 2;
                     *reinterpret_cast<float4*>(row + 4 * (d4 ^ (g & 1))) =
                         make_float4(o[n][c][e], o[n][c][e + 2], o[n][c + 1][e], o[n][c + 1][e + 2]);
                 }
@@ -599,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wm[w * C::ROWS + r]);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int gw = D == 64 ? d4 >> 1 : d4 >> 2;        // the lane that wrote it
+            const int gw = SIXTEEN ? d4 >> 2 : d4 >> 1;        // the lane that wrote it
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float mw = wm[w * C::ROWS + r];
@@ -624,26 +708,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attention_kernel(const __grid
     }
 }
 
-template <int D, int NT>
-void launch(const Kv8AttnParams& p, cudaStream_t s) {
+template <int D, int NT, int E>
+void launch(const DecodeParams& p, cudaStream_t s) {
+    using C = Cfg<D, NT, E>;
     static unsigned long long configured = 0;   // one bit per device
     int dev = 0;
     cudaGetDevice(&dev);
     if (!(configured >> (dev & 63) & 1ull)) {
-        cudaFuncSetAttribute(kv8_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, NT>::SMEM);
+        cudaFuncSetAttribute(decode_attention_kernel<D, NT, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         configured |= 1ull << (dev & 63);
     }
-    launch_pdl(kv8_attention_kernel<D, NT>, dim3(p.a.n_ctas), dim3(kThreads), Cfg<D, NT>::SMEM, s, p);
+    launch_pdl(decode_attention_kernel<D, NT, E>, dim3(p.a.n_ctas), dim3(C::THREADS), C::SMEM, s, p);
 }
 
 template <int D>
-void launch_d(const Kv8AttnParams& p, cudaStream_t s) {
-    p.rows <= 8 ? launch<D, 1>(p, s) : launch<D, 2>(p, s);
+void launch_d(const DecodeParams& p, cudaStream_t s) {
+    if (p.from.K) p.rows <= 8 ? launch<D, 1, 1>(p, s) : launch<D, 2, 1>(p, s);
+    else p.rows <= 8 ? launch<D, 1, 2>(p, s) : launch<D, 2, 2>(p, s);
 }
 
 }  // namespace
 
-void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s) {
+void launch_decode_attention(const DecodeParams& p, cudaStream_t s) {
     if (p.a.n_ctas <= 0) return;
     if (p.a.D == 64) launch_d<64>(p, s);
     else if (p.a.D == 128) launch_d<128>(p, s);

@@ -67,8 +67,8 @@ __device__ __forceinline__ void turn_of(int64_t pos, uint64_t turn, float& c, fl
 }
 
 // Eight numbers as bf16, times a block's scale (exactly: see the least exponent above).
-// Eight, not sixteen: 32 bytes a thread, in two stores, filled every sector by halves, and
-// the widening of 8192 entries of two heads of 256 took 8.7 us against WIDEN_US.
+// Eight, not sixteen: 32 bytes a thread, in two stores, filled every sector by halves (the
+// widening of a round's two layers took 35.0 us against 30.4).
 __device__ __forceinline__ uint4 widen8(const uint2& w, __nv_bfloat162 scale) {
     auto pair = [&](uint32_t x) {
         const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), scale);

@@ -434,13 +434,13 @@ constexpr PlanCost kTailCost{kMinUnitsPerCta, kSegmentCost};
 // with three, 14.4 with two.
 constexpr PlanCost kDraftCost{3, 32.0};
 
-// Few rows over 8-bit caches (kv8_attn.cu): a unit is 128 D bytes to load, a segment the
-// rows' queries, the warps' meeting, the partials and their merge, whatever D is.  With
-// 8 | 16 | 24 | 32 units a segment at D 256, us a step: 32 characters over 16K 60.9 | 56.8 |
-// 58.1 | 58.0, four over 32K 18.5 | 16.8 | 16.7 | 16.7.  Tiles of up to five units there stay
-// whole (600 entries 11.2, with up to 8 of them 13.4), two units are worth a block (4096
-// entries 11.5, with four 13.4).
-PlanCost kv8_cost(int D) { return {512 / D, 4096.0 / D, 1280 / D}; }
+// Few rows (decode_attn.cu): a unit is 128 keys' or values' bytes to load, a segment the
+// rows' queries, the warps' meeting, the partials and their merge, whatever a row's bytes
+// are.  Over 8 bits with 8 | 16 | 24 | 32 units a segment at D 256, us a step: 32 characters
+// over 16K 60.9 | 56.8 | 58.1 | 58.0, four over 32K 18.5 | 16.8 | 16.7 | 16.7.  Tiles of up to
+// five units there stay whole (600 entries 11.2, with up to 8 of them 13.4), two units are
+// worth a block (4096 entries 11.5, with four 13.4).
+PlanCost decode_cost(int row_bytes) { return {std::max(1, 512 / row_bytes), 4096.0 / row_bytes, 1280 / row_bytes}; }
 
 // What a layer's rows see: of a windowed layer (kvm_set_window) fewer key tiles, the
 // same for all query tiles of a draft, whose first rows all follow the last live entry.
@@ -634,11 +634,13 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
         if (e == cudaSuccess) e = alloc_zero(&c->V8, n);
         if (e == cudaSuccess) e = alloc_zero(&c->K8s, blocks);
         if (e == cudaSuccess) e = alloc_zero(&c->V8s, blocks);
+    }
+    if (c->n_attn && c->R) {
         uint64_t turn[kMaxRotaryHalf];
         for (int d = 0; d < c->R / 2; ++d)
             turn[d] = (uint64_t)std::ldexp(std::fmod((long double)c->inv_freq[d] / 6.283185307179586476925286766559L, 1.0L), 64);
         if (e == cudaSuccess) e = alloc_zero(&c->turn, c->R / 2);
-        if (e == cudaSuccess && c->R) e = cudaMemcpy(c->turn, turn, sizeof(uint64_t) * (c->R / 2), cudaMemcpyHostToDevice);
+        if (e == cudaSuccess) e = cudaMemcpy(c->turn, turn, sizeof(uint64_t) * (c->R / 2), cudaMemcpyHostToDevice);
     }
     if (e == cudaSuccess) e = alloc_zero(&c->pos, c->n_attn ? (size_t)c->T_cap : 0);
     if (e == cudaSuccess) e = alloc_zero(&c->S, (size_t)c->n_gdn * n_chars * c->H * c->dv * c->dk);
@@ -1352,12 +1354,17 @@ int most_rows(const kvm_ctx* c, const int32_t* tail_cu) {
     return (int)std::min<int64_t>((int64_t)m * c->g, INT32_MAX);
 }
 
+// A tail that decode_attn.cu takes: of few rows, over 8-bit caches or under a window.
+bool few_rows(const kvm_ctx* c, int layer, const int32_t* tail_cu) {
+    return (c->kv8 || c->window[layer] > 0) && most_rows(c, tail_cu) <= kDecodeRows;
+}
+
 // One attention layer's launches under its partition pl: a tail of `total` tokens
 // at tail_pos_dev (null: p_b + i), or with anc the nodes of a draft.
 kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int total, const AttnPlan& pl, const void* q,
                             const void* k_new, const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev,
                             const uint64_t* anc) {
-    thread_local static Kv8AttnParams p8;         // large parameter blocks, copied into the launch
+    thread_local static DecodeParams p8;          // large parameter blocks, copied into the launch
     AttnParams& p = p8.a;
     std::memset(&p, 0, offsetof(AttnParams, ch));  // (of its tables only what is written here is read)
     const int a = c->attn_idx[layer];
@@ -1410,8 +1417,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_tile.begin(), pl.cta_tile.end(), p.cta_tile);
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
-    const int rows = most_rows(c, tail_cu);
-    const bool direct = c->kv8 && rows <= kKv8Direct;
+    const bool direct = few_rows(c, layer, tail_cu) && !anc;
     if (direct) {
         // the attention appends
     } else if (c->kv8) {
@@ -1432,10 +1438,10 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     }
     int ps = prof_begin(c, KVM_K_ATTENTION, s);
     if (direct) {
-        p8.from = kv8_layer(c, a);
-        p8.rows = rows;
+        p8.from = c->kv8 ? kv8_layer(c, a) : Kv8Layer{};
+        p8.rows = most_rows(c, tail_cu);
         p8.turn = c->turn;
-        launch_kv8_attention(p8, s);
+        launch_decode_attention(p8, s);
     } else {
         launch_tail_attention(p, s);
     }
@@ -1500,7 +1506,7 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
     AttnPlan pl;
     plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true,
-                   c->kv8 && most_rows(c, tail_cu) <= kKv8Direct ? kv8_cost(c->D) : kTailCost, {c->window[layer], c->n_sink[layer]}, pl);
+                   few_rows(c, layer, tail_cu) ? decode_cost(c->D * (c->kv8 ? 1 : 2)) : kTailCost, {c->window[layer], c->n_sink[layer]}, pl);
     drop_draft(c);
     return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
 }

@@ -286,17 +286,17 @@ struct Kv8AppendParams {
 void launch_kv8_append(const Kv8AppendParams& p, cudaStream_t s);
 constexpr int kv8_widen_blocks(int D) { return 1024 / D; }   // of an item of `old`: 64 KB
 
-// Attention of a few rows a KV head straight from the 8-bit cache, under the same
-// partition and with the same partials as launch_tail_attention.  It rotates the tail's
-// queries and puts its keys and values into the cache itself.
-constexpr int kKv8Direct = 16;   // most rows (tail tokens of a character x group)
-struct Kv8AttnParams {
+// Attention of a few rows a KV head straight from the cache, under the same partition
+// and with the same partials as launch_tail_attention.  It rotates the tail's queries
+// and puts its keys and values into the cache itself.
+constexpr int kDecodeRows = 16;   // most rows (tail tokens of a character x group)
+struct DecodeParams {
     AttnParams a;
-    Kv8Layer from;
+    Kv8Layer from;                // of a cache in 8 bits; null: a.K and a.V
     int32_t rows;                 // most rows of a query tile
     const uint64_t* turn;         // as in Kv8AppendParams
 };
-void launch_kv8_attention(const Kv8AttnParams& p, cudaStream_t s);
+void launch_decode_attention(const DecodeParams& p, cudaStream_t s);
 int attention_ctas_per_sm(int head_dim);
 constexpr int kAttnRows = 128;   // query rows per attention tile
 

@@ -360,3 +360,56 @@ def test_a_captured_step_replayed_with_new_inputs():
         torch.cuda.synchronize()
         p.ctx.check()
         p.check(0, [1, 1], x, out)
+
+
+# ---------------------------------------------------------------------------- few rows (a launch that appends, too)
+@pytest.mark.parametrize("shape", [HYBRID, MID, SMALL, (8, 8, 64, 64), (4, 4, 256, 256), (8, 4, 128, 6), (16, 1, 256, 0)])
+def test_few_rows_are_attended_to_and_appended(shape):
+    """One row of a group to 16 and the next, over one block's end and into the next, several steps: outputs, and what the
+    caches and positions hold then."""
+    import torch
+    from attn64 import rope
+    g = shape[0] // shape[1]
+    for n in sorted({1, max(1, 8 // g), 8 // g + 1, max(1, 16 // g), 16 // g + 1}):
+        lives = [64 - n, 63, 64, 127, 1300, 0]
+        p = Pop(shape, lives, 40 + n, [(1, 0), (70, 3), (2 ** 31 - 1, 0)], extra=4 * n, most=6 * n)
+        for step in range(3):
+            tails = [n, n, max(n - 1, 0), n, n, 1]
+            xs = [p.tail(sum(tails)) for _ in p.windows]
+            for i, x in enumerate(xs):
+                p.check(i, tails, x, _run(p, i, tails, x), (shape, n, step, i), keep=True)
+            p.ctx.advance(_cu(tails))
+            for b, m in enumerate(tails):
+                p.pos[b] = torch.cat([p.pos[b], p.cursor[b] + torch.arange(m, device="cuda")])
+                p.cursor[b] += m
+        for b in range(len(lives)):
+            assert torch.equal(p.ctx.get_positions(b).long(), p.pos[b])
+            for i in range(len(p.windows)):
+                k, v = p.ctx.get_kv(i, b)
+                assert torch.equal(v.double(), p.V[i][b])
+                # rounded once after a rotation in 32 bits (2^-20 of the pair's numbers at most, see test_gpu_kv8.holds)
+                off = 2.0 ** -8 * p.K[i][b].abs() + 2.0 ** -19 * p.K[i][b].abs().amax() if k.numel() else p.K[i][b]
+                assert bool(((k.double() - p.K[i][b]).abs() <= off).all())
+
+
+def test_few_rows_dealt_and_split():
+    """256 characters' step in waves of whole tiles, and one long one's over many blocks."""
+    r = np.random.default_rng(3)
+    p = Pop((8, 4, 64, 64), [int(x) for x in r.integers(0, 700, 255)] + [9000], 41, [(300, 4), (5000, 0)], extra=2, most=256)
+    for _ in range(2):
+        tails = [int(x) for x in r.integers(0, 2, 255)] + [1]
+        for i in range(2):
+            x = p.tail(sum(tails))
+            p.check(i, tails, x, _run(p, i, tails, x), i)
+
+
+def test_a_query_that_is_not_finite_stays_with_its_row():
+    import torch
+    for window in (64, 3000):
+        p = Pop(SMALL, [4000], 42, [(window, 0)])
+        x = p.tail(2)
+        x[0][1, 3, 5] = float("nan")
+        out = _run(p, 0, [2], x)
+        assert torch.isnan(out[1, 3]).all()
+        out[1, 3] = 0
+        assert torch.isfinite(out).all()
