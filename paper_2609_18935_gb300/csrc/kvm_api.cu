@@ -559,11 +559,20 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     if (m->n_layers <= 0 || !m->layer_kind) return fail(KVM_E_INVAL, "model has no layers");
     if (n_chars <= 0 || n_chars > kMaxChars) return fail(KVM_E_INVAL, "n_chars must be in [1,%d]", kMaxChars);
     if (max_tail_tokens <= 0) return fail(KVM_E_INVAL, "max_tail_tokens must be positive");
-    kvm_ctx* c = new kvm_ctx();
+    // whatever ends this early, an exception of the host's allocator too, frees what was made
+    struct Made {
+        kvm_ctx* c = new kvm_ctx();
+        ~Made() {
+            if (!c) return;
+            free_all(c);
+            delete c;
+        }
+    } made;
+    kvm_ctx* c = made.c;
     c->n_layers = m->n_layers;
     for (int l = 0; l < m->n_layers; ++l) {
         const int k = m->layer_kind[l];
-        if (k != KVM_LAYER_ATTN && k != KVM_LAYER_GDN) { delete c; return fail(KVM_E_INVAL, "bad layer kind"); }
+        if (k != KVM_LAYER_ATTN && k != KVM_LAYER_GDN) return fail(KVM_E_INVAL, "bad layer kind");
         c->kind.push_back(k);
         c->layer_name.push_back("layer " + std::to_string(l) + (k == KVM_LAYER_ATTN ? " (attention)" : " (delta rule)"));
         c->attn_idx.push_back(k == KVM_LAYER_ATTN ? c->n_attn++ : -1);
@@ -572,25 +581,24 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     if (c->n_attn > 0) {
         c->Hq = m->n_q_heads; c->Hkv = m->n_kv_heads; c->D = m->head_dim; c->R = m->rotary_dim;
         c->theta = m->rope_theta;
-        if (c->Hkv <= 0 || c->Hq <= 0 || c->Hq % c->Hkv) { delete c; return fail(KVM_E_UNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads"); }
+        if (c->Hkv <= 0 || c->Hq <= 0 || c->Hq % c->Hkv) return fail(KVM_E_UNSUPPORTED, "n_q_heads must be a multiple of n_kv_heads");
         c->g = c->Hq / c->Hkv;
-        if (c->g > 64 || (c->g & (c->g - 1))) { delete c; return fail(KVM_E_UNSUPPORTED, "group size must be a power of two <= 64"); }
-        if (c->D != 64 && c->D != 128 && c->D != 256) { delete c; return fail(KVM_E_UNSUPPORTED, "head_dim must be 64, 128 or 256"); }
-        if (c->R < 0 || c->R > c->D || (c->R & 1)) { delete c; return fail(KVM_E_UNSUPPORTED, "rotary_dim must be even and <= head_dim"); }
-        if (!(c->theta > 0)) { delete c; return fail(KVM_E_INVAL, "rope_theta must be positive"); }
+        if (c->g > 64 || (c->g & (c->g - 1))) return fail(KVM_E_UNSUPPORTED, "group size must be a power of two <= 64");
+        if (c->D != 64 && c->D != 128 && c->D != 256) return fail(KVM_E_UNSUPPORTED, "head_dim must be 64, 128 or 256");
+        if (c->R < 0 || c->R > c->D || (c->R & 1)) return fail(KVM_E_UNSUPPORTED, "rotary_dim must be even and <= head_dim");
+        if (!(c->theta > 0)) return fail(KVM_E_INVAL, "rope_theta must be positive");
         for (int d = 0; d < c->R / 2; ++d) c->inv_freq[d] = std::pow(c->theta, -2.0 * d / c->R);
         c->kv8 = kv8;
     }
     if (c->n_gdn > 0) {
         c->H = m->n_gdn_heads; c->dk = m->d_k; c->dv = m->d_v;
-        if (c->H <= 0) { delete c; return fail(KVM_E_INVAL, "n_gdn_heads must be positive"); }
-        if (c->dk != 64 && c->dk != 128) { delete c; return fail(KVM_E_UNSUPPORTED, "d_k must be 64 or 128"); }
-        if (c->dv <= 0 || c->dv % 32 || c->dv > 128) { delete c; return fail(KVM_E_UNSUPPORTED, "d_v must be a multiple of 32, <= 128"); }
-        if (m->conv_kernel != 0 && m->conv_kernel != 4) { delete c; return fail(KVM_E_UNSUPPORTED, "conv_kernel must be 0 or 4"); }
+        if (c->H <= 0) return fail(KVM_E_INVAL, "n_gdn_heads must be positive");
+        if (c->dk != 64 && c->dk != 128) return fail(KVM_E_UNSUPPORTED, "d_k must be 64 or 128");
+        if (c->dv <= 0 || c->dv % 32 || c->dv > 128) return fail(KVM_E_UNSUPPORTED, "d_v must be a multiple of 32, <= 128");
+        if (m->conv_kernel != 0 && m->conv_kernel != 4) return fail(KVM_E_UNSUPPORTED, "conv_kernel must be 0 or 4");
         c->conv = m->conv_kernel;
         c->conv_ch = c->H * (2 * c->dk + c->dv);
     } else if (m->conv_kernel != 0 && m->conv_kernel != 4) {
-        delete c;
         return fail(KVM_E_UNSUPPORTED, "conv_kernel must be 0 or 4");
     }
     c->window.assign(c->n_layers, 0);
@@ -598,20 +606,20 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     c->B = n_chars;
     c->max_tail = max_tail_tokens;
     for (int b = 0; b < n_chars; ++b) {
-        if (capacity[b] <= 0) { delete c; return fail(KVM_E_INVAL, "capacity of character %d must be positive", b); }
+        if (capacity[b] <= 0) return fail(KVM_E_INVAL, "capacity of character %d must be positive", b);
         const int cp = (capacity[b] + 63) / 64 * 64;   // slab offsets stay 64-row aligned
         c->cap.push_back(cp);
         c->cap_off.push_back((int)c->T_cap);
         c->T_cap += cp;
     }
-    if (c->T_cap > INT32_MAX) { delete c; return fail(KVM_E_CAPACITY, "total capacity too large"); }
+    if (c->T_cap > INT32_MAX) return fail(KVM_E_CAPACITY, "total capacity too large");
     c->live.assign(n_chars, 0);
     c->cursor.assign(n_chars, 0);
     c->hpos.assign(n_chars, {});
 
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, c->device);
-    if (e != cudaSuccess) { delete c; return fail(KVM_E_CUDA, "no CUDA device: %s", cudaGetErrorString(e)); }
+    if (e != cudaSuccess) return fail(KVM_E_CUDA, "no CUDA device: %s", cudaGetErrorString(e));
 
     const int kv_layers = c->kv8 ? 1 : c->n_attn;          // of the bf16 slabs
     const size_t layer_elems = (size_t)c->Hkv * c->T_cap * c->D, kv_elems = (size_t)kv_layers * layer_elems;
@@ -719,8 +727,6 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
     }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
-        free_all(c);
-        delete c;
         return fail(KVM_E_CUDA, "allocation failed: %s", cudaGetErrorString(e));
     }
     if (c->n_attn > 0) {
@@ -733,11 +739,10 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
         if (kd[1] > (uint64_t)INT32_MAX ||
             !encode_bf16_sw128(&c->tmap_k, c->K, 2, kd, ks, kb) ||
             !encode_bf16_sw128(&c->tmap_v, c->V, 2, kd, ks, kb)) {
-            free_all(c);
-            delete c;
             return fail(KVM_E_CUDA, "creating the TMA tensor maps failed");
         }
     }
+    made.c = nullptr;
     *out = c;
     return KVM_OK;
 }
@@ -745,12 +750,12 @@ kvm_status create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capac
 
 extern "C" kvm_status kvm_create(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity,
                                  int32_t max_tail_tokens, kvm_ctx** out) {
-    return create(m, n_chars, capacity, max_tail_tokens, false, out);
+    return guarded([&] { return create(m, n_chars, capacity, max_tail_tokens, false, out); });
 }
 
 extern "C" kvm_status kvm_create_kv8(const kvm_model_desc* m, int32_t n_chars, const int32_t* capacity,
                                      int32_t max_tail_tokens, kvm_ctx** out) {
-    return create(m, n_chars, capacity, max_tail_tokens, true, out);
+    return guarded([&] { return create(m, n_chars, capacity, max_tail_tokens, true, out); });
 }
 
 extern "C" kvm_status kvm_destroy(kvm_ctx* c) {
