@@ -121,8 +121,8 @@ kvm_status kvm_create(const kvm_model_desc* model, int32_t n_chars,
  *    (in a tail's key before its rotation);
  *  - drafts and kvm_rerotate_keys return KVM_E_UNSUPPORTED; kvm_fork takes two contexts
  *    of this kind; the context's device must be current (KVM_E_INVAL).
- * One layer's caches in bf16 are part of the workspace: tails of more than 16 rows
- * (tokens times group size) of a character and removals go by way of them. */
+ * One layer's caches in bf16 are part of the workspace: tails with more than 16 rows
+ * (tokens times group size) of a character go by way of them. */
 kvm_status kvm_create_kv8(const kvm_model_desc* model, int32_t n_chars,
                           const int32_t* capacity, int32_t max_tail_tokens,
                           kvm_ctx** out);
@@ -261,7 +261,9 @@ kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* live, const
 /* kvm_plan_attention_launch for a layer with a window (kvm_set_window): a query
  * tile whose first token is at live index x attends to fewer 64-key tiles.  Its
  * units are, in this order, the key tiles below min(ceil(n_sink / 64), f) with
- * f = floor(max(0, x + 1 - window) / 64), and those from f on. */
+ * f = floor(max(0, x + 1 - window) / 64), and those from f on.  (Of a windowed layer's
+ * or an 8-bit cache's tails with at most 16 rows a character the cut weighs segments and
+ * units otherwise; its form is the same.) */
 kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t window, int32_t n_sink,
                                      int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks, int32_t* n_tiles,

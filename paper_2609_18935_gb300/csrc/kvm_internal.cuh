@@ -255,8 +255,7 @@ void launch_kv8_widen(const Kv8CopyParams& p, cudaStream_t s);
 
 // A tail's rotated keys and its values into the blocks behind the live entries, and
 // its rotated queries into q_rot; those blocks and the older ones in sight as bf16 rows
-// of K and V.  All of a character in one line of the constant cache: a block's first
-// misses there, one after another, took 4 of the launch's 11 us.
+// of K and V.
 struct Kv8AppendChar {
     int32_t cap_off;      // slot offset of the character in the slabs
     int32_t L, M;         // live entries, tail tokens

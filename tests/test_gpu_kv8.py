@@ -277,7 +277,7 @@ def test_memory_that_no_kernel_reaches():
 
 
 # ---------------------------------------------------------------------------- tails
-@pytest.mark.parametrize("shape", [HYBRID, MID, SMALL, (8, 8, 128, 64), (64, 1, 64, 6), (16, 1, 256, 0)])
+@pytest.mark.parametrize("shape", [HYBRID, MID, SMALL, (8, 8, 128, 64), (64, 1, 64, 6), (16, 1, 256, 0), (4, 4, 256, 256), (8, 2, 128, 24)])
 @pytest.mark.parametrize("lives,tails", [([500, 0, 63, 1300, 64], [70, 5, 1, 33, 0]), ([500, 0, 63, 1300, 64, 1, 127], [1] * 7), ([0], [1]), ([0], [700]),
                                          ([4000, 10], [2, 1]), ([9000], [1]), ([3000] * 9, [1, 0, 1, 1, 1, 1, 1, 1, 1])])
 def test_tails(shape, lives, tails):
