@@ -572,3 +572,35 @@ def test_the_same_calls_give_the_same_bits():
                 runs.append(out)
         got.append(runs)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("bits,window", [(8, 0), (8, 100), (16, 100)])
+def test_offsets_past_32_bits(bits, window):
+    """A character behind another's nine million slots (its caches' offsets are past 2^32 bytes) gives the bits that it gives
+    on its own: few rows, a tail, a removal, what is read out."""
+    import torch
+    from paper_2609_18935_gb300 import kvm
+    hq, hkv, d, rot = HYBRID
+    g = torch.Generator(device="cuda").manual_seed(33)
+    k, v = _normal(g, hkv, 700, d, unit=True), _normal(g, hkv, 700, d)
+    steps = [[_normal(g, n, h, d, unit=h == hkv) for h in (hq, hkv, hkv)] for n in (1, 40, 2)]
+    got = []
+    for ahead in (64, 9_000_000):
+        ctx = kvm.Context([kvm.LAYER_ATTN], hq, hkv, d, rot, 1.0e4, 8, 64, 64, [ahead, 1000], 64, kv_bits=bits)
+        if window:
+            ctx.set_window(0, window, 4)
+        ctx.load_prefix(1, 700, 700, np.arange(700, dtype=np.int32))
+        ctx.set_kv(0, 1, k, v)
+        out = []
+        for i, x in enumerate(steps):
+            n = x[0].shape[0]
+            o = torch.empty_like(x[0])
+            ctx.update_round([0, 0, 2], [5, 300], [9, 391], [0, 0, n], {0: dict(zip("qkv", x))}, {0: o})
+            ctx.check()
+            out += [o, *ctx.get_kv(0, 1), ctx.get_positions(1)]
+        if bits == 8:
+            out.append(ctx.attn_probe(0, 1, steps[2][0])[0])
+        got.append(out)
+        ctx.destroy()
+        torch.cuda.empty_cache()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
