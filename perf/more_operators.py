@@ -440,11 +440,6 @@ def work(case):
 
 
 # ---------------------------------------------------------------------------- the same in 64 bits
-def _two(e):
-    """2^e in 64 bits from its bits (the GPU's pow and log2 are off by a unit there, and numbers on ties change sides)."""
-    return ((e.long() + 1023) << 52).view(torch.float64)
-
-
 def _exact_held(rows):
     """rows [hkv][n][d] in 64 bits from a block's first row on, as 8 bits hold them."""
     out = torch.empty_like(rows)
@@ -452,10 +447,10 @@ def _exact_held(rows):
         y = rows[:, lo:lo + BLOCK]
         top = y.abs().amax((1, 2), keepdim=True)
         e = torch.ceil(torch.log2(top / 448.0)).clamp(min=-117.0)
-        e = torch.where(top <= 448.0 * _two(e - 1), e - 1, torch.where(top > 448.0 * _two(e), e + 1, e)).clamp(min=-117.0)
-        y = y / _two(e)
-        grid = _two(torch.frexp(y.abs().clamp(min=2.0 ** -6))[1] - 4)
-        out[:, lo:lo + BLOCK] = torch.round(y / grid) * grid * _two(e)
+        e = torch.where(top <= 448.0 * 2.0 ** (e - 1), e - 1, torch.where(top > 448.0 * 2.0 ** e, e + 1, e)).clamp(min=-117.0)
+        y = y / 2.0 ** e
+        grid = 2.0 ** (torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+        out[:, lo:lo + BLOCK] = torch.round(y / grid) * grid * 2.0 ** e
     return out
 
 
