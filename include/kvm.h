@@ -320,7 +320,8 @@ kvm_status kvm_kv_compact(kvm_ctx* ctx, const int32_t* span_cu,
  * kvm_set_window).
  * tail_cu host [n_chars+1]; q device [sum M][n_q_heads][D] bf16;
  * k_new, v_new device [sum M][n_kv_heads][D] bf16; out device
- * [sum M][n_q_heads][D] bf16.  Does not move live lengths or cursors (see
+ * [sum M][n_q_heads][D] bf16.  out may overlie any of the inputs: they are
+ * read before an output takes their place.  Does not move live lengths or cursors (see
  * kvm_advance), so every attention layer of a round appends at the same
  * slots.  Errors: KVM_E_INVAL, KVM_E_CAPACITY. */
 kvm_status kvm_tail_attn_prefill(kvm_ctx* ctx, int32_t layer, const int32_t* tail_cu,

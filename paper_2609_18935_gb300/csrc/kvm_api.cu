@@ -1359,16 +1359,27 @@ int most_rows(const kvm_ctx* c, const int32_t* tail_cu) {
     return (int)std::min<int64_t>((int64_t)m * c->g, INT32_MAX);
 }
 
-// A tail that decode_attn.cu takes: of few rows, over 8-bit caches or under a window.
-bool few_rows(const kvm_ctx* c, int layer, const int32_t* tail_cu) {
-    return (c->kv8 || c->window[layer] > 0) && most_rows(c, tail_cu) <= kDecodeRows;
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+// A tail that decode_attn.cu takes: of few rows, over 8-bit caches or under a window.  In its one
+// launch a block stores its rows' outputs while others still read their inputs, so of an
+// out that overlies them it bears out == q alone (a whole query tile's rows are one block's, a
+// shared one's are stored by the merge); the other tails read every input in a launch before.
+bool few_rows(const kvm_ctx* c, int layer, const int32_t* tail_cu, int total, const void* q, const void* k_new, const void* v_new,
+              const void* out) {
+    if (!(c->kv8 || c->window[layer] > 0) || most_rows(c, tail_cu) > kDecodeRows) return false;
+    const size_t nq = (size_t)total * c->Hq * c->D * 2, nk = (size_t)total * c->Hkv * c->D * 2;
+    return !(out != q && overlap(out, nq, q, nq)) && !overlap(out, nq, k_new, nk) && !overlap(out, nq, v_new, nk);
 }
 
 // One attention layer's launches under its partition pl: a tail of `total` tokens
-// at tail_pos_dev (null: p_b + i), or with anc the nodes of a draft.
+// at tail_pos_dev (null: p_b + i), `direct` where few_rows takes it, or with anc the nodes of a draft.
 kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int total, const AttnPlan& pl, const void* q,
                             const void* k_new, const void* v_new, void* out, cudaStream_t s, const int32_t* tail_pos_dev,
-                            const uint64_t* anc) {
+                            const uint64_t* anc, bool direct) {
     thread_local static DecodeParams p8;          // large parameter blocks, copied into the launch
     AttnParams& p = p8.a;
     std::memset(&p, 0, offsetof(AttnParams, ch));  // (of its tables only what is written here is read)
@@ -1422,7 +1433,6 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
     std::copy(pl.cta_tile.begin(), pl.cta_tile.end(), p.cta_tile);
     std::copy(pl.cta_k.begin(), pl.cta_k.end(), p.cta_k);
 
-    const bool direct = few_rows(c, layer, tail_cu) && !anc;
     if (direct) {
         // the attention appends
     } else if (c->kv8) {
@@ -1509,11 +1519,12 @@ kvm_status do_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, const voi
 
     std::vector<int> Ms(c->B);
     for (int b = 0; b < c->B; ++b) Ms[b] = tail_cu[b + 1] - tail_cu[b];
+    const bool direct = few_rows(c, layer, tail_cu, total, q, k_new, v_new, out);
     AttnPlan pl;
     plan_attention(c->B, c->live.data(), Ms.data(), c->Hkv, kAttnRows / c->g, attention_grid_cap(c->num_sms, c->D), true,
-                   few_rows(c, layer, tail_cu) ? decode_cost(c->D * (c->kv8 ? 1 : 2)) : kTailCost, {c->window[layer], c->n_sink[layer]}, pl);
+                   direct ? decode_cost(c->D * (c->kv8 ? 1 : 2)) : kTailCost, {c->window[layer], c->n_sink[layer]}, pl);
     drop_draft(c);
-    return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr);
+    return launch_attention(c, layer, tail_cu, total, pl, q, k_new, v_new, out, s, tail_pos_dev, nullptr, direct);
 }
 
 // Rows of S per eight lanes of the token-by-token delta rule: four (k and q
@@ -1984,11 +1995,6 @@ bool aligned16(std::initializer_list<const void*> ps) {
     return (bits & 15) == 0;
 }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + nb && y < x + na;
-}
-
 // The trees of kvm_draft_begin.
 kvm_status check_tree(int B, const int32_t* node_cu, const int32_t* parent) {
     if (!node_cu) return fail(KVM_E_INVAL, "node_cu is NULL");
@@ -2149,7 +2155,7 @@ kvm_status draft_attn(kvm_ctx* c, int layer, const void* q, const void* k_new, c
         if (overlap(out, nq, q, nq) || overlap(out, nq, k_new, nk) || overlap(out, nq, v_new, nk))
             return fail(KVM_E_INVAL, "out overlaps an input");
         st = launch_attention(c, layer, c->draft_cu.data(), total, c->draft_plans[c->draft_plan_of[layer]], q, k_new, v_new, out, s, c->draft_pos,
-                              c->draft_anc);
+                              c->draft_anc, false);
         if (st) return st;
     }
     c->draft_done[layer] = 1;
