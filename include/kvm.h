@@ -237,7 +237,8 @@ kvm_status kvm_plan_spans_from_positions(int32_t live, const int32_t* positions,
  * [max_blocks + 1].  *n_tiles = number of query tiles.  split_first_block
  * host [max_blocks]: for each of the *n_split query tiles that several
  * blocks share, the first block that starts inside it (its partials are
- * merged by the combine kernel).  Errors: KVM_E_INVAL, KVM_E_UNSUPPORTED. */
+ * merged by the combine kernel).  Errors: KVM_E_INVAL (live + tail past 2^31 - 129, too,
+ * and more than 2^31 - 1 query tiles), KVM_E_UNSUPPORTED, KVM_E_CAPACITY (host memory). */
 kvm_status kvm_plan_attention(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
                               int32_t n_q_heads, int32_t n_kv_heads, int32_t max_blocks,
                               int32_t* n_blocks, int32_t* n_tiles, int32_t* block_tile,

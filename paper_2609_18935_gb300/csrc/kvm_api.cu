@@ -1054,11 +1054,15 @@ kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_
         return fail(KVM_E_INVAL, "max_blocks must be in [1,%d]", kMaxAttnCtas);
     if (tail_cu[0] != 0) return fail(KVM_E_INVAL, "tail_cu[0] must be 0");
     std::vector<int> L(live, live + n_chars), M(n_chars);
+    int64_t tiles = 0;
     for (int b = 0; b < n_chars; ++b) {
+        if (tail_cu[b + 1] < tail_cu[b]) return fail(KVM_E_INVAL, "tail_cu not monotone at character %d", b);
         M[b] = tail_cu[b + 1] - tail_cu[b];
-        if (M[b] < 0) return fail(KVM_E_INVAL, "tail_cu not monotone at character %d", b);
         if (L[b] < 0) return fail(KVM_E_INVAL, "negative live length at character %d", b);
+        if (L[b] > INT32_MAX - kAttnRows - M[b]) return fail(KVM_E_INVAL, "character %d: live %d + tail %d pass 32 bits", b, L[b], M[b]);
+        tiles += (int64_t)n_kv_heads * ((M[b] + (int64_t)kAttnRows / g - 1) / (kAttnRows / g));
     }
+    if (tiles > INT32_MAX) return fail(KVM_E_INVAL, "too many query tiles");
     AttnPlan pl;
     plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, kTailCost, sight, pl);
     if (n_waves) *n_waves = pl.waves;
@@ -1076,8 +1080,10 @@ extern "C" kvm_status kvm_plan_attention(int32_t n_chars, const int32_t* live, c
                                          int32_t n_q_heads, int32_t n_kv_heads, int32_t max_blocks,
                                          int32_t* n_blocks, int32_t* n_tiles, int32_t* block_tile,
                                          int32_t* block_key, int32_t* n_split, int32_t* split_first_block) {
-    return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, nullptr, n_blocks, n_tiles,
-                              block_tile, block_key, n_split, split_first_block);
+    return guarded([&] {
+        return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, nullptr, n_blocks, n_tiles,
+                                  block_tile, block_key, n_split, split_first_block);
+    });
 }
 
 extern "C" kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
@@ -1086,8 +1092,10 @@ extern "C" kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* 
                                                 int32_t* block_tile, int32_t* block_key, int32_t* n_split,
                                                 int32_t* split_first_block) {
     if (!n_waves) return fail(KVM_E_INVAL, "NULL argument");
-    return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
-                              block_tile, block_key, n_split, split_first_block);
+    return guarded([&] {
+        return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
+                                  block_tile, block_key, n_split, split_first_block);
+    });
 }
 
 extern "C" kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,

@@ -101,3 +101,30 @@ def test_bad_windows_are_refused(window, sinks):
         kvm.plan_attention_window([100], [0, 5], 16, 2, window, sinks, 152)
     assert e.value.code == kvm.KVM_E_INVAL
     assert kvm.load_library().kvm_set_window(None, 0, 64, 0) == kvm.KVM_E_INVAL
+
+
+@pytest.mark.parametrize("live,cu", [([2 ** 31 - 1], [0, 5]), ([2 ** 31 - 133], [0, 5]), ([0], [0, 2 ** 31 - 1]), ([5, 2 ** 31 - 130], [0, 7, 9])])
+def test_lengths_past_32_bits_are_refused(live, cu):
+    """A key list ends at live + tail, rounded up to whole tiles in 32 bits."""
+    for call in (lambda: kvm.plan_attention(live, cu, 16, 2, 152), lambda: kvm.plan_attention_launch(live, cu, 16, 2, 152),
+                 lambda: kvm.plan_attention_window(live, cu, 16, 2, 1000, 4, 152)):
+        with pytest.raises(kvm.KvmError) as e:
+            call()
+        assert e.value.code == kvm.KVM_E_INVAL
+
+
+def test_the_longest_lengths_are_planned():
+    L, n = 2 ** 31 - 134, 5
+    nk = -(-(L + n) // 64)
+    plan = kvm.plan_attention_launch([L], [0, n], 16, 2, 152)
+    assert plan["n_blocks"] == 152 and abs(plan["block_key"][1] - 2 * nk / 152) < 10
+    # in a window's sight: its 64-key tiles and one of sinks
+    f = (L + 1 - 1000) // 64
+    plan = kvm.plan_attention_window([L], [0, n], 16, 2, 1000, 4, 152)
+    assert plan["n_tiles"] == 2 and 1 <= plan["n_blocks"] <= 2 * (nk - f + 1) // 4
+
+
+def test_tiles_past_32_bits_are_refused():
+    with pytest.raises(kvm.KvmError) as e:
+        kvm.plan_attention_launch([0], [0, 2 ** 31 - 129], 64 * 64, 64, 152)
+    assert e.value.code == kvm.KVM_E_INVAL
