@@ -262,14 +262,25 @@ kvm_status kvm_plan_attention_launch(int32_t n_chars, const int32_t* live, const
 /* kvm_plan_attention_launch for a layer with a window (kvm_set_window): a query
  * tile whose first token is at live index x attends to fewer 64-key tiles.  Its
  * units are, in this order, the key tiles below min(ceil(n_sink / 64), f) with
- * f = floor(max(0, x + 1 - window) / 64), and those from f on.  (Of a windowed layer's
- * or an 8-bit cache's tails with at most 16 rows a character the cut weighs segments and
- * units otherwise; its form is the same.) */
+ * f = floor(max(0, x + 1 - window) / 64), and those from f on.  (Tails of at most 16
+ * rows a character: kvm_plan_attention_few.) */
 kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t window, int32_t n_sink,
                                      int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks, int32_t* n_tiles,
                                      int32_t* block_tile, int32_t* block_key, int32_t* n_split,
                                      int32_t* split_first_block);
+
+/* The partition of a tail that one launch appends and attends to: of a windowed layer or an
+ * 8-bit cache, with at most 16 rows (tokens times group size) a character.  row_bytes: of a key
+ * in the cache, head_dim times 1 or 2.  As kvm_plan_attention_window (window 0: whole caches),
+ * with other weights: a block has at least max(1, 512 / row_bytes) units, a segment counts as
+ * 4096 / row_bytes of them, and lists of at most 1280 / row_bytes units get a block each.
+ * Errors: KVM_E_INVAL, KVM_E_UNSUPPORTED (row_bytes, a character of more rows). */
+kvm_status kvm_plan_attention_few(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
+                                  int32_t n_q_heads, int32_t n_kv_heads, int32_t row_bytes, int32_t window,
+                                  int32_t n_sink, int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks,
+                                  int32_t* n_tiles, int32_t* block_tile, int32_t* block_key, int32_t* n_split,
+                                  int32_t* split_first_block);
 
 /* Partition of a character population over ranks (one GPU per rank):
  * characters are independent, so each rank maintains its own share with no

@@ -1042,7 +1042,8 @@ namespace {
 kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_t* tail_cu, int32_t n_q_heads,
                               int32_t n_kv_heads, int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks,
                               int32_t* n_tiles, int32_t* block_tile, int32_t* block_key, int32_t* n_split,
-                              int32_t* split_first_block, const Sight& sight = {}) {
+                              int32_t* split_first_block, const Sight& sight = {}, const PlanCost& cost_of = kTailCost,
+                              int64_t most_rows = INT64_MAX) {
     if (n_chars <= 0 || n_chars > kMaxChars) return fail(KVM_E_INVAL, "n_chars must be in [1,%d]", kMaxChars);
     if (!live || !tail_cu || !n_blocks || !n_tiles || !block_tile || !block_key || !n_split || !split_first_block)
         return fail(KVM_E_INVAL, "NULL argument");
@@ -1059,12 +1060,13 @@ kvm_status plan_attention_out(int32_t n_chars, const int32_t* live, const int32_
         if (tail_cu[b + 1] < tail_cu[b]) return fail(KVM_E_INVAL, "tail_cu not monotone at character %d", b);
         M[b] = tail_cu[b + 1] - tail_cu[b];
         if (L[b] < 0) return fail(KVM_E_INVAL, "negative live length at character %d", b);
+        if ((int64_t)M[b] * g > most_rows) return fail(KVM_E_UNSUPPORTED, "character %d: %d tokens of %d heads pass %d rows", b, M[b], g, (int)most_rows);
         if (L[b] > INT32_MAX - kAttnRows - M[b]) return fail(KVM_E_INVAL, "character %d: live %d + tail %d pass 32 bits", b, L[b], M[b]);
         tiles += (int64_t)n_kv_heads * ((M[b] + (int64_t)kAttnRows / g - 1) / (kAttnRows / g));
     }
     if (tiles > INT32_MAX) return fail(KVM_E_INVAL, "too many query tiles");
     AttnPlan pl;
-    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, kTailCost, sight, pl);
+    plan_attention(n_chars, L.data(), M.data(), n_kv_heads, kAttnRows / g, max_blocks, n_waves != nullptr, cost_of, sight, pl);
     if (n_waves) *n_waves = pl.waves;
     *n_blocks = pl.n_ctas;
     *n_tiles = pl.n_tiles;
@@ -1109,6 +1111,22 @@ extern "C" kvm_status kvm_plan_attention_window(int32_t n_chars, const int32_t* 
         if (st) return st;
         return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
                                   block_tile, block_key, n_split, split_first_block, {window, n_sink});
+    });
+}
+
+extern "C" kvm_status kvm_plan_attention_few(int32_t n_chars, const int32_t* live, const int32_t* tail_cu,
+                                             int32_t n_q_heads, int32_t n_kv_heads, int32_t row_bytes, int32_t window,
+                                             int32_t n_sink, int32_t max_blocks, int32_t* n_waves, int32_t* n_blocks,
+                                             int32_t* n_tiles, int32_t* block_tile, int32_t* block_key, int32_t* n_split,
+                                             int32_t* split_first_block) {
+    return guarded([&]() -> kvm_status {
+        if (!n_waves) return fail(KVM_E_INVAL, "NULL argument");
+        if (row_bytes != 64 && row_bytes != 128 && row_bytes != 256 && row_bytes != 512)
+            return fail(KVM_E_UNSUPPORTED, "row_bytes must be 64, 128, 256 or 512");
+        const kvm_status st = check_window(window, n_sink);
+        if (st) return st;
+        return plan_attention_out(n_chars, live, tail_cu, n_q_heads, n_kv_heads, max_blocks, n_waves, n_blocks, n_tiles,
+                                  block_tile, block_key, n_split, split_first_block, {window, n_sink}, decode_cost(row_bytes), kDecodeRows);
     });
 }
 

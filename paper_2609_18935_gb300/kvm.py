@@ -114,6 +114,10 @@ _SIGS = {
                                             C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                             C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                             C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
+    "kvm_plan_attention_few": (C.c_int, [C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_int32,
+                                         C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
     "kvm_set_window": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]),
     "kvm_plan_partition": (C.c_int, [C.c_int32, C.POINTER(C.c_int64), C.c_int32, C.POINTER(C.c_int32),
                                      C.POINTER(C.c_int64)]),
@@ -327,6 +331,11 @@ def plan_attention_window(live, tail_cu, n_q_heads, n_kv_heads, window, n_sink, 
     return _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, True, (int(window), int(n_sink)))
 
 
+def plan_attention_few(live, tail_cu, n_q_heads, n_kv_heads, row_bytes, window, n_sink, max_blocks):
+    """kvm_plan_attention_few: the partition of at most 16 rows a character over a windowed layer or an 8-bit cache."""
+    return _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, True, (int(row_bytes), int(window), int(n_sink)))
+
+
 def _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, launch, window=None):
     load_library()
     L, cu = _i32(live), _i32(tail_cu)
@@ -336,7 +345,7 @@ def _plan_attention(live, tail_cu, n_q_heads, n_kv_heads, max_blocks, launch, wi
     head = (len(L), _p32(L), _p32(cu), int(n_q_heads), int(n_kv_heads))
     call = _lib.kvm_plan_attention_launch if launch else _lib.kvm_plan_attention
     if window is not None:
-        call, head = _lib.kvm_plan_attention_window, (*head, *window)
+        call, head = _lib.kvm_plan_attention_window if len(window) == 2 else _lib.kvm_plan_attention_few, (*head, *window)
     head = (*head, int(max_blocks), *((C.byref(nw),) if launch else ()))
     rest = (C.byref(nb), C.byref(nt), _p32(tile), _p32(key), C.byref(ns), _p32(split))
     _check(call(*head, *rest))
