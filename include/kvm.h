@@ -103,8 +103,8 @@ kvm_status kvm_create(const kvm_model_desc* model, int32_t n_chars,
                       const int32_t* capacity, int32_t max_tail_tokens,
                       kvm_ctx** out);
 
-/* kvm_create with the attention caches in 8 bits: half the memory and half of what
- * a decode step reads.  Keys and values are e4m3 numbers times a power of two for
+/* kvm_create with the attention caches in 8 bits: half a layer's memory, and half of what
+ * a step of few rows reads (below).  Keys and values are e4m3 numbers times a power of two for
  * each block of 64 live slots of a KV head, K and V apart: 2^e with e the smallest
  * integer, -117 <= e <= 119, for which the block's largest magnitude is at most
  * 448 * 2^e; each number is rounded to the nearest, ties to even (to 2^-4 of its value
@@ -115,14 +115,19 @@ kvm_status kvm_create(const kvm_model_desc* model, int32_t n_chars,
  *  - kvm_set_kv and tails round what they store (a tail's keys once, after their
  *    rotation), the attention and the probe read what the cache then holds, kvm_get_kv
  *    returns it in bf16, exactly.  A tail's first entries share a block with older ones,
- *    which take over its scale, whether the tail becomes live or not.  A removal forms the
+ *    which take over its scale, whether the tail becomes live or not: under a larger one
+ *    their numbers below 2^-6 of it are rounded again, for good.  A removal forms the
  *    blocks from its first entry's on anew;
  *  - numbers that are not finite are stored as 0 and reported by kvm_check
  *    (in a tail's key before its rotation);
  *  - drafts and kvm_rerotate_keys return KVM_E_UNSUPPORTED; kvm_fork takes two contexts
  *    of this kind; the context's device must be current (KVM_E_INVAL).
- * One layer's caches in bf16 are part of the workspace: tails with more than 16 rows
- * (tokens times group size) of a character go by way of them. */
+ * A call in which every character has at most 16 rows (tokens times group size) reads the
+ * blocks themselves.  One character with more, or a group of 32 or 64, and the call widens all
+ * blocks in sight of all its characters into one layer's bf16 caches, which are part of the
+ * workspace: five bytes moved a number where a bf16 cache's step reads two, so such steps can
+ * take longer than over bf16.  With that layer n attention layers take n / 2 + 1 layers' bf16
+ * memory: less than kvm_create from three on. */
 kvm_status kvm_create_kv8(const kvm_model_desc* model, int32_t n_chars,
                           const int32_t* capacity, int32_t max_tail_tokens,
                           kvm_ctx** out);

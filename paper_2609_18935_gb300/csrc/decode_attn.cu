@@ -8,11 +8,13 @@
 // 8-bit numbers become f16 (one instruction a pair), exactly; their blocks' scales stay
 // outside, of K in the scores, of V as the sums are added up.  A query, rounded to bf16,
 // is f16 times a power of two of its row (down to 2^-39 of the row's largest).  A weight is
-// rounded to f16: 2^-12 of it, or 2^-33 of the reference's where it is small, 2^-9 of a
-// row's sum after 2^24 keys.  As bf16 (a pair in five instructions, K and V), 903
-// instructions a step, 32 characters' step over 16K (284 MB) took 64.4 us, so 60.0, and 54.4
-// (5.2 TB/s) with longer ranges and what follows; m16n8k32 on e4m3 itself, with a query as
-// two such numbers, ran as many instructions as the bf16 form.
+// rounded to f16: off by up to 2^-11 of it, or 2^-32 of its warp's reference where it is small
+// (f16 has steps of 2^-24 there, and weights are taken 2^7 higher).  The sum is of the weights
+// before that rounding.  So a warp's part of a row is off by up to 2^-32 a key of its own largest
+// weight, 2^-8 after 2^24 keys of one warp (a block's warps share a tile's keys, and a long tile's
+// are shared by many blocks); a key at 2^-32 of the reference or below counts in the sum alone.
+// As bf16 (a byte permute, a shift, a mask and a product a pair) 32 characters' step over 16K
+// (284 MB) took 64.4 us, so 60.0, and 54.4 (5.2 TB/s) with longer ranges and what follows.
 // bf16 caches: the words are the products' operands as they are.  Under a window of 4096
 // the same characters take 46.5 us (259 MB, 5.6 TB/s), one over 512 entries 6.4; by way of
 // rope_append and the tensor-core attention 49.5 and 9.4.
@@ -26,9 +28,9 @@
 // block an SM, partials of shared tiles for attn_combine.  A warp takes every WARPS-th
 // 16 keys of a segment through a ring of its own in shared memory (cp.async, no barrier
 // but the warp's), keeps its own softmax reference, sum and output in registers, and the
-// block's warps meet at the segment's end.  The loop runs at the memory's speed (54 GB/s an
-// SM); of 9 us for one character over 32K (7 units a block) 3.3 are the queries, 3.5 the
-// loop, 1 the meeting.
+// block's warps meet at the segment's end.  Of 9 us for one character over 32K (7 units a
+// block) 3.3 are the queries, beside which the rings' first stages are loaded, 3.5 the loop, 1
+// the meeting.
 //
 // Layout.  The sum over d takes any order, the same for K and Q: lane (g, j) = (lane / 4,
 // lane mod 4) reads 16 bytes of key g (and g + 8) at a time, and two words of them are its
@@ -56,7 +58,8 @@ constexpr float kUp = 7.f;                     // weights are taken 2^7 higher: 
 
 // E: bytes of a cache's number, 1 (e4m3) or 2 (bf16).  Eight warps: twelve and sixteen (of
 // fewer stages) took longer over 8 bits, 62.1 against 60.9 us for 32 characters over 16K,
-// 8.1 against 7.3 for one over 512, more of them meet at the end.
+// 8.1 against 7.3 for one over 512, more of them meet at the end.  Six where a key is 512 bytes:
+// a warp's two stages are 32 KB, and eight warps' rings would be 256 of the 227 there are.
 template <int D, int NT, int E>
 struct Cfg {
     static constexpr int WARPS = D * E == 512 ? 6 : 8;
