@@ -571,7 +571,7 @@ def run_kvm(args):
                            "per_launch_unit": "flop" if bound == "tensor" else "byte"}
     # the dominant kernel family is the one with the largest share of the step
     dominant = max(rooflines, key=lambda k: rooflines[k]["share"]) if rooflines else None
-    kfile = {"tail_attention": "tail_attn_tc.cu", "gdn": "gdn_scan_tc.cu", "kv_compact": "kv_compact.cu",
+    kfile = {"tail_attention": "tail_attn_tc.cuh", "gdn": "gdn_scan_tc.cu", "kv_compact": "kv_compact.cu",
              "rope_append": "tail_attn.cu"}
     roofline = None
     if dominant:
