@@ -1492,6 +1492,7 @@ kvm_status launch_attention(kvm_ctx* c, int layer, const int32_t* tail_cu, int t
         thread_local static CombineParams cp;
         cp.Hq = c->Hq; cp.D = c->D; cp.g = c->g;
         cp.n_split_tiles = (int)pl.split_cb.size();
+        // (windowed layers too: 32 characters' step 47.7 us against 46.8, 4001 and 90 tokens 60.3 against 62.1, others the same)
         cp.many_parts = anc || c->kv8;
         cp.part_o = c->part_o;
         cp.part_ml = c->part_ml;
